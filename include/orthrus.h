@@ -50,6 +50,12 @@ typedef enum {
     ORTHRUS_VIEW_AR_VERIFY = 1  /* in-block keys causal: row i sees in-block rows 0..i */
 } orthrus_view;
 
+typedef enum {
+    ORTHRUS_F32 = 0,
+    ORTHRUS_BF16 = 1, /* upper 16 bits of an IEEE fp32 value */
+    ORTHRUS_F16 = 2   /* IEEE binary16 */
+} orthrus_dtype;
+
 /*
  * num_splits value that asks for the balanced partition.  A fixed split count cuts every
  * sequence into the same number of pieces (each sequence by its own length, read on the device;
@@ -280,6 +286,114 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
                                                  int32_t *accept_len, int32_t *num_committed,
                                                  int32_t *out_tokens, int32_t *next_anchor,
                                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One token per logits row by temperature, top-k, top-p and min-p from a given uniform number: what draws a block's
+ * drafts from the diffusion view's logits (the caller's part of Section 3.3), and the next token in plain decoding (K = 1).
+ * For row (b, k) with logits x, M = max_v x_v and weights w_v = exp((x_v - M) / T_b), take the tokens in falling order of
+ * x, equal ones in rising order of v.  The filters apply one after the other:
+ *   top-k   the first top_k[b] tokens;                 off where top_k[b] <= 0 or >= V
+ *   top-p   the shortest prefix of those whose weight is at least top_p[b] times theirs (never empty);
+ *                                                      off where top_p[b] >= 1 or NaN; <= 0 keeps the first alone
+ *   min-p   those of them with w_v >= min_p[b];        off where min_p[b] <= 0 or NaN; > 1 counts as 1
+ * The token is the smallest v at which the sum of the kept weights of tokens 0..v exceeds u[b][k] times the sum of all
+ * kept weights; its log-probability is ln(w_v / that sum).  T_b <= 0 or NaN: the largest logit (smallest index on ties),
+ * log-probability 0.  A NaN logit counts as -inf, +inf as the largest float; a row of nothing but -inf has token -1 and
+ * log-probability -inf.  u outside [0, 1) counts as the nearest float in it, NaN as 0.
+ * The result is a deterministic function of the inputs: sums run over whole numbers (fixed point of 39 bits or more
+ * below the largest weight), weights are formed in 64 bits.
+ *
+ *   logits       [dev] [B, K, V] of logits_type, any alignment of the type's own; row (b, k) starts at element
+ *                (b*K + k) * logits_stride_row (0: dense, = V), so that the padding of an output head can stay
+ *   temperature  [dev] fp32 [B]
+ *   top_k [dev] int32 [B], top_p, min_p [dev] fp32 [B]: each may be NULL (off for every sequence)
+ *   u            [dev] fp32 [B, K]
+ *   tokens       [dev] int32 [B, K]        written
+ *   logprobs     [dev] fp32 [B, K] or NULL written if given
+ *   p            batch, block_k and vocab are used
+ *   workspace/workspace_bytes: at least orthrus_sample_workspace_bytes(p)
+ * Supported: V <= 2097152.
+ */
+int64_t orthrus_sample_workspace_bytes(const orthrus_params *p);
+orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
+                                     int64_t logits_stride_row, const float *temperature, const int32_t *top_k,
+                                     const float *top_p, const float *min_p, const float *u, int32_t *tokens,
+                                     float *logprobs, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * orthrus_sampling_consensus_commit for requests that sample under filters: p_k and q_k are the distributions that the
+ * sequence's temperature, top-k, top-p and min-p leave of the AR and of the diffusion logits (orthrus_sample_tokens defines
+ * them, also for special logits), and the drafts are draws from q_k, for instance by orthrus_sample_tokens.  Keep rule, replacement
+ * (argmax_v [log max(0, p_j(v) - q_j(v)) + gumbel[b][v]], from p_j itself where the difference is nowhere positive),
+ * outputs, commit and capacity error are those of orthrus_sampling_consensus_commit, so that the emitted tokens are
+ * distributed as draws from p.  A sequence with T_b <= 0 is verified greedily: its draft is kept iff it is the largest AR
+ * logit.  Where a rejected row's AR logits are nothing but -inf the emitted token is -1.  out_tokens may be draft_tokens.
+ *
+ *   ar_logits, diff_logits [dev] [B, K, V] of logits_type, both with logits_stride_row as in orthrus_sample_tokens
+ *   temperature, top_k, top_p, min_p as in orthrus_sample_tokens, applied to both views
+ *   remaining arguments as in orthrus_sampling_consensus_commit
+ *   workspace/workspace_bytes: at least orthrus_filtered_workspace_bytes(p)
+ * Probabilities are formed in 64 bits.  Supported: V <= 2097152.
+ */
+int64_t orthrus_filtered_workspace_bytes(const orthrus_params *p);
+orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,
+                                                 const void *ar_logits, const void *diff_logits, int64_t logits_stride_row,
+                                                 const float *temperature, const int32_t *top_k, const float *top_p,
+                                                 const float *min_p, const int32_t *draft_tokens, const float *accept_u,
+                                                 const float *gumbel, const void *k_blk_ar, const void *v_blk_ar,
+                                                 void *k_pool, void *v_pool, const int32_t *page_table, int32_t *seq_lens,
+                                                 int32_t *accept_len, int32_t *num_committed, int32_t *out_tokens,
+                                                 int32_t *next_anchor, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Page tables and slot maps from request lengths, on the device.  Free pages wait in a ring: free_pages[(head + i) %
+ * num_pages] for i < count, with head = free_state[0] and count = free_state[1].  An entry of page_table is mapped if it lies in
+ * [0, num_pages).  Per sequence b with L = seq_lens[b] and n = new_lens[b]:
+ *   n >= 0  the sequence is about to hold n more tokens: each of the entries L/P .. (L+n-1)/P that is not mapped gets a page
+ *           from the head of the ring, in the order of sequences and entries.  A sequence is granted if the pages that it
+ *           lacks, with those that the sequences before it lack, are in the ring when the call begins (one that
+ *           lacks none is always granted).  granted[b] = n, or 0 with its entries left alone.
+ *   n < 0   the request is over: all its mapped entries go to the tail of the ring in order and become -1, granted[b] = 0.
+ *           Pages that come back are handed out from the next call on.
+ * token_starts[b] = sum of granted[0..b-1] (B+1 values); slot_map[token_starts[b] + i] = page * P + offset of token
+ * position L + i for i < granted[b].  Slots behind the last token are left as they were.  seq_lens are not changed.
+ *
+ *   seq_lens, new_lens [dev] int32 [B] (read only)
+ *   page_table   [dev] int32 [B, max_pages_per_seq]; free_pages [dev] int32 [num_pages]; free_state [dev] int32 [2]
+ *   granted      [dev] int32 [B]; token_starts [dev] int32 [B+1]; slot_map [dev] int32 [max_tokens]
+ *   p            batch, page_size, max_pages_per_seq, max_seq_len and num_pages are used (and checked with the pool's fields)
+ *   workspace/workspace_bytes: at least orthrus_page_tables_workspace_bytes(p)
+ * Device-side errors (ORTHRUS_ECAPACITY in the context's error word): a sequence that is not granted because the ring runs
+ * short, because L < 0 or L + n > max_seq_len, or because L is inside a page that is not mapped; slots at and
+ * behind max_tokens (not written); a page id outside [0, num_pages) taken from the ring (slot -1); more pages coming back
+ * than the ring has room for (a page mapped twice; the last ones are dropped).  Nothing is written out of bounds.
+ * Supported: num_pages * page_size < 2^31.
+ */
+int64_t orthrus_page_tables_workspace_bytes(const orthrus_params *p);
+orthrus_status orthrus_page_tables_update(orthrus_ctx *ctx, const orthrus_params *p, const int32_t *seq_lens,
+                                          const int32_t *new_lens, int32_t *page_table, int32_t *free_pages,
+                                          int32_t *free_state, int32_t *granted, int32_t *token_starts, int32_t *slot_map,
+                                          int64_t max_tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Writes the K/V rows of packed new tokens to their slots (page * P + offset, for instance from
+ * orthrus_page_tables_update) in the cache of every layer: for t < N and layer < num_layers, row t of k_new / v_new goes to
+ * offset slot_map[t] % P of page slot_map[t] / P.  A negative slot's row is not written.  Slots must be distinct: of rows
+ * with the same slot the cache holds an unspecified mix.
+ *
+ *   num_rows     [host] N >= 0
+ *   k_new, v_new [dev] bf16 [num_layers, N, H_kv, d], dense or strided by blk_stride_* in params (0: dense, with
+ *                blk_stride_layer = N * blk_stride_row): element (layer, t, g, c) is at
+ *                layer * blk_stride_layer + t * blk_stride_row + g * blk_stride_head + c
+ *   slot_map     [dev] int32 [N]
+ *   num_valid    [dev] int32 [1] or NULL: rows at and behind it are not written (token_starts + B of the table update)
+ *   k_pool, v_pool [dev] bf16, updated in place, strides in params
+ * Device-side error: a slot at or behind num_pages * P is not written and sets the context's error word
+ * (ORTHRUS_ECAPACITY).  Rows are copied bit for bit.
+ */
+orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32_t num_rows, const void *k_new,
+                                const void *v_new, const int32_t *slot_map, const int32_t *num_valid, void *k_pool,
+                                void *v_pool, void *stream);
 
 /*
  * AR-view prefill attention of one layer — Section 3.1 (first paragraph) and Section 3.3: the frozen AR

@@ -298,3 +298,179 @@ def block_mask_attn(sm_scale: float, block_k: int, anchors: np.ndarray, q_diff: 
         p /= p.sum(axis=1, keepdims=True)
         out[:, h] = p @ vals
     return out
+
+
+# ---- the operators around the decode step: plain numpy, fp64, one row or request after another
+
+def filter_row(x: np.ndarray, temperature: float, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+    """What temperature, top-k, top-p and min-p leave of one logits row: (kept tokens in rising order, their
+    probabilities), both empty for a row of nothing but -inf."""
+    idx, w = _filter_weights(x, temperature, top_k, top_p, min_p)
+    return idx, w / w.sum()
+
+
+def _filter_weights(x, temperature, top_k, top_p, min_p):
+    """The same with the weights before they are normalised (whole numbers stay whole: equal logits weigh 1 each).
+
+    Literal: sort by (logit falling, index rising), weights exp((x - max) / T); the first top_k; of those the shortest
+    prefix holding top_p of their weight; of those the ones with a weight of at least min_p; renormalise.
+    """
+    x = np.asarray(x, dtype=np.float64).copy()
+    x[np.isnan(x)] = -np.inf
+    x = np.minimum(x, np.float64(np.finfo(np.float32).max))
+    order = np.lexsort((np.arange(x.size), -x))
+    order = order[x[order] > -np.inf]
+    if order.size == 0:
+        return order, np.empty(0)
+    if not temperature > 0:
+        return order[:1], np.ones(1)
+    w = np.exp((x[order] - x[order[0]]) / np.float64(min(temperature, np.finfo(np.float32).max)))
+    if 0 < top_k < x.size:
+        order, w = order[:top_k], w[:top_k]
+    if top_p < 1:
+        sums = np.cumsum(w)
+        n = int(np.count_nonzero(sums < np.float64(top_p) * sums[-1])) + 1
+        order, w = order[:max(n, 1)], w[:max(n, 1)]
+    if min_p > 0:
+        keep = w >= min(np.float64(min_p), 1.0)
+        order, w = order[keep], w[keep]
+    by_index = np.argsort(order)
+    return order[by_index], w[by_index]
+
+
+def sample_tokens(logits: np.ndarray, temperature, top_k, top_p, min_p, u: np.ndarray):
+    """Tokens [B,K] and log-probabilities: the first kept token whose running probability exceeds u.
+
+    ``logits`` [B,K,V] (any float type numpy can widen); the filters are arrays [B] or None.  Also returns, per row, how
+    far u is from the nearest value at which the token would change.
+    """
+    B, K, V = logits.shape
+    tokens, lp, margin = np.full((B, K), -1, np.int32), np.full((B, K), -np.inf), np.full((B, K), np.inf)
+    for b in range(B):
+        f = (float(temperature[b]), 0 if top_k is None else int(top_k[b]), 1.0 if top_p is None else float(top_p[b]),
+             0.0 if min_p is None else float(min_p[b]))
+        for k in range(K):
+            idx, w = _filter_weights(logits[b, k], *f)
+            if not idx.size:
+                continue
+            v = float(u[b, k])
+            v = 0.0 if np.isnan(v) else min(max(v, 0.0), 1.0 - 2.0 ** -24)
+            sums = np.cumsum(w)
+            i = min(int(np.count_nonzero(sums <= v * sums[-1])), idx.size - 1)
+            tokens[b, k] = idx[i]
+            lp[b, k] = np.log(w[i] / sums[-1]) if w[i] > 0 else -np.inf
+            if idx.size > 1:
+                margin[b, k] = np.min(np.abs(sums[:-1] / sums[-1] - v))
+    return tokens, lp, margin
+
+
+def filtered_consensus_commit(ar_logits, diff_logits, temperature, top_k, top_p, min_p, draft_tokens, accept_u, gumbel,
+                              k_blk_ar=None, v_blk_ar=None, k_pool=None, v_pool=None, page_table=None, seq_lens=None):
+    """The keep/replace rule of ``sampling_consensus_commit`` on the filtered distributions, and the commit
+    (pools [layers,pages,H_kv,P,d] and ``seq_lens`` updated in place; an unmapped position leaves the sequence alone)."""
+    B, K, V = ar_logits.shape
+    accept_len, num_committed, next_anchor = (np.zeros(B, np.int32) for _ in range(3))
+    out_tokens = np.full((B, K), -1, np.int32)
+    status = 0
+    margin = np.inf
+    for b in range(B):
+        f = (float(temperature[b]), 0 if top_k is None else int(top_k[b]), 1.0 if top_p is None else float(top_p[b]),
+             0.0 if min_p is None else float(min_p[b]))
+        j = 0
+        while j < K:
+            p, q = np.zeros(V), np.zeros(V)
+            for x, into in ((ar_logits[b, j], p), (diff_logits[b, j], q)):
+                idx, prob = filter_row(x, *f)
+                into[idx] = prob
+            x = int(draft_tokens[b, j])
+            if 0 <= x < V:
+                a, c = float(accept_u[b, j]) * q[x], p[x]
+                margin = min(margin, abs(a - c) / max(a, c) if max(a, c) > 0 else np.inf)
+                if a < c:
+                    out_tokens[b, j] = next_anchor[b] = x
+                    j += 1
+                    continue
+            r = p - q
+            if not (r > 0).any():
+                r = p
+            score = np.full(V, -np.inf)
+            pos = r > 0
+            score[pos] = np.log(r[pos]) + gumbel[b].astype(np.float64)[pos]
+            out_tokens[b, j] = next_anchor[b] = int(np.argmax(score)) if pos.any() else -1
+            break
+        accept_len[b] = j
+        m = num_committed[b] = min(j + 1, K)
+        if k_blk_ar is None:
+            continue
+        P, L = k_pool.shape[3], int(seq_lens[b])
+        slots = [(L + i) // P for i in range(m)]
+        pages = [int(page_table[b, s]) if s < page_table.shape[1] else -1 for s in slots]
+        if any(not 0 <= g < k_pool.shape[1] for g in pages):
+            num_committed[b], status = 0, -4
+            continue
+        for i, g in enumerate(pages):
+            k_pool[:, g, :, (L + i) % P] = k_blk_ar[:, b, i]
+            v_pool[:, g, :, (L + i) % P] = v_blk_ar[:, b, i]
+        seq_lens[b] = L + m
+    return dict(accept_len=accept_len, num_committed=num_committed, out_tokens=out_tokens, next_anchor=next_anchor,
+                status=status, margin=margin)
+
+
+def page_tables_update(seq_lens, new_lens, page_table, free_pages, free_state, page_size: int, max_seq_len: int, max_tokens: int,
+                       slot_map: np.ndarray):
+    """Pages and slots for requests that grow, pages back from those that ended; tables, ring and ``slot_map`` in place.
+    Returns granted, token_starts and the status (0 or -4)."""
+    B, width = page_table.shape
+    N, P = free_pages.size, page_size
+    mapped = lambda page: 0 <= page < N  # noqa: E731
+    head, count = int(free_state[0]) % N, min(max(int(free_state[1]), 0), N)
+    granted, starts = np.zeros(B, np.int32), np.zeros(B + 1, np.int32)
+    wanted, taken, back, status, tokens = 0, 0, [], 0, 0
+    for b in range(B):
+        L, n, row = int(seq_lens[b]), int(new_lens[b]), page_table[b]
+        starts[b] = min(tokens, 2 ** 31 - 1)
+        if n < 0:
+            for e in range(width):
+                if mapped(row[e]):
+                    back.append(int(row[e]))
+                    row[e] = -1
+            continue
+        if L < 0 or L + n > max_seq_len or (n > 0 and L % P and not mapped(row[L // P])):
+            status = -4
+            continue
+        lacks = [e for e in range(L // P, (L + n - 1) // P + 1) if not mapped(row[e])] if n else []
+        wanted += len(lacks)
+        if lacks and wanted > count:
+            status = -4
+            continue
+        for e in lacks:
+            row[e] = free_pages[(head + taken) % N]
+            taken += 1
+        granted[b] = n
+        for i in range(n):
+            page = int(row[(L + i) // P])
+            status = status if mapped(page) else -4
+            if tokens + i < max_tokens:
+                slot_map[tokens + i] = page * P + (L + i) % P if mapped(page) else -1
+        tokens += n
+    starts[B] = min(tokens, 2 ** 31 - 1)
+    if len(back) > N - count or tokens > max_tokens:
+        status = -4
+    for i, page in enumerate(back[:N - count]):
+        free_pages[(head + count + i) % N] = page
+    free_state[0], free_state[1] = (head + taken) % N, count - taken + min(len(back), N - count)
+    return granted, starts, status
+
+
+def kv_store(k_new, v_new, slot_map, k_pool, v_pool, num_valid=None):
+    """Rows [layers,N,H_kv,d] to their slots of the pools [layers,pages,H_kv,P,d], in place; the status (0 or -4)."""
+    P, slots, status = k_pool.shape[3], k_pool.shape[1] * k_pool.shape[3], 0
+    n = len(slot_map) if num_valid is None else min(max(int(num_valid), 0), len(slot_map))
+    for t in range(n):
+        s = int(slot_map[t])
+        if s >= slots:
+            status = -4
+        elif s >= 0:
+            k_pool[:, s // P, :, s % P] = k_new[:, t]
+            v_pool[:, s // P, :, s % P] = v_new[:, t]
+    return status

@@ -23,6 +23,10 @@ ORTHRUS_EHIP = -5
 ORTHRUS_VIEW_DIFFUSION = 0
 ORTHRUS_VIEW_AR_VERIFY = 1
 
+ORTHRUS_F32 = 0
+ORTHRUS_BF16 = 1
+ORTHRUS_F16 = 2
+
 EXPORTED = [
     "orthrus_create", "orthrus_destroy", "orthrus_status_string", "orthrus_attn_workspace_bytes",
     "orthrus_consensus_workspace_bytes", "orthrus_sampling_workspace_bytes", "orthrus_attn_num_splits",
@@ -32,6 +36,9 @@ EXPORTED = [
     "orthrus_attn_timing", "orthrus_attn_timing_read", "orthrus_attn_timing_samples", "orthrus_last_device_error",
     "orthrus_attn_num_splits_on", "orthrus_attn_workspace_bytes_on", "orthrus_build_id", "orthrus_kv_stream_probe",
     "orthrus_noalloc_scratch_bytes", "orthrus_consensus_commit_noalloc",
+    "orthrus_sample_workspace_bytes", "orthrus_sample_tokens", "orthrus_filtered_workspace_bytes",
+    "orthrus_filtered_consensus_commit", "orthrus_page_tables_workspace_bytes", "orthrus_page_tables_update",
+    "orthrus_kv_store",
 ]
 
 
@@ -138,6 +145,21 @@ def _load() -> ctypes.CDLL:
     lib.orthrus_consensus_commit_noalloc.restype = ctypes.c_int
     lib.orthrus_consensus_commit_noalloc.argtypes = [vp, pp, vp, i32p, vp, vp, vp, vp, i32p, i32p, i32p, i32p, i32p,
                                                      i32p, vp]
+    for name in ("sample", "filtered", "page_tables"):
+        f = getattr(lib, "orthrus_%s_workspace_bytes" % name)
+        f.restype, f.argtypes = ctypes.c_int64, [pp]
+    lib.orthrus_sample_tokens.restype = ctypes.c_int
+    lib.orthrus_sample_tokens.argtypes = [vp, pp, ctypes.c_int, vp, ctypes.c_int64, vp, i32p, vp, vp, vp, i32p, vp, vp,
+                                          ctypes.c_size_t, vp]
+    lib.orthrus_filtered_consensus_commit.restype = ctypes.c_int
+    lib.orthrus_filtered_consensus_commit.argtypes = [vp, pp, ctypes.c_int, vp, vp, ctypes.c_int64, vp, i32p, vp, vp, i32p,
+                                                      vp, vp, vp, vp, vp, vp, i32p, i32p, i32p, i32p, i32p, i32p, vp,
+                                                      ctypes.c_size_t, vp]
+    lib.orthrus_page_tables_update.restype = ctypes.c_int
+    lib.orthrus_page_tables_update.argtypes = [vp, pp, i32p, i32p, i32p, i32p, i32p, i32p, i32p, i32p, ctypes.c_int64, vp,
+                                               ctypes.c_size_t, vp]
+    lib.orthrus_kv_store.restype = ctypes.c_int
+    lib.orthrus_kv_store.argtypes = [vp, pp, ctypes.c_int32, vp, vp, i32p, i32p, vp, vp, vp]
     lib.orthrus_kv_stream_probe.restype = ctypes.c_int
     lib.orthrus_kv_stream_probe.argtypes = [vp, pp, vp, vp, i32p, i32p, vp]
     return lib
@@ -328,6 +350,74 @@ def orthrus_prefill_attn(ctx, p: orthrus_params, max_new_tokens: int, q, k_new, 
                                    _ptr(out), _ptr(workspace), _nbytes(workspace), _stream_handle(stream))
     if st != ORTHRUS_OK:
         raise OrthrusError(st, "orthrus_prefill_attn")
+
+
+def orthrus_sample_workspace_bytes(p: orthrus_params) -> int:
+    n = _lib.orthrus_sample_workspace_bytes(ctypes.byref(p))
+    if n < 0:
+        raise OrthrusError(int(n), "orthrus_sample_workspace_bytes")
+    return int(n)
+
+
+def orthrus_sample_tokens(ctx, p: orthrus_params, logits_type: int, logits, logits_stride_row: int, temperature, top_k, top_p,
+                          min_p, u, tokens, logprobs=None, workspace=None, stream=None, check: bool = True) -> int:
+    st = _lib.orthrus_sample_tokens(ctx, ctypes.byref(p), int(logits_type), _ptr(logits), int(logits_stride_row),
+                                    _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(tokens),
+                                    _ptr(logprobs), _ptr(workspace), _nbytes(workspace), _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_sample_tokens")
+    return st
+
+
+def orthrus_filtered_workspace_bytes(p: orthrus_params) -> int:
+    n = _lib.orthrus_filtered_workspace_bytes(ctypes.byref(p))
+    if n < 0:
+        raise OrthrusError(int(n), "orthrus_filtered_workspace_bytes")
+    return int(n)
+
+
+def orthrus_filtered_consensus_commit(ctx, p: orthrus_params, logits_type: int, ar_logits, diff_logits,
+                                      logits_stride_row: int, temperature, top_k, top_p, min_p, draft_tokens, accept_u,
+                                      gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
+                                      num_committed, out_tokens, next_anchor, workspace=None, stream=None,
+                                      check: bool = True) -> int:
+    st = _lib.orthrus_filtered_consensus_commit(
+        ctx, ctypes.byref(p), int(logits_type), _ptr(ar_logits), _ptr(diff_logits), int(logits_stride_row),
+        _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(draft_tokens), _ptr(accept_u), _ptr(gumbel),
+        _ptr(k_blk_ar), _ptr(v_blk_ar), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(seq_lens), _ptr(accept_len),
+        _ptr(num_committed), _ptr(out_tokens), _ptr(next_anchor), _ptr(workspace), _nbytes(workspace),
+        _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_filtered_consensus_commit")
+    return st
+
+
+def orthrus_page_tables_workspace_bytes(p: orthrus_params) -> int:
+    n = _lib.orthrus_page_tables_workspace_bytes(ctypes.byref(p))
+    if n < 0:
+        raise OrthrusError(int(n), "orthrus_page_tables_workspace_bytes")
+    return int(n)
+
+
+def orthrus_page_tables_update(ctx, p: orthrus_params, seq_lens, new_lens, page_table, free_pages, free_state, granted,
+                               token_starts, slot_map, max_tokens: int, workspace=None, stream=None,
+                               check: bool = True) -> int:
+    st = _lib.orthrus_page_tables_update(ctx, ctypes.byref(p), _ptr(seq_lens), _ptr(new_lens), _ptr(page_table),
+                                         _ptr(free_pages), _ptr(free_state), _ptr(granted), _ptr(token_starts),
+                                         _ptr(slot_map), int(max_tokens), _ptr(workspace), _nbytes(workspace),
+                                         _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_page_tables_update")
+    return st
+
+
+def orthrus_kv_store(ctx, p: orthrus_params, num_rows: int, k_new, v_new, slot_map, num_valid, k_pool, v_pool, stream=None,
+                     check: bool = True) -> int:
+    st = _lib.orthrus_kv_store(ctx, ctypes.byref(p), int(num_rows), _ptr(k_new), _ptr(v_new), _ptr(slot_map),
+                               _ptr(num_valid), _ptr(k_pool), _ptr(v_pool), _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_kv_store")
+    return st
 
 
 def orthrus_graph_begin(ctx, stream) -> None:

@@ -140,6 +140,61 @@ int32_t attn_splits_for(const orthrus_params *p, int num_cus)
     return plan.bal_wgs > 0 ? 0 : plan.num_splits;
 }
 
+// ---- sampling filters, page tables
+
+orthrus_status check_filter_params(const orthrus_params *p)
+{
+    const orthrus_status s = check_params(p, false, true, false);
+    if (s != ORTHRUS_OK) return s;
+    return p->vocab > (1 << 21) ? ORTHRUS_EUNSUPPORTED : ORTHRUS_OK;
+}
+
+// `words`: the addresses of every 4-byte operand, or-ed together.
+orthrus_status check_logits(const orthrus_params *p, orthrus_dtype type, uintptr_t logits, int64_t stride_row, uintptr_t words)
+{
+    if (type != ORTHRUS_F32 && type != ORTHRUS_BF16 && type != ORTHRUS_F16) return ORTHRUS_EINVAL;
+    if (stride_row != 0 && stride_row < p->vocab) return ORTHRUS_EINVAL;
+    if ((logits & (type == ORTHRUS_F32 ? 3 : 1)) || (words & 3)) return ORTHRUS_EINVAL;
+    return ORTHRUS_OK;
+}
+
+orthrus::FilterArgs filter_args(const orthrus_params *p, orthrus_dtype type, const void *logits0, const void *logits1,
+                                int64_t stride_row, const float *temperature, const int32_t *top_k, const float *top_p,
+                                const float *min_p)
+{
+    orthrus::FilterArgs a = {};
+    a.logits[0] = logits0; a.logits[1] = logits1;
+    a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+    a.stride_row = stride_row ? stride_row : p->vocab;
+    a.rows = p->batch * p->block_k; a.block_k = p->block_k; a.vocab = p->vocab;
+    a.dtype = (int)type;
+    return a;
+}
+
+// Workspace of the filtered consensus: byte offsets of its parts.
+struct FilteredLayout {
+    size_t cuts, info, filter, total;
+};
+FilteredLayout filtered_layout(const orthrus_params *p)
+{
+    const size_t rows = (size_t)p->batch * p->block_k;
+    FilteredLayout l;
+    l.cuts = 0;
+    l.info = align_up(2 * rows * sizeof(orthrus::RowCut), 256);
+    l.filter = l.info + align_up((size_t)p->batch * 3 * sizeof(int32_t), 256);
+    l.total = l.filter + align_up(orthrus::filter_workspace_bytes((int64_t)rows, p->vocab, 2), 256);
+    return l;
+}
+
+orthrus_status check_table_params(const orthrus_params *p)
+{
+    const orthrus_status s = check_params(p, false, false, true);
+    if (s != ORTHRUS_OK) return s;
+    if (p->max_seq_len < 0 || (int64_t)p->max_seq_len > (int64_t)p->max_pages_per_seq * p->page_size)
+        return ORTHRUS_EINVAL;
+    return p->num_pages > 0x7fffffff / p->page_size ? ORTHRUS_EUNSUPPORTED : ORTHRUS_OK;
+}
+
 }  // namespace
 
 // Kernel arguments of a decode-mode attention launch for `plan`.
@@ -659,6 +714,164 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
     a.draw_chunks = p->vocab / de + (p->vocab % de ? 1 : 0);
     hipError_t e = orthrus::launch_sampling_consensus(a, (hipStream_t)stream);
     return e == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+int64_t orthrus_sample_workspace_bytes(const orthrus_params *p)
+{
+    const orthrus_status s = check_filter_params(p);
+    return s != ORTHRUS_OK ? (int64_t)s : (int64_t)orthrus::filter_workspace_bytes((int64_t)p->batch * p->block_k, p->vocab, 1);
+}
+
+orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
+                                     int64_t logits_stride_row, const float *temperature, const int32_t *top_k,
+                                     const float *top_p, const float *min_p, const float *u, int32_t *tokens,
+                                     float *logprobs, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    orthrus_status s = check_filter_params(p);
+    if (s != ORTHRUS_OK) return s;
+    if (!logits || !temperature || !u || !tokens) return ORTHRUS_EINVAL;
+    s = check_logits(p, logits_type, (uintptr_t)logits, logits_stride_row,
+                     (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)u |
+                         (uintptr_t)tokens | (uintptr_t)logprobs);
+    if (s != ORTHRUS_OK) return s;
+    if (p->batch == 0) return ORTHRUS_OK;
+    const int64_t rows = (int64_t)p->batch * p->block_k;
+    const size_t need = orthrus::filter_workspace_bytes(rows, p->vocab, 1);
+    if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return ORTHRUS_EWORKSPACE;
+    orthrus::FilterArgs a = filter_args(p, logits_type, logits, nullptr, logits_stride_row, temperature, top_k, top_p, min_p);
+    a.u = u; a.tokens = tokens; a.logprobs = logprobs;
+    a.workspace = workspace;
+    return orthrus::launch_sample_tokens(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+int64_t orthrus_filtered_workspace_bytes(const orthrus_params *p)
+{
+    const orthrus_status s = check_filter_params(p);
+    return s != ORTHRUS_OK ? (int64_t)s : (int64_t)filtered_layout(p).total;
+}
+
+orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,
+                                                 const void *ar_logits, const void *diff_logits, int64_t logits_stride_row,
+                                                 const float *temperature, const int32_t *top_k, const float *top_p,
+                                                 const float *min_p, const int32_t *draft_tokens, const float *accept_u,
+                                                 const float *gumbel, const void *k_blk_ar, const void *v_blk_ar,
+                                                 void *k_pool, void *v_pool, const int32_t *page_table, int32_t *seq_lens,
+                                                 int32_t *accept_len, int32_t *num_committed, int32_t *out_tokens,
+                                                 int32_t *next_anchor, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    if ((k_blk_ar == nullptr) != (v_blk_ar == nullptr)) return ORTHRUS_EINVAL;
+    const bool do_commit = k_blk_ar != nullptr;
+    orthrus_status s = check_filter_params(p);
+    if (s == ORTHRUS_OK) s = check_params(p, false, true, do_commit);
+    if (s != ORTHRUS_OK) return s;
+    if (!ar_logits || !diff_logits || !temperature || !draft_tokens || !accept_u || !gumbel || !accept_len || !num_committed ||
+        !out_tokens || !next_anchor)
+        return ORTHRUS_EINVAL;
+    s = check_logits(p, logits_type, (uintptr_t)ar_logits | (uintptr_t)diff_logits, logits_stride_row,
+                     (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)draft_tokens |
+                         (uintptr_t)accept_u | (uintptr_t)gumbel | (uintptr_t)accept_len | (uintptr_t)num_committed |
+                         (uintptr_t)out_tokens | (uintptr_t)next_anchor);
+    if (s != ORTHRUS_OK) return s;
+    if (do_commit) {
+        if (!k_pool || !v_pool || !page_table || !seq_lens || p->num_layers <= 0) return ORTHRUS_EINVAL;
+        if (p->num_layers > 65535) return ORTHRUS_EUNSUPPORTED;
+        const uintptr_t al = (uintptr_t)k_blk_ar | (uintptr_t)v_blk_ar | (uintptr_t)k_pool | (uintptr_t)v_pool;
+        if (al & 15) return ORTHRUS_EINVAL;
+    }
+    if (p->batch == 0) return ORTHRUS_OK;
+    const FilteredLayout l = filtered_layout(p);
+    if (!workspace || workspace_bytes < l.total || ((uintptr_t)workspace & 255)) return ORTHRUS_EWORKSPACE;
+
+    orthrus::FilteredArgs a;
+    orthrus::ConsensusArgs &c = a.c;
+    c.ar_logits = nullptr; c.draft_tokens = draft_tokens;
+    c.k_blk_ar = (const uint16_t *)k_blk_ar; c.v_blk_ar = (const uint16_t *)v_blk_ar;
+    c.k_pool = (uint16_t *)k_pool; c.v_pool = (uint16_t *)v_pool;
+    c.page_table = page_table; c.seq_lens = seq_lens;
+    c.accept_len = accept_len; c.num_committed = num_committed; c.out_tokens = out_tokens; c.next_anchor = next_anchor;
+    c.part_val = nullptr; c.part_idx = nullptr;
+    c.commit_info = (int32_t *)((char *)workspace + l.info); c.decided = c.commit_info + p->batch; c.copy_apart = 0;
+    c.err_word = ctx->err_word;
+    c.stride_layer = p->pool_stride_layer; c.stride_page = p->pool_stride_page;
+    c.stride_head = p->pool_stride_head; c.stride_tok = p->pool_stride_tok; c.num_pages = p->num_pages;
+    c.blk_stride_head = p->blk_stride_head ? p->blk_stride_head : p->head_dim;
+    c.blk_stride_row = p->blk_stride_row ? p->blk_stride_row : (int64_t)p->num_kv_heads * p->head_dim;
+    c.blk_stride_layer = p->blk_stride_layer ? p->blk_stride_layer : (int64_t)p->batch * p->block_k * c.blk_stride_row;
+    c.batch = p->batch; c.block_k = p->block_k; c.vocab = p->vocab; c.num_layers = p->num_layers;
+    c.num_kv_heads = p->num_kv_heads; c.head_dim = p->head_dim;
+    c.page_shift = do_commit ? log2_exact(p->page_size) : 0; c.max_pages_per_seq = p->max_pages_per_seq;
+    c.chunks = 0; c.chunk_elems = 0; c.do_commit = do_commit ? 1 : 0;
+    a.f = filter_args(p, logits_type, ar_logits, diff_logits, logits_stride_row, temperature, top_k, top_p, min_p);
+    a.f.cuts = (orthrus::RowCut *)((char *)workspace + l.cuts);
+    a.f.workspace = (char *)workspace + l.filter;
+    a.accept_u = accept_u; a.gumbel = gumbel;
+    a.replacement = c.decided + p->batch;
+    return orthrus::launch_filtered_consensus(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+int64_t orthrus_page_tables_workspace_bytes(const orthrus_params *p)
+{
+    const orthrus_status s = check_table_params(p);
+    return s != ORTHRUS_OK ? (int64_t)s : (int64_t)align_up(((size_t)3 * p->batch + 2) * sizeof(int32_t), 256);
+}
+
+orthrus_status orthrus_page_tables_update(orthrus_ctx *ctx, const orthrus_params *p, const int32_t *seq_lens,
+                                          const int32_t *new_lens, int32_t *page_table, int32_t *free_pages,
+                                          int32_t *free_state, int32_t *granted, int32_t *token_starts, int32_t *slot_map,
+                                          int64_t max_tokens, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    const orthrus_status s = check_table_params(p);
+    if (s != ORTHRUS_OK) return s;
+    if (!seq_lens || !new_lens || !page_table || !free_pages || !free_state || !granted || !token_starts || max_tokens < 0 ||
+        (!slot_map && max_tokens > 0))
+        return ORTHRUS_EINVAL;
+    const uintptr_t al = (uintptr_t)seq_lens | (uintptr_t)new_lens | (uintptr_t)page_table | (uintptr_t)free_pages |
+                         (uintptr_t)free_state | (uintptr_t)granted | (uintptr_t)token_starts | (uintptr_t)slot_map;
+    if (al & 3) return ORTHRUS_EINVAL;
+    if (max_tokens > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
+    const size_t need = (size_t)orthrus_page_tables_workspace_bytes(p);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255)) return ORTHRUS_EWORKSPACE;
+    orthrus::TablesArgs a;
+    a.seq_lens = seq_lens; a.new_lens = new_lens;
+    a.page_table = page_table; a.free_pages = free_pages; a.free_state = free_state;
+    a.granted = granted; a.token_starts = token_starts; a.slot_map = slot_map;
+    a.need = (int32_t *)workspace; a.first = a.need + p->batch; a.pages_before = a.first + p->batch;
+    a.ring_before = a.pages_before + p->batch;
+    a.err_word = ctx->err_word;
+    a.num_pages = p->num_pages; a.max_tokens = max_tokens;
+    a.batch = p->batch; a.page_shift = log2_exact(p->page_size); a.max_pages_per_seq = p->max_pages_per_seq;
+    a.max_seq_len = p->max_seq_len;
+    return orthrus::launch_page_tables(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32_t num_rows, const void *k_new,
+                                const void *v_new, const int32_t *slot_map, const int32_t *num_valid, void *k_pool,
+                                void *v_pool, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    const orthrus_status s = check_params(p, false, false, true);
+    if (s != ORTHRUS_OK) return s;
+    if (num_rows < 0 || p->num_layers <= 0 || !k_new || !v_new || !slot_map || !k_pool || !v_pool) return ORTHRUS_EINVAL;
+    if (p->num_layers > 65535 || p->num_pages > 0x7fffffff / p->page_size) return ORTHRUS_EUNSUPPORTED;
+    if (((uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) return ORTHRUS_EINVAL;
+    if (((uintptr_t)slot_map | (uintptr_t)num_valid) & 3) return ORTHRUS_EINVAL;
+    if (num_rows == 0) return ORTHRUS_OK;
+    orthrus::StoreArgs a;
+    a.k_new = (const uint16_t *)k_new; a.v_new = (const uint16_t *)v_new;
+    a.slot_map = slot_map; a.num_valid = num_valid;
+    a.k_pool = (uint16_t *)k_pool; a.v_pool = (uint16_t *)v_pool;
+    a.err_word = ctx->err_word;
+    a.blk_stride_head = p->blk_stride_head ? p->blk_stride_head : p->head_dim;
+    a.blk_stride_row = p->blk_stride_row ? p->blk_stride_row : (int64_t)p->num_kv_heads * p->head_dim;
+    a.blk_stride_layer = p->blk_stride_layer ? p->blk_stride_layer : (int64_t)num_rows * a.blk_stride_row;
+    a.stride_layer = p->pool_stride_layer; a.stride_page = p->pool_stride_page;
+    a.stride_head = p->pool_stride_head; a.stride_tok = p->pool_stride_tok; a.num_pages = p->num_pages;
+    a.rows = num_rows; a.num_layers = p->num_layers; a.num_kv_heads = p->num_kv_heads; a.head_dim = p->head_dim;
+    a.page_shift = log2_exact(p->page_size);
+    return orthrus::launch_kv_store(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
 
 orthrus_status orthrus_last_device_error(orthrus_ctx *ctx, void *stream, int32_t *code)

@@ -80,6 +80,62 @@ struct SamplingArgs {
     int draw_chunks;          // draw_chunk_elems()-sized pieces of a row
 };
 
+// What the filters keep of one logits row: tokens whose logit orders above `key`, those at it up to index `tie`, of them
+// the ones with a weight of at least min_w; z is the sum of the kept weights (0: the row holds nothing but -inf).
+struct RowCut {
+    double z;
+    float top;       // the row's largest logit; weights are relative to it
+    float min_w;
+    uint32_t key;    // order_key of the last logit kept
+    int32_t tie;
+};
+
+struct FilterArgs {
+    const void *logits[2];   // sampling: one set of rows; consensus: the AR and the diffusion view's
+    const float *temperature;  // [B], as the next three (those: NULL = off)
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    const float *u;          // sampling: [rows]
+    int32_t *tokens;
+    float *logprobs;         // or NULL
+    RowCut *cuts;            // consensus: [view][rows]
+    void *workspace;         // filter_workspace_bytes
+    int64_t stride_row;      // elements between rows
+    int rows, block_k, vocab;
+    int dtype;               // orthrus_dtype
+};
+
+struct FilteredArgs {
+    ConsensusArgs c;
+    FilterArgs f;
+    const float *accept_u;   // [B][K]
+    const float *gumbel;     // [B][V]
+    int32_t *replacement;    // [B] (workspace)
+};
+
+struct TablesArgs {
+    const int32_t *seq_lens, *new_lens;
+    int32_t *page_table, *free_pages, *free_state;
+    int32_t *granted, *token_starts, *slot_map;
+    // workspace: per sequence the pages that it lacks (-1 - the pages that it returns, INT32_MIN if its lengths are bad), the
+    // first of them (-1 - it where there are holes behind it), the pages taken or returned by the sequences before it; the
+    // ring's head and count before the call
+    int32_t *need, *first, *pages_before, *ring_before;
+    int32_t *err_word;
+    int64_t num_pages, max_tokens;
+    int batch, page_shift, max_pages_per_seq, max_seq_len;
+};
+
+struct StoreArgs {
+    const uint16_t *k_new, *v_new;
+    const int32_t *slot_map, *num_valid;
+    uint16_t *k_pool, *v_pool;
+    int32_t *err_word;
+    int64_t blk_stride_layer, blk_stride_row, blk_stride_head;
+    int64_t stride_layer, stride_page, stride_head, stride_tok, num_pages;
+    int rows, num_layers, num_kv_heads, head_dim, page_shift;
+};
+
 // ---- commit helpers shared by the greedy and the sampling consensus kernels (device code)
 #if defined(__HIPCC__)
 // Copy rows 0..m-1 of the AR view's block K/V of (sequence b, layer) to token positions L..L+m-1 of the
@@ -200,6 +256,11 @@ hipError_t launch_prefill_attn(const AttnArgs &a, int head_dim, int num_cus, hip
 hipError_t launch_prefill_split(const AttnArgs &a, int head_dim, int num_cus, hipStream_t stream);
 hipError_t launch_consensus(ConsensusArgs a, hipStream_t stream);
 hipError_t launch_sampling_consensus(const SamplingArgs &a, hipStream_t stream);
+size_t filter_workspace_bytes(int64_t rows, int vocab, int views);
+hipError_t launch_sample_tokens(const FilterArgs &a, hipStream_t stream);
+hipError_t launch_filtered_consensus(const FilteredArgs &a, hipStream_t stream);
+hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream);
+hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
 int consensus_chunk_elems();
 int draw_chunk_elems();
 // Static device scratch of the allocation-free consensus entry point: looked up once per device (with

@@ -25,6 +25,17 @@ def bits_to_numpy(t: torch.Tensor) -> np.ndarray:
     return a.view(np.uint16) if a.dtype == np.int16 else a
 
 
+_LOGITS_TYPES = {torch.float32: B.ORTHRUS_F32, torch.bfloat16: B.ORTHRUS_BF16, torch.float16: B.ORTHRUS_F16}
+
+
+def _logits_type(*logits) -> int:
+    """The ABI's name of the logits' type; every tensor of a call has the same."""
+    t = _LOGITS_TYPES.get(logits[0].dtype)
+    if t is None or any(x.dtype != logits[0].dtype for x in logits):
+        raise ValueError("logits must be float32, bfloat16 or float16, all of one type")
+    return t
+
+
 class DecodeStep:
     """Owns an orthrus context plus the attention / consensus workspaces for fixed shapes."""
 
@@ -114,6 +125,47 @@ class DecodeStep:
             self.prefill_ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         return B.orthrus_prefill_attn(self.ctx, self.params, max_new_tokens, q, k_new, v_new, new_lens, k_pool,
                                       v_pool, page_table, seq_lens, out, self.prefill_ws, stream)
+
+    def _workspace(self, name, need):
+        """The buffer kept for one kind of call (made on its first use, not inside a captured sequence)."""
+        ws = getattr(self, name, None)
+        if ws is None or ws.numel() < need:
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            setattr(self, name, ws)
+        return ws
+
+    def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, logprobs=None, stream=None,
+                      logits_stride_row=0):
+        """One token per logits row [batch, block_k, vocab] by each sequence's temperature, top-k, top-p and min-p (each of
+        the last three a [batch] tensor or None) from the uniform numbers u [batch, block_k]."""
+        ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
+        return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits), logits, logits_stride_row, temperature,
+                                       top_k, top_p, min_p, u, tokens, logprobs, ws, stream)
+
+    def filtered_consensus_commit(self, ar_logits, diff_logits, temperature, top_k, top_p, min_p, draft_tokens, accept_u,
+                                  gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
+                                  num_committed, out_tokens, next_anchor, stream=None, logits_stride_row=0):
+        """sampling_consensus_commit where both views' distributions are filtered as in sample_tokens."""
+        ws = self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes(self.params))
+        return B.orthrus_filtered_consensus_commit(self.ctx, self.params, _logits_type(ar_logits, diff_logits), ar_logits,
+                                                   diff_logits, logits_stride_row, temperature, top_k, top_p, min_p,
+                                                   draft_tokens, accept_u, gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool,
+                                                   page_table, seq_lens, accept_len, num_committed, out_tokens,
+                                                   next_anchor, ws, stream)
+
+    def update_page_tables(self, seq_lens, new_lens, page_table, free_pages, free_state, granted, token_starts, slot_map,
+                           stream=None):
+        """Pages for the sequences that grow by new_lens tokens, pages back from those with new_lens < 0, and the slots of
+        the new tokens (packed; slot_map's length is the bound on their number)."""
+        ws = self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes(self.params))
+        return B.orthrus_page_tables_update(self.ctx, self.params, seq_lens, new_lens, page_table, free_pages, free_state,
+                                            granted, token_starts, slot_map, 0 if slot_map is None else slot_map.numel(),
+                                            ws, stream)
+
+    def store_kv(self, k_new, v_new, slot_map, k_pool, v_pool, num_valid=None, stream=None):
+        """Copies packed K/V rows [num_layers, N, H_kv, d] (N = slot_map's length) to their slots in every layer's cache."""
+        return B.orthrus_kv_store(self.ctx, self.params, slot_map.numel(), k_new, v_new, slot_map, num_valid, k_pool,
+                                  v_pool, stream)
 
     def attn_timing(self, enable: bool) -> None:
         """Attach HIP events to the attention kernels of the following attn() calls (or stop doing so)."""

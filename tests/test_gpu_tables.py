@@ -1,0 +1,222 @@
+"""GPU tests of orthrus_page_tables_update and orthrus_kv_store against the oracle: every table entry, slot, ring position
+and cache byte must be identical, and what the calls do not own must be left as it was."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def _rt():
+    from paper_2605_12825_amd import runtime
+    return runtime
+
+
+def _step(**kw):
+    full = dict(batch=1, num_q_heads=2, num_kv_heads=2, head_dim=64, block_k=1, page_size=16, max_pages_per_seq=4,
+                max_seq_len=64, num_pages=8)
+    full.update(kw)
+    return _rt().DecodeStep(**full)
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _update(step, old, new, table, ring, state, slots):
+    B = table.shape[0]
+    t, r, s, m = _dev(table), _dev(ring), _dev(state), _dev(slots)
+    granted, starts = torch.full((B,), -7, dtype=torch.int32, device="cuda"), torch.full((B + 1,), -7, dtype=torch.int32, device="cuda")
+    step.update_page_tables(_dev(old), _dev(new), t, r, s, granted, starts, m)
+    torch.cuda.synchronize()
+    return [x.cpu().numpy() for x in (granted, starts, t, r, s, m)], step.device_error()
+
+
+def _check(old, new, table, ring, state, P, bound, slots):
+    old, new = np.asarray(old, np.int32), np.asarray(new, np.int32)
+    step = _step(batch=len(old), page_size=P, max_pages_per_seq=table.shape[1], max_seq_len=bound, num_pages=ring.size)
+    got, err = _update(step, old, new, table, ring, state, slots)
+    step.close()
+    t, r, s, m = table.copy(), ring.copy(), state.copy(), slots.copy()
+    granted, starts, status = oracle.page_tables_update(old, new, t, r, s, P, bound, slots.size, m)
+    for name, a, b in zip(("granted", "starts", "table", "ring", "state", "slots"), got, (granted, starts, t, r, s, m)):
+        np.testing.assert_array_equal(a, b, err_msg=name)
+    assert err == status
+    return granted, t, r, s
+
+
+def _tables(rng, old, width, P, spare, holes=0.0):
+    """Rows mapped for their cached tokens (with holes, if asked), the other pages in the ring."""
+    B = len(old)
+    held = [(int(o) + P - 1) // P for o in old]
+    pages = sum(held) + spare
+    perm = rng.permutation(pages).astype(np.int32)
+    table = np.full((B, width), -1, np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = perm[at:at + h]
+        at += h
+    ring = np.full(pages, -1, np.int32)
+    head = int(rng.integers(pages))
+    ring[(head + np.arange(spare)) % pages] = perm[at:]
+    return table, ring, np.array([head, spare], np.int32)
+
+
+@pytest.mark.parametrize("batch", [1, 2, 63, 64, 65, 1000, 1024, 1025, 3000])
+@pytest.mark.parametrize("most", [1, 17, 300])
+def test_growth_and_return(batch, most):
+    rng = np.random.default_rng(batch * 7 + most)
+    P = int(rng.choice([16, 32, 128]))
+    old = rng.integers(0, 200, batch)
+    new = rng.integers(0, most + 1, batch)
+    new[rng.random(batch) < 0.2] = -1
+    width = (200 + most) // P + 3
+    table, ring, state = _tables(rng, old, width, P, spare=batch * (most // P + 2))
+    _check(old, new, table, ring, state, P, width * P, np.full(int(np.maximum(new, 0).sum()) + 9, -9, np.int32))
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 4095, 4096, 4097, 70000])
+@pytest.mark.parametrize("L", [0, 1, 16, 12345])
+def test_one_long_sequence(n, L):
+    rng = np.random.default_rng(n + L)
+    width = (n + L) // 16 + 2
+    table, ring, state = _tables(rng, [L], width, 16, spare=n // 16 + 5)
+    _check([L], [n], table, ring, state, 16, n + L, np.full(n, -9, np.int32))
+
+
+def test_nothing_to_do_and_every_sequence_over():
+    rng = np.random.default_rng(1)
+    old = rng.integers(0, 100, 40)
+    table, ring, state = _tables(rng, old, 9, 16, spare=3)
+    _check(old, np.zeros(40), table, ring, state, 16, 144, np.full(4, -9, np.int32))
+    _, t, _, s = _check(old, np.full(40, -1), table, ring, state, 16, 144, np.full(4, -9, np.int32))
+    assert (t == -1).all() and s[1] == ring.size
+
+
+def test_entries_mapped_ahead_and_holes():
+    """A row that is mapped further than its length (a block that was not all kept) and rows with holes in any place."""
+    rng = np.random.default_rng(2)
+    B, P, width = 50, 16, 700
+    old = rng.integers(0, 300, B)
+    table, ring, state = _tables(rng, old + 60, width, P, spare=B * 660)
+    for b in range(B):
+        if b % 3 == 1:     # pages missing in the middle of the new range
+            first = (old[b] + P - 1) // P
+            gone = first + rng.integers(0, 4, 2)
+            table[b, gone] = -1
+        if b % 3 == 2:     # ids that no pool has
+            table[b, (old[b] + P - 1) // P:] = rng.choice([-5, 1 << 30, -2 ** 31], width - (old[b] + P - 1) // P)
+    new = rng.integers(1, 100, B)
+    new[::7] = 10000
+    new[5::9] = -1
+    _check(old, new, table, ring, state, P, width * P, np.full(int(np.maximum(new, 0).sum()) + 3, -9, np.int32))
+
+
+def test_short_ring_grants_the_first_ones():
+    rng = np.random.default_rng(3)
+    for spare in (0, 1, 7, 30):
+        old, new = rng.integers(0, 64, 30), rng.integers(1, 80, 30)
+        old[10], new[10] = 3, 5          # lacks nothing
+        new[20] = -1
+        table, ring, state = _tables(rng, old, 12, 16, spare=spare)
+        granted, _, _, _ = _check(old, new, table, ring, state, 16, 192, np.full(3000, -9, np.int32))
+        assert granted[10] == 5
+
+
+def test_bad_lengths_torn_pages_bad_ring_and_short_slot_map():
+    rng = np.random.default_rng(4)
+    old, new = np.array([-1, 5, 140, 7, 20, 0, 33, -9]), np.array([3, 2 ** 31 - 1, 10, 4, 6, 9, 40, -1])
+    table, ring, state = _tables(rng, np.maximum(old, 0), 9, 16, spare=9)
+    table[3, 0] = -1                     # its cached tokens' page
+    _check(old, new, table, ring, state, 16, 144, np.full(100, -9, np.int32))
+    _check(old, new, table, ring, state, 16, 144, np.full(11, -9, np.int32))     # slots run out
+    ring[(state[0] + 1) % ring.size] = ring.size                                 # a page that does not exist
+    _check(old, new, table, ring, state, 16, 144, np.full(100, -9, np.int32))
+    for s in ([-5, 9], [10 ** 9, 9], [3, -4], [3, 10 ** 9]):                     # a ring state out of range
+        st = np.array(s, np.int32)
+        want = np.array([s[0] % ring.size, 0], np.int32)
+        assert want[0] >= 0
+        _check(old, new, table, ring, st, 16, 144, np.full(100, -9, np.int32))
+
+
+def test_pages_come_back_once_too_often():
+    table = np.array([[0, 1, 2], [0, 1, 2], [-1, -1, -1]], np.int32)
+    ring, state = np.arange(6, dtype=np.int32), np.array([4, 2], np.int32)
+    _check([48, 48, 0], [-1, -1, 20], table, ring, state, 16, 48, np.full(30, -9, np.int32))
+
+
+def test_steps_in_a_row_keep_every_page():
+    rng = np.random.default_rng(6)
+    B, width, P, N = 24, 20, 16, 300
+    step = _step(batch=B, max_pages_per_seq=width, max_seq_len=width * P, num_pages=N)
+    t, r, s = _dev(np.full((B, width), -1, np.int32)), _dev(rng.permutation(N).astype(np.int32)), _dev(np.array([250, N], np.int32))
+    m, granted = torch.zeros(4000, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    starts, lens = torch.zeros(B + 1, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    for i in range(50):
+        new = torch.from_numpy(np.where(rng.random(B) < 0.15, -1, rng.integers(0, 60, B)).astype(np.int32)).cuda()
+        step.update_page_tables(lens, new, t, r, s, granted, starts, m)
+        lens.copy_(torch.where(new < 0, 0, lens + granted))
+    torch.cuda.synchronize()
+    step.device_error()
+    step.close()
+    table, ring, (head, count) = t.cpu().numpy(), r.cpu().numpy(), s.cpu().tolist()
+    free = [int(ring[(head + i) % N]) for i in range(count)]
+    assert sorted(free + table[table >= 0].tolist()) == list(range(N))
+    for b, L in enumerate(lens.cpu().tolist()):
+        assert (table[b, :(L + P - 1) // P] >= 0).all()
+
+
+# ---- the store
+
+@pytest.mark.parametrize("layers,N,H,d,P", [(1, 1, 8, 128, 16), (3, 37, 2, 64, 16), (2, 700, 4, 128, 32), (1, 3001, 1, 64, 64),
+                                            (1, 5, 160, 128, 16)])
+@pytest.mark.parametrize("fused", [False, True])
+def test_store(layers, N, H, d, P, fused):
+    rng = np.random.default_rng(N + H)
+    pages = N // P + 3
+    bits = lambda *s: rng.integers(0, 1 << 16, s, dtype=np.uint16)  # noqa: E731
+    kp, vp = bits(layers, pages, H, P, d), bits(layers, pages, H, P, d)
+    slots = rng.permutation(pages * P)[:N].astype(np.int32)
+    slots[rng.random(N) < 0.1] = -1
+    if N > 4:
+        slots[2] = -2 ** 31
+    D = _rt().to_device_bits
+    extra = 3 * H if fused else 0
+    rows = bits(layers, N, 2 * H + extra, d) if fused else None
+    k, v = (rows[:, :, extra:extra + H], rows[:, :, extra + H:]) if fused else (bits(layers, N, H, d), bits(layers, N, H, d))
+    row = (2 * H + extra) * d if fused else 0
+    step = _step(num_q_heads=H, num_kv_heads=H, head_dim=d, page_size=P, num_pages=pages, num_layers=layers,
+                 pool_strides=(pages * H * P * d, H * P * d, P * d, d), block_strides=(0, 0, row, 0, 0))
+    dkp, dvp, ds = D(kp), D(vp), _dev(slots)
+    if fused:
+        x = D(rows)
+        dk, dv = x[:, :, extra:extra + H], x[:, :, extra + H:]
+    else:
+        dk, dv = D(k), D(v)
+    for valid in (N // 2, None):
+        step.store_kv(dk, dv, ds, dkp, dvp, None if valid is None else _dev(np.array([valid], np.int32)))
+        torch.cuda.synchronize()
+        assert oracle.kv_store(k, v, slots, kp, vp, valid) == 0 == step.device_error()
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dkp), kp)
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dvp), vp)
+    step.close()
+
+
+def test_store_with_bad_slots_and_counts():
+    H, d, P, pages, N = 2, 64, 16, 4, 9
+    rng = np.random.default_rng(9)
+    bits = lambda *s: rng.integers(0, 1 << 16, s, dtype=np.uint16)  # noqa: E731
+    kp, vp, k, v = bits(1, pages, H, P, d), bits(1, pages, H, P, d), bits(1, N, H, d), bits(1, N, H, d)
+    slots = np.array([5, 64, 63, 2 ** 31 - 1, -1, 0, 17, 40, 8], np.int32)
+    D = _rt().to_device_bits
+    step = _step(num_q_heads=H, num_kv_heads=H, head_dim=d, num_pages=pages)
+    dkp, dvp = D(kp), D(vp)
+    for valid in (-3, 0, 1, 10 ** 9):
+        step.store_kv(D(k), D(v), _dev(slots), dkp, dvp, _dev(np.array([valid], np.int32)))
+        torch.cuda.synchronize()
+        assert oracle.kv_store(k, v, slots, kp, vp, valid) == step.device_error()
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dkp), kp)
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dvp), vp)
+    step.close()

@@ -1,0 +1,124 @@
+"""Refusals of the sampling, page-table and store entry points: found on the host before anything touches a device, so they
+are checked here with addresses that are never read (a call that were not refused would end in ORTHRUS_EHIP)."""
+import ctypes
+
+import pytest
+
+import paper_2605_12825_amd as orthrus
+from paper_2605_12825_amd import binding as B
+
+A = 1 << 20      # an aligned address
+_keep = ctypes.create_string_buffer(1 << 12)
+CTX = ctypes.addressof(_keep)
+
+
+class _Space:
+    def __init__(self, nbytes, at=A):
+        self.nbytes, self.at = nbytes, at
+
+    def data_ptr(self):
+        return self.at
+
+
+def _params(**kw):
+    full = dict(batch=3, num_q_heads=8, num_kv_heads=2, head_dim=128, block_k=4, page_size=16, max_pages_per_seq=9,
+                max_seq_len=100, num_pages=50, vocab=1000)
+    full.update(kw)
+    return orthrus.make_params(**full)
+
+
+def _sample(p=None, ctx=CTX, logits_type=0, stride=0, ws=None, **kw):
+    a = dict(logits=A, temperature=A, top_k=A, top_p=A, min_p=A, u=A, tokens=A, logprobs=A)
+    a.update(kw)
+    return orthrus.orthrus_sample_tokens(ctx, p or _params(), logits_type, a["logits"], stride, a["temperature"], a["top_k"],
+                                         a["top_p"], a["min_p"], a["u"], a["tokens"], a["logprobs"],
+                                         ws or _Space(1 << 40), 0, check=False)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ctx=None), B.ORTHRUS_EINVAL), (dict(logits=None), B.ORTHRUS_EINVAL), (dict(temperature=None), B.ORTHRUS_EINVAL),
+    (dict(u=None), B.ORTHRUS_EINVAL), (dict(tokens=None), B.ORTHRUS_EINVAL), (dict(logits_type=3), B.ORTHRUS_EINVAL),
+    (dict(logits_type=-1), B.ORTHRUS_EINVAL), (dict(stride=999), B.ORTHRUS_EINVAL), (dict(stride=-1), B.ORTHRUS_EINVAL),
+    (dict(logits=A + 2), B.ORTHRUS_EINVAL), (dict(logits=A + 1, logits_type=1), B.ORTHRUS_EINVAL),
+    (dict(u=A + 2), B.ORTHRUS_EINVAL), (dict(logprobs=A + 1), B.ORTHRUS_EINVAL), (dict(top_k=A + 3), B.ORTHRUS_EINVAL),
+    (dict(p=_params(vocab=0)), B.ORTHRUS_EINVAL), (dict(p=_params(vocab=(1 << 21) + 1)), B.ORTHRUS_EUNSUPPORTED),
+    (dict(p=_params(block_k=33)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(block_k=0)), B.ORTHRUS_EINVAL),
+    (dict(p=_params(batch=-1)), B.ORTHRUS_EINVAL), (dict(p=_params(batch=70000)), B.ORTHRUS_EUNSUPPORTED),
+    (dict(p=_params(batch=0)), B.ORTHRUS_OK),
+])
+def test_sample_tokens(kw, status):
+    assert _sample(**kw) == status
+
+
+def _filtered(p=None, ctx=CTX, logits_type=0, stride=0, ws=None, **kw):
+    names = ("ar_logits", "diff_logits", "temperature", "top_k", "top_p", "min_p", "draft_tokens", "accept_u", "gumbel",
+             "k_blk_ar", "v_blk_ar", "k_pool", "v_pool", "page_table", "seq_lens", "accept_len", "num_committed",
+             "out_tokens", "next_anchor")
+    a = dict.fromkeys(names, A)
+    a.update(kw)
+    v = [a[n] for n in names]
+    return orthrus.orthrus_filtered_consensus_commit(ctx, p or _params(), logits_type, v[0], v[1], stride, *v[2:],
+                                                     workspace=ws or _Space(1 << 40), stream=0, check=False)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ctx=None), B.ORTHRUS_EINVAL), (dict(diff_logits=None), B.ORTHRUS_EINVAL), (dict(gumbel=None), B.ORTHRUS_EINVAL),
+    (dict(accept_u=None), B.ORTHRUS_EINVAL), (dict(temperature=None), B.ORTHRUS_EINVAL), (dict(k_blk_ar=None), B.ORTHRUS_EINVAL),
+    (dict(v_pool=None), B.ORTHRUS_EINVAL), (dict(seq_lens=None), B.ORTHRUS_EINVAL), (dict(next_anchor=None), B.ORTHRUS_EINVAL),
+    (dict(stride=5), B.ORTHRUS_EINVAL), (dict(logits_type=9), B.ORTHRUS_EINVAL), (dict(k_pool=A + 8), B.ORTHRUS_EINVAL),
+    (dict(diff_logits=A + 2), B.ORTHRUS_EINVAL), (dict(gumbel=A + 2), B.ORTHRUS_EINVAL),
+    (dict(p=_params(vocab=1 << 22)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(num_layers=0)), B.ORTHRUS_EINVAL),
+    (dict(p=_params(num_layers=70000)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(page_size=24)), B.ORTHRUS_EUNSUPPORTED),
+    (dict(ws=_Space(16)), B.ORTHRUS_EWORKSPACE), (dict(ws=_Space(1 << 40, A + 128)), B.ORTHRUS_EWORKSPACE),
+    (dict(p=_params(batch=0)), B.ORTHRUS_OK),
+])
+def test_filtered_consensus(kw, status):
+    assert _filtered(**kw) == status
+
+
+def _tables(p=None, ctx=CTX, max_tokens=10, ws=None, **kw):
+    names = ("seq_lens", "new_lens", "page_table", "free_pages", "free_state", "granted", "token_starts", "slot_map")
+    a = dict.fromkeys(names, A)
+    a.update(kw)
+    return orthrus.orthrus_page_tables_update(ctx, p or _params(), *[a[n] for n in names], max_tokens, ws or _Space(1 << 30), 0,
+                                              check=False)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ctx=None), B.ORTHRUS_EINVAL), (dict(seq_lens=None), B.ORTHRUS_EINVAL), (dict(free_state=None), B.ORTHRUS_EINVAL),
+    (dict(slot_map=None), B.ORTHRUS_EINVAL), (dict(token_starts=None), B.ORTHRUS_EINVAL), (dict(max_tokens=-1), B.ORTHRUS_EINVAL),
+    (dict(max_tokens=1 << 31), B.ORTHRUS_EUNSUPPORTED), (dict(granted=A + 2), B.ORTHRUS_EINVAL),
+    (dict(p=_params(max_seq_len=9 * 16 + 1)), B.ORTHRUS_EINVAL), (dict(p=_params(max_seq_len=-1)), B.ORTHRUS_EINVAL),
+    (dict(p=_params(num_pages=1 << 27)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(num_pages=0)), B.ORTHRUS_EINVAL),
+    (dict(ws=_Space(8)), B.ORTHRUS_EWORKSPACE), (dict(ws=_Space(1 << 30, A + 4)), B.ORTHRUS_EWORKSPACE),
+])
+def test_page_tables(kw, status):
+    assert _tables(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ctx=None), B.ORTHRUS_EINVAL), (dict(k=None), B.ORTHRUS_EINVAL), (dict(slots=None), B.ORTHRUS_EINVAL),
+    (dict(vp=None), B.ORTHRUS_EINVAL), (dict(n=-1), B.ORTHRUS_EINVAL), (dict(k=A + 8), B.ORTHRUS_EINVAL),
+    (dict(slots=A + 2), B.ORTHRUS_EINVAL), (dict(count=A + 1), B.ORTHRUS_EINVAL), (dict(p=_params(num_layers=0)), B.ORTHRUS_EINVAL),
+    (dict(p=_params(num_pages=1 << 27)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(head_dim=96)), B.ORTHRUS_EUNSUPPORTED),
+    (dict(p=_params(blk_stride_row=100)), B.ORTHRUS_EUNSUPPORTED), (dict(n=0), B.ORTHRUS_OK),
+])
+def test_kv_store(kw, status):
+    a = dict(ctx=CTX, p=_params(), n=5, k=A, v=A, slots=A, count=None, kp=A, vp=A)
+    a.update(kw)
+    assert orthrus.orthrus_kv_store(a["ctx"], a["p"], a["n"], a["k"], a["v"], a["slots"], a["count"], a["kp"], a["vp"], 0,
+                                    check=False) == status
+
+
+def test_workspace_queries():
+    for f in (orthrus.orthrus_sample_workspace_bytes, orthrus.orthrus_filtered_workspace_bytes):
+        assert f(_params()) >= 0 and f(_params(batch=0)) >= 0
+        with pytest.raises(orthrus.OrthrusError):
+            f(_params(vocab=1 << 22))
+    # per row and view what its filters keep (24 bytes), three words per sequence
+    assert orthrus.orthrus_filtered_workspace_bytes(_params()) >= 2 * 12 * 24 + 3 * 3 * 4
+    assert orthrus.orthrus_page_tables_workspace_bytes(_params()) >= (3 * 3 + 2) * 4
+    with pytest.raises(orthrus.OrthrusError):
+        orthrus.orthrus_page_tables_workspace_bytes(_params(max_seq_len=9 * 16 + 1))
+    with pytest.raises(orthrus.OrthrusError):
+        orthrus.orthrus_page_tables_workspace_bytes(_params(num_pages=1 << 27))
