@@ -738,6 +738,7 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
     if (p->batch == 0) return ORTHRUS_OK;
     const int64_t rows = (int64_t)p->batch * p->block_k;
     const size_t need = orthrus::filter_workspace_bytes(rows, p->vocab, 1);
+    if (rows * 2 * (((int64_t)p->vocab + 2047) / 2048 + 1) > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
     if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return ORTHRUS_EWORKSPACE;
     orthrus::FilterArgs a = filter_args(p, logits_type, logits, nullptr, logits_stride_row, temperature, top_k, top_p, min_p);
     a.u = u; a.tokens = tokens; a.logprobs = logprobs;

@@ -9,7 +9,12 @@
 // the weights are taken in 64 bits, because a token next to a cut or to the uniform number is decided by the last bits
 // of a sum over the vocabulary: with a sum good to 1e-7 one row in a few thousand would draw another token.
 //
-//   filter_row_kernel      one workgroup per row (and view).
+//   filter_scan_kernel     grid (row, chunk): the one pass over the logits.  Leaves per chunk its maximum, the sum of its
+//                          weights and a list of its largest logits, some hundred of them.
+//   filter_pick_kernel     one workgroup per row (and view): cuts and token from the lists of its chunks, which hold every
+//                          logit down to the least that one of them lists; a row without filters from the chunks' sums and
+//                          one chunk read again.  A row whose cut lies below the lists goes to the next kernel.
+//   filter_wide_kernel     one workgroup per such row, several passes over it.
 //   filtered_draw_kernel   one workgroup per sequence: keep decisions, the replacement drawn from the first rejected row.
 //   filtered_commit_kernel grid (sequence, layer): outputs and the commit, as sample_commit_kernel does it.
 #include "orthrus_internal.h"
@@ -19,9 +24,6 @@
 namespace orthrus {
 
 typedef unsigned long long u64;
-
-constexpr int kRowThreads = 1024;
-constexpr int kBins = 2048;
 
 // ---- logits, their order and their weights
 
@@ -52,14 +54,19 @@ __device__ __forceinline__ uint32_t order_key(float x)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// 2^t for t <= 0: t = n + f with n whole and |f| <= 1/2, 2^f by a polynomial in f that interpolates 2^f at the Chebyshev
-// nodes of [-1/2, 1/2] (off by 4e-14 at most, exactly 1 at 0), n added to the exponent.  Below 2^-1000: 2^-1000.
-__device__ __forceinline__ double exp2_neg(double t)
+// Weight of a logit d <= 0 away from the row's maximum: 2^(d * scale) with scale = log2(e) / T.  d * scale = n + f with n whole and
+// |f| <= 1/2; 2^f by a polynomial that interpolates it at the Chebyshev nodes of [-1/2, 1/2] (off by 4e-14 at most, exactly 1
+// at 0), n added to the exponent.  d is exact and the product rounded once at f, so equal logits weigh exactly 1 at any
+// temperature.  Weights end at 2^-1000 (d = floor).
+struct Scale {
+    double scale, floor;
+};
+__device__ __forceinline__ double weight(double d, const Scale &t)
 {
-    t = fmax(t, -1000.0);
+    d = fmax(d, t.floor);
     constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to a whole number, in the low bits
-    const double s = t + kRound;
-    const double f = t - (s - kRound);
+    const double s = fma(d, t.scale, kRound);
+    const double f = fma(d, t.scale, -(s - kRound));
     double q = 0x1.b63880a30e9ffp-24;
     q = fma(q, f, 0x1.63d136366db24p-20);
     q = fma(q, f, 0x1.ffcb9515a8016p-17);
@@ -72,12 +79,10 @@ __device__ __forceinline__ double exp2_neg(double t)
     const double p = fma(q, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(s) << 20), __double2loint(p));
 }
-
-// Weight of a logit relative to the row's maximum; scale = log2(e) / T.
-__device__ __forceinline__ double weight(float x, float top, double scale) { return exp2_neg(((double)x - (double)top) * scale); }
+__device__ __forceinline__ double weight(float x, float top, const Scale &t) { return weight((double)x - (double)top, t); }
 
 struct RowFilter {
-    double scale;  // log2(e) / T
+    Scale t;
     int top_k;     // 0: off
     double top_p;  // >= 1: off
     double min_p;  // 0: off
@@ -90,7 +95,8 @@ __device__ __forceinline__ RowFilter row_filter(const FilterArgs &a, int b)
     const int k = a.top_k ? a.top_k[b] : 0;
     const float p = a.top_p ? a.top_p[b] : 1.f, m = a.min_p ? a.min_p[b] : 0.f;
     const bool greedy = !(t > 0.f);  // T <= 0 or NaN: the largest logit, the lowest index among equals
-    f.scale = greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)fminf(t, FLT_MAX);
+    f.t.scale = greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)fminf(t, FLT_MAX);
+    f.t.floor = -1000.0 / f.t.scale;
     f.top_k = greedy ? 1 : k > 0 && k < a.vocab ? k : 0;
     f.top_p = greedy || !(p < 1.f) ? 1.0 : fmax((double)p, 0.0);
     f.min_p = greedy || !(m > 0.f) ? 0.0 : (double)fminf(m, 1.f);
@@ -112,245 +118,884 @@ struct Crossing {
     u64 at;       // the bin's own amount
 };
 
-struct RowShared {
-    u64 bins[kBins];
-    u64 wave_sum[kRowThreads / 64];
-    double wave_z[kRowThreads / 64];
-    float wave_max[kRowThreads / 64];
-    int wave_alive[kRowThreads / 64];
+// Bins of a workgroup of THREADS, PER of them to a thread.  Every function contains barriers.
+template <int THREADS, int PER> struct Bins {
+    static constexpr int kCount = THREADS * PER;
+    u64 amount[kCount];
+    u64 wave_sum[THREADS / 64];
     Crossing hit;
-};
 
-__device__ __forceinline__ void clear_bins(RowShared &s, int tid)
-{
-    __syncthreads();
-    for (int i = tid; i < kBins; i += kRowThreads) s.bins[i] = 0;
-    __syncthreads();
-}
-
-// Contains barriers; target >= 1.
-__device__ __forceinline__ Crossing find_crossing(RowShared &s, int tid, u64 target)
-{
-    static_assert(kBins == 2 * kRowThreads, "two bins to a thread");
-    __syncthreads();
-    const u64 h0 = s.bins[2 * tid], h1 = s.bins[2 * tid + 1];
-    u64 sum = h0 + h1;
-    const int lane = tid & 63;
+    __device__ __forceinline__ void clear(int tid)
+    {
+        __syncthreads();
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const u64 o = __shfl_up(sum, off);
-        if (lane >= off) sum += o;
+        for (int i = 0; i < PER; ++i) amount[i * THREADS + tid] = 0;
+        __syncthreads();
     }
-    if (lane == 63) s.wave_sum[tid >> 6] = sum;
-    if (tid == 0) s.hit = {-1, 0, 0};
-    __syncthreads();
-    u64 before = sum - h0 - h1;
-    for (int w = 0; w < (tid >> 6); ++w) before += s.wave_sum[w];
-    if (before < target && target <= before + h0) s.hit = {2 * tid, before, h0};
-    else if (before + h0 < target && target <= before + h0 + h1) s.hit = {2 * tid + 1, before + h0, h1};
-    __syncthreads();
-    return s.hit;
-}
+
+    // target >= 1
+    __device__ __forceinline__ Crossing crossing(int tid, u64 target)
+    {
+        __syncthreads();
+        u64 h[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { h[i] = amount[tid * PER + i]; sum += h[i]; }
+        u64 run = sum;
+        const int lane = tid & 63;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const u64 o = __shfl_up(run, off);
+            if (lane >= off) run += o;
+        }
+        if (lane == 63) wave_sum[tid >> 6] = run;
+        if (tid == 0) hit = {-1, 0, 0};
+        __syncthreads();
+        u64 before = run - sum;
+        for (int w = 0; w < (tid >> 6); ++w) before += wave_sum[w];
+        if (before < target && target <= before + sum) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (before < target && target <= before + h[i]) hit = {tid * PER + i, before, h[i]};
+                before += h[i];
+            }
+        }
+        __syncthreads();
+        return hit;
+    }
+
+    __device__ __forceinline__ u64 sum_of(int tid, u64 v)
+    {
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+        __syncthreads();
+        if ((tid & 63) == 0) wave_sum[tid >> 6] = v;
+        __syncthreads();
+        v = 0;
+        for (int w = 0; w < THREADS / 64; ++w) v += wave_sum[w];
+        return v;
+    }
+};
 
 __device__ __forceinline__ u64 to_fixed(double w, double unit) { return (u64)(w * unit + 0.5); }
 
-// One row in the hands of a workgroup.  Every method is called by all threads and contains barriers.
-template <int DT> struct RowScan {
-    RowShared &s;
-    const void *row;
-    int vocab, tid, idx_shift;   // idx_shift: tokens to a bin of the searches by index
-    float top;
-    double scale, unit;          // unit: fixed-point value of the weight 1
-    RowCut cut;
+// ---- the pass over the logits
 
-    __device__ __forceinline__ float at(int i) const { return logit<DT>(row, i); }
-    __device__ __forceinline__ double weight_of(float x) const { return weight(x, top, scale); }
+constexpr int kScanThreads = 256;
 
-    // Maximum, number of logits above -inf.
-    __device__ __forceinline__ int find_top()
-    {
-        top = -INFINITY;
-        int alive = 0;
-        for (int i = tid; i < vocab; i += kRowThreads) {
-            const float x = at(i);
-            top = fmaxf(top, x);
-            alive += x > -INFINITY;
-        }
+template <int DT> struct Vector {
+    static constexpr int kCount = DT == 0 ? 4 : 8;  // logits to 16 bytes
+};
+
+// The logits of 16 bytes as they are.
+template <int DT> __device__ __forceinline__ void unpack(uint4 q, float *x)
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-            top = fmaxf(top, __shfl_xor(top, off));
-            alive += __shfl_xor(alive, off);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == 0) {
+            x[i] = __uint_as_float(w[i]);
+        } else if constexpr (DT == 1) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const uint16_t lo = (uint16_t)w[i], hi = (uint16_t)(w[i] >> 16);
+            x[2 * i] = (float)__builtin_bit_cast(_Float16, lo);
+            x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, hi);
         }
-        if ((tid & 63) == 0) { s.wave_max[tid >> 6] = top; s.wave_alive[tid >> 6] = alive; }
-        __syncthreads();
-        alive = 0;
-        for (int w = 0; w < kRowThreads / 64; ++w) { top = fmaxf(top, s.wave_max[w]); alive += s.wave_alive[w]; }
-        return alive;
     }
+}
 
-    // The sum of all weights sets the fixed point: sums stay below 2^61.
-    __device__ __forceinline__ void find_unit()
+// A chunk of a row: kScanThreads * PER logits from a 16-byte boundary on, so that all but a row's first and last vector are
+// loaded whole.  `first` is the row index of its first logit (negative in a row that starts inside a vector).
+template <int DT, int PER> struct Chunk {
+    static constexpr int kVec = Vector<DT>::kCount, kLoads = PER / kVec, kElems = kScanThreads * PER;
+    const void *row;
+    int first, vocab;
+
+    __device__ __forceinline__ Chunk(const void *r, int chunk, int v) : row(r), vocab(v)
     {
-        double z = 0.0;
-        for (int i = tid; i < vocab; i += kRowThreads) z += weight_of(at(i));
+        const int skew = (int)((uintptr_t)r / (16 / kVec)) & (kVec - 1);
+        first = chunk * kElems - skew;
+    }
+    __device__ __forceinline__ int index(int load, int tid) const { return first + (load * kScanThreads + tid) * kVec; }
+    // (raw: not cleaned)
+    __device__ __forceinline__ void load(int tid, float (&x)[PER]) const
+    {
+        const uint4 *at = (const uint4 *)((const char *)row + (int64_t)first * (16 / kVec)) + tid;
+        if (first >= 0 && first + kElems <= vocab) {
+            uint4 q[kLoads];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) q[u] = at[u * kScanThreads];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) unpack<DT>(q[u], &x[u * kVec]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const int i = index(u, tid);
+                if (i >= 0 && i + kVec <= vocab) {
+                    unpack<DT>(at[u * kScanThreads], &x[u * kVec]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < kVec; ++r)
+                        x[u * kVec + r] = i + r >= 0 && i + r < vocab ? raw_logit<DT>(row, i + r) : -INFINITY;
+                }
+            }
+        }
+    }
+};
+
+// Which rows need the sum of all their weights: those that neither top-k nor the greedy rule cuts.
+__device__ __forceinline__ bool wants_sum(const RowFilter &f) { return f.top_k == 0; }
+
+// GROUP lanes share one of the maxima whose least is the list's threshold: with n groups the list holds n logits at least and
+// about n * ln(n) in a row without order.
+template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThreads) filter_scan_kernel(const FilterArgs a)
+{
+    const int rr = blockIdx.x / a.chunks, chunk = blockIdx.x - rr * a.chunks, tid = threadIdx.x;
+    const int side = rr >= a.rows, row = rr - side * a.rows, lane = tid & 63, wave = tid >> 6;
+    if (blockIdx.x == 0 && tid == 0) a.unresolved[0] = 0;
+    const RowFilter f = row_filter(a, row / a.block_k);
+    const Chunk<DT, PER> c(logit_row<DT>(a, side, row), chunk, a.vocab);
+    float x[PER];
+    c.load(tid, x);
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) top = fmaxf(top, x[i]);
+#pragma unroll
+    for (int off = 1; off < GROUP; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+    float tau = top;
+#pragma unroll
+    for (int off = GROUP; off < 64; off <<= 1) {
+        top = fmaxf(top, __shfl_xor(top, off));
+        tau = fminf(tau, __shfl_xor(tau, off));
+    }
+    __shared__ float s_top[4], s_tau[4];
+    __shared__ double s_sum[4];
+    __shared__ int s_count;
+    if (lane == 0) { s_top[wave] = top; s_tau[wave] = tau; }
+    if (tid == 0) s_count = 0;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    tau = fminf(fminf(s_tau[0], s_tau[1]), fminf(s_tau[2], s_tau[3]));
+    // A NaN drops out of every maximum, comparison and weight below by itself; +inf takes the long way.
+    if (!(top > -INFINITY)) top = -INFINITY;
+    if (!(tau > -INFINITY)) tau = -INFINITY;
+    if (top == INFINITY) {
+        top = FLT_MAX;
+        tau = fminf(tau, FLT_MAX);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
+    }
+    // ---- the list: whatever reaches the threshold, in no order (what is made of it does not depend on one)
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += x[i] >= tau && x[i] > -INFINITY;
+    int before = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(before, off);
+        if (lane >= off) before += o;
+    }
+    int base = 0;
+    if (lane == 63) base = atomicAdd(&s_count, before);
+    base = __shfl(base, 63) + before - mine;
+    uint2 *list = a.lists + ((int64_t)rr * a.chunks + chunk) * a.list_cap;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (x[i] >= tau && x[i] > -INFINITY) {
+            if (base < a.list_cap) list[base] = make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, tid) + i % c.kVec);
+            ++base;
+        }
+    }
+    // ---- the weights, relative to the chunk's maximum
+    double sum = 0.0;
+    if (wants_sum(f) && top > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum += weight(x[i], top, f.t);
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
+    }
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        const int n = s_count;
+        ChunkStat r;
+        r.sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+        r.top = top;
+        r.tau = n <= a.list_cap ? tau : INFINITY;   // more equal ones than the list holds: nothing is listed
+        r.count = n <= a.list_cap ? n : 0;
+        a.stats[(int64_t)rr * a.chunks + chunk] = r;
+    }
+}
+
+// ---- cuts and token from the lists
+
+constexpr int kPickThreads = 256;
+constexpr int kPickEach = 12, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
+constexpr int kMaxChunks = 1024;
+
+struct PickShared {
+    Bins<kPickThreads, 4> bins;
+    uint32_t key[kPickEntries];
+    int index[kPickEntries];
+    float top[4], tau[4];
+    double z[4];
+    int count;
+    uint32_t token_key;
+};
+
+// The crossing of a running sum over entries ordered by `digit` (rising), ten bits at a time; an entry with amount 0 is not there.
+struct Picked {
+    uint32_t digit;
+    u64 before, here;   // amounts of smaller digits, of this one (0: not reached)
+};
+__device__ __forceinline__ Picked pick_digit(PickShared &s, int tid, const uint32_t (&digit)[kPickEach], const u64 (&amount)[kPickEach],
+                                             int bits, u64 target)
+{
+    Picked r = {0, 0, 0};
+    int shift = bits;
+#pragma unroll 1
+    do {
+        const int next = max(0, shift - 10);
+        s.bins.clear(tid);
+#pragma unroll
+        for (int e = 0; e < kPickEach; ++e)
+            if (amount[e] && (shift >= 32 || digit[e] >> shift == r.digit))
+                atomicAdd(&s.bins.amount[(digit[e] >> next) & ((1u << (shift - next)) - 1)], amount[e]);
+        const Crossing c = s.bins.crossing(tid, target - r.before);
+        if (c.bin < 0) return {0, 0, 0};
+        r.before += c.before;
+        r.here = c.at;
+        r.digit = r.digit << (shift - next) | (uint32_t)c.bin;
+        shift = next;
+    } while (shift > 0);
+    return r;
+}
+
+__device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+__device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
+
+template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThreads) filter_pick_kernel(const FilterArgs a)
+{
+    const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ PickShared s;
+    const RowFilter f = row_filter(a, row / a.block_k);
+    const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
+    // ---- the row's maximum, what its lists hold whole, the sum of its weights
+    ChunkStat st[kMaxChunks / kPickThreads];
+    float top = -INFINITY, tau = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
+        st[i] = {0.0, -INFINITY, -INFINITY, 0};
+        if (i * kPickThreads + tid < a.chunks) st[i] = stats[i * kPickThreads + tid];
+        top = fmaxf(top, st[i].top);
+        tau = fmaxf(tau, st[i].tau);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, off));
+        tau = fmaxf(tau, __shfl_xor(tau, off));
+    }
+    if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    top = fmaxf(fmaxf(s.top[0], s.top[1]), fmaxf(s.top[2], s.top[3]));
+    tau = fmaxf(fmaxf(s.tau[0], s.tau[1]), fmaxf(s.tau[2], s.tau[3]));
+    RowCut cut = {0.0, top, (float)f.min_p, 0u, 0x7fffffff};
+    int token = -1;
+    double own = 1.0;
+    bool resolved = true;
+    if (top > -INFINITY) {
+        double part[kMaxChunks / kPickThreads], z = 0.0;   // the chunks' sums, relative to the row's maximum
+#pragma unroll
+        for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
+            part[i] = st[i].sum * weight(st[i].top, top, f.t);
+            z += part[i];
+        }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
-        if ((tid & 63) == 0) s.wave_z[tid >> 6] = z;
+        if (lane == 0) s.z[wave] = z;
         __syncthreads();
-        z = 0.0;
-        for (int w = 0; w < kRowThreads / 64; ++w) z += s.wave_z[w];
-        unit = exp2((double)min(50, 60 - ilogb(z)));
+        z = s.z[0] + s.z[1] + s.z[2] + s.z[3];
+        if (f.top_k == 0 && f.top_p >= 1.0 && f.min_p == 0.0) {
+            // ---- no filter: the chunk at which the running sum crosses, and its logits once more
+            cut.z = z;
+            if constexpr (DRAW) {
+                const double unit = exp2((double)min(50, 60 - ilogb(z)));
+                s.bins.clear(tid);
+                u64 sum = 0;
+#pragma unroll
+                for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
+                    const u64 m = to_fixed(part[i], unit);
+                    s.bins.amount[i * kPickThreads + tid] = m;
+                    sum += m;
+                }
+                const u64 total = s.bins.sum_of(tid, sum);
+                const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
+                const u64 target = (u64)((double)u * (double)total) + 1;
+                const Crossing at = s.bins.crossing(tid, target);
+                const Chunk<DT, PER> c(logit_row<DT>(a, side, row), at.bin, a.vocab);
+                float x[PER];
+                c.load(tid, x);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
+                // 1024 bins: a vector of a thread to a bin (or as many of them as make 1024)
+                constexpr int kPerBin = c.kElems / 1024;
+                s.bins.clear(tid);
+                int last = -1;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const u64 m = x[i] > -INFINITY ? to_fixed(weight(x[i], top, f.t), unit) : 0;
+                    const int place = (i / c.kVec * kScanThreads + tid) * c.kVec + i % c.kVec;
+                    if (m) { atomicAdd(&s.bins.amount[place / kPerBin], m); last = max(last, place); }
+                }
+                Crossing in = s.bins.crossing(tid, target - at.before);
+                if (tid == 0) s.count = -1;
+                __syncthreads();
+                atomicMax(&s.count, last);
+                __syncthreads();
+                if (in.bin < 0) {   // the chunk's sum was rounded apart from its parts': its last token that weighs anything
+                    token = s.count;
+                } else {
+                    s.bins.clear(tid);
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const int place = (i / c.kVec * kScanThreads + tid) * c.kVec + i % c.kVec;
+                        if (place / kPerBin == in.bin)
+                            s.bins.amount[place % kPerBin] = x[i] > -INFINITY ? to_fixed(weight(x[i], top, f.t), unit) : 0;
+                    }
+                    token = in.bin * kPerBin + s.bins.crossing(tid, target - at.before - in.before).bin;
+                }
+                token += c.first;
+                own = weight(logit<DT>(c.row, token), top, f.t);
+            }
+        } else if (tau == INFINITY) {
+            resolved = false;
+        } else {
+            // ---- every logit down to tau
+            const bool whole = tau == -INFINITY;   // that is all there are
+            for (int c = wave; c < a.chunks; c += kPickThreads / 64) {
+                const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * a.list_cap;
+                const int n = stats[c].count;
+                for (int i = lane; i < n; i += 64) {
+                    const uint2 v = list[i];
+                    const float x = __uint_as_float(v.x);
+                    if (x >= tau) {
+                        const int at = atomicAdd(&s.count, 1);
+                        if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)v.y; }
+                    }
+                }
+            }
+            __syncthreads();
+            const int n = s.count;
+            resolved = n <= kPickEntries;
+            if (resolved) {
+                const uint32_t top_key = order_key(top + 0.f);
+                const int key_bits = bits_of(top_key - (whole ? order_key(-FLT_MAX) : order_key(tau + 0.f)));
+                const int index_bits = bits_of((uint32_t)(a.vocab - 1));
+                constexpr double kUnit = 0x1p50;
+                uint32_t fall[kPickEach], index[kPickEach];   // fall: distance from the top in order
+                u64 one[kPickEach], mass[kPickEach];
+#pragma unroll
+                for (int e = 0; e < kPickEach; ++e) {
+                    const int i = e * kPickThreads + tid;
+                    const bool there = i < n;
+                    const uint32_t key = there ? s.key[i] : top_key;
+                    fall[e] = top_key - key;
+                    index[e] = there ? (uint32_t)s.index[i] : 0u;
+                    one[e] = there;
+                    mass[e] = there ? to_fixed(weight(key_logit(key), top, f.t), kUnit) : 0;
+                }
+                uint32_t cut_fall = 0xffffffffu;
+                int cut_tie = 0x7fffffff;
+                // index of the n-th entry at `at`
+                auto nth_at = [&](uint32_t at, u64 nth) __attribute__((always_inline)) {
+                    u64 here[kPickEach];
+#pragma unroll
+                    for (int e = 0; e < kPickEach; ++e) here[e] = fall[e] == at ? one[e] : 0;
+                    return (int)pick_digit(s, tid, index, here, index_bits, nth).digit;
+                };
+                auto apply = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int e = 0; e < kPickEach; ++e)
+                        if (fall[e] > cut_fall || (fall[e] == cut_fall && (int)index[e] > cut_tie)) one[e] = mass[e] = 0;
+                };
+                if (f.top_k > 0) {
+                    if (f.top_k < n) {
+                        const Picked k = pick_digit(s, tid, fall, one, key_bits, (u64)f.top_k);
+                        cut_fall = k.digit;
+                        if (k.before + k.here > (u64)f.top_k) cut_tie = nth_at(k.digit, (u64)f.top_k - k.before);
+                        apply();
+                    } else {
+                        resolved = f.top_k == n || whole;
+                    }
+                }
+                u64 known = 0;
+#pragma unroll
+                for (int e = 0; e < kPickEach; ++e) known += mass[e];
+                known = s.bins.sum_of(tid, known);
+                if (resolved && f.top_p < 1.0) {
+                    const double all = f.top_k > 0 || whole ? (double)known : z * kUnit;
+                    const double target = fmax(1.0, ceil(f.top_p * all));
+                    resolved = target <= (double)known;
+                    if (resolved) {
+                        const Picked p = pick_digit(s, tid, fall, mass, key_bits, min(known, (u64)target));
+                        const u64 each = to_fixed(weight(key_logit(top_key - p.digit), top, f.t), kUnit);
+                        const u64 nth = (min(known, (u64)target) - p.before + each - 1) / each;
+                        if (p.digit < cut_fall) cut_tie = 0x7fffffff;
+                        cut_fall = p.digit;
+                        if (nth * each < p.here) cut_tie = min(cut_tie, nth_at(p.digit, nth));
+                        apply();
+                    }
+                }
+                if (f.min_p > 0.0) {
+                    // (without other cuts: what is not listed has to be below the line)
+                    if (f.top_k == 0 && f.top_p >= 1.0) resolved = whole || weight(tau, top, f.t) < f.min_p;
+#pragma unroll
+                    for (int e = 0; e < kPickEach; ++e)
+                        if (!(weight(key_logit(top_key - fall[e]), top, f.t) >= f.min_p)) mass[e] = 0;
+                }
+                if (resolved) {
+                    u64 total = 0;
+#pragma unroll
+                    for (int e = 0; e < kPickEach; ++e) total += mass[e];
+                    total = s.bins.sum_of(tid, total);
+                    cut.z = (double)total / kUnit;
+                    cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
+                    cut.tie = cut_tie;
+                    if constexpr (DRAW) {
+                        const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
+                        token = (int)pick_digit(s, tid, index, mass, index_bits, (u64)((double)u * (double)total) + 1).digit;
+#pragma unroll
+                        for (int e = 0; e < kPickEach; ++e)
+                            if (mass[e] && (int)index[e] == token) s.token_key = top_key - fall[e];
+                        __syncthreads();
+                        own = weight(key_logit(s.token_key), top, f.t);
+                    }
+                }
+            }
+        }
     }
+    if (tid == 0) {
+        if (!resolved) {
+            a.unresolved[1 + atomicAdd(a.unresolved, 1)] = rr;
+        } else if (DRAW) {
+            a.tokens[row] = token;
+            if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(own / cut.z);
+        } else {
+            a.cuts[rr] = cut;
+        }
+    }
+}
 
-    __device__ __forceinline__ u64 amount(float x, int i, double min_w) const
+// ---- rows whose cut lies below the lists
+
+// A whole row in the hands of a workgroup, read in blocks: a wave takes a block of 512 vectors, eight loads at a time, so
+// that a block's sum is one reduction.  Cuts are found by a histogram over 4096 steps of the logit (a hundredth of a
+// binade of the weight each) and then among the logits of one step, gathered in the second pass, which also sums what lies
+// above them; steps that hold more logits than the gather has room for (rows of equal logits) go digit by digit.
+constexpr int kWideThreads = 512, kWideWaves = kWideThreads / 64;
+constexpr int kWideEach = 8, kWideEntries = kWideThreads * kWideEach;
+constexpr int kSteps = 4096, kMaxBlocks = 1024;
+
+struct WideShared {
+    Bins<kWideThreads, 2> bins;
+    Bins<kWideThreads, kSteps / kWideThreads> steps;
+    u64 block[kMaxBlocks];
+    uint32_t key[kWideEntries];
+    int index[kWideEntries];
+    float top[kWideWaves], tau[kWideWaves];
+    double z[kWideWaves];
+    int count;
+};
+
+template <int DT> struct WideRow {
+    static constexpr int kVec = Vector<DT>::kCount, kBlock = 512 * kVec;
+    WideShared &s;
+    const void *row;
+    int vocab, skew, blocks, tid;
+    float top, step_scale;       // step of a logit: (top - x) * step_scale
+    Scale t;
+    double unit;                 // fixed-point value of the weight 1
+    RowCut cut;
+
+    __device__ __forceinline__ double weight_of(float x) const { return weight(x, top, t); }
+    __device__ __forceinline__ u64 mass_of(float x) const { return to_fixed(weight_of(x), unit); }
+    __device__ __forceinline__ int step_of(float x) const { return (int)fminf((top - x) * step_scale, (float)(kSteps - 1)); }
+    // weight of what the cut and min-p keep
+    __device__ __forceinline__ u64 kept_mass(float x, int i) const
     {
         const double w = weight_of(x);
-        return kept(cut, x, i) && w >= min_w ? to_fixed(w, unit) : 0;
+        return kept(cut, x, i) && w >= (double)cut.min_w ? to_fixed(w, unit) : 0;
     }
 
-    // Weight of what the cut keeps.
-    __device__ __forceinline__ u64 mass(double min_w)
+    // visit(x, index) for every logit of the wave's block
+    template <typename F> __device__ __forceinline__ void block_logits(int blk, F visit)
     {
-        u64 m = 0;
-        for (int i = tid; i < vocab; i += kRowThreads) m += amount(at(i), i, min_w);
+        const int lane = tid & 63;
+        uint4 q[8];
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) m += __shfl_xor(m, off);
-        __syncthreads();
-        if ((tid & 63) == 0) s.wave_sum[tid >> 6] = m;
-        __syncthreads();
-        m = 0;
-        for (int w = 0; w < kRowThreads / 64; ++w) m += s.wave_sum[w];
-        return m;
+        for (int u = 0; u < 8; ++u) {
+            const int i = (blk * 512 + u * 64 + lane) * kVec - skew;
+            q[u] = make_uint4(0, 0, 0, 0);
+            if (i >= 0 && i + kVec <= vocab) q[u] = *(const uint4 *)((const char *)row + (int64_t)i * (16 / kVec));
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = (blk * 512 + u * 64 + lane) * kVec - skew;
+            if (i >= 0 && i + kVec <= vocab) {
+                float x[kVec];
+                unpack<DT>(q[u], x);
+#pragma unroll
+                for (int r = 0; r < kVec; ++r) visit(clean_logit(x[r]), i + r);
+            } else {
+                for (int r = 0; r < kVec; ++r)
+                    if (i + r >= 0 && i + r < vocab) visit(logit<DT>(row, i + r), i + r);
+            }
+        }
+    }
+    template <typename F> __device__ __forceinline__ void each_logit(F visit)
+    {
+        for (int blk = tid >> 6; blk < blocks; blk += kWideWaves) block_logits(blk, visit);
     }
 
-    // The logit at which a sum in falling order reaches `target` (MASS: of weights, else of ones): eleven, eleven and ten
-    // bits of the order at a time.  Returns its key, what lies above it and what lies at it (nothing: never reached).
+    // s.block[]: the sums of amount_at(x, index) over the blocks; returns their sum.
+    template <typename F> __device__ __forceinline__ u64 sum_blocks(F amount_at)
+    {
+        __syncthreads();
+        u64 all = 0;
+        for (int blk = tid >> 6; blk < blocks; blk += kWideWaves) {
+            u64 sum = 0;
+            block_logits(blk, [&](float x, int i) __attribute__((always_inline)) { sum += amount_at(x, i); });
+            all += sum;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
+            if ((tid & 63) == 0) s.block[blk] = sum;
+        }
+        return s.bins.sum_of(tid, all);
+    }
+
+    // With s.block[] made of amount_at: the first index at which the running sum reaches the target (-1: none).
+    template <typename F> __device__ __forceinline__ int find_in_blocks(u64 target, F amount_at)
+    {
+        static_assert(kMaxBlocks == 2 * kWideThreads, "two blocks to a thread");
+        __syncthreads();
+        const u64 b0 = 2 * tid < blocks ? s.block[2 * tid] : 0, b1 = 2 * tid + 1 < blocks ? s.block[2 * tid + 1] : 0;
+        s.bins.clear(tid);
+        s.bins.amount[2 * tid] = b0;
+        s.bins.amount[2 * tid + 1] = b1;
+        const Crossing at = s.bins.crossing(tid, target);
+        if (at.bin < 0) return -1;
+        // the block's vectors, one to a thread
+        const int first = (at.bin * 512 + tid) * kVec - skew;
+        u64 part[kVec], sum = 0;
+#pragma unroll
+        for (int r = 0; r < kVec; ++r) {
+            const int i = first + r;
+            part[r] = i >= 0 && i < vocab ? amount_at(logit<DT>(row, i), i) : 0;
+            sum += part[r];
+        }
+        s.bins.clear(tid);
+        s.bins.amount[tid] = sum;
+        const Crossing in = s.bins.crossing(tid, target - at.before);
+        if (tid == in.bin) {
+            u64 run = at.before + in.before;
+            int found = -1;
+#pragma unroll
+            for (int r = 0; r < kVec; ++r) {
+                run += part[r];
+                if (found < 0 && run >= target) found = first + r;
+            }
+            s.count = found;
+        }
+        __syncthreads();
+        const int found = in.bin < 0 ? -1 : s.count;
+        __syncthreads();
+        return found;
+    }
+
+    __device__ __forceinline__ int nth_of_key(uint32_t key, u64 n)
+    {
+        auto there = [&](float x, int) __attribute__((always_inline)) { return (u64)(order_key(x) == key); };
+        sum_blocks(there);
+        const int i = find_in_blocks(n, there);
+        return i < 0 ? 0x7fffffff : i;
+    }
+
     struct Selected {
         uint32_t key;
-        u64 above, here;
+        u64 above, here;  // amounts above the logit, at it (0: never reached)
     };
-    template <bool MASS> __device__ __forceinline__ Selected select(u64 target)
+
+    // The logit at which a sum in falling order reaches the target, digit by digit.
+    template <bool MASS> __device__ __forceinline__ Selected select_digits(u64 target)
     {
         Selected r = {0, 0, 0};
         uint32_t prefix = 0;
 #pragma unroll 1
-        for (int level = 0; level < 3; ++level) {
-            const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-            clear_bins(s, tid);
-            for (int i = tid; i < vocab; i += kRowThreads) {
-                const float x = at(i);
-                const uint32_t falling = ~order_key(x);
-                if (x > -INFINITY && (level == 0 || falling >> (shift + bits) == prefix))
-                    atomicAdd(&s.bins[(falling >> shift) & ((1u << bits) - 1)], MASS ? to_fixed(weight_of(x), unit) : 1ull);
-            }
-            const Crossing c = find_crossing(s, tid, target - r.above);
+        for (int shift = 32; shift > 0;) {
+            const int next = max(0, shift - 12);
+            s.steps.clear(tid);
+            each_logit([&](float x, int) __attribute__((always_inline)) {
+                const uint32_t fall = ~order_key(x);
+                if (x > -INFINITY && (shift == 32 || fall >> shift == prefix))
+                    atomicAdd(&s.steps.amount[(fall >> next) & ((1u << (shift - next)) - 1)], MASS ? mass_of(x) : 1ull);
+            });
+            const Crossing c = s.steps.crossing(tid, target - r.above);
             if (c.bin < 0) return {0, 0, 0};
             r.above += c.before;
             r.here = c.at;
-            prefix = prefix << bits | (uint32_t)c.bin;
+            prefix = prefix << (shift - next) | (uint32_t)c.bin;
+            shift = next;
         }
         r.key = ~prefix;
         return r;
     }
 
-    // First token in index order at which the running sum of `amount_at(token)` reaches the target; -1: none.
-    template <typename F> __device__ __forceinline__ int first_index(u64 target, F amount_at)
+    // Cuts where the sum in falling order (MASS: of weights, else of ones) reaches the target.  `summed`: s.block[] then holds
+    // the kept weights, else it does not.  Returns the weight of what is kept without regard to min-p (0: not known).
+    template <bool MASS> __device__ __forceinline__ u64 cut_at(u64 target, bool &summed)
     {
-        clear_bins(s, tid);
-        for (int i = tid; i < vocab; i += kRowThreads) {
-            const u64 n = amount_at(i);
-            if (n) atomicAdd(&s.bins[i >> idx_shift], n);
+        summed = false;
+        s.steps.clear(tid);
+        each_logit([&](float x, int) __attribute__((always_inline)) {
+            if (x > -INFINITY) atomicAdd(&s.steps.amount[step_of(x)], MASS ? mass_of(x) : 1ull);
+        });
+        const Crossing c = s.steps.crossing(tid, target);
+        if (MASS && c.bin < 0) return 0;   // everything together does not reach it: no cut
+        if (c.bin < 0) return 0;
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        u64 over = 0;   // weight of the steps above
+        const double min_w = (double)cut.min_w;
+        sum_blocks([&](float x, int i) __attribute__((always_inline)) {
+            const int st = x > -INFINITY ? step_of(x) : kSteps;
+            if (st < c.bin) {
+                const double w = weight_of(x);
+                const u64 m = to_fixed(w, unit);
+                over += m;
+                return w >= min_w ? m : 0;
+            }
+            if (st == c.bin) {
+                const int at = atomicAdd(&s.count, 1);
+                if (at < kWideEntries) { s.key[at] = order_key(x); s.index[at] = i; }
+            }
+            return (u64)0;
+        });
+        over = s.bins.sum_of(tid, over);
+        const int n = s.count;
+        __syncthreads();
+        if (n > kWideEntries) {
+            const Selected r = select_digits<MASS>(target);
+            if (r.here == 0) return 0;
+            const u64 each = MASS ? mass_of(key_logit(r.key)) : 1;
+            const u64 nth = (target - r.above + each - 1) / each;
+            if (r.key > cut.key) cut.tie = 0x7fffffff;
+            cut.key = r.key;
+            if (nth * each < r.here) cut.tie = min(cut.tie, nth_of_key(r.key, nth));
+            return 0;
         }
-        const Crossing c = find_crossing(s, tid, target);
-        if (c.bin < 0 || idx_shift == 0) return c.bin;
-        const int base = c.bin << idx_shift, end = min(vocab, base + (1 << idx_shift));
-        clear_bins(s, tid);
-        for (int i = base + tid; i < end; i += kRowThreads) s.bins[i - base] = amount_at(i);
-        return base + find_crossing(s, tid, target - c.before).bin;
-    }
-
-    __device__ __forceinline__ int nth_of_key(uint32_t key, u64 n)
-    {
-        const int i = first_index(n, [&](int j) __attribute__((always_inline)) { return (u64)(order_key(at(j)) == key); });
-        return i < 0 ? 0x7fffffff : i;
-    }
-
-    __device__ __forceinline__ void cut_top_k(int k)
-    {
-        const Selected r = select<false>((u64)k);
-        cut.key = r.key;
-        if (r.above + r.here > (u64)k) cut.tie = nth_of_key(r.key, (u64)k - r.above);
-    }
-
-    // Shortest prefix of what is kept so far that holds the share p of its weight.
-    __device__ __forceinline__ void cut_top_p(double p)
-    {
-        const u64 target = max(1ull, (u64)ceil(p * (double)mass(0.0)));
-        const Selected r = select<true>(target);
-        if (r.here == 0) return;
-        const u64 each = to_fixed(weight_of(__uint_as_float(r.key >> 31 ? r.key & 0x7fffffffu : ~r.key)), unit);
-        const u64 n = (target - r.above + each - 1) / each;   // so many of the tokens at that logit
-        if (r.key > cut.key) cut.tie = 0x7fffffff;
-        cut.key = r.key;
-        if (n * each < r.here) cut.tie = min(cut.tie, nth_of_key(r.key, n));
+        // ---- among the gathered logits
+        uint32_t fall[kWideEach], index[kWideEach];
+        u64 mass[kWideEach];
+#pragma unroll
+        for (int e = 0; e < kWideEach; ++e) {
+            const int i = e * kWideThreads + tid;
+            fall[e] = i < n ? ~s.key[i] : 0xffffffffu;
+            index[e] = i < n ? (uint32_t)s.index[i] : 0u;
+            mass[e] = i < n ? mass_of(key_logit(~fall[e])) : 0;
+        }
+        auto digit_at = [&](bool by_index, uint32_t at, bool ones, u64 goal) __attribute__((always_inline)) {
+            Selected r = {0, 0, 0};
+            uint32_t prefix = 0;
+#pragma unroll 1
+            for (int shift = by_index ? bits_of((uint32_t)(vocab - 1)) : 32; shift > 0;) {
+                const int next = max(0, shift - 10);
+                s.bins.clear(tid);
+#pragma unroll
+                for (int e = 0; e < kWideEach; ++e) {
+                    const uint32_t d = by_index ? index[e] : fall[e];
+                    if (e * kWideThreads + tid < n && (!by_index || fall[e] == at) && (shift == 32 || d >> shift == prefix))
+                        atomicAdd(&s.bins.amount[(d >> next) & ((1u << (shift - next)) - 1)], ones ? 1ull : mass[e]);
+                }
+                const Crossing x = s.bins.crossing(tid, goal - r.above);
+                if (x.bin < 0) return Selected{0, 0, 0};
+                r.above += x.before;
+                r.here = x.at;
+                prefix = prefix << (shift - next) | (uint32_t)x.bin;
+                shift = next;
+            }
+            r.key = prefix;
+            return r;
+        };
+        const u64 goal = target - c.before;
+        const Selected r = digit_at(false, 0, !MASS, goal);
+        if (r.here == 0) return 0;
+        const u64 each = MASS ? mass_of(key_logit(~r.key)) : 1;
+        const u64 nth = (goal - r.above + each - 1) / each;
+        if (~r.key > cut.key) cut.tie = 0x7fffffff;
+        cut.key = ~r.key;
+        if (nth * each < r.here) cut.tie = min(cut.tie, (int)digit_at(true, r.key, true, nth).key);
+        u64 more = 0;
+#pragma unroll
+        for (int e = 0; e < kWideEach; ++e) {
+            const float x = key_logit(~fall[e]);
+            if (e * kWideThreads + tid < n && kept(cut, x, (int)index[e])) {
+                more += mass[e];
+                if (weight_of(x) >= min_w) atomicAdd(&s.block[((int)index[e] + skew) / kBlock], mass[e]);
+            }
+        }
+        summed = true;
+        return over + s.bins.sum_of(tid, more);
     }
 };
 
-template <int DT, bool DRAW> __global__ void __launch_bounds__(kRowThreads) filter_row_kernel(const FilterArgs a)
+template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) filter_wide_kernel(const FilterArgs a)
 {
-    const int row = blockIdx.x, side = blockIdx.y, tid = threadIdx.x;
-    __shared__ RowShared s;
-    const RowFilter f = row_filter(a, row / a.block_k);
-    RowScan<DT> r = {s, logit_row<DT>(a, side, row), a.vocab, tid, 0, 0.f, f.scale, 1.0, {0.0, 0.f, 0.f, 0u, 0x7fffffff}};
-    while (((a.vocab - 1) >> r.idx_shift) >= kBins) ++r.idx_shift;
-    const int alive = r.find_top();
-    int token = -1;
-    double own_weight = 0.0;
-    r.cut.top = r.top;
-    r.cut.min_w = (float)f.min_p;
-    if (alive > 0) {
-        r.find_unit();
-        if (f.top_k > 0 && f.top_k < alive) r.cut_top_k(f.top_k);
-        if (f.top_p < 1.0) r.cut_top_p(f.top_p);
-        const u64 total = r.mass(f.min_p);
-        r.cut.z = (double)total / r.unit;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, count = a.unresolved[0];
+    __shared__ WideShared s;
+    for (int at = blockIdx.x; at < count; at += gridDim.x) {
+        const int rr = a.unresolved[1 + at], side = rr >= a.rows, row = rr - side * a.rows;
+        const RowFilter f = row_filter(a, row / a.block_k);
+        const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
+        float top = -INFINITY, tau = INFINITY;
+        for (int c = tid; c < a.chunks; c += kWideThreads) { top = fmaxf(top, stats[c].top); tau = fminf(tau, stats[c].tau); }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) { top = fmaxf(top, __shfl_xor(top, off)); tau = fminf(tau, __shfl_xor(tau, off)); }
+        if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
+        __syncthreads();
+        for (int w = 0; w < kWideWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fminf(tau, s.tau[w]); }
+        double z = 0.0;
+        for (int c = tid; c < a.chunks; c += kWideThreads) z += stats[c].sum * weight(stats[c].top, top, f.t);
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
+        if (lane == 0) s.z[wave] = z;
+        __syncthreads();
+        z = 0.0;
+        for (int w = 0; w < kWideWaves; ++w) z += s.z[w];
+        const void *logits = logit_row<DT>(a, side, row);
+        const int skew = (int)((uintptr_t)logits / (16 / WideRow<DT>::kVec)) & (WideRow<DT>::kVec - 1);
+        // fixed point: the sum of all weights (at most one each) stays below 2^61
+        const double unit = exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab)));
+        WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
+                         (float)(f.t.scale * (kSteps / 40.0)), f.t, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff}};
+        bool summed = false;
+        u64 z1 = 0;
+        if (f.top_k > 0) {
+            // steps that reach well below the lists' logits, whatever the temperature
+            const float by_weight = r.step_scale;
+            if (top - tau > 0.f && top - tau < INFINITY) r.step_scale = kSteps / (8.f * (top - tau));
+            z1 = r.template cut_at<false>((u64)f.top_k, summed);
+            r.step_scale = by_weight;
+        } else if (f.top_p < 1.0) {
+            z1 = (u64)(z * unit);
+        }
+        if (f.top_p < 1.0) {
+            const float min_w = r.cut.min_w;
+            if (z1 == 0) {
+                r.cut.min_w = 0.f;
+                z1 = r.sum_blocks([&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); });
+                r.cut.min_w = min_w;
+            }
+            r.template cut_at<true>(max((u64)1, (u64)ceil(f.top_p * (double)z1)), summed);
+        }
+        auto amount = [&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); };
+        u64 total;
+        if (summed) {
+            __syncthreads();
+            u64 part = 0;
+            for (int blk = tid; blk < r.blocks; blk += kWideThreads) part += s.block[blk];
+            total = s.bins.sum_of(tid, part);
+        } else {
+            total = r.sum_blocks(amount);
+        }
+        r.cut.z = (double)total / unit;
+        int token = -1;
         if (DRAW) {
             const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
-            token = r.first_index((u64)((double)u * (double)total) + 1,
-                                  [&](int i) __attribute__((always_inline)) { return r.amount(r.at(i), i, f.min_p); });
-            own_weight = r.weight_of(r.at(token));
+            token = r.find_in_blocks((u64)((double)u * (double)total) + 1, amount);
         }
-    }
-    if (tid == 0) {
-        if (DRAW) {
-            a.tokens[row] = token;
-            if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(own_weight / r.cut.z);
-        } else {
-            a.cuts[(int64_t)side * a.rows + row] = r.cut;
+        if (tid == 0) {
+            if (DRAW) {
+                a.tokens[row] = token;
+                if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(r.weight_of(logit<DT>(logits, token)) / r.cut.z);
+            } else {
+                a.cuts[rr] = r.cut;
+            }
         }
+        __syncthreads();
     }
 }
 
-size_t filter_workspace_bytes(int64_t, int, int) { return 0; }
+// ---- launch plan: chunk size, workspace
 
-template <bool DRAW> static hipError_t launch_filter_rows(const FilterArgs &a, hipStream_t stream)
+struct FilterPlan {
+    int per, chunks, list_cap;
+    size_t stats, lists, unresolved, total;   // byte offsets
+};
+
+// Chunks of 8192 logits, of 2048 where those would be fewer than two to a CU: a chunk's time is then its latency, and the
+// small ones' lists of 128 hold about as much of a row.
+static FilterPlan filter_plan(int64_t rows, int vocab)   // rows of all views
 {
-    const dim3 grid((unsigned)a.rows, DRAW ? 1u : 2u);
-    if (a.dtype == 0) hipLaunchKernelGGL((filter_row_kernel<0, DRAW>), grid, dim3(kRowThreads), 0, stream, a);
-    else if (a.dtype == 1) hipLaunchKernelGGL((filter_row_kernel<1, DRAW>), grid, dim3(kRowThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filter_row_kernel<2, DRAW>), grid, dim3(kRowThreads), 0, stream, a);
+    FilterPlan p;
+    const int64_t big = ((int64_t)vocab + 7 + 8191) / 8192;
+    p.per = rows * big < 512 ? 8 : 32;
+    const int elems = kScanThreads * p.per;
+    p.chunks = (int)(((int64_t)vocab + 7 + elems - 1) / elems);
+    if (p.chunks > kMaxChunks) { p.per = 32; p.chunks = (int)big; }
+    p.list_cap = p.per == 32 ? 256 : 128;
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    p.stats = 0;
+    p.lists = up((size_t)rows * p.chunks * sizeof(ChunkStat));
+    p.unresolved = p.lists + up((size_t)rows * p.chunks * p.list_cap * sizeof(uint2));
+    p.total = p.unresolved + up((size_t)(rows + 1) * sizeof(int32_t));
+    return p;
+}
+
+size_t filter_workspace_bytes(int64_t rows, int vocab, int views) { return rows > 0 ? filter_plan(rows * views, vocab).total : 0; }
+
+template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArgs &a, const FilterPlan &p, int rows, hipStream_t stream)
+{
+    const dim3 scan((unsigned)rows * (unsigned)p.chunks);
+    if (p.per == 32) hipLaunchKernelGGL((filter_scan_kernel<DT, 32, 8>), scan, dim3(kScanThreads), 0, stream, a);
+    else hipLaunchKernelGGL((filter_scan_kernel<DT, 8, 16>), scan, dim3(kScanThreads), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.per == 32) hipLaunchKernelGGL((filter_pick_kernel<DT, 32, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
+    else hipLaunchKernelGGL((filter_pick_kernel<DT, 8, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(rows < 512 ? rows : 512), dim3(kWideThreads), 0, stream, a);
     return hipGetLastError();
 }
 
-hipError_t launch_sample_tokens(const FilterArgs &a, hipStream_t stream) { return launch_filter_rows<true>(a, stream); }
+template <bool DRAW> static hipError_t launch_filters(FilterArgs a, hipStream_t stream)
+{
+    const int rows = a.rows * (DRAW ? 1 : 2);
+    const FilterPlan p = filter_plan(rows, a.vocab);
+    char *ws = (char *)a.workspace;
+    a.stats = (ChunkStat *)(ws + p.stats);
+    a.lists = (uint2 *)(ws + p.lists);
+    a.unresolved = (int32_t *)(ws + p.unresolved);
+    a.chunks = p.chunks;
+    a.list_cap = p.list_cap;
+    if (a.dtype == 0) return launch_filters_of<0, DRAW>(a, p, rows, stream);
+    if (a.dtype == 1) return launch_filters_of<1, DRAW>(a, p, rows, stream);
+    return launch_filters_of<2, DRAW>(a, p, rows, stream);
+}
+
+hipError_t launch_sample_tokens(const FilterArgs &a, hipStream_t stream) { return launch_filters<true>(a, stream); }
 
 // ---- consensus
 
+constexpr int kDrawThreads = 1024;
+
 // Probability that a row's filters leave a token (0: cut, or an empty row).
-__device__ __forceinline__ double kept_prob(const RowCut &c, double scale, float x, int i)
+__device__ __forceinline__ double kept_prob(const RowCut &c, const Scale &t, float x, int i)
 {
     if (!kept(c, x, i)) return 0.0;
-    const double t = ((double)x - (double)c.top) * scale, w = t < -1000.0 ? 0.0 : exp2_neg(t);
+    const double d = (double)x - (double)c.top, w = d <= t.floor ? 0.0 : weight(d, t);
     return w >= (double)c.min_w ? w / c.z : 0.0;
 }
 
@@ -363,19 +1008,19 @@ struct Candidate {
     }
 };
 
-template <int DT> __global__ void __launch_bounds__(kRowThreads) filtered_draw_kernel(const FilteredArgs a)
+template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const FilteredArgs a)
 {
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int K = a.c.block_k, V = a.c.vocab;
-    const double scale = row_filter(a.f, b).scale;
+    const Scale t = row_filter(a.f, b).t;
     __shared__ int s_keep[32];
-    __shared__ Candidate s_best[2][kRowThreads / 64];
+    __shared__ Candidate s_best[2][kDrawThreads / 64];
     if (tid < K) {
         const int row = b * K + tid, x = a.c.draft_tokens[row];
         bool keep = false;
         if (x >= 0 && x < V) {
-            const double p = kept_prob(a.f.cuts[row], scale, logit<DT>(logit_row<DT>(a.f, 0, row), x), x);
-            const double q = kept_prob(a.f.cuts[a.f.rows + row], scale, logit<DT>(logit_row<DT>(a.f, 1, row), x), x);
+            const double p = kept_prob(a.f.cuts[row], t, logit<DT>(logit_row<DT>(a.f, 0, row), x), x);
+            const double q = kept_prob(a.f.cuts[a.f.rows + row], t, logit<DT>(logit_row<DT>(a.f, 1, row), x), x);
             keep = (double)a.accept_u[row] * q < p;
         }
         s_keep[tid] = keep;
@@ -392,10 +1037,10 @@ template <int DT> __global__ void __launch_bounds__(kRowThreads) filtered_draw_k
     const void *pr = logit_row<DT>(a.f, 0, row), *qr = logit_row<DT>(a.f, 1, row);
     const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
     Candidate more = {-INFINITY, 0x7fffffff}, any = {-INFINITY, 0x7fffffff};  // best among p > q, best of p
-    for (int i = tid; i < V; i += kRowThreads) {
-        const double p = kept_prob(cp, scale, logit<DT>(pr, i), i);
+    for (int i = tid; i < V; i += kDrawThreads) {
+        const double p = kept_prob(cp, t, logit<DT>(pr, i), i);
         if (p > 0.0) {
-            const double q = kept_prob(cq, scale, logit<DT>(qr, i), i), g = (double)a.gumbel[(int64_t)b * V + i];
+            const double q = kept_prob(cq, t, logit<DT>(qr, i), i), g = (double)a.gumbel[(int64_t)b * V + i];
             if (p > q) more.take(log(p - q) + g, i);
             any.take(log(p) + g, i);
         }
@@ -410,7 +1055,7 @@ template <int DT> __global__ void __launch_bounds__(kRowThreads) filtered_draw_k
     if (lane == 0) { s_best[0][wave] = more; s_best[1][wave] = any; }
     __syncthreads();
     if (tid == 0) {
-        for (int w = 1; w < kRowThreads / 64; ++w) {
+        for (int w = 1; w < kDrawThreads / 64; ++w) {
             more.take(s_best[0][w].score, s_best[0][w].index);
             any.take(s_best[1][w].score, s_best[1][w].index);
         }
@@ -461,11 +1106,11 @@ __global__ void __launch_bounds__(256) filtered_commit_kernel(const FilteredArgs
 hipError_t launch_filtered_consensus(const FilteredArgs &a, hipStream_t stream)
 {
     const ConsensusArgs &c = a.c;
-    hipError_t e = launch_filter_rows<false>(a.f, stream);
+    hipError_t e = launch_filters<false>(a.f, stream);
     if (e != hipSuccess) return e;
-    if (a.f.dtype == 0) hipLaunchKernelGGL((filtered_draw_kernel<0>), dim3(c.batch), dim3(kRowThreads), 0, stream, a);
-    else if (a.f.dtype == 1) hipLaunchKernelGGL((filtered_draw_kernel<1>), dim3(c.batch), dim3(kRowThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filtered_draw_kernel<2>), dim3(c.batch), dim3(kRowThreads), 0, stream, a);
+    if (a.f.dtype == 0) hipLaunchKernelGGL((filtered_draw_kernel<0>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
+    else if (a.f.dtype == 1) hipLaunchKernelGGL((filtered_draw_kernel<1>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
+    else hipLaunchKernelGGL((filtered_draw_kernel<2>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(filtered_commit_kernel, dim3(c.batch, c.do_commit ? c.num_layers : 1), dim3(256), 0, stream, a);

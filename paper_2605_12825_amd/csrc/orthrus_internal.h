@@ -90,6 +90,13 @@ struct RowCut {
     int32_t tie;
 };
 
+// What the pass over the logits leaves of one chunk of a row.
+struct ChunkStat {
+    double sum;      // of the weights, relative to `top`
+    float top, tau;  // the largest logit; the list holds every logit from tau up (+inf: nothing is listed)
+    int32_t count;   // entries of the list
+};
+
 struct FilterArgs {
     const void *logits[2];   // sampling: one set of rows; consensus: the AR and the diffusion view's
     const float *temperature;  // [B], as the next three (those: NULL = off)
@@ -99,7 +106,11 @@ struct FilterArgs {
     int32_t *tokens;
     float *logprobs;         // or NULL
     RowCut *cuts;            // consensus: [view][rows]
-    void *workspace;         // filter_workspace_bytes
+    void *workspace;         // filter_workspace_bytes; the next five lie in it or follow from its plan
+    ChunkStat *stats;        // [view][row][chunk]
+    uint2 *lists;            // [view][row][chunk][list_cap]: (logit, index)
+    int32_t *unresolved;     // [0]: count, then rows (view * rows + row)
+    int chunks, list_cap;
     int64_t stride_row;      // elements between rows
     int rows, block_k, vocab;
     int dtype;               // orthrus_dtype
