@@ -173,7 +173,7 @@ orthrus::FilterArgs filter_args(const orthrus_params *p, orthrus_dtype type, con
 
 // Workspace of the filtered consensus: byte offsets of its parts.
 struct FilteredLayout {
-    size_t cuts, info, filter, total;
+    size_t cuts, info, best, filter, total;
 };
 FilteredLayout filtered_layout(const orthrus_params *p)
 {
@@ -181,7 +181,8 @@ FilteredLayout filtered_layout(const orthrus_params *p)
     FilteredLayout l;
     l.cuts = 0;
     l.info = align_up(2 * rows * sizeof(orthrus::RowCut), 256);
-    l.filter = l.info + align_up((size_t)p->batch * 3 * sizeof(int32_t), 256);
+    l.best = l.info + align_up((size_t)p->batch * 2 * sizeof(int32_t), 256);
+    l.filter = l.best + align_up((size_t)p->batch * orthrus::draw_pieces(p->vocab) * sizeof(orthrus::DrawBest), 256);
     l.total = l.filter + align_up(orthrus::filter_workspace_bytes((int64_t)rows, p->vocab, 2), 256);
     return l;
 }
@@ -808,7 +809,8 @@ orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus
     a.f.cuts = (orthrus::RowCut *)((char *)workspace + l.cuts);
     a.f.workspace = (char *)workspace + l.filter;
     a.accept_u = accept_u; a.gumbel = gumbel;
-    a.replacement = c.decided + p->batch;
+    a.best = (orthrus::DrawBest *)((char *)workspace + l.best);
+    a.pieces = orthrus::draw_pieces(p->vocab);
     return orthrus::launch_filtered_consensus(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
 

@@ -244,11 +244,24 @@ template <int DT, int PER> struct Chunk {
     }
 };
 
-// Which rows need the sum of all their weights: those that neither top-k nor the greedy rule cuts.
-__device__ __forceinline__ bool wants_sum(const RowFilter &f) { return f.top_k == 0; }
+// Which rows need the sum of all their weights: those that a share of it cuts, and those that nothing cuts.
+__device__ __forceinline__ bool wants_sum(const RowFilter &f) { return f.top_k == 0 && (f.top_p < 1.0 || f.min_p == 0.0); }
 
-// GROUP lanes share one of the maxima whose least is the list's threshold: with n groups the list holds n logits at least and
-// about n * ln(n) in a row without order.
+// The three least of two sorted triples.
+struct Least {
+    float a, b, c;
+    __device__ __forceinline__ void merge(float a2, float b2, float c2)
+    {
+        const float c3 = fminf(fminf(c, c2), fminf(fmaxf(b, a2), fmaxf(a, b2)));
+        b = fminf(fminf(b, b2), fmaxf(a, a2));
+        a = fminf(a, a2);
+        c = c3;
+    }
+};
+
+// The list's threshold is the third least of the maxima of 256 / GROUP groups of lanes (of those that hold anything): of
+// 32 groups 82 logits +- 20 reach it in a row without order, of 16 groups 30 +- 10.  (The least one of all leaves 130 +- 41,
+// with a tail that overran the list in one chunk of 200 and so in every fourth row.)
 template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThreads) filter_scan_kernel(const FilterArgs a)
 {
     const int rr = blockIdx.x / a.chunks, chunk = blockIdx.x - rr * a.chunks, tid = threadIdx.x;
@@ -263,49 +276,71 @@ template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThr
     for (int i = 1; i < PER; ++i) top = fmaxf(top, x[i]);
 #pragma unroll
     for (int off = 1; off < GROUP; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
-    float tau = top;
+    const bool hollow = !(top > -INFINITY);   // (also where all are NaN)
+    Least low = {hollow ? INFINITY : top, INFINITY, INFINITY};
+    if (hollow) top = -INFINITY;
 #pragma unroll
     for (int off = GROUP; off < 64; off <<= 1) {
         top = fmaxf(top, __shfl_xor(top, off));
-        tau = fminf(tau, __shfl_xor(tau, off));
+        low.merge(__shfl_xor(low.a, off), __shfl_xor(low.b, off), __shfl_xor(low.c, off));
     }
-    __shared__ float s_top[4], s_tau[4];
+    __shared__ float4 s_low[4];
     __shared__ double s_sum[4];
-    __shared__ int s_count;
-    if (lane == 0) { s_top[wave] = top; s_tau[wave] = tau; }
-    if (tid == 0) s_count = 0;
+    __shared__ int s_count[4], s_hollow[4];
+    const bool hollow_wave = __ballot(hollow) != 0;
+    if (lane == 0) {
+        s_low[wave] = make_float4(low.a, low.b, low.c, top);
+        s_hollow[wave] = hollow_wave;
+    }
     __syncthreads();
-    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-    tau = fminf(fminf(s_tau[0], s_tau[1]), fminf(s_tau[2], s_tau[3]));
-    // A NaN drops out of every maximum, comparison and weight below by itself; +inf takes the long way.
-    if (!(top > -INFINITY)) top = -INFINITY;
-    if (!(tau > -INFINITY)) tau = -INFINITY;
-    if (top == INFINITY) {
+    float4 l = s_low[0];
+    low = {l.x, l.y, l.z};
+    top = l.w;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        l = s_low[w];
+        low.merge(l.x, l.y, l.z);
+        top = fmaxf(top, l.w);
+    }
+    float tau = low.c < INFINITY ? low.c : low.b < INFINITY ? low.b : low.a < INFINITY ? low.a : -INFINITY;
+    if (top == INFINITY) {   // +inf counts as the largest float.  (A NaN drops out of all that follows by itself.)
         top = FLT_MAX;
-        tau = fminf(tau, FLT_MAX);
 #pragma unroll
         for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
+        tau = low.a < INFINITY ? fminf(tau, FLT_MAX) : FLT_MAX;
     }
-    // ---- the list: whatever reaches the threshold, in no order (what is made of it does not depend on one)
+    if (s_hollow[0] | s_hollow[1] | s_hollow[2] | s_hollow[3]) {   // few logits, the others masked: list them all if there is room
+        int alive = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) alive += __popcll(__ballot(x[i] > -INFINITY));
+        if (lane == 0) s_count[wave] = alive;
+        __syncthreads();
+        if (s_count[0] + s_count[1] + s_count[2] + s_count[3] <= a.list_cap) tau = -INFINITY;
+        __syncthreads();
+    }
+    // ---- the list, in the order of waves, loads and lanes
+    const float line = fmaxf(tau, -FLT_MAX);   // (-inf is never listed)
+    u64 reach[PER];
     int mine = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) mine += x[i] >= tau && x[i] > -INFINITY;
-    int before = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(before, off);
-        if (lane >= off) before += o;
-    }
-    int base = 0;
-    if (lane == 63) base = atomicAdd(&s_count, before);
-    base = __shfl(base, 63) + before - mine;
-    uint2 *list = a.lists + ((int64_t)rr * a.chunks + chunk) * a.list_cap;
-#pragma unroll
     for (int i = 0; i < PER; ++i) {
-        if (x[i] >= tau && x[i] > -INFINITY) {
-            if (base < a.list_cap) list[base] = make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, tid) + i % c.kVec);
-            ++base;
-        }
+        reach[i] = __ballot(x[i] >= line);
+        mine += __popcll(reach[i]);
+    }
+    if (lane == 0) s_count[wave] = mine;
+    __syncthreads();
+    const int n = s_count[0] + s_count[1] + s_count[2] + s_count[3];
+    if (n <= a.list_cap) {
+        uint2 *list = a.lists + ((int64_t)rr * a.chunks + chunk) * a.list_cap;
+        for (int w = 0; w < wave; ++w) list += s_count[w];
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (reach[i]) {
+                if (reach[i] >> lane & 1)
+                    list[__builtin_amdgcn_mbcnt_hi((uint32_t)(reach[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach[i], 0))] =
+                        make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, tid) + i % c.kVec);
+                list += __popcll(reach[i]);
+            }
     }
     // ---- the weights, relative to the chunk's maximum
     double sum = 0.0;
@@ -318,7 +353,6 @@ template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThr
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
     if (tid == 0) {
-        const int n = s_count;
         ChunkStat r;
         r.sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
         r.top = top;
@@ -330,16 +364,17 @@ template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThr
 
 // ---- cuts and token from the lists
 
-constexpr int kPickThreads = 256;
-constexpr int kPickEach = 12, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
-constexpr int kMaxChunks = 1024;
+constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
+constexpr int kPickEach = 6, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
+constexpr int kMaxChunks = 1024, kChunksEach = kMaxChunks / kPickThreads;
 
 struct PickShared {
-    Bins<kPickThreads, 4> bins;
+    Bins<kPickThreads, 2> bins;
     uint32_t key[kPickEntries];
     int index[kPickEntries];
-    float top[4], tau[4];
-    double z[4];
+    uint16_t listed[kMaxChunks];
+    float top[kPickWaves], tau[kPickWaves];
+    double z[kPickWaves];
     int count;
     uint32_t token_key;
 };
@@ -375,21 +410,37 @@ __device__ __forceinline__ Picked pick_digit(PickShared &s, int tid, const uint3
 __device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
 
+// PER: logits to a thread of the scan's chunks; 0: there was no scan, the row has at most kPickEntries logits and is read here.
 template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThreads) filter_pick_kernel(const FilterArgs a)
 {
     const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ PickShared s;
     const RowFilter f = row_filter(a, row / a.block_k);
-    const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
-    // ---- the row's maximum, what its lists hold whole, the sum of its weights
-    ChunkStat st[kMaxChunks / kPickThreads];
+    const void *logits = logit_row<DT>(a, side, row);
+    uint32_t fall[kPickEach], index[kPickEach];   // fall: distance from the top in order
+    // ---- the row's maximum, down to where its lists hold everything
     float top = -INFINITY, tau = -INFINITY;
+    ChunkStat st[kChunksEach];
+    if constexpr (PER > 0) {
+        const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
 #pragma unroll
-    for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
-        st[i] = {0.0, -INFINITY, -INFINITY, 0};
-        if (i * kPickThreads + tid < a.chunks) st[i] = stats[i * kPickThreads + tid];
-        top = fmaxf(top, st[i].top);
-        tau = fmaxf(tau, st[i].tau);
+        for (int i = 0; i < kChunksEach; ++i) {
+            const int c = i * kPickThreads + tid;
+            st[i] = {0.0, -INFINITY, -INFINITY, 0};
+            if (c < a.chunks) st[i] = stats[c];
+            s.listed[c] = (uint16_t)st[i].count;
+            top = fmaxf(top, st[i].top);
+            tau = fmaxf(tau, st[i].tau);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPickEach; ++e) {
+            const int i = e * kPickThreads + tid;
+            const float x = i < a.vocab ? logit<DT>(logits, i) : -INFINITY;
+            fall[e] = order_key(x);   // (a key until the top is known)
+            index[e] = (uint32_t)i;
+            top = fmaxf(top, x);
+        }
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
@@ -399,57 +450,65 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
     if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
     if (tid == 0) s.count = 0;
     __syncthreads();
-    top = fmaxf(fmaxf(s.top[0], s.top[1]), fmaxf(s.top[2], s.top[3]));
-    tau = fmaxf(fmaxf(s.tau[0], s.tau[1]), fmaxf(s.tau[2], s.tau[3]));
-    RowCut cut = {0.0, top, (float)f.min_p, 0u, 0x7fffffff};
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fmaxf(tau, s.tau[w]); }
+    RowCut cut = {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0};
     int token = -1;
     double own = 1.0;
     bool resolved = true;
     if (top > -INFINITY) {
-        double part[kMaxChunks / kPickThreads], z = 0.0;   // the chunks' sums, relative to the row's maximum
+        const bool plain = f.top_k == 0 && f.top_p >= 1.0 && f.min_p == 0.0;
+        const float u = DRAW ? fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f) : 0.f;
+        double part[kChunksEach], z = 0.0;   // the chunks' sums, relative to the row's maximum
+        if constexpr (PER > 0) {
 #pragma unroll
-        for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
-            part[i] = st[i].sum * weight(st[i].top, top, f.t);
-            z += part[i];
+            for (int i = 0; i < kChunksEach; ++i) {
+                part[i] = st[i].sum * weight(st[i].top, top, f.t);
+                z += part[i];
+            }
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
+            if (lane == 0) s.z[wave] = z;
+            __syncthreads();
+            z = 0.0;
+#pragma unroll
+            for (int w = 0; w < kPickWaves; ++w) z += s.z[w];
         }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
-        if (lane == 0) s.z[wave] = z;
-        __syncthreads();
-        z = s.z[0] + s.z[1] + s.z[2] + s.z[3];
-        if (f.top_k == 0 && f.top_p >= 1.0 && f.min_p == 0.0) {
+        if (PER > 0 && plain) {
             // ---- no filter: the chunk at which the running sum crosses, and its logits once more
             cut.z = z;
-            if constexpr (DRAW) {
+            if constexpr (DRAW && PER > 0) {
                 const double unit = exp2((double)min(50, 60 - ilogb(z)));
                 s.bins.clear(tid);
                 u64 sum = 0;
 #pragma unroll
-                for (int i = 0; i < kMaxChunks / kPickThreads; ++i) {
+                for (int i = 0; i < kChunksEach; ++i) {
                     const u64 m = to_fixed(part[i], unit);
                     s.bins.amount[i * kPickThreads + tid] = m;
                     sum += m;
                 }
                 const u64 total = s.bins.sum_of(tid, sum);
-                const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
                 const u64 target = (u64)((double)u * (double)total) + 1;
                 const Crossing at = s.bins.crossing(tid, target);
-                const Chunk<DT, PER> c(logit_row<DT>(a, side, row), at.bin, a.vocab);
-                float x[PER];
-                c.load(tid, x);
-#pragma unroll
-                for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
-                // 1024 bins: a vector of a thread to a bin (or as many of them as make 1024)
-                constexpr int kPerBin = c.kElems / 1024;
-                s.bins.clear(tid);
+                // 1024 bins, a few neighbours to each; a thread looks at logits 512 apart
+                constexpr int kElems = kScanThreads * PER, kPerBin = kElems / 1024, kEach = kElems / kPickThreads;
+                const int first = at.bin * kElems - ((int)((uintptr_t)logits / (16 / Vector<DT>::kCount)) & (Vector<DT>::kCount - 1));
+                u64 m[kEach];
                 int last = -1;
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const u64 m = x[i] > -INFINITY ? to_fixed(weight(x[i], top, f.t), unit) : 0;
-                    const int place = (i / c.kVec * kScanThreads + tid) * c.kVec + i % c.kVec;
-                    if (m) { atomicAdd(&s.bins.amount[place / kPerBin], m); last = max(last, place); }
+                for (int e = 0; e < kEach; ++e) {
+                    const int i = first + e * kPickThreads + tid;
+                    const float x = i >= 0 && i < a.vocab ? logit<DT>(logits, i) : -INFINITY;
+                    m[e] = x > -INFINITY ? to_fixed(weight(x, top, f.t), unit) : 0;
                 }
-                Crossing in = s.bins.crossing(tid, target - at.before);
+                s.bins.clear(tid);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e)
+                    if (m[e]) {
+                        last = e * kPickThreads + tid;
+                        atomicAdd(&s.bins.amount[last / kPerBin], m[e]);
+                    }
+                const Crossing in = s.bins.crossing(tid, target - at.before);
                 if (tid == 0) s.count = -1;
                 __syncthreads();
                 atomicMax(&s.count, last);
@@ -459,112 +518,153 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                 } else {
                     s.bins.clear(tid);
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        const int place = (i / c.kVec * kScanThreads + tid) * c.kVec + i % c.kVec;
-                        if (place / kPerBin == in.bin)
-                            s.bins.amount[place % kPerBin] = x[i] > -INFINITY ? to_fixed(weight(x[i], top, f.t), unit) : 0;
+                    for (int e = 0; e < kEach; ++e) {
+                        const int place = e * kPickThreads + tid;
+                        if (place / kPerBin == in.bin) s.bins.amount[place % kPerBin] = m[e];
                     }
                     token = in.bin * kPerBin + s.bins.crossing(tid, target - at.before - in.before).bin;
                 }
-                token += c.first;
-                own = weight(logit<DT>(c.row, token), top, f.t);
+                token += first;
+                own = weight(logit<DT>(logits, token), top, f.t);
             }
         } else if (tau == INFINITY) {
             resolved = false;
         } else {
             // ---- every logit down to tau
             const bool whole = tau == -INFINITY;   // that is all there are
-            for (int c = wave; c < a.chunks; c += kPickThreads / 64) {
-                const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * a.list_cap;
-                const int n = stats[c].count;
-                for (int i = lane; i < n; i += 64) {
-                    const uint2 v = list[i];
-                    const float x = __uint_as_float(v.x);
-                    if (x >= tau) {
-                        const int at = atomicAdd(&s.count, 1);
-                        if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)v.y; }
+            const uint32_t top_key = order_key(top);
+            int n;
+            if constexpr (PER > 0) {
+                constexpr int kAhead = 4;   // lists of a wave whose first two loads go out together
+                for (int c0 = wave; c0 < a.chunks; c0 += kAhead * kPickWaves) {
+                    uint2 v[2 * kAhead];
+                    int have[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int c = c0 + u * kPickWaves;
+                        have[u] = c < a.chunks ? s.listed[c] : 0;
+                        const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * a.list_cap;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            v[2 * u + h] = make_uint2(0xff800000u, 0);   // -inf
+                            if (h * 64 + lane < have[u]) v[2 * u + h] = list[h * 64 + lane];
+                        }
                     }
+                    auto keep = [&](uint2 q) __attribute__((always_inline)) {
+                        const float x = __uint_as_float(q.x);
+                        if (x >= tau && x > -INFINITY) {
+                            const int at = atomicAdd(&s.count, 1);
+                            if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)q.y; }
+                        }
+                    };
+#pragma unroll
+                    for (int u = 0; u < 2 * kAhead; ++u) keep(v[u]);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        for (int i = 128 + lane; i < have[u]; i += 64)
+                            keep(a.lists[((int64_t)rr * a.chunks + c0 + u * kPickWaves) * a.list_cap + i]);
                 }
+                __syncthreads();
+                n = s.count;
+                resolved = n <= kPickEntries;
+            } else {
+                n = a.vocab;
             }
-            __syncthreads();
-            const int n = s.count;
-            resolved = n <= kPickEntries;
             if (resolved) {
-                const uint32_t top_key = order_key(top + 0.f);
                 const int key_bits = bits_of(top_key - (whole ? order_key(-FLT_MAX) : order_key(tau + 0.f)));
                 const int index_bits = bits_of((uint32_t)(a.vocab - 1));
                 constexpr double kUnit = 0x1p50;
-                uint32_t fall[kPickEach], index[kPickEach];   // fall: distance from the top in order
-                u64 one[kPickEach], mass[kPickEach];
+                uint32_t live = 0;           // entry e is there
+                u64 mass[kPickEach], known = 0;
 #pragma unroll
                 for (int e = 0; e < kPickEach; ++e) {
                     const int i = e * kPickThreads + tid;
-                    const bool there = i < n;
-                    const uint32_t key = there ? s.key[i] : top_key;
+                    bool there = i < n;
+                    uint32_t key;
+                    if constexpr (PER > 0) {
+                        key = there ? s.key[i] : top_key;
+                        index[e] = there ? (uint32_t)s.index[i] : 0u;
+                    } else {
+                        key = fall[e];
+                        there = there && key >= order_key(-FLT_MAX);
+                    }
+                    live |= (uint32_t)there << e;
                     fall[e] = top_key - key;
-                    index[e] = there ? (uint32_t)s.index[i] : 0u;
-                    one[e] = there;
                     mass[e] = there ? to_fixed(weight(key_logit(key), top, f.t), kUnit) : 0;
+                    known += mass[e];
+                }
+                if constexpr (PER == 0) {
+                    if (f.top_k > 0) n = (int)s.bins.sum_of(tid, (u64)__popc(live));
                 }
                 uint32_t cut_fall = 0xffffffffu;
                 int cut_tie = 0x7fffffff;
-                // index of the n-th entry at `at`
-                auto nth_at = [&](uint32_t at, u64 nth) __attribute__((always_inline)) {
-                    u64 here[kPickEach];
+                auto count_of = [&](bool only, uint32_t at, u64 (&one)[kPickEach]) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int e = 0; e < kPickEach; ++e) here[e] = fall[e] == at ? one[e] : 0;
-                    return (int)pick_digit(s, tid, index, here, index_bits, nth).digit;
+                    for (int e = 0; e < kPickEach; ++e) one[e] = (live >> e & 1) && (!only || fall[e] == at);
+                };
+                auto nth_at = [&](uint32_t at, u64 nth) __attribute__((always_inline)) {   // index of the n-th entry there
+                    u64 one[kPickEach];
+                    count_of(true, at, one);
+                    return (int)pick_digit(s, tid, index, one, index_bits, nth).digit;
                 };
                 auto apply = [&]() __attribute__((always_inline)) {
+                    known = 0;
 #pragma unroll
-                    for (int e = 0; e < kPickEach; ++e)
-                        if (fall[e] > cut_fall || (fall[e] == cut_fall && (int)index[e] > cut_tie)) one[e] = mass[e] = 0;
+                    for (int e = 0; e < kPickEach; ++e) {
+                        if (fall[e] > cut_fall || (fall[e] == cut_fall && (int)index[e] > cut_tie)) {
+                            mass[e] = 0;
+                            live &= ~(1u << e);
+                        }
+                        known += mass[e];
+                    }
                 };
-                if (f.top_k > 0) {
-                    if (f.top_k < n) {
-                        const Picked k = pick_digit(s, tid, fall, one, key_bits, (u64)f.top_k);
-                        cut_fall = k.digit;
-                        if (k.before + k.here > (u64)f.top_k) cut_tie = nth_at(k.digit, (u64)f.top_k - k.before);
-                        apply();
+                if (f.top_k > 0 && f.top_k < n) {
+                    u64 one[kPickEach];
+                    count_of(false, 0, one);
+                    const Picked k = pick_digit(s, tid, fall, one, key_bits, (u64)f.top_k);
+                    cut_fall = k.digit;
+                    if (k.before + k.here > (u64)f.top_k) cut_tie = nth_at(k.digit, (u64)f.top_k - k.before);
+                    apply();
+                }
+                // what min-p keeps is known if what is not listed is below its line; the other cuts are then only
+                // asked whether they cut higher
+                const bool min_p_known = whole || (f.min_p > 0.0 && weight(tau, top, f.t) < f.min_p);
+                const bool top_k_known = f.top_k <= n || whole;
+                resolved = (f.top_k > 0 && top_k_known) || min_p_known || (f.top_k == 0 && f.top_p < 1.0);
+                if (f.top_p < 1.0) {
+                    if (top_k_known) {
+                        known = s.bins.sum_of(tid, known);
+                        const double all = f.top_k > 0 || whole ? (double)known : z * kUnit;
+                        const double target = fmax(1.0, ceil(f.top_p * all));
+                        if (target <= (double)known) {
+                            const u64 goal = min(known, (u64)target);
+                            const Picked p = pick_digit(s, tid, fall, mass, key_bits, goal);
+                            const u64 each = to_fixed(weight(key_logit(top_key - p.digit), top, f.t), kUnit);
+                            const u64 nth = (goal - p.before + each - 1) / each;
+                            if (p.digit < cut_fall) cut_tie = 0x7fffffff;
+                            cut_fall = p.digit;
+                            if (nth * each < p.here) cut_tie = min(cut_tie, nth_at(p.digit, nth));
+                            apply();
+                        } else {
+                            resolved = min_p_known;
+                        }
                     } else {
-                        resolved = f.top_k == n || whole;
+                        resolved = false;
                     }
-                }
-                u64 known = 0;
-#pragma unroll
-                for (int e = 0; e < kPickEach; ++e) known += mass[e];
-                known = s.bins.sum_of(tid, known);
-                if (resolved && f.top_p < 1.0) {
-                    const double all = f.top_k > 0 || whole ? (double)known : z * kUnit;
-                    const double target = fmax(1.0, ceil(f.top_p * all));
-                    resolved = target <= (double)known;
-                    if (resolved) {
-                        const Picked p = pick_digit(s, tid, fall, mass, key_bits, min(known, (u64)target));
-                        const u64 each = to_fixed(weight(key_logit(top_key - p.digit), top, f.t), kUnit);
-                        const u64 nth = (min(known, (u64)target) - p.before + each - 1) / each;
-                        if (p.digit < cut_fall) cut_tie = 0x7fffffff;
-                        cut_fall = p.digit;
-                        if (nth * each < p.here) cut_tie = min(cut_tie, nth_at(p.digit, nth));
-                        apply();
-                    }
-                }
-                if (f.min_p > 0.0) {
-                    // (without other cuts: what is not listed has to be below the line)
-                    if (f.top_k == 0 && f.top_p >= 1.0) resolved = whole || weight(tau, top, f.t) < f.min_p;
-#pragma unroll
-                    for (int e = 0; e < kPickEach; ++e)
-                        if (!(weight(key_logit(top_key - fall[e]), top, f.t) >= f.min_p)) mass[e] = 0;
                 }
                 if (resolved) {
-                    u64 total = 0;
+                    known = 0;
 #pragma unroll
-                    for (int e = 0; e < kPickEach; ++e) total += mass[e];
-                    total = s.bins.sum_of(tid, total);
+                    for (int e = 0; e < kPickEach; ++e) {
+                        if (f.min_p > 0.0 && !(weight(key_logit(top_key - fall[e]), top, f.t) >= f.min_p)) mass[e] = 0;
+                        known += mass[e];
+                    }
+                    const u64 total = s.bins.sum_of(tid, known);
                     cut.z = (double)total / kUnit;
                     cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
                     cut.tie = cut_tie;
+                    cut.listed = PER > 0;
                     if constexpr (DRAW) {
-                        const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
                         token = (int)pick_digit(s, tid, index, mass, index_bits, (u64)((double)u * (double)total) + 1).digit;
 #pragma unroll
                         for (int e = 0; e < kPickEach; ++e)
@@ -878,7 +978,7 @@ template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) fil
         // fixed point: the sum of all weights (at most one each) stays below 2^61
         const double unit = exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab)));
         WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
-                         (float)(f.t.scale * (kSteps / 40.0)), f.t, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff}};
+                         (float)(f.t.scale * (kSteps / 40.0)), f.t, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0}};
         bool summed = false;
         u64 z1 = 0;
         if (f.top_k > 0) {
@@ -934,22 +1034,23 @@ struct FilterPlan {
     size_t stats, lists, unresolved, total;   // byte offsets
 };
 
-// Chunks of 8192 logits, of 2048 where those would be fewer than two to a CU: a chunk's time is then its latency, and the
-// small ones' lists of 128 hold about as much of a row.
+// A row of at most kPickEntries logits needs no scan.  Else chunks of 8192 logits, of 2048 where those would be fewer than two
+// to a CU: a chunk's time is then its latency.
 static FilterPlan filter_plan(int64_t rows, int vocab)   // rows of all views
 {
     FilterPlan p;
     const int64_t big = ((int64_t)vocab + 7 + 8191) / 8192;
-    p.per = rows * big < 512 ? 8 : 32;
-    const int elems = kScanThreads * p.per;
+    p.per = vocab <= kPickEntries ? 0 : rows * big < 512 ? 8 : 32;
+    const int elems = kScanThreads * (p.per ? p.per : 32);
     p.chunks = (int)(((int64_t)vocab + 7 + elems - 1) / elems);
     if (p.chunks > kMaxChunks) { p.per = 32; p.chunks = (int)big; }
+    if (p.per == 0) p.chunks = 0;
     p.list_cap = p.per == 32 ? 256 : 128;
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     p.stats = 0;
     p.lists = up((size_t)rows * p.chunks * sizeof(ChunkStat));
     p.unresolved = p.lists + up((size_t)rows * p.chunks * p.list_cap * sizeof(uint2));
-    p.total = p.unresolved + up((size_t)(rows + 1) * sizeof(int32_t));
+    p.total = p.per == 0 ? 0 : p.unresolved + up((size_t)(rows + 1) * sizeof(int32_t));
     return p;
 }
 
@@ -957,6 +1058,10 @@ size_t filter_workspace_bytes(int64_t rows, int vocab, int views) { return rows 
 
 template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArgs &a, const FilterPlan &p, int rows, hipStream_t stream)
 {
+    if (p.per == 0) {
+        hipLaunchKernelGGL((filter_pick_kernel<DT, 0, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
+        return hipGetLastError();
+    }
     const dim3 scan((unsigned)rows * (unsigned)p.chunks);
     if (p.per == 32) hipLaunchKernelGGL((filter_scan_kernel<DT, 32, 8>), scan, dim3(kScanThreads), 0, stream, a);
     else hipLaunchKernelGGL((filter_scan_kernel<DT, 8, 16>), scan, dim3(kScanThreads), 0, stream, a);
@@ -970,7 +1075,7 @@ template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArg
     return hipGetLastError();
 }
 
-template <bool DRAW> static hipError_t launch_filters(FilterArgs a, hipStream_t stream)
+template <bool DRAW> static hipError_t launch_filters(FilterArgs &a, hipStream_t stream)
 {
     const int rows = a.rows * (DRAW ? 1 : 2);
     const FilterPlan p = filter_plan(rows, a.vocab);
@@ -985,11 +1090,11 @@ template <bool DRAW> static hipError_t launch_filters(FilterArgs a, hipStream_t 
     return launch_filters_of<2, DRAW>(a, p, rows, stream);
 }
 
-hipError_t launch_sample_tokens(const FilterArgs &a, hipStream_t stream) { return launch_filters<true>(a, stream); }
+hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream) { return launch_filters<true>(a, stream); }
 
 // ---- consensus
 
-constexpr int kDrawThreads = 1024;
+constexpr int kDrawThreads = 256, kDrawPiece = 8192;
 
 // Probability that a row's filters leave a token (0: cut, or an empty row).
 __device__ __forceinline__ double kept_prob(const RowCut &c, const Scale &t, float x, int i)
@@ -1008,27 +1113,31 @@ struct Candidate {
     }
 };
 
+// Grid (piece, sequence).  Every workgroup repeats the keep decisions of its sequence (three dependent round trips), the first
+// records them.  The first rejected row's kept tokens are in the row's lists, which the first workgroup goes through, or
+// anywhere (no filter, a wide cut): then each goes through its piece of the row.
 template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const FilteredArgs a)
 {
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = blockIdx.y, piece = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int K = a.c.block_k, V = a.c.vocab;
     const Scale t = row_filter(a.f, b).t;
     __shared__ int s_keep[32];
     __shared__ Candidate s_best[2][kDrawThreads / 64];
     if (tid < K) {
         const int row = b * K + tid, x = a.c.draft_tokens[row];
+        const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
+        const float u = a.accept_u[row];
         bool keep = false;
         if (x >= 0 && x < V) {
-            const double p = kept_prob(a.f.cuts[row], t, logit<DT>(logit_row<DT>(a.f, 0, row), x), x);
-            const double q = kept_prob(a.f.cuts[a.f.rows + row], t, logit<DT>(logit_row<DT>(a.f, 1, row), x), x);
-            keep = (double)a.accept_u[row] * q < p;
+            const float xp = logit<DT>(logit_row<DT>(a.f, 0, row), x), xq = logit<DT>(logit_row<DT>(a.f, 1, row), x);
+            keep = (double)u * kept_prob(cq, t, xq, x) < kept_prob(cp, t, xp, x);
         }
         s_keep[tid] = keep;
     }
     __syncthreads();
     const unsigned long long rej = ~__ballot(lane >= K || s_keep[lane < K ? lane : 0]);
     const int j = rej ? __ffsll((long long)rej) - 1 : K;
-    if (tid == 0) {
+    if (piece == 0 && tid == 0) {
         a.c.decided[b] = j;
         if (a.c.do_commit) commit_snapshot(a.c, b);
     }
@@ -1036,13 +1145,37 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
     const int row = b * K + j;
     const void *pr = logit_row<DT>(a.f, 0, row), *qr = logit_row<DT>(a.f, 1, row);
     const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
+    const float *gr = a.gumbel + (int64_t)b * V;
     Candidate more = {-INFINITY, 0x7fffffff}, any = {-INFINITY, 0x7fffffff};  // best among p > q, best of p
-    for (int i = tid; i < V; i += kDrawThreads) {
-        const double p = kept_prob(cp, t, logit<DT>(pr, i), i);
+    auto visit = [&](float xp, int i) __attribute__((always_inline)) {
+        const double p = kept_prob(cp, t, xp, i);
         if (p > 0.0) {
-            const double q = kept_prob(cq, t, logit<DT>(qr, i), i), g = (double)a.gumbel[(int64_t)b * V + i];
+            const double q = kept_prob(cq, t, logit<DT>(qr, i), i), g = (double)gr[i];
             if (p > q) more.take(log(p - q) + g, i);
             any.take(log(p) + g, i);
+        }
+    };
+    if (!cp.listed) {
+        const int end = min(V, (piece + 1) * kDrawPiece);
+        for (int i0 = piece * kDrawPiece + tid; i0 < end; i0 += 8 * kDrawThreads) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = i0 + e * kDrawThreads < end ? logit<DT>(pr, i0 + e * kDrawThreads) : -INFINITY;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {   // (one copy of the visit: the logits move down by one)
+                visit(x[0], i0 + e * kDrawThreads);
+#pragma unroll
+                for (int r = 0; r < 7; ++r) x[r] = x[r + 1];
+            }
+        }
+    } else if (piece == 0) {
+        for (int c = wave; c < a.f.chunks; c += kDrawThreads / 64) {
+            const uint2 *list = a.f.lists + ((int64_t)row * a.f.chunks + c) * a.f.list_cap;
+            const int n = a.f.stats[(int64_t)row * a.f.chunks + c].count;
+            for (int i = lane; i < n; i += 64) {
+                const uint2 v = list[i];
+                visit(__uint_as_float(v.x) + 0.f, (int)v.y);
+            }
         }
     }
 #pragma unroll
@@ -1059,7 +1192,7 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
             more.take(s_best[0][w].score, s_best[0][w].index);
             any.take(s_best[1][w].score, s_best[1][w].index);
         }
-        a.replacement[b] = more.index != 0x7fffffff ? more.index : any.index != 0x7fffffff ? any.index : -1;
+        a.best[(int64_t)b * gridDim.x + piece] = {more.score, any.score, more.index, any.index};
     }
 }
 
@@ -1079,7 +1212,22 @@ __global__ void __launch_bounds__(256) filtered_commit_kernel(const FilteredArgs
         if (c.do_commit) probe = commit_probe(c, b, lane);
         const int m = min(j + 1, K);
         if (lead) {
-            const int repl = j < K ? a.replacement[b] : -1;
+            Candidate more = {-INFINITY, 0x7fffffff}, any = {-INFINITY, 0x7fffffff};
+            if (j < K) {
+                for (int i = lane; i < a.pieces; i += 64) {
+                    const DrawBest d = a.best[(int64_t)b * a.pieces + i];
+                    more.take(d.more, d.more_index);
+                    any.take(d.any, d.any_index);
+                }
+#pragma unroll
+                for (int off = 32; off >= 1; off >>= 1) {
+                    const double v0 = __shfl_xor(more.score, off), v1 = __shfl_xor(any.score, off);
+                    const int i0 = __shfl_xor(more.index, off), i1 = __shfl_xor(any.index, off);
+                    more.take(v0, i0);
+                    any.take(v1, i1);
+                }
+            }
+            const int repl = more.index != 0x7fffffff ? more.index : any.index != 0x7fffffff ? any.index : -1;
             const int draft = lane < K ? c.draft_tokens[(int64_t)b * K + lane] : -1;
             if (lane < K) c.out_tokens[(int64_t)b * K + lane] = lane < j ? draft : lane == j ? repl : -1;
             const int last = __shfl(draft, K - 1);
@@ -1103,14 +1251,17 @@ __global__ void __launch_bounds__(256) filtered_commit_kernel(const FilteredArgs
     if (s_m > 0) append_rows(c, b, layer, s_L, s_m, tid, 256, s_pg);
 }
 
-hipError_t launch_filtered_consensus(const FilteredArgs &a, hipStream_t stream)
+int draw_pieces(int vocab) { return (vocab + kDrawPiece - 1) / kDrawPiece; }
+
+hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream)
 {
     const ConsensusArgs &c = a.c;
     hipError_t e = launch_filters<false>(a.f, stream);
     if (e != hipSuccess) return e;
-    if (a.f.dtype == 0) hipLaunchKernelGGL((filtered_draw_kernel<0>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
-    else if (a.f.dtype == 1) hipLaunchKernelGGL((filtered_draw_kernel<1>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filtered_draw_kernel<2>), dim3(c.batch), dim3(kDrawThreads), 0, stream, a);
+    const dim3 grid((unsigned)a.pieces, (unsigned)c.batch);
+    if (a.f.dtype == 0) hipLaunchKernelGGL((filtered_draw_kernel<0>), grid, dim3(kDrawThreads), 0, stream, a);
+    else if (a.f.dtype == 1) hipLaunchKernelGGL((filtered_draw_kernel<1>), grid, dim3(kDrawThreads), 0, stream, a);
+    else hipLaunchKernelGGL((filtered_draw_kernel<2>), grid, dim3(kDrawThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(filtered_commit_kernel, dim3(c.batch, c.do_commit ? c.num_layers : 1), dim3(256), 0, stream, a);

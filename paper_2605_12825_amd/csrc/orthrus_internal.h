@@ -88,6 +88,7 @@ struct RowCut {
     float min_w;
     uint32_t key;    // order_key of the last logit kept
     int32_t tie;
+    int32_t listed;  // 1: all that is kept is in the lists of the row's chunks
 };
 
 // What the pass over the logits leaves of one chunk of a row.
@@ -116,12 +117,19 @@ struct FilterArgs {
     int dtype;               // orthrus_dtype
 };
 
+// Best candidates of a piece of the replacement's draw: among tokens with p > q, among all with p > 0 (index INT_MAX: none).
+struct DrawBest {
+    double more, any;
+    int32_t more_index, any_index;
+};
+
 struct FilteredArgs {
     ConsensusArgs c;
     FilterArgs f;
     const float *accept_u;   // [B][K]
     const float *gumbel;     // [B][V]
-    int32_t *replacement;    // [B] (workspace)
+    DrawBest *best;          // [B][pieces] (workspace)
+    int pieces;
 };
 
 struct TablesArgs {
@@ -268,8 +276,9 @@ hipError_t launch_prefill_split(const AttnArgs &a, int head_dim, int num_cus, hi
 hipError_t launch_consensus(ConsensusArgs a, hipStream_t stream);
 hipError_t launch_sampling_consensus(const SamplingArgs &a, hipStream_t stream);
 size_t filter_workspace_bytes(int64_t rows, int vocab, int views);
-hipError_t launch_sample_tokens(const FilterArgs &a, hipStream_t stream);
-hipError_t launch_filtered_consensus(const FilteredArgs &a, hipStream_t stream);
+hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream);
+int draw_pieces(int vocab);
+hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream);
 hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream);
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
 int consensus_chunk_elems();

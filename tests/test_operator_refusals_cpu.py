@@ -115,8 +115,8 @@ def test_workspace_queries():
         assert f(_params()) >= 0 and f(_params(batch=0)) >= 0
         with pytest.raises(orthrus.OrthrusError):
             f(_params(vocab=1 << 22))
-    # per row and view what its filters keep (24 bytes), three words per sequence
-    assert orthrus.orthrus_filtered_workspace_bytes(_params()) >= 2 * 12 * 24 + 3 * 3 * 4
+    # per row and view what its filters keep (24 bytes and more), two words per sequence
+    assert orthrus.orthrus_filtered_workspace_bytes(_params()) >= 2 * 12 * 24 + 3 * 2 * 4
     assert orthrus.orthrus_page_tables_workspace_bytes(_params()) >= (3 * 3 + 2) * 4
     with pytest.raises(orthrus.OrthrusError):
         orthrus.orthrus_page_tables_workspace_bytes(_params(max_seq_len=9 * 16 + 1))
