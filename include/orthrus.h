@@ -312,7 +312,7 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
  *   logprobs     [dev] fp32 [B, K] or NULL written if given
  *   p            batch, block_k and vocab are used
  *   workspace/workspace_bytes: at least orthrus_sample_workspace_bytes(p)
- * Supported: V <= 2097152.
+ * Supported: V <= 1048576.
  */
 int64_t orthrus_sample_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
@@ -333,7 +333,7 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
  *   temperature, top_k, top_p, min_p as in orthrus_sample_tokens, applied to both views
  *   remaining arguments as in orthrus_sampling_consensus_commit
  *   workspace/workspace_bytes: at least orthrus_filtered_workspace_bytes(p)
- * Probabilities are formed in 64 bits.  Supported: V <= 2097152.
+ * Probabilities are formed in 64 bits.  Supported: V <= 1048576.
  */
 int64_t orthrus_filtered_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,

@@ -146,7 +146,8 @@ orthrus_status check_filter_params(const orthrus_params *p)
 {
     const orthrus_status s = check_params(p, false, true, false);
     if (s != ORTHRUS_OK) return s;
-    return p->vocab > (1 << 21) ? ORTHRUS_EUNSUPPORTED : ORTHRUS_OK;
+    if (p->vocab > (1 << 20) || !orthrus::filter_fits((int64_t)p->batch * p->block_k, p->vocab, 2)) return ORTHRUS_EUNSUPPORTED;
+    return ORTHRUS_OK;
 }
 
 // `words`: the addresses of every 4-byte operand, or-ed together.
@@ -739,7 +740,6 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
     if (p->batch == 0) return ORTHRUS_OK;
     const int64_t rows = (int64_t)p->batch * p->block_k;
     const size_t need = orthrus::filter_workspace_bytes(rows, p->vocab, 1);
-    if (rows * 2 * (((int64_t)p->vocab + 2047) / 2048 + 1) > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
     if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return ORTHRUS_EWORKSPACE;
     orthrus::FilterArgs a = filter_args(p, logits_type, logits, nullptr, logits_stride_row, temperature, top_k, top_p, min_p);
     a.u = u; a.tokens = tokens; a.logprobs = logprobs;

@@ -20,6 +20,7 @@
 #include "orthrus_internal.h"
 
 #include <cfloat>
+#include <type_traits>
 
 namespace orthrus {
 
@@ -110,6 +111,67 @@ __device__ __forceinline__ bool kept(const RowCut &c, float x, int i)
     return x > -INFINITY && (key > c.key || (key == c.key && i <= c.tie));
 }
 
+// ---- exchange between lanes, within a row of sixteen without a trip through LDS
+
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;  // DPP: lanes xor 1, xor 2, 7 - i, 15 - i
+template <int CTRL> __device__ __forceinline__ float swap_f32(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL> __device__ __forceinline__ u64 swap_u64(u64 x)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, 0xf, 0xf, true);
+    return (u64)hi << 32 | lo;
+}
+template <int CTRL> __device__ __forceinline__ double swap_f64(double x)
+{
+    return __longlong_as_double((long long)swap_u64<CTRL>((u64)__double_as_longlong(x)));
+}
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = fmaxf(x, swap_f32<kSwap1>(x));
+    x = fmaxf(x, swap_f32<kSwap2>(x));
+    x = fmaxf(x, swap_f32<kMirror8>(x));
+    x = fmaxf(x, swap_f32<kMirror16>(x));
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ double wave_sum(double x)   // the same order in every lane up to mirroring
+{
+    x += swap_f64<kSwap1>(x);
+    x += swap_f64<kSwap2>(x);
+    x += swap_f64<kMirror8>(x);
+    x += swap_f64<kMirror16>(x);
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+__device__ __forceinline__ u64 wave_sum(u64 x)
+{
+    x += swap_u64<kSwap1>(x);
+    x += swap_u64<kSwap2>(x);
+    x += swap_u64<kMirror8>(x);
+    x += swap_u64<kMirror16>(x);
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+// Inclusive sum in lane order: shifts within rows of sixteen, then the last lane of a row to the rows behind it.
+__device__ __forceinline__ u64 wave_scan(u64 x)
+{
+    auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, ctrl.value, rows.value, 0xf, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), ctrl.value, rows.value, 0xf, false);
+        x += (u64)hi << 32 | lo;
+    };
+    step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());   // row_shr 1, 2, 4, 8
+    step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());   // row_bcast 15 to rows 1 and 3
+    step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());   // row_bcast 31 to rows 2 and 3
+    return x;
+}
+
 // ---- running sums over bins in LDS
 
 struct Crossing {
@@ -118,16 +180,16 @@ struct Crossing {
     u64 at;       // the bin's own amount
 };
 
-// Bins of a workgroup of THREADS, PER of them to a thread.  Every function contains barriers.
+// Bins of a workgroup of THREADS, PER of them to a thread.  They are zero except between the first amount that is added and
+// the search, which leaves zeros behind.  Every function contains barriers, the last of them behind its last access.
 template <int THREADS, int PER> struct Bins {
-    static constexpr int kCount = THREADS * PER;
+    static constexpr int kCount = THREADS * PER, kWaves = THREADS / 64;
     u64 amount[kCount];
-    u64 wave_sum[THREADS / 64];
+    u64 wave_total[kWaves];
     Crossing hit;
 
-    __device__ __forceinline__ void clear(int tid)
+    __device__ __forceinline__ void clear(int tid)   // once, before the first use
     {
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; ++i) amount[i * THREADS + tid] = 0;
         __syncthreads();
@@ -140,18 +202,15 @@ template <int THREADS, int PER> struct Bins {
         u64 h[PER], sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) { h[i] = amount[tid * PER + i]; sum += h[i]; }
-        u64 run = sum;
-        const int lane = tid & 63;
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const u64 o = __shfl_up(run, off);
-            if (lane >= off) run += o;
-        }
-        if (lane == 63) wave_sum[tid >> 6] = run;
+        for (int i = 0; i < PER; ++i) amount[tid * PER + i] = 0;
+        const u64 run = wave_scan(sum);
+        if ((tid & 63) == 63) wave_total[tid >> 6] = run;
         if (tid == 0) hit = {-1, 0, 0};
         __syncthreads();
         u64 before = run - sum;
-        for (int w = 0; w < (tid >> 6); ++w) before += wave_sum[w];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) before += w < (tid >> 6) ? wave_total[w] : 0;
         if (before < target && target <= before + sum) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
@@ -160,18 +219,20 @@ template <int THREADS, int PER> struct Bins {
             }
         }
         __syncthreads();
-        return hit;
+        const Crossing c = hit;
+        __syncthreads();
+        return c;
     }
 
     __device__ __forceinline__ u64 sum_of(int tid, u64 v)
     {
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-        __syncthreads();
-        if ((tid & 63) == 0) wave_sum[tid >> 6] = v;
+        v = wave_sum(v);
+        if ((tid & 63) == 0) wave_total[tid >> 6] = v;
         __syncthreads();
         v = 0;
-        for (int w = 0; w < THREADS / 64; ++w) v += wave_sum[w];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += wave_total[w];
+        __syncthreads();
         return v;
     }
 };
@@ -180,7 +241,7 @@ __device__ __forceinline__ u64 to_fixed(double w, double unit) { return (u64)(w 
 
 // ---- the pass over the logits
 
-constexpr int kScanThreads = 256;
+constexpr int kScanThreads = 256;  // four waves
 
 template <int DT> struct Vector {
     static constexpr int kCount = DT == 0 ? 4 : 8;  // logits to 16 bytes
@@ -205,35 +266,45 @@ template <int DT> __device__ __forceinline__ void unpack(uint4 q, float *x)
     }
 }
 
-// A chunk of a row: kScanThreads * PER logits from a 16-byte boundary on, so that all but a row's first and last vector are
+// A chunk of a row, one wave's: kChunk logits from a 16-byte boundary on, so that all but a row's first and last vector are
 // loaded whole.  `first` is the row index of its first logit (negative in a row that starts inside a vector).
-template <int DT, int PER> struct Chunk {
-    static constexpr int kVec = Vector<DT>::kCount, kLoads = PER / kVec, kElems = kScanThreads * PER;
+constexpr int kEach = 32, kChunk = 64 * kEach, kListCap = 128;
+
+template <int DT> __device__ __forceinline__ int row_skew(const void *row)   // logits between the boundary and the row's start
+{
+    constexpr int kVec = Vector<DT>::kCount;
+    return (int)((uintptr_t)row / (16 / kVec)) & (kVec - 1);
+}
+
+template <int DT> struct Chunk {
+    static constexpr int kVec = Vector<DT>::kCount, kLoads = kEach / kVec;
     const void *row;
     int first, vocab;
 
-    __device__ __forceinline__ Chunk(const void *r, int chunk, int v) : row(r), vocab(v)
-    {
-        const int skew = (int)((uintptr_t)r / (16 / kVec)) & (kVec - 1);
-        first = chunk * kElems - skew;
-    }
-    __device__ __forceinline__ int index(int load, int tid) const { return first + (load * kScanThreads + tid) * kVec; }
+    __device__ __forceinline__ int index(int load, int lane) const { return first + (load * 64 + lane) * kVec; }
     // (raw: not cleaned)
-    __device__ __forceinline__ void load(int tid, float (&x)[PER]) const
+    template <bool NT> __device__ __forceinline__ void load(int lane, float (&x)[kEach]) const
     {
-        const uint4 *at = (const uint4 *)((const char *)row + (int64_t)first * (16 / kVec)) + tid;
-        if (first >= 0 && first + kElems <= vocab) {
+        typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+        const u32x4 *at = (const u32x4 *)((const char *)row + (int64_t)first * (16 / kVec)) + lane;
+        auto one = [&](int u) __attribute__((always_inline)) {
+            u32x4 q;
+            if constexpr (NT) q = __builtin_nontemporal_load(at + u * 64);
+            else q = at[u * 64];
+            return make_uint4(q[0], q[1], q[2], q[3]);
+        };
+        if (first >= 0 && first + kChunk <= vocab) {
             uint4 q[kLoads];
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) q[u] = at[u * kScanThreads];
+            for (int u = 0; u < kLoads; ++u) q[u] = one(u);
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) unpack<DT>(q[u], &x[u * kVec]);
         } else {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
-                const int i = index(u, tid);
+                const int i = index(u, lane);
                 if (i >= 0 && i + kVec <= vocab) {
-                    unpack<DT>(at[u * kScanThreads], &x[u * kVec]);
+                    unpack<DT>(one(u), &x[u * kVec]);
                 } else {
 #pragma unroll
                     for (int r = 0; r < kVec; ++r)
@@ -259,86 +330,66 @@ struct Least {
     }
 };
 
-// The list's threshold is the third least of the maxima of 256 / GROUP groups of lanes (of those that hold anything): of
-// 32 groups 82 logits +- 20 reach it in a row without order, of 16 groups 30 +- 10.  (The least one of all leaves 130 +- 41,
-// with a tail that overran the list in one chunk of 200 and so in every fourth row.)
-template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThreads) filter_scan_kernel(const FilterArgs a)
+// A wave to a chunk, without a word to the others: waves that wait for their loads then run beside waves that compute.
+// The list's threshold is the third least of the maxima of sixteen groups of four lanes (of those that hold anything): 30
+// logits +- 10 reach it in a row without order.  (The least one of all leaves 38 more with a tail that overruns a list of
+// 128 in one chunk of 200.)  NT: the logits are more than the last-level cache holds.
+template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filter_scan_kernel(const FilterArgs a)
 {
-    const int rr = blockIdx.x / a.chunks, chunk = blockIdx.x - rr * a.chunks, tid = threadIdx.x;
-    const int side = rr >= a.rows, row = rr - side * a.rows, lane = tid & 63, wave = tid >> 6;
-    if (blockIdx.x == 0 && tid == 0) a.unresolved[0] = 0;
+    const int lane = threadIdx.x & 63;
+    const uint32_t item = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item == 0 && lane == 0) a.unresolved[0] = 0;
+    const int rr = (int)(item / (uint32_t)a.chunks), chunk = (int)(item - (uint32_t)rr * a.chunks);
+    if (rr >= a.all_rows) return;
+    const int side = rr >= a.rows, row = rr - side * a.rows;
     const RowFilter f = row_filter(a, row / a.block_k);
-    const Chunk<DT, PER> c(logit_row<DT>(a, side, row), chunk, a.vocab);
-    float x[PER];
-    c.load(tid, x);
+    const void *logits = logit_row<DT>(a, side, row);
+    const Chunk<DT> c = {logits, chunk * kChunk - row_skew<DT>(logits), a.vocab};
+    float x[kEach];
+    c.template load<NT>(lane, x);
     float top = x[0];
 #pragma unroll
-    for (int i = 1; i < PER; ++i) top = fmaxf(top, x[i]);
-#pragma unroll
-    for (int off = 1; off < GROUP; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+    for (int i = 1; i < kEach; ++i) top = fmaxf(top, x[i]);
+    top = fmaxf(top, swap_f32<kSwap1>(top));
+    top = fmaxf(top, swap_f32<kSwap2>(top));
     const bool hollow = !(top > -INFINITY);   // (also where all are NaN)
     Least low = {hollow ? INFINITY : top, INFINITY, INFINITY};
     if (hollow) top = -INFINITY;
-#pragma unroll
-    for (int off = GROUP; off < 64; off <<= 1) {
-        top = fmaxf(top, __shfl_xor(top, off));
-        low.merge(__shfl_xor(low.a, off), __shfl_xor(low.b, off), __shfl_xor(low.c, off));
-    }
-    __shared__ float4 s_low[4];
-    __shared__ double s_sum[4];
-    __shared__ int s_count[4], s_hollow[4];
-    const bool hollow_wave = __ballot(hollow) != 0;
-    if (lane == 0) {
-        s_low[wave] = make_float4(low.a, low.b, low.c, top);
-        s_hollow[wave] = hollow_wave;
-    }
-    __syncthreads();
-    float4 l = s_low[0];
-    low = {l.x, l.y, l.z};
-    top = l.w;
-#pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        l = s_low[w];
-        low.merge(l.x, l.y, l.z);
-        top = fmaxf(top, l.w);
-    }
+    low.merge(swap_f32<kMirror8>(low.a), swap_f32<kMirror8>(low.b), swap_f32<kMirror8>(low.c));
+    low.merge(swap_f32<kMirror16>(low.a), swap_f32<kMirror16>(low.b), swap_f32<kMirror16>(low.c));
+    low.merge(__shfl_xor(low.a, 16), __shfl_xor(low.b, 16), __shfl_xor(low.c, 16));
+    low.merge(__shfl_xor(low.a, 32), __shfl_xor(low.b, 32), __shfl_xor(low.c, 32));
+    top = wave_max(top);
     float tau = low.c < INFINITY ? low.c : low.b < INFINITY ? low.b : low.a < INFINITY ? low.a : -INFINITY;
     if (top == INFINITY) {   // +inf counts as the largest float.  (A NaN drops out of all that follows by itself.)
         top = FLT_MAX;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = clean_logit(x[i]);
+        for (int i = 0; i < kEach; ++i) x[i] = clean_logit(x[i]);
         tau = low.a < INFINITY ? fminf(tau, FLT_MAX) : FLT_MAX;
     }
-    if (s_hollow[0] | s_hollow[1] | s_hollow[2] | s_hollow[3]) {   // few logits, the others masked: list them all if there is room
+    if (__ballot(hollow) != 0) {   // few logits, the others masked: list them all if there is room
         int alive = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) alive += __popcll(__ballot(x[i] > -INFINITY));
-        if (lane == 0) s_count[wave] = alive;
-        __syncthreads();
-        if (s_count[0] + s_count[1] + s_count[2] + s_count[3] <= a.list_cap) tau = -INFINITY;
-        __syncthreads();
+        for (int i = 0; i < kEach; ++i) alive += __popcll(__ballot(x[i] > -INFINITY));
+        if (alive <= kListCap) tau = -INFINITY;
     }
-    // ---- the list, in the order of waves, loads and lanes
+    // ---- the list, in the order of loads and lanes
     const float line = fmaxf(tau, -FLT_MAX);   // (-inf is never listed)
-    u64 reach[PER];
-    int mine = 0;
+    u64 reach[kEach];
+    int n = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = 0; i < kEach; ++i) {
         reach[i] = __ballot(x[i] >= line);
-        mine += __popcll(reach[i]);
+        n += __popcll(reach[i]);
     }
-    if (lane == 0) s_count[wave] = mine;
-    __syncthreads();
-    const int n = s_count[0] + s_count[1] + s_count[2] + s_count[3];
-    if (n <= a.list_cap) {
-        uint2 *list = a.lists + ((int64_t)rr * a.chunks + chunk) * a.list_cap;
-        for (int w = 0; w < wave; ++w) list += s_count[w];
+    if (n <= kListCap) {
+        uint2 *list = a.lists + (int64_t)item * kListCap;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
+        for (int i = 0; i < kEach; ++i)
             if (reach[i]) {
                 if (reach[i] >> lane & 1)
                     list[__builtin_amdgcn_mbcnt_hi((uint32_t)(reach[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach[i], 0))] =
-                        make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, tid) + i % c.kVec);
+                        make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, lane) + i % c.kVec);
                 list += __popcll(reach[i]);
             }
     }
@@ -346,19 +397,16 @@ template <int DT, int PER, int GROUP> __global__ void __launch_bounds__(kScanThr
     double sum = 0.0;
     if (wants_sum(f) && top > -INFINITY) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sum += weight(x[i], top, f.t);
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
+        for (int i = 0; i < kEach; ++i) sum += weight(x[i], top, f.t);
+        sum = wave_sum(sum);
     }
-    if (lane == 0) s_sum[wave] = sum;
-    __syncthreads();
-    if (tid == 0) {
+    if (lane == 0) {
         ChunkStat r;
-        r.sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+        r.sum = sum;
         r.top = top;
-        r.tau = n <= a.list_cap ? tau : INFINITY;   // more equal ones than the list holds: nothing is listed
-        r.count = n <= a.list_cap ? n : 0;
-        a.stats[(int64_t)rr * a.chunks + chunk] = r;
+        r.tau = n <= kListCap ? tau : INFINITY;   // more equal ones than the list holds: nothing is listed
+        r.count = n <= kListCap ? n : 0;
+        a.stats[item] = r;
     }
 }
 
@@ -392,7 +440,6 @@ __device__ __forceinline__ Picked pick_digit(PickShared &s, int tid, const uint3
 #pragma unroll 1
     do {
         const int next = max(0, shift - 10);
-        s.bins.clear(tid);
 #pragma unroll
         for (int e = 0; e < kPickEach; ++e)
             if (amount[e] && (shift >= 32 || digit[e] >> shift == r.digit))
@@ -410,8 +457,8 @@ __device__ __forceinline__ Picked pick_digit(PickShared &s, int tid, const uint3
 __device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
 
-// PER: logits to a thread of the scan's chunks; 0: there was no scan, the row has at most kPickEntries logits and is read here.
-template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThreads) filter_pick_kernel(const FilterArgs a)
+// SCANNED: the row's chunks have been listed; else it has at most kPickEntries logits and is read here.
+template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads) filter_pick_kernel(const FilterArgs a)
 {
     const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ PickShared s;
@@ -421,7 +468,7 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
     // ---- the row's maximum, down to where its lists hold everything
     float top = -INFINITY, tau = -INFINITY;
     ChunkStat st[kChunksEach];
-    if constexpr (PER > 0) {
+    if constexpr (SCANNED) {
         const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
 #pragma unroll
         for (int i = 0; i < kChunksEach; ++i) {
@@ -442,14 +489,11 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
             top = fmaxf(top, x);
         }
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        top = fmaxf(top, __shfl_xor(top, off));
-        tau = fmaxf(tau, __shfl_xor(tau, off));
-    }
+    top = wave_max(top);
+    tau = wave_max(tau);
     if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
     if (tid == 0) s.count = 0;
-    __syncthreads();
+    s.bins.clear(tid);
 #pragma unroll
     for (int w = 0; w < kPickWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fmaxf(tau, s.tau[w]); }
     RowCut cut = {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0};
@@ -460,26 +504,24 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
         const bool plain = f.top_k == 0 && f.top_p >= 1.0 && f.min_p == 0.0;
         const float u = DRAW ? fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f) : 0.f;
         double part[kChunksEach], z = 0.0;   // the chunks' sums, relative to the row's maximum
-        if constexpr (PER > 0) {
+        if constexpr (SCANNED) {
 #pragma unroll
             for (int i = 0; i < kChunksEach; ++i) {
                 part[i] = st[i].sum * weight(st[i].top, top, f.t);
                 z += part[i];
             }
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
+            z = wave_sum(z);
             if (lane == 0) s.z[wave] = z;
             __syncthreads();
             z = 0.0;
 #pragma unroll
             for (int w = 0; w < kPickWaves; ++w) z += s.z[w];
         }
-        if (PER > 0 && plain) {
+        if (SCANNED && plain) {
             // ---- no filter: the chunk at which the running sum crosses, and its logits once more
             cut.z = z;
-            if constexpr (DRAW && PER > 0) {
+            if constexpr (DRAW && SCANNED) {
                 const double unit = exp2((double)min(50, 60 - ilogb(z)));
-                s.bins.clear(tid);
                 u64 sum = 0;
 #pragma unroll
                 for (int i = 0; i < kChunksEach; ++i) {
@@ -491,19 +533,18 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                 const u64 target = (u64)((double)u * (double)total) + 1;
                 const Crossing at = s.bins.crossing(tid, target);
                 // 1024 bins, a few neighbours to each; a thread looks at logits 512 apart
-                constexpr int kElems = kScanThreads * PER, kPerBin = kElems / 1024, kEach = kElems / kPickThreads;
-                const int first = at.bin * kElems - ((int)((uintptr_t)logits / (16 / Vector<DT>::kCount)) & (Vector<DT>::kCount - 1));
-                u64 m[kEach];
+                constexpr int kPerBin = kChunk / 1024, kPlaces = kChunk / kPickThreads;
+                const int first = at.bin * kChunk - row_skew<DT>(logits);
+                u64 m[kPlaces];
                 int last = -1;
 #pragma unroll
-                for (int e = 0; e < kEach; ++e) {
+                for (int e = 0; e < kPlaces; ++e) {
                     const int i = first + e * kPickThreads + tid;
                     const float x = i >= 0 && i < a.vocab ? logit<DT>(logits, i) : -INFINITY;
                     m[e] = x > -INFINITY ? to_fixed(weight(x, top, f.t), unit) : 0;
                 }
-                s.bins.clear(tid);
 #pragma unroll
-                for (int e = 0; e < kEach; ++e)
+                for (int e = 0; e < kPlaces; ++e)
                     if (m[e]) {
                         last = e * kPickThreads + tid;
                         atomicAdd(&s.bins.amount[last / kPerBin], m[e]);
@@ -516,9 +557,8 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                 if (in.bin < 0) {   // the chunk's sum was rounded apart from its parts': its last token that weighs anything
                     token = s.count;
                 } else {
-                    s.bins.clear(tid);
 #pragma unroll
-                    for (int e = 0; e < kEach; ++e) {
+                    for (int e = 0; e < kPlaces; ++e) {
                         const int place = e * kPickThreads + tid;
                         if (place / kPerBin == in.bin) s.bins.amount[place % kPerBin] = m[e];
                     }
@@ -534,35 +574,38 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
             const bool whole = tau == -INFINITY;   // that is all there are
             const uint32_t top_key = order_key(top);
             int n;
-            if constexpr (PER > 0) {
-                constexpr int kAhead = 4;   // lists of a wave whose first two loads go out together
-                for (int c0 = wave; c0 < a.chunks; c0 += kAhead * kPickWaves) {
+            if constexpr (SCANNED) {
+                // a list to half a wave, five of them at a time, two loads to each
+                constexpr int kAhead = 5, kHalves = kPickThreads / 32;
+                const int half = tid >> 5, at32 = tid & 31;
+                auto keep = [&](uint2 q) __attribute__((always_inline)) {
+                    const float x = __uint_as_float(q.x);
+                    if (x >= tau && x > -INFINITY) {
+                        const int at = atomicAdd(&s.count, 1);
+                        if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)q.y; }
+                    }
+                };
+                for (int c0 = half; c0 < a.chunks; c0 += kAhead * kHalves) {
                     uint2 v[2 * kAhead];
-                    int have[kAhead];
+                    int most = 0;
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u) {
-                        const int c = c0 + u * kPickWaves;
-                        have[u] = c < a.chunks ? s.listed[c] : 0;
-                        const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * a.list_cap;
+                        const int c = c0 + u * kHalves, have = c < a.chunks ? s.listed[c] : 0;
+                        const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * kListCap;
+                        most = max(most, have);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             v[2 * u + h] = make_uint2(0xff800000u, 0);   // -inf
-                            if (h * 64 + lane < have[u]) v[2 * u + h] = list[h * 64 + lane];
+                            if (h * 32 + at32 < have) v[2 * u + h] = list[h * 32 + at32];
                         }
                     }
-                    auto keep = [&](uint2 q) __attribute__((always_inline)) {
-                        const float x = __uint_as_float(q.x);
-                        if (x >= tau && x > -INFINITY) {
-                            const int at = atomicAdd(&s.count, 1);
-                            if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)q.y; }
-                        }
-                    };
 #pragma unroll
                     for (int u = 0; u < 2 * kAhead; ++u) keep(v[u]);
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u)
-                        for (int i = 128 + lane; i < have[u]; i += 64)
-                            keep(a.lists[((int64_t)rr * a.chunks + c0 + u * kPickWaves) * a.list_cap + i]);
+                    if (most > 64)
+                        for (int u = 0; u < kAhead; ++u) {
+                            const int c = c0 + u * kHalves, have = c < a.chunks ? s.listed[c] : 0;
+                            for (int i = 64 + at32; i < have; i += 32) keep(a.lists[((int64_t)rr * a.chunks + c) * kListCap + i]);
+                        }
                 }
                 __syncthreads();
                 n = s.count;
@@ -581,7 +624,7 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                     const int i = e * kPickThreads + tid;
                     bool there = i < n;
                     uint32_t key;
-                    if constexpr (PER > 0) {
+                    if constexpr (SCANNED) {
                         key = there ? s.key[i] : top_key;
                         index[e] = there ? (uint32_t)s.index[i] : 0u;
                     } else {
@@ -593,7 +636,7 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                     mass[e] = there ? to_fixed(weight(key_logit(key), top, f.t), kUnit) : 0;
                     known += mass[e];
                 }
-                if constexpr (PER == 0) {
+                if constexpr (!SCANNED) {
                     if (f.top_k > 0) n = (int)s.bins.sum_of(tid, (u64)__popc(live));
                 }
                 uint32_t cut_fall = 0xffffffffu;
@@ -663,7 +706,7 @@ template <int DT, int PER, bool DRAW> __global__ void __launch_bounds__(kPickThr
                     cut.z = (double)total / kUnit;
                     cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
                     cut.tie = cut_tie;
-                    cut.listed = PER > 0;
+                    cut.listed = SCANNED;
                     if constexpr (DRAW) {
                         token = (int)pick_digit(s, tid, index, mass, index_bits, (u64)((double)u * (double)total) + 1).digit;
 #pragma unroll
@@ -781,7 +824,6 @@ template <int DT> struct WideRow {
         static_assert(kMaxBlocks == 2 * kWideThreads, "two blocks to a thread");
         __syncthreads();
         const u64 b0 = 2 * tid < blocks ? s.block[2 * tid] : 0, b1 = 2 * tid + 1 < blocks ? s.block[2 * tid + 1] : 0;
-        s.bins.clear(tid);
         s.bins.amount[2 * tid] = b0;
         s.bins.amount[2 * tid + 1] = b1;
         const Crossing at = s.bins.crossing(tid, target);
@@ -795,7 +837,6 @@ template <int DT> struct WideRow {
             part[r] = i >= 0 && i < vocab ? amount_at(logit<DT>(row, i), i) : 0;
             sum += part[r];
         }
-        s.bins.clear(tid);
         s.bins.amount[tid] = sum;
         const Crossing in = s.bins.crossing(tid, target - at.before);
         if (tid == in.bin) {
@@ -835,7 +876,6 @@ template <int DT> struct WideRow {
 #pragma unroll 1
         for (int shift = 32; shift > 0;) {
             const int next = max(0, shift - 12);
-            s.steps.clear(tid);
             each_logit([&](float x, int) __attribute__((always_inline)) {
                 const uint32_t fall = ~order_key(x);
                 if (x > -INFINITY && (shift == 32 || fall >> shift == prefix))
@@ -857,7 +897,6 @@ template <int DT> struct WideRow {
     template <bool MASS> __device__ __forceinline__ u64 cut_at(u64 target, bool &summed)
     {
         summed = false;
-        s.steps.clear(tid);
         each_logit([&](float x, int) __attribute__((always_inline)) {
             if (x > -INFINITY) atomicAdd(&s.steps.amount[step_of(x)], MASS ? mass_of(x) : 1ull);
         });
@@ -911,7 +950,6 @@ template <int DT> struct WideRow {
 #pragma unroll 1
             for (int shift = by_index ? bits_of((uint32_t)(vocab - 1)) : 32; shift > 0;) {
                 const int next = max(0, shift - 10);
-                s.bins.clear(tid);
 #pragma unroll
                 for (int e = 0; e < kWideEach; ++e) {
                     const uint32_t d = by_index ? index[e] : fall[e];
@@ -954,6 +992,8 @@ template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) fil
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, count = a.unresolved[0];
     __shared__ WideShared s;
+    s.bins.clear(tid);
+    s.steps.clear(tid);
     for (int at = blockIdx.x; at < count; at += gridDim.x) {
         const int rr = a.unresolved[1 + at], side = rr >= a.rows, row = rr - side * a.rows;
         const RowFilter f = row_filter(a, row / a.block_k);
@@ -974,7 +1014,7 @@ template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) fil
         z = 0.0;
         for (int w = 0; w < kWideWaves; ++w) z += s.z[w];
         const void *logits = logit_row<DT>(a, side, row);
-        const int skew = (int)((uintptr_t)logits / (16 / WideRow<DT>::kVec)) & (WideRow<DT>::kVec - 1);
+        const int skew = row_skew<DT>(logits);
         // fixed point: the sum of all weights (at most one each) stays below 2^61
         const double unit = exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab)));
         WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
@@ -1030,64 +1070,61 @@ template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) fil
 // ---- launch plan: chunk size, workspace
 
 struct FilterPlan {
-    int per, chunks, list_cap;
+    int chunks;   // 0: no scan
     size_t stats, lists, unresolved, total;   // byte offsets
 };
 
-// A row of at most kPickEntries logits needs no scan.  Else chunks of 8192 logits, of 2048 where those would be fewer than two
-// to a CU: a chunk's time is then its latency.
 static FilterPlan filter_plan(int64_t rows, int vocab)   // rows of all views
 {
-    FilterPlan p;
-    const int64_t big = ((int64_t)vocab + 7 + 8191) / 8192;
-    p.per = vocab <= kPickEntries ? 0 : rows * big < 512 ? 8 : 32;
-    const int elems = kScanThreads * (p.per ? p.per : 32);
-    p.chunks = (int)(((int64_t)vocab + 7 + elems - 1) / elems);
-    if (p.chunks > kMaxChunks) { p.per = 32; p.chunks = (int)big; }
-    if (p.per == 0) p.chunks = 0;
-    p.list_cap = p.per == 32 ? 256 : 128;
+    FilterPlan p = {};
+    if (vocab <= kPickEntries) return p;
+    p.chunks = (vocab + 7 + kChunk - 1) / kChunk;   // (a row may start seven logits behind a boundary)
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    p.stats = 0;
     p.lists = up((size_t)rows * p.chunks * sizeof(ChunkStat));
-    p.unresolved = p.lists + up((size_t)rows * p.chunks * p.list_cap * sizeof(uint2));
-    p.total = p.per == 0 ? 0 : p.unresolved + up((size_t)(rows + 1) * sizeof(int32_t));
+    p.unresolved = p.lists + up((size_t)rows * p.chunks * kListCap * sizeof(uint2));
+    p.total = p.unresolved + up((size_t)(rows + 1) * sizeof(int32_t));
     return p;
 }
 
-size_t filter_workspace_bytes(int64_t rows, int vocab, int views) { return rows > 0 ? filter_plan(rows * views, vocab).total : 0; }
+// Chunks are counted in 32 bits.
+bool filter_fits(int64_t rows, int vocab, int views) { return rows * views * filter_plan(1, vocab).chunks < 0x7fffffff; }
+size_t filter_workspace_bytes(int64_t rows, int vocab, int views) { return filter_plan(rows * views, vocab).total; }
 
-template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArgs &a, const FilterPlan &p, int rows, hipStream_t stream)
+// Logits of more than this leave nothing behind in the last-level cache that a later kernel of the call would find.
+constexpr int64_t kKeepBytes = (int64_t)192 << 20;
+
+template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArgs &a, hipStream_t stream)
 {
-    if (p.per == 0) {
-        hipLaunchKernelGGL((filter_pick_kernel<DT, 0, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
+    if (a.chunks == 0) {
+        hipLaunchKernelGGL((filter_pick_kernel<DT, false, DRAW>), dim3(a.all_rows), dim3(kPickThreads), 0, stream, a);
         return hipGetLastError();
     }
-    const dim3 scan((unsigned)rows * (unsigned)p.chunks);
-    if (p.per == 32) hipLaunchKernelGGL((filter_scan_kernel<DT, 32, 8>), scan, dim3(kScanThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filter_scan_kernel<DT, 8, 16>), scan, dim3(kScanThreads), 0, stream, a);
+    const dim3 scan((unsigned)(((int64_t)a.all_rows * a.chunks + 3) / 4));
+    if ((int64_t)a.all_rows * a.vocab * (DT == 0 ? 4 : 2) > kKeepBytes)
+        hipLaunchKernelGGL((filter_scan_kernel<DT, true>), scan, dim3(kScanThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((filter_scan_kernel<DT, false>), scan, dim3(kScanThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.per == 32) hipLaunchKernelGGL((filter_pick_kernel<DT, 32, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filter_pick_kernel<DT, 8, DRAW>), dim3(rows), dim3(kPickThreads), 0, stream, a);
+    hipLaunchKernelGGL((filter_pick_kernel<DT, true, DRAW>), dim3(a.all_rows), dim3(kPickThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(rows < 512 ? rows : 512), dim3(kWideThreads), 0, stream, a);
+    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(a.all_rows < 512 ? a.all_rows : 512), dim3(kWideThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 template <bool DRAW> static hipError_t launch_filters(FilterArgs &a, hipStream_t stream)
 {
-    const int rows = a.rows * (DRAW ? 1 : 2);
-    const FilterPlan p = filter_plan(rows, a.vocab);
+    a.all_rows = a.rows * (DRAW ? 1 : 2);
+    const FilterPlan p = filter_plan(a.all_rows, a.vocab);
     char *ws = (char *)a.workspace;
     a.stats = (ChunkStat *)(ws + p.stats);
     a.lists = (uint2 *)(ws + p.lists);
     a.unresolved = (int32_t *)(ws + p.unresolved);
     a.chunks = p.chunks;
-    a.list_cap = p.list_cap;
-    if (a.dtype == 0) return launch_filters_of<0, DRAW>(a, p, rows, stream);
-    if (a.dtype == 1) return launch_filters_of<1, DRAW>(a, p, rows, stream);
-    return launch_filters_of<2, DRAW>(a, p, rows, stream);
+    if (a.dtype == 0) return launch_filters_of<0, DRAW>(a, stream);
+    if (a.dtype == 1) return launch_filters_of<1, DRAW>(a, stream);
+    return launch_filters_of<2, DRAW>(a, stream);
 }
 
 hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream) { return launch_filters<true>(a, stream); }
@@ -1170,7 +1207,7 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
         }
     } else if (piece == 0) {
         for (int c = wave; c < a.f.chunks; c += kDrawThreads / 64) {
-            const uint2 *list = a.f.lists + ((int64_t)row * a.f.chunks + c) * a.f.list_cap;
+            const uint2 *list = a.f.lists + ((int64_t)row * a.f.chunks + c) * kListCap;
             const int n = a.f.stats[(int64_t)row * a.f.chunks + c].count;
             for (int i = lane; i < n; i += 64) {
                 const uint2 v = list[i];

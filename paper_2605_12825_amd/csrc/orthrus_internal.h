@@ -107,11 +107,11 @@ struct FilterArgs {
     int32_t *tokens;
     float *logprobs;         // or NULL
     RowCut *cuts;            // consensus: [view][rows]
-    void *workspace;         // filter_workspace_bytes; the next five lie in it or follow from its plan
+    void *workspace;         // filter_workspace_bytes; the next lie in it or follow from its plan
     ChunkStat *stats;        // [view][row][chunk]
-    uint2 *lists;            // [view][row][chunk][list_cap]: (logit, index)
+    uint2 *lists;            // [view][row][chunk][128]: (logit, index)
     int32_t *unresolved;     // [0]: count, then rows (view * rows + row)
-    int chunks, list_cap;
+    int chunks, all_rows;
     int64_t stride_row;      // elements between rows
     int rows, block_k, vocab;
     int dtype;               // orthrus_dtype
@@ -275,6 +275,7 @@ hipError_t launch_prefill_attn(const AttnArgs &a, int head_dim, int num_cus, hip
 hipError_t launch_prefill_split(const AttnArgs &a, int head_dim, int num_cus, hipStream_t stream);
 hipError_t launch_consensus(ConsensusArgs a, hipStream_t stream);
 hipError_t launch_sampling_consensus(const SamplingArgs &a, hipStream_t stream);
+bool filter_fits(int64_t rows, int vocab, int views);
 size_t filter_workspace_bytes(int64_t rows, int vocab, int views);
 hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream);
 int draw_pieces(int vocab);
