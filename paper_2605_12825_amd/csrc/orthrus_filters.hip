@@ -97,7 +97,7 @@ __device__ __forceinline__ RowFilter row_filter(const FilterArgs &a, int b)
     const float p = a.top_p ? a.top_p[b] : 1.f, m = a.min_p ? a.min_p[b] : 0.f;
     const bool greedy = !(t > 0.f);  // T <= 0 or NaN: the largest logit, the lowest index among equals
     f.t.scale = greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)fminf(t, FLT_MAX);
-    f.t.floor = -1000.0 / f.t.scale;
+    f.t.floor = (greedy ? 1.0 : (double)fminf(t, FLT_MAX)) * -693.14718055994531;
     f.top_k = greedy ? 1 : k > 0 && k < a.vocab ? k : 0;
     f.top_p = greedy || !(p < 1.f) ? 1.0 : fmax((double)p, 0.0);
     f.min_p = greedy || !(m > 0.f) ? 0.0 : (double)fminf(m, 1.f);
@@ -154,6 +154,12 @@ __device__ __forceinline__ u64 wave_sum(u64 x)
     x += swap_u64<kMirror16>(x);
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
+}
+// A value that all lanes hold, in scalar registers.
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+__device__ __forceinline__ double uniform(double x)
+{
+    return __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(x)), __builtin_amdgcn_readfirstlane(__double2loint(x)));
 }
 // Inclusive sum in lane order: shifts within rows of sixteen, then the last lane of a row to the rows behind it.
 __device__ __forceinline__ u64 wave_scan(u64 x)
@@ -342,7 +348,6 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
     const int rr = (int)(item / (uint32_t)a.chunks), chunk = (int)(item - (uint32_t)rr * a.chunks);
     if (rr >= a.all_rows) return;
     const int side = rr >= a.rows, row = rr - side * a.rows;
-    const RowFilter f = row_filter(a, row / a.block_k);
     const void *logits = logit_row<DT>(a, side, row);
     const Chunk<DT> c = {logits, chunk * kChunk - row_skew<DT>(logits), a.vocab};
     float x[kEach];
@@ -373,32 +378,35 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
         for (int i = 0; i < kEach; ++i) alive += __popcll(__ballot(x[i] > -INFINITY));
         if (alive <= kListCap) tau = -INFINITY;
     }
-    // ---- the list, in the order of loads and lanes
+    // ---- the list, in the order of loads and lanes; through LDS, so that it leaves with one store (stores of one or two
+    // lanes each took 24 us of 113)
+    __shared__ uint2 s_list[kScanThreads / 64][kListCap];
+    uint2 *mine = s_list[threadIdx.x >> 6];
     const float line = fmaxf(tau, -FLT_MAX);   // (-inf is never listed)
-    u64 reach[kEach];
     int n = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        reach[i] = __ballot(x[i] >= line);
-        n += __popcll(reach[i]);
+        const bool hit = x[i] >= line;
+        const u64 hits = __ballot(hit);
+        if (hits) {
+            const int more = n + __popcll(hits);
+            if (more <= kListCap && hit)
+                mine[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0))] =
+                    make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, lane) + i % c.kVec);
+            n = more;
+        }
     }
-    if (n <= kListCap) {
-        uint2 *list = a.lists + (int64_t)item * kListCap;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (reach[i]) {
-                if (reach[i] >> lane & 1)
-                    list[__builtin_amdgcn_mbcnt_hi((uint32_t)(reach[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach[i], 0))] =
-                        make_uint2(__float_as_uint(x[i]), c.index(i / c.kVec, lane) + i % c.kVec);
-                list += __popcll(reach[i]);
-            }
-    }
+    if (n <= kListCap)
+        for (int i = lane; i < n; i += 64) a.lists[(int64_t)item * kListCap + i] = mine[i];
     // ---- the weights, relative to the chunk's maximum
     double sum = 0.0;
-    if (wants_sum(f) && top > -INFINITY) {
+    if (top > -INFINITY) {
+        const RowFilter f = row_filter(a, row / a.block_k);
+        if (wants_sum(f)) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) sum += weight(x[i], top, f.t);
-        sum = wave_sum(sum);
+            for (int i = 0; i < kEach; ++i) sum += weight(x[i], top, f.t);
+            sum = wave_sum(sum);
+        }
     }
     if (lane == 0) {
         ChunkStat r;
@@ -412,12 +420,12 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
 
 // ---- cuts and token from the lists
 
-constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
-constexpr int kPickEach = 6, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
-constexpr int kMaxChunks = 1024, kChunksEach = kMaxChunks / kPickThreads;
+constexpr int kPickThreads = 256, kPickWaves = kPickThreads / 64;
+constexpr int kPickEach = 8, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
+constexpr int kMaxChunks = 768, kChunksEach = kMaxChunks / kPickThreads;
 
 struct PickShared {
-    Bins<kPickThreads, 2> bins;
+    Bins<kPickThreads, 4> bins;
     uint32_t key[kPickEntries];
     int index[kPickEntries];
     uint16_t listed[kMaxChunks];
@@ -458,7 +466,7 @@ __device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_floa
 __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
 
 // SCANNED: the row's chunks have been listed; else it has at most kPickEntries logits and is read here.
-template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads) filter_pick_kernel(const FilterArgs a)
+template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads, 3) filter_pick_kernel(const FilterArgs a)
 {
     const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ PickShared s;
@@ -532,7 +540,7 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
                 const u64 total = s.bins.sum_of(tid, sum);
                 const u64 target = (u64)((double)u * (double)total) + 1;
                 const Crossing at = s.bins.crossing(tid, target);
-                // 1024 bins, a few neighbours to each; a thread looks at logits 512 apart
+                // 1024 bins, a few neighbours to each; a thread looks at logits 256 apart
                 constexpr int kPerBin = kChunk / 1024, kPlaces = kChunk / kPickThreads;
                 const int first = at.bin * kChunk - row_skew<DT>(logits);
                 u64 m[kPlaces];
@@ -706,7 +714,18 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
                     cut.z = (double)total / kUnit;
                     cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
                     cut.tie = cut_tie;
-                    cut.listed = SCANNED;
+                    if constexpr (!DRAW && SCANNED) {
+                        // what is kept, in place of the first of the row's lists, for the replacement's draw
+                        __syncthreads();
+                        if (tid == 0) s.count = 0;
+                        __syncthreads();
+                        uint2 *list = a.lists + (int64_t)rr * a.chunks * kListCap;
+#pragma unroll
+                        for (int e = 0; e < kPickEach; ++e)
+                            if (mass[e]) list[atomicAdd(&s.count, 1)] = make_uint2(__float_as_uint(key_logit(top_key - fall[e])), index[e]);
+                        __syncthreads();
+                        cut.listed = s.count;
+                    }
                     if constexpr (DRAW) {
                         token = (int)pick_digit(s, tid, index, mass, index_bits, (u64)((double)u * (double)total) + 1).digit;
 #pragma unroll
@@ -738,13 +757,14 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
 // binade of the weight each) and then among the logits of one step, gathered in the second pass, which also sums what lies
 // above them; steps that hold more logits than the gather has room for (rows of equal logits) go digit by digit.
 constexpr int kWideThreads = 512, kWideWaves = kWideThreads / 64;
-constexpr int kWideEach = 8, kWideEntries = kWideThreads * kWideEach;
-constexpr int kSteps = 4096, kMaxBlocks = 1024;
+constexpr int kWideEntries = 4096;
+constexpr int kSteps = 4096, kMaxBlocks = 520;   // of 2048 logits (or 4096): 2^20 and what a row's start takes
 
 struct WideShared {
     Bins<kWideThreads, 2> bins;
-    Bins<kWideThreads, kSteps / kWideThreads> steps;
+    Bins<kWideThreads, (kSteps + kWideThreads - 1) / kWideThreads> steps;
     u64 block[kMaxBlocks];
+    u64 mass[kWideEntries];
     uint32_t key[kWideEntries];
     int index[kWideEntries];
     float top[kWideWaves], tau[kWideWaves];
@@ -772,26 +792,30 @@ template <int DT> struct WideRow {
         return kept(cut, x, i) && w >= (double)cut.min_w ? to_fixed(w, unit) : 0;
     }
 
-    // visit(x, index) for every logit of the wave's block
+    // visit(x, index) for every logit of the wave's block, two vectors ahead of it.
     template <typename F> __device__ __forceinline__ void block_logits(int blk, F visit)
     {
-        const int lane = tid & 63;
-        uint4 q[8];
-#pragma unroll
+        const int lane = tid & 63, first = (blk * 512 + lane) * kVec - skew;
+        auto load = [&](int u) __attribute__((always_inline)) {
+            const int i = first + u * 64 * kVec;
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (u < 8 && i >= 0 && i + kVec <= vocab) q = *(const uint4 *)((const char *)row + (int64_t)i * (16 / kVec));
+            return q;
+        };
+        uint4 q0 = load(0), q1 = load(1);
+#pragma unroll 1
         for (int u = 0; u < 8; ++u) {
-            const int i = (blk * 512 + u * 64 + lane) * kVec - skew;
-            q[u] = make_uint4(0, 0, 0, 0);
-            if (i >= 0 && i + kVec <= vocab) q[u] = *(const uint4 *)((const char *)row + (int64_t)i * (16 / kVec));
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int i = (blk * 512 + u * 64 + lane) * kVec - skew;
+            const uint4 q = q0;
+            q0 = q1;
+            q1 = load(u + 2);
+            const int i = first + u * 64 * kVec;
             if (i >= 0 && i + kVec <= vocab) {
                 float x[kVec];
-                unpack<DT>(q[u], x);
+                unpack<DT>(q, x);
 #pragma unroll
                 for (int r = 0; r < kVec; ++r) visit(clean_logit(x[r]), i + r);
             } else {
+#pragma unroll 1
                 for (int r = 0; r < kVec; ++r)
                     if (i + r >= 0 && i + r < vocab) visit(logit<DT>(row, i + r), i + r);
             }
@@ -821,15 +845,15 @@ template <int DT> struct WideRow {
     // With s.block[] made of amount_at: the first index at which the running sum reaches the target (-1: none).
     template <typename F> __device__ __forceinline__ int find_in_blocks(u64 target, F amount_at)
     {
-        static_assert(kMaxBlocks == 2 * kWideThreads, "two blocks to a thread");
+        static_assert(kMaxBlocks <= 2 * kWideThreads, "two blocks to a thread at most");
         __syncthreads();
         const u64 b0 = 2 * tid < blocks ? s.block[2 * tid] : 0, b1 = 2 * tid + 1 < blocks ? s.block[2 * tid + 1] : 0;
         s.bins.amount[2 * tid] = b0;
         s.bins.amount[2 * tid + 1] = b1;
         const Crossing at = s.bins.crossing(tid, target);
         if (at.bin < 0) return -1;
-        // the block's vectors, one to a thread
-        const int first = (at.bin * 512 + tid) * kVec - skew;
+        // the block's 512 vectors, one to a thread
+        const int first = tid < 512 ? (at.bin * 512 + tid) * kVec - skew : vocab;
         u64 part[kVec], sum = 0;
 #pragma unroll
         for (int r = 0; r < kVec; ++r) {
@@ -894,37 +918,60 @@ template <int DT> struct WideRow {
 
     // Cuts where the sum in falling order (MASS: of weights, else of ones) reaches the target.  `summed`: s.block[] then holds
     // the kept weights, else it does not.  Returns the weight of what is kept without regard to min-p (0: not known).
+    // The first pass's weights are single precision (they only say which step to gather); the second's sums say whether it was
+    // the right one.
     template <bool MASS> __device__ __forceinline__ u64 cut_at(u64 target, bool &summed)
     {
         summed = false;
+        const float rate = (float)t.scale;
         each_logit([&](float x, int) __attribute__((always_inline)) {
-            if (x > -INFINITY) atomicAdd(&s.steps.amount[step_of(x)], MASS ? mass_of(x) : 1ull);
+            if (x > -INFINITY)
+                atomicAdd(&s.steps.amount[step_of(x)],
+                          MASS ? (u64)(uint32_t)(__builtin_amdgcn_exp2f((x - top) * rate) * 0x1p31f) : 1ull);
         });
-        const Crossing c = s.steps.crossing(tid, target);
-        if (MASS && c.bin < 0) return 0;   // everything together does not reach it: no cut
-        if (c.bin < 0) return 0;
-        if (tid == 0) s.count = 0;
-        __syncthreads();
-        u64 over = 0;   // weight of the steps above
+        const double goal1 = MASS ? (double)target * (0x1p31 / unit) : (double)target;
+        const Crossing c = s.steps.crossing(tid, max((u64)1, (u64)goal1));
+        if (!MASS && c.bin < 0) return 0;   // everything together does not reach it: no cut
+        int step = c.bin < 0 ? kSteps - 1 : c.bin;
         const double min_w = (double)cut.min_w;
-        sum_blocks([&](float x, int i) __attribute__((always_inline)) {
-            const int st = x > -INFINITY ? step_of(x) : kSteps;
-            if (st < c.bin) {
-                const double w = weight_of(x);
-                const u64 m = to_fixed(w, unit);
-                over += m;
-                return w >= min_w ? m : 0;
-            }
-            if (st == c.bin) {
-                const int at = atomicAdd(&s.count, 1);
-                if (at < kWideEntries) { s.key[at] = order_key(x); s.index[at] = i; }
-            }
-            return (u64)0;
-        });
-        over = s.bins.sum_of(tid, over);
-        const int n = s.count;
+        u64 over, at_step = 0;   // weight of the steps above, of this one
+        int n;
+#pragma unroll 1
+        for (int round = 0;; ++round) {
+            if (tid == 0) s.count = 0;
+            __syncthreads();
+            over = 0;
+            u64 here = 0;
+            sum_blocks([&](float x, int i) __attribute__((always_inline)) {
+                const int st = x > -INFINITY ? step_of(x) : kSteps;
+                u64 m = 0;
+                if (st <= step) {
+                    const double w = weight_of(x);
+                    m = to_fixed(w, unit);
+                    if (st == step) {
+                        here += m;
+                        m = 0;
+                        const int at = atomicAdd(&s.count, 1);
+                        if (at < kWideEntries) { s.key[at] = order_key(x); s.index[at] = i; }
+                    } else {
+                        over += m;
+                        if (!(w >= min_w)) m = 0;
+                    }
+                }
+                return m;
+            });
+            over = s.bins.sum_of(tid, over);
+            n = s.count;
+            if (!MASS) break;
+            at_step = s.bins.sum_of(tid, here);
+            // (the rounding of single precision can miss by a step or two)
+            const int other = target <= over ? step - 1 : target > over + at_step ? step + 1 : step;
+            if (other == step || other < 0 || other >= kSteps || round == 8) break;
+            step = other;
+        }
         __syncthreads();
-        if (n > kWideEntries) {
+        if (MASS && target > over + at_step && step == kSteps - 1) return 0;   // all of it does not reach the target: no cut
+        if (n > kWideEntries || (MASS && (target <= over || target > over + at_step))) {
             const Selected r = select_digits<MASS>(target);
             if (r.here == 0) return 0;
             const u64 each = MASS ? mass_of(key_logit(r.key)) : 1;
@@ -935,60 +982,72 @@ template <int DT> struct WideRow {
             return 0;
         }
         // ---- among the gathered logits
-        uint32_t fall[kWideEach], index[kWideEach];
-        u64 mass[kWideEach];
-#pragma unroll
-        for (int e = 0; e < kWideEach; ++e) {
-            const int i = e * kWideThreads + tid;
-            fall[e] = i < n ? ~s.key[i] : 0xffffffffu;
-            index[e] = i < n ? (uint32_t)s.index[i] : 0u;
-            mass[e] = i < n ? mass_of(key_logit(~fall[e])) : 0;
-        }
-        auto digit_at = [&](bool by_index, uint32_t at, bool ones, u64 goal) __attribute__((always_inline)) {
-            Selected r = {0, 0, 0};
-            uint32_t prefix = 0;
-#pragma unroll 1
-            for (int shift = by_index ? bits_of((uint32_t)(vocab - 1)) : 32; shift > 0;) {
-                const int next = max(0, shift - 10);
-#pragma unroll
-                for (int e = 0; e < kWideEach; ++e) {
-                    const uint32_t d = by_index ? index[e] : fall[e];
-                    if (e * kWideThreads + tid < n && (!by_index || fall[e] == at) && (shift == 32 || d >> shift == prefix))
-                        atomicAdd(&s.bins.amount[(d >> next) & ((1u << (shift - next)) - 1)], ones ? 1ull : mass[e]);
-                }
-                const Crossing x = s.bins.crossing(tid, goal - r.above);
-                if (x.bin < 0) return Selected{0, 0, 0};
-                r.above += x.before;
-                r.here = x.at;
-                prefix = prefix << (shift - next) | (uint32_t)x.bin;
-                shift = next;
-            }
-            r.key = prefix;
-            return r;
-        };
-        const u64 goal = target - c.before;
-        const Selected r = digit_at(false, 0, !MASS, goal);
+        for (int i = tid; i < n; i += kWideThreads) s.mass[i] = mass_of(key_logit(s.key[i]));
+        const u64 goal = target - (MASS ? over : c.before);
+        const Selected r = select_gathered<MASS>(n, goal);
         if (r.here == 0) return 0;
-        const u64 each = MASS ? mass_of(key_logit(~r.key)) : 1;
+        const u64 each = MASS ? mass_of(key_logit(r.key)) : 1;
         const u64 nth = (goal - r.above + each - 1) / each;
-        if (~r.key > cut.key) cut.tie = 0x7fffffff;
-        cut.key = ~r.key;
-        if (nth * each < r.here) cut.tie = min(cut.tie, (int)digit_at(true, r.key, true, nth).key);
+        if (r.key > cut.key) cut.tie = 0x7fffffff;
+        cut.key = r.key;
+        if (nth * each < r.here) cut.tie = min(cut.tie, nth_gathered(n, r.key, nth));
         u64 more = 0;
-#pragma unroll
-        for (int e = 0; e < kWideEach; ++e) {
-            const float x = key_logit(~fall[e]);
-            if (e * kWideThreads + tid < n && kept(cut, x, (int)index[e])) {
-                more += mass[e];
-                if (weight_of(x) >= min_w) atomicAdd(&s.block[((int)index[e] + skew) / kBlock], mass[e]);
+        for (int i = tid; i < n; i += kWideThreads) {
+            const float x = key_logit(s.key[i]);
+            const int index = s.index[i];
+            if (kept(cut, x, index)) {
+                more += s.mass[i];
+                if (weight_of(x) >= min_w) atomicAdd(&s.block[(index + skew) / kBlock], s.mass[i]);
             }
         }
         summed = true;
         return over + s.bins.sum_of(tid, more);
     }
+
+    // The same searches among the n gathered logits, ten bits at a time.
+    template <bool MASS> __device__ __forceinline__ Selected select_gathered(int n, u64 target)
+    {
+        Selected r = {0, 0, 0};
+        uint32_t prefix = 0;
+#pragma unroll 1
+        for (int shift = 32; shift > 0;) {
+            const int next = max(0, shift - 10);
+            for (int i = tid; i < n; i += kWideThreads) {
+                const uint32_t fall = ~s.key[i];
+                if (shift == 32 || fall >> shift == prefix)
+                    atomicAdd(&s.bins.amount[(fall >> next) & ((1u << (shift - next)) - 1)], MASS ? s.mass[i] : 1ull);
+            }
+            const Crossing c = s.bins.crossing(tid, target - r.above);
+            if (c.bin < 0) return {0, 0, 0};
+            r.above += c.before;
+            r.here = c.at;
+            prefix = prefix << (shift - next) | (uint32_t)c.bin;
+            shift = next;
+        }
+        r.key = ~prefix;
+        return r;
+    }
+    __device__ __forceinline__ int nth_gathered(int n, uint32_t key, u64 nth)
+    {
+        uint32_t prefix = 0;
+#pragma unroll 1
+        for (int shift = bits_of((uint32_t)(vocab - 1)); shift > 0;) {
+            const int next = max(0, shift - 10);
+            for (int i = tid; i < n; i += kWideThreads) {
+                const uint32_t d = (uint32_t)s.index[i];
+                if (s.key[i] == key && d >> shift == prefix) atomicAdd(&s.bins.amount[(d >> next) & ((1u << (shift - next)) - 1)], 1ull);
+            }
+            const Crossing c = s.bins.crossing(tid, nth);
+            if (c.bin < 0) return 0x7fffffff;
+            nth -= c.before;
+            prefix = prefix << (shift - next) | (uint32_t)c.bin;
+            shift = next;
+        }
+        return (int)prefix;
+    }
 };
 
-template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) filter_wide_kernel(const FilterArgs a)
+template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads, 2) filter_wide_kernel(const FilterArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, count = a.unresolved[0];
     __shared__ WideShared s;
@@ -1016,9 +1075,10 @@ template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads) fil
         const void *logits = logit_row<DT>(a, side, row);
         const int skew = row_skew<DT>(logits);
         // fixed point: the sum of all weights (at most one each) stays below 2^61
-        const double unit = exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab)));
+        const double unit = uniform(exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab))));
+        top = uniform(top);
         WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
-                         (float)(f.t.scale * (kSteps / 40.0)), f.t, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0}};
+                         uniform((float)(f.t.scale * (kSteps / 40.0))), {uniform(f.t.scale), uniform(f.t.floor)}, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0}};
         bool summed = false;
         u64 z1 = 0;
         if (f.top_k > 0) {
@@ -1109,7 +1169,7 @@ template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArg
     hipLaunchKernelGGL((filter_pick_kernel<DT, true, DRAW>), dim3(a.all_rows), dim3(kPickThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(a.all_rows < 512 ? a.all_rows : 512), dim3(kWideThreads), 0, stream, a);
+    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(a.all_rows < a.num_cus ? a.all_rows : a.num_cus), dim3(kWideThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -1184,35 +1244,41 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
     const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
     const float *gr = a.gumbel + (int64_t)b * V;
     Candidate more = {-INFINITY, 0x7fffffff}, any = {-INFINITY, 0x7fffffff};  // best among p > q, best of p
-    auto visit = [&](float xp, int i) __attribute__((always_inline)) {
+    float more_near = -INFINITY, any_near = -INFINITY;   // single precision: the full logarithm only for what comes near the best
+    auto visit = [&](float xp, float xq, float g, int i) __attribute__((always_inline)) {
         const double p = kept_prob(cp, t, xp, i);
         if (p > 0.0) {
-            const double q = kept_prob(cq, t, logit<DT>(qr, i), i), g = (double)gr[i];
-            if (p > q) more.take(log(p - q) + g, i);
-            any.take(log(p) + g, i);
+            const double q = kept_prob(cq, t, xq, i), r = p - q;
+            auto consider = [&](double v, float &near, Candidate &best) __attribute__((always_inline)) {
+                const float f = (float)v, score = __logf(f) + g;
+                if (!(score < near - 0.01f) || f < 1e-30f) {
+                    best.take(log(v) + (double)g, i);
+                    near = fmaxf(near, score);
+                }
+            };
+            if (r > 0.0) consider(r, more_near, more);
+            consider(p, any_near, any);
         }
     };
     if (!cp.listed) {
         const int end = min(V, (piece + 1) * kDrawPiece);
-        for (int i0 = piece * kDrawPiece + tid; i0 < end; i0 += 8 * kDrawThreads) {
-            float x[8];
+        for (int i0 = piece * kDrawPiece + tid; i0 < end; i0 += 4 * kDrawThreads) {
+            float x[4], y[4], g[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = i0 + e * kDrawThreads < end ? logit<DT>(pr, i0 + e * kDrawThreads) : -INFINITY;
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {   // (one copy of the visit: the logits move down by one)
-                visit(x[0], i0 + e * kDrawThreads);
-#pragma unroll
-                for (int r = 0; r < 7; ++r) x[r] = x[r + 1];
+            for (int e = 0; e < 4; ++e) {
+                const int i = i0 + e * kDrawThreads;
+                x[e] = i < end ? logit<DT>(pr, i) : -INFINITY;
+                y[e] = i < end ? logit<DT>(qr, i) : -INFINITY;
+                g[e] = i < end ? gr[i] : 0.f;
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) visit(x[e], y[e], g[e], i0 + e * kDrawThreads);
         }
     } else if (piece == 0) {
-        for (int c = wave; c < a.f.chunks; c += kDrawThreads / 64) {
-            const uint2 *list = a.f.lists + ((int64_t)row * a.f.chunks + c) * kListCap;
-            const int n = a.f.stats[(int64_t)row * a.f.chunks + c].count;
-            for (int i = lane; i < n; i += 64) {
-                const uint2 v = list[i];
-                visit(__uint_as_float(v.x) + 0.f, (int)v.y);
-            }
+        const uint2 *list = a.f.lists + (int64_t)row * a.f.chunks * kListCap;
+        for (int at = tid; at < cp.listed; at += kDrawThreads) {
+            const uint2 v = list[at];
+            visit(__uint_as_float(v.x), logit<DT>(qr, (int)v.y), gr[v.y], (int)v.y);
         }
     }
 #pragma unroll

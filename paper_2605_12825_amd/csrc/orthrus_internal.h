@@ -88,7 +88,7 @@ struct RowCut {
     float min_w;
     uint32_t key;    // order_key of the last logit kept
     int32_t tie;
-    int32_t listed;  // 1: all that is kept is in the lists of the row's chunks
+    int32_t listed;  // so many kept tokens stand in the row's lists, 0: they do not
 };
 
 // What the pass over the logits leaves of one chunk of a row.
@@ -109,9 +109,9 @@ struct FilterArgs {
     RowCut *cuts;            // consensus: [view][rows]
     void *workspace;         // filter_workspace_bytes; the next lie in it or follow from its plan
     ChunkStat *stats;        // [view][row][chunk]
-    uint2 *lists;            // [view][row][chunk][128]: (logit, index)
+    uint2 *lists;            // [view][row][chunk][128]: (logit, index); consensus: then the row's kept tokens, packed
     int32_t *unresolved;     // [0]: count, then rows (view * rows + row)
-    int chunks, all_rows;
+    int chunks, all_rows, num_cus;
     int64_t stride_row;      // elements between rows
     int rows, block_k, vocab;
     int dtype;               // orthrus_dtype
