@@ -18,13 +18,11 @@
 //   filtered_draw_kernel   one workgroup per sequence: keep decisions, the replacement drawn from the first rejected row.
 //   filtered_commit_kernel grid (sequence, layer): outputs and the commit, as sample_commit_kernel does it.
 #include "orthrus_internal.h"
+#include "orthrus_lanes.h"
 
 #include <cfloat>
-#include <type_traits>
 
 namespace orthrus {
-
-typedef unsigned long long u64;
 
 // ---- logits, their order and their weights
 
@@ -109,73 +107,6 @@ __device__ __forceinline__ bool kept(const RowCut &c, float x, int i)
 {
     const uint32_t key = order_key(x);
     return x > -INFINITY && (key > c.key || (key == c.key && i <= c.tie));
-}
-
-// ---- exchange between lanes, within a row of sixteen without a trip through LDS
-
-constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;  // DPP: lanes xor 1, xor 2, 7 - i, 15 - i
-template <int CTRL> __device__ __forceinline__ float swap_f32(float x)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
-template <int CTRL> __device__ __forceinline__ u64 swap_u64(u64 x)
-{
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, 0xf, 0xf, true);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, 0xf, 0xf, true);
-    return (u64)hi << 32 | lo;
-}
-template <int CTRL> __device__ __forceinline__ double swap_f64(double x)
-{
-    return __longlong_as_double((long long)swap_u64<CTRL>((u64)__double_as_longlong(x)));
-}
-__device__ __forceinline__ float wave_max(float x)
-{
-    x = fmaxf(x, swap_f32<kSwap1>(x));
-    x = fmaxf(x, swap_f32<kSwap2>(x));
-    x = fmaxf(x, swap_f32<kMirror8>(x));
-    x = fmaxf(x, swap_f32<kMirror16>(x));
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ double wave_sum(double x)   // the same order in every lane up to mirroring
-{
-    x += swap_f64<kSwap1>(x);
-    x += swap_f64<kSwap2>(x);
-    x += swap_f64<kMirror8>(x);
-    x += swap_f64<kMirror16>(x);
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-__device__ __forceinline__ u64 wave_sum(u64 x)
-{
-    x += swap_u64<kSwap1>(x);
-    x += swap_u64<kSwap2>(x);
-    x += swap_u64<kMirror8>(x);
-    x += swap_u64<kMirror16>(x);
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-// A value that all lanes hold, in scalar registers.
-__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
-__device__ __forceinline__ double uniform(double x)
-{
-    return __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(x)), __builtin_amdgcn_readfirstlane(__double2loint(x)));
-}
-// Inclusive sum in lane order: shifts within rows of sixteen, then the last lane of a row to the rows behind it.
-__device__ __forceinline__ u64 wave_scan(u64 x)
-{
-    auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, ctrl.value, rows.value, 0xf, false);
-        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), ctrl.value, rows.value, 0xf, false);
-        x += (u64)hi << 32 | lo;
-    };
-    step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());   // row_shr 1, 2, 4, 8
-    step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
-    step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
-    step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
-    step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());   // row_bcast 15 to rows 1 and 3
-    step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());   // row_bcast 31 to rows 2 and 3
-    return x;
 }
 
 // ---- running sums over bins in LDS
@@ -420,87 +351,95 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
 
 // ---- cuts and token from the lists
 
-constexpr int kPickThreads = 256, kPickWaves = kPickThreads / 64;
-constexpr int kPickEach = 8, kPickEntries = kPickThreads * kPickEach;  // logits of a row's lists that are looked at
-constexpr int kMaxChunks = 768, kChunksEach = kMaxChunks / kPickThreads;
-
-struct PickShared {
-    Bins<kPickThreads, 4> bins;
-    uint32_t key[kPickEntries];
-    int index[kPickEntries];
-    uint16_t listed[kMaxChunks];
-    float top[kPickWaves], tau[kPickWaves];
-    double z[kPickWaves];
-    int count;
-    uint32_t token_key;
-};
-
-// The crossing of a running sum over entries ordered by `digit` (rising), ten bits at a time; an entry with amount 0 is not there.
-struct Picked {
-    uint32_t digit;
-    u64 before, here;   // amounts of smaller digits, of this one (0: not reached)
-};
-__device__ __forceinline__ Picked pick_digit(PickShared &s, int tid, const uint32_t (&digit)[kPickEach], const u64 (&amount)[kPickEach],
-                                             int bits, u64 target)
-{
-    Picked r = {0, 0, 0};
-    int shift = bits;
-#pragma unroll 1
-    do {
-        const int next = max(0, shift - 10);
-#pragma unroll
-        for (int e = 0; e < kPickEach; ++e)
-            if (amount[e] && (shift >= 32 || digit[e] >> shift == r.digit))
-                atomicAdd(&s.bins.amount[(digit[e] >> next) & ((1u << (shift - next)) - 1)], amount[e]);
-        const Crossing c = s.bins.crossing(tid, target - r.before);
-        if (c.bin < 0) return {0, 0, 0};
-        r.before += c.before;
-        r.here = c.at;
-        r.digit = r.digit << (shift - next) | (uint32_t)c.bin;
-        shift = next;
-    } while (shift > 0);
-    return r;
-}
+constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
+constexpr int kPickEntries = 1792;   // logits of a row's lists that are looked at
+constexpr int kMaxChunks = 1024, kChunksEach = kMaxChunks / kPickThreads;
 
 __device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
 
+// The crossing of a running sum of amounts over n entries ordered by a number of `bits` bits, ten bits at a time.
+struct Found {
+    uint32_t number;
+    u64 before, here;   // amounts of smaller numbers, of this one (0: never reached)
+};
+template <typename B, typename N, typename A>
+__device__ __forceinline__ Found search_entries(B &bins, int tid, int threads, int n, int bits, u64 target, N number_of, A amount_of)
+{
+    static_assert(B::kCount >= 1024, "ten bits");
+    Found r = {0, 0, 0};
+#pragma unroll 1
+    for (int shift = bits; shift > 0;) {
+        const int next = max(0, shift - 10);
+        for (int i = tid; i < n; i += threads) {
+            const uint32_t d = number_of(i);
+            if (shift >= 32 || d >> shift == r.number) {
+                const u64 m = amount_of(i);
+                if (m) atomicAdd(&bins.amount[(d >> next) & ((1u << (shift - next)) - 1)], m);
+            }
+        }
+        const Crossing c = bins.crossing(tid, target - r.before);
+        if (c.bin < 0) return {0, 0, 0};
+        r.before += c.before;
+        r.here = c.at;
+        r.number = r.number << (shift - next) | (uint32_t)c.bin;
+        shift = next;
+    }
+    return r;
+}
+
+constexpr int kFew = 64;   // so many logits are ranked one against the other, in the lanes of a wave
+
+struct PickShared {
+    Bins<kPickThreads, 2> bins;
+    u64 mass[kPickEntries];
+    uint32_t key[kPickEntries];
+    int index[kPickEntries];
+    ulonglong2 few[kFew];           // (order, weight)
+    uint8_t listed[kMaxChunks];
+    float top[kPickWaves], tau[kPickWaves];
+    double z[kPickWaves];
+    u64 before[kFew], run[kFew];   // of the few: weight of those in front by order, by index
+    int rank[kFew];
+    int count, few_count;
+};
+
 // SCANNED: the row's chunks have been listed; else it has at most kPickEntries logits and is read here.
-template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads, 3) filter_pick_kernel(const FilterArgs a)
+template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads, 4) filter_pick_kernel(const FilterArgs a)
 {
     const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ PickShared s;
     const RowFilter f = row_filter(a, row / a.block_k);
     const void *logits = logit_row<DT>(a, side, row);
-    uint32_t fall[kPickEach], index[kPickEach];   // fall: distance from the top in order
     // ---- the row's maximum, down to where its lists hold everything
     float top = -INFINITY, tau = -INFINITY;
     ChunkStat st[kChunksEach];
+    // A list to a wave; the loads of the first ones go out with those of the counts, which say later how much of them is one.
+    constexpr int kAhead = 10;
+    const uint2 *lists = a.lists + (int64_t)rr * a.chunks * kListCap;
+    uint2 ahead[SCANNED ? kAhead : 1];
     if constexpr (SCANNED) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (wave + k * kPickWaves < a.chunks) ahead[k] = lists[(int64_t)(wave + k * kPickWaves) * kListCap + lane];
         const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
 #pragma unroll
         for (int i = 0; i < kChunksEach; ++i) {
             const int c = i * kPickThreads + tid;
             st[i] = {0.0, -INFINITY, -INFINITY, 0};
             if (c < a.chunks) st[i] = stats[c];
-            s.listed[c] = (uint16_t)st[i].count;
+            s.listed[c] = (uint8_t)st[i].count;
             top = fmaxf(top, st[i].top);
             tau = fmaxf(tau, st[i].tau);
         }
     } else {
-#pragma unroll
-        for (int e = 0; e < kPickEach; ++e) {
-            const int i = e * kPickThreads + tid;
-            const float x = i < a.vocab ? logit<DT>(logits, i) : -INFINITY;
-            fall[e] = order_key(x);   // (a key until the top is known)
-            index[e] = (uint32_t)i;
-            top = fmaxf(top, x);
-        }
+        for (int i = tid; i < a.vocab; i += kPickThreads) top = fmaxf(top, logit<DT>(logits, i));
     }
     top = wave_max(top);
     tau = wave_max(tau);
     if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
-    if (tid == 0) s.count = 0;
+    if (tid == 0) s.count = s.few_count = 0;
+    if (tid < kFew) { s.before[tid] = s.run[tid] = 0; s.rank[tid] = 0; }
     s.bins.clear(tid);
 #pragma unroll
     for (int w = 0; w < kPickWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fmaxf(tau, s.tau[w]); }
@@ -580,159 +519,208 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
         } else {
             // ---- every logit down to tau
             const bool whole = tau == -INFINITY;   // that is all there are
-            const uint32_t top_key = order_key(top);
-            int n;
+            const uint32_t top_key = order_key(top + 0.f);
+            auto put = [&](int at, uint32_t x, int i) __attribute__((always_inline)) {   // (the logit's bits; its order later)
+                s.key[at] = x;
+                s.index[at] = i;
+            };
             if constexpr (SCANNED) {
-                // a list to half a wave, five of them at a time, two loads to each
-                constexpr int kAhead = 5, kHalves = kPickThreads / 32;
-                const int half = tid >> 5, at32 = tid & 31;
-                auto keep = [&](uint2 q) __attribute__((always_inline)) {
-                    const float x = __uint_as_float(q.x);
-                    if (x >= tau && x > -INFINITY) {
-                        const int at = atomicAdd(&s.count, 1);
-                        if (at < kPickEntries) { s.key[at] = order_key(x + 0.f); s.index[at] = (int)q.y; }
-                    }
-                };
-                for (int c0 = half; c0 < a.chunks; c0 += kAhead * kHalves) {
-                    uint2 v[2 * kAhead];
-                    int most = 0;
+                for (int c0 = wave; c0 < a.chunks; c0 += kAhead * kPickWaves) {
+                    if (c0 >= kAhead * kPickWaves) {
 #pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const int c = c0 + u * kHalves, have = c < a.chunks ? s.listed[c] : 0;
-                        const uint2 *list = a.lists + ((int64_t)rr * a.chunks + c) * kListCap;
+                        for (int k = 0; k < kAhead; ++k)
+                            if (c0 + k * kPickWaves < a.chunks) ahead[k] = lists[(int64_t)(c0 + k * kPickWaves) * kListCap + lane];
+                    }
+                    bool hit[kAhead];
+                    int count = 0, most = 0;
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k) {
+                        const int c = c0 + k * kPickWaves, have = c < a.chunks ? s.listed[c] : 0;
+                        hit[k] = lane < have && __uint_as_float(ahead[k].x) >= tau;
+                        count += __popcll(__ballot(hit[k]));
                         most = max(most, have);
+                    }
+                    int at = 0;
+                    if (lane == 0) at = atomicAdd(&s.count, count);
+                    at = __builtin_amdgcn_readfirstlane(at);
+                    if (at + count <= kPickEntries) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            v[2 * u + h] = make_uint2(0xff800000u, 0);   // -inf
-                            if (h * 32 + at32 < have) v[2 * u + h] = list[h * 32 + at32];
+                        for (int k = 0; k < kAhead; ++k) {
+                            const u64 hits = __ballot(hit[k]);
+                            if (hit[k])
+                                put(at + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0)),
+                                    ahead[k].x, (int)ahead[k].y);
+                            at += __popcll(hits);
                         }
                     }
-#pragma unroll
-                    for (int u = 0; u < 2 * kAhead; ++u) keep(v[u]);
                     if (most > 64)
-                        for (int u = 0; u < kAhead; ++u) {
-                            const int c = c0 + u * kHalves, have = c < a.chunks ? s.listed[c] : 0;
-                            for (int i = 64 + at32; i < have; i += 32) keep(a.lists[((int64_t)rr * a.chunks + c) * kListCap + i]);
+                        for (int k = 0; k < kAhead; ++k) {
+                            const int c = c0 + k * kPickWaves, have = c < a.chunks ? s.listed[c] : 0;
+                            for (int i = 64 + lane; i < have; i += 64) {
+                                const uint2 w = lists[(int64_t)c * kListCap + i];
+                                if (__uint_as_float(w.x) >= tau) {
+                                    const int more = atomicAdd(&s.count, 1);
+                                    if (more < kPickEntries) put(more, w.x, (int)w.y);
+                                }
+                            }
                         }
                 }
-                __syncthreads();
-                n = s.count;
-                resolved = n <= kPickEntries;
             } else {
-                n = a.vocab;
+                for (int i = tid; i < a.vocab; i += kPickThreads) {
+                    const float x = logit<DT>(logits, i);
+                    if (x > -INFINITY) put(atomicAdd(&s.count, 1), __float_as_uint(x), i);
+                }
             }
+            __syncthreads();
+            const int n = s.count;
+            resolved = n <= kPickEntries;
             if (resolved) {
-                const int key_bits = bits_of(top_key - (whole ? order_key(-FLT_MAX) : order_key(tau + 0.f)));
-                const int index_bits = bits_of((uint32_t)(a.vocab - 1));
                 constexpr double kUnit = 0x1p50;
-                uint32_t live = 0;           // entry e is there
-                u64 mass[kPickEach], known = 0;
-#pragma unroll
-                for (int e = 0; e < kPickEach; ++e) {
-                    const int i = e * kPickThreads + tid;
-                    bool there = i < n;
-                    uint32_t key;
-                    if constexpr (SCANNED) {
-                        key = there ? s.key[i] : top_key;
-                        index[e] = there ? (uint32_t)s.index[i] : 0u;
-                    } else {
-                        key = fall[e];
-                        there = there && key >= order_key(-FLT_MAX);
-                    }
-                    live |= (uint32_t)there << e;
-                    fall[e] = top_key - key;
-                    mass[e] = there ? to_fixed(weight(key_logit(key), top, f.t), kUnit) : 0;
-                    known += mass[e];
+                const int key_bits = bits_of(top_key - (whole ? order_key(-FLT_MAX) : order_key(tau + 0.f)));
+                const int index_bits = bits_of((uint32_t)(a.vocab - 1)), coarse = max(0, key_bits - 10);
+                auto fall_of = [&](int i) __attribute__((always_inline)) { return top_key - s.key[i]; };
+                auto weight_of = [&](int i) __attribute__((always_inline)) { return weight(key_logit(s.key[i]), top, f.t); };
+                u64 known = 0;
+                for (int i = tid; i < n; i += kPickThreads) {
+                    const float x = __uint_as_float(s.key[i]);
+                    const u64 m = to_fixed(weight(x, top, f.t), kUnit);
+                    s.key[i] = order_key(x + 0.f);
+                    s.mass[i] = m;
+                    known += m;
                 }
-                if constexpr (!SCANNED) {
-                    if (f.top_k > 0) n = (int)s.bins.sum_of(tid, (u64)__popc(live));
-                }
-                uint32_t cut_fall = 0xffffffffu;
-                int cut_tie = 0x7fffffff;
-                auto count_of = [&](bool only, uint32_t at, u64 (&one)[kPickEach]) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int e = 0; e < kPickEach; ++e) one[e] = (live >> e & 1) && (!only || fall[e] == at);
-                };
-                auto nth_at = [&](uint32_t at, u64 nth) __attribute__((always_inline)) {   // index of the n-th entry there
-                    u64 one[kPickEach];
-                    count_of(true, at, one);
-                    return (int)pick_digit(s, tid, index, one, index_bits, nth).digit;
-                };
-                auto apply = [&]() __attribute__((always_inline)) {
-                    known = 0;
-#pragma unroll
-                    for (int e = 0; e < kPickEach; ++e) {
-                        if (fall[e] > cut_fall || (fall[e] == cut_fall && (int)index[e] > cut_tie)) {
-                            mass[e] = 0;
-                            live &= ~(1u << e);
-                        }
-                        known += mass[e];
-                    }
-                };
-                if (f.top_k > 0 && f.top_k < n) {
-                    u64 one[kPickEach];
-                    count_of(false, 0, one);
-                    const Picked k = pick_digit(s, tid, fall, one, key_bits, (u64)f.top_k);
-                    cut_fall = k.digit;
-                    if (k.before + k.here > (u64)f.top_k) cut_tie = nth_at(k.digit, (u64)f.top_k - k.before);
-                    apply();
-                }
-                // what min-p keeps is known if what is not listed is below its line; the other cuts are then only
-                // asked whether they cut higher
+                known = s.bins.sum_of(tid, known);
+                // what min-p keeps is known if what is not listed is below its line; the other cuts are then only asked
+                // whether they cut higher
                 const bool min_p_known = whole || (f.min_p > 0.0 && weight(tau, top, f.t) < f.min_p);
-                const bool top_k_known = f.top_k <= n || whole;
-                resolved = (f.top_k > 0 && top_k_known) || min_p_known || (f.top_k == 0 && f.top_p < 1.0);
-                if (f.top_p < 1.0) {
-                    if (top_k_known) {
-                        known = s.bins.sum_of(tid, known);
-                        const double all = f.top_k > 0 || whole ? (double)known : z * kUnit;
-                        const double target = fmax(1.0, ceil(f.top_p * all));
-                        if (target <= (double)known) {
-                            const u64 goal = min(known, (u64)target);
-                            const Picked p = pick_digit(s, tid, fall, mass, key_bits, goal);
-                            const u64 each = to_fixed(weight(key_logit(top_key - p.digit), top, f.t), kUnit);
-                            const u64 nth = (goal - p.before + each - 1) / each;
-                            if (p.digit < cut_fall) cut_tie = 0x7fffffff;
-                            cut_fall = p.digit;
-                            if (nth * each < p.here) cut_tie = min(cut_tie, nth_at(p.digit, nth));
-                            apply();
-                        } else {
-                            resolved = min_p_known;
-                        }
-                    } else {
-                        resolved = false;
-                    }
-                }
+                const bool by_k = f.top_k > 0 && f.top_k < n, top_k_known = f.top_k <= n || whole;
+                const double all = f.top_k > 0 || whole ? (double)known : z * kUnit;   // (where top-k cuts nothing more)
+                const double share = f.top_p < 1.0 && !by_k ? fmax(1.0, ceil(f.top_p * all)) : 0.0;
+                const bool by_p = f.top_p < 1.0 && !by_k && share <= (double)known;
+                if (f.top_p < 1.0) resolved = top_k_known && (by_k || by_p || min_p_known);
+                else resolved = (f.top_k > 0 && top_k_known) || min_p_known;
                 if (resolved) {
-                    known = 0;
-#pragma unroll
-                    for (int e = 0; e < kPickEach; ++e) {
-                        if (f.min_p > 0.0 && !(weight(key_logit(top_key - fall[e]), top, f.t) >= f.min_p)) mass[e] = 0;
-                        known += mass[e];
+                    // ---- the few that can be kept: everything down to the step in which the first cut falls
+                    int step = 1024;
+                    if (by_k || by_p) {
+                        for (int i = tid; i < n; i += kPickThreads) atomicAdd(&s.bins.amount[fall_of(i) >> coarse], by_k ? 1ull : s.mass[i]);
+                        step = s.bins.crossing(tid, by_k ? (u64)f.top_k : min(known, (u64)share)).bin;
                     }
-                    const u64 total = s.bins.sum_of(tid, known);
-                    cut.z = (double)total / kUnit;
-                    cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
-                    cut.tie = cut_tie;
-                    if constexpr (!DRAW && SCANNED) {
-                        // what is kept, in place of the first of the row's lists, for the replacement's draw
+                    const bool by_m = !by_k && !by_p && f.min_p > 0.0;
+                    for (int i = tid; i < n; i += kPickThreads)
+                        if ((int)(fall_of(i) >> coarse) <= step && !(by_m && !(weight_of(i) >= f.min_p))) {
+                            const int at = atomicAdd(&s.few_count, 1);
+                            if (at < kFew) s.few[at] = make_ulonglong2((u64)s.key[i] << 32 | (uint32_t)~s.index[i], s.mass[i]);
+                        }
+                    __syncthreads();
+                    const int m = s.few_count;
+                    u64 total;
+                    if (m <= kFew) {
+                        // every wave has them all in its lanes and compares them with an eighth of them
+                        const ulonglong2 e = lane < m ? s.few[lane] : make_ulonglong2(0, 0);
+                        const uint32_t key = (uint32_t)(e.x >> 32);
+                        const int index = (int)~(uint32_t)e.x;
+                        u64 before = 0;
+                        int rank = 0;
+                        for (int i = wave; i < m; i += kPickWaves) {
+                            const u64 w = lane_value(e.y, i);
+                            if (lane_value(e.x, i) > e.x) { before += w; ++rank; }
+                        }
+                        if (lane < m) { atomicAdd(&s.before[lane], before); atomicAdd(&s.rank[lane], rank); }
                         __syncthreads();
-                        if (tid == 0) s.count = 0;
-                        __syncthreads();
-                        uint2 *list = a.lists + (int64_t)rr * a.chunks * kListCap;
-#pragma unroll
-                        for (int e = 0; e < kPickEach; ++e)
-                            if (mass[e]) list[atomicAdd(&s.count, 1)] = make_uint2(__float_as_uint(key_logit(top_key - fall[e])), index[e]);
-                        __syncthreads();
-                        cut.listed = s.count;
-                    }
-                    if constexpr (DRAW) {
-                        token = (int)pick_digit(s, tid, index, mass, index_bits, (u64)((double)u * (double)total) + 1).digit;
-#pragma unroll
-                        for (int e = 0; e < kPickEach; ++e)
-                            if (mass[e] && (int)index[e] == token) s.token_key = top_key - fall[e];
-                        __syncthreads();
-                        own = weight(key_logit(s.token_key), top, f.t);
+                        before = s.before[lane];
+                        rank = s.rank[lane];
+                        bool in = lane < m && (!by_k || rank < f.top_k);
+                        if (f.top_p < 1.0) {
+                            const double z1 = by_k ? (double)wave_sum(in ? e.y : (u64)0) : all;
+                            in = in && (double)before < fmax(1.0, ceil(f.top_p * z1));
+                        }
+                        const u64 mine = in && (f.min_p == 0.0 || weight(key_logit(key), top, f.t) >= f.min_p) ? e.y : 0;
+                        total = wave_sum(mine);
+                        if constexpr (DRAW) {
+                            const u64 target = (u64)((double)u * (double)total) + 1;
+                            u64 run = 0;
+                            for (int i = wave; i < m; i += kPickWaves) {
+                                const u64 w = lane_value(mine, i);
+                                if (__builtin_amdgcn_readlane(index, i) < index) run += w;
+                            }
+                            if (lane < m) atomicAdd(&s.run[lane], run);
+                            __syncthreads();
+                            run = s.run[lane];
+                            const int from = __ffsll((long long)__ballot(run < target && target <= run + mine)) - 1;
+                            token = __builtin_amdgcn_readlane(index, from);
+                            own = weight(key_logit((uint32_t)__builtin_amdgcn_readlane((int)key, from)), top, f.t);
+                        } else {
+                            // those in front, up to the last that both cuts leave: the first so many of the order
+                            const int last = __popcll(__ballot(in)) - 1;
+                            const int from = __ffsll((long long)__ballot(in && rank == last)) - 1;
+                            cut.key = (uint32_t)__builtin_amdgcn_readlane((int)key, from);
+                            cut.tie = __builtin_amdgcn_readlane(index, from);
+                            if constexpr (SCANNED) {
+                                const u64 keeps = __ballot(mine != 0);
+                                cut.listed = __popcll(keeps);
+                                if (wave == 0 && mine)
+                                    a.lists[(int64_t)rr * a.chunks * kListCap +
+                                            __builtin_amdgcn_mbcnt_hi((uint32_t)(keeps >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)keeps, 0))] =
+                                        make_uint2(__float_as_uint(key_logit(key)), index);
+                            }
+                        }
+                        cut.z = (double)total / kUnit;
+                    } else {
+                        // ---- many: the same cuts digit by digit
+                        auto index_of = [&](int i) __attribute__((always_inline)) { return (uint32_t)s.index[i]; };
+                        auto mass_of = [&](int i) __attribute__((always_inline)) { return s.mass[i]; };
+                        uint32_t cut_fall = 0xffffffffu;
+                        int cut_tie = 0x7fffffff;
+                        auto cut_at = [&](const Found &c, u64 nth, u64 here) __attribute__((always_inline)) {
+                            if (c.number < cut_fall) cut_tie = 0x7fffffff;
+                            cut_fall = c.number;
+                            if (nth < here)   // not all of those at the cut's logit: the n-th of them by index
+                                cut_tie = min(cut_tie, (int)search_entries(s.bins, tid, kPickThreads, n, index_bits, nth, index_of,
+                                                                           [&](int i) __attribute__((always_inline)) { return (u64)(fall_of(i) == cut_fall); }).number);
+                            u64 sum = 0;
+                            for (int i = tid; i < n; i += kPickThreads) {
+                                const uint32_t d = fall_of(i);
+                                if (d > cut_fall || (d == cut_fall && s.index[i] > cut_tie)) s.mass[i] = 0;
+                                sum += s.mass[i];
+                            }
+                            return s.bins.sum_of(tid, sum);
+                        };
+                        double z1 = all;
+                        if (by_k) {
+                            const Found k = search_entries(s.bins, tid, kPickThreads, n, key_bits, (u64)f.top_k, fall_of,
+                                                           [&](int) __attribute__((always_inline)) { return (u64)1; });
+                            known = cut_at(k, (u64)f.top_k - k.before, k.here);
+                            z1 = (double)known;
+                        }
+                        if (by_p || (by_k && f.top_p < 1.0)) {
+                            const u64 goal = min(known, (u64)fmax(1.0, ceil(f.top_p * z1)));
+                            const Found p = search_entries(s.bins, tid, kPickThreads, n, key_bits, goal, fall_of, mass_of);
+                            const u64 each = to_fixed(weight(key_logit(top_key - p.number), top, f.t), kUnit);
+                            cut_at(p, (goal - p.before + each - 1) / each, p.here / each);
+                        }
+                        u64 sum = 0;
+                        for (int i = tid; i < n; i += kPickThreads) {
+                            if (f.min_p > 0.0 && !(weight_of(i) >= f.min_p)) s.mass[i] = 0;
+                            sum += s.mass[i];
+                        }
+                        total = s.bins.sum_of(tid, sum);
+                        cut.z = (double)total / kUnit;
+                        cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
+                        cut.tie = cut_tie;
+                        if constexpr (DRAW) {
+                            token = (int)search_entries(s.bins, tid, kPickThreads, n, index_bits, (u64)((double)u * (double)total) + 1,
+                                                        index_of, mass_of).number;
+                            own = weight(logit<DT>(logits, token), top, f.t);
+                        } else if constexpr (SCANNED) {
+                            if (tid == 0) s.count = 0;
+                            __syncthreads();
+                            for (int i = tid; i < n; i += kPickThreads)
+                                if (s.mass[i])
+                                    a.lists[(int64_t)rr * a.chunks * kListCap + atomicAdd(&s.count, 1)] =
+                                        make_uint2(__float_as_uint(key_logit(s.key[i])), s.index[i]);
+                            __syncthreads();
+                            cut.listed = s.count;
+                        }
                     }
                 }
             }
@@ -984,13 +972,18 @@ template <int DT> struct WideRow {
         // ---- among the gathered logits
         for (int i = tid; i < n; i += kWideThreads) s.mass[i] = mass_of(key_logit(s.key[i]));
         const u64 goal = target - (MASS ? over : c.before);
-        const Selected r = select_gathered<MASS>(n, goal);
+        const Found r = search_entries(s.bins, tid, kWideThreads, n, 32, goal, [&](int i) __attribute__((always_inline)) { return ~s.key[i]; },
+                                       [&](int i) __attribute__((always_inline)) { return MASS ? s.mass[i] : 1ull; });
         if (r.here == 0) return 0;
-        const u64 each = MASS ? mass_of(key_logit(r.key)) : 1;
-        const u64 nth = (goal - r.above + each - 1) / each;
-        if (r.key > cut.key) cut.tie = 0x7fffffff;
-        cut.key = r.key;
-        if (nth * each < r.here) cut.tie = min(cut.tie, nth_gathered(n, r.key, nth));
+        const uint32_t key = ~r.number;
+        const u64 each = MASS ? mass_of(key_logit(key)) : 1;
+        const u64 nth = (goal - r.before + each - 1) / each;
+        if (key > cut.key) cut.tie = 0x7fffffff;
+        cut.key = key;
+        if (nth * each < r.here)
+            cut.tie = min(cut.tie, (int)search_entries(s.bins, tid, kWideThreads, n, bits_of((uint32_t)(vocab - 1)), nth,
+                                                       [&](int i) __attribute__((always_inline)) { return (uint32_t)s.index[i]; },
+                                                       [&](int i) __attribute__((always_inline)) { return (u64)(s.key[i] == key); }).number);
         u64 more = 0;
         for (int i = tid; i < n; i += kWideThreads) {
             const float x = key_logit(s.key[i]);
@@ -1004,47 +997,6 @@ template <int DT> struct WideRow {
         return over + s.bins.sum_of(tid, more);
     }
 
-    // The same searches among the n gathered logits, ten bits at a time.
-    template <bool MASS> __device__ __forceinline__ Selected select_gathered(int n, u64 target)
-    {
-        Selected r = {0, 0, 0};
-        uint32_t prefix = 0;
-#pragma unroll 1
-        for (int shift = 32; shift > 0;) {
-            const int next = max(0, shift - 10);
-            for (int i = tid; i < n; i += kWideThreads) {
-                const uint32_t fall = ~s.key[i];
-                if (shift == 32 || fall >> shift == prefix)
-                    atomicAdd(&s.bins.amount[(fall >> next) & ((1u << (shift - next)) - 1)], MASS ? s.mass[i] : 1ull);
-            }
-            const Crossing c = s.bins.crossing(tid, target - r.above);
-            if (c.bin < 0) return {0, 0, 0};
-            r.above += c.before;
-            r.here = c.at;
-            prefix = prefix << (shift - next) | (uint32_t)c.bin;
-            shift = next;
-        }
-        r.key = ~prefix;
-        return r;
-    }
-    __device__ __forceinline__ int nth_gathered(int n, uint32_t key, u64 nth)
-    {
-        uint32_t prefix = 0;
-#pragma unroll 1
-        for (int shift = bits_of((uint32_t)(vocab - 1)); shift > 0;) {
-            const int next = max(0, shift - 10);
-            for (int i = tid; i < n; i += kWideThreads) {
-                const uint32_t d = (uint32_t)s.index[i];
-                if (s.key[i] == key && d >> shift == prefix) atomicAdd(&s.bins.amount[(d >> next) & ((1u << (shift - next)) - 1)], 1ull);
-            }
-            const Crossing c = s.bins.crossing(tid, nth);
-            if (c.bin < 0) return 0x7fffffff;
-            nth -= c.before;
-            prefix = prefix << (shift - next) | (uint32_t)c.bin;
-            shift = next;
-        }
-        return (int)prefix;
-    }
 };
 
 template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads, 2) filter_wide_kernel(const FilterArgs a)
@@ -1191,7 +1143,7 @@ hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream) { return launc
 
 // ---- consensus
 
-constexpr int kDrawThreads = 256, kDrawPiece = 8192;
+constexpr int kDrawThreads = 512, kDrawPiece = 8192;
 
 // Probability that a row's filters leave a token (0: cut, or an empty row).
 __device__ __forceinline__ double kept_prob(const RowCut &c, const Scale &t, float x, int i)
@@ -1257,22 +1209,29 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
                 }
             };
             if (r > 0.0) consider(r, more_near, more);
-            consider(p, any_near, any);
+            else if (more_near == -INFINITY) consider(p, any_near, any);   // (asked for only where nothing is positive)
         }
     };
     if (!cp.listed) {
         const int end = min(V, (piece + 1) * kDrawPiece);
-        for (int i0 = piece * kDrawPiece + tid; i0 < end; i0 += 4 * kDrawThreads) {
-            float x[4], y[4], g[4];
+        constexpr int kAtOnce = 8;
+        for (int i0 = piece * kDrawPiece; i0 < end; i0 += kAtOnce * kDrawThreads) {   // (the same rounds for all lanes)
+            float x[kAtOnce], y[kAtOnce], g[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = i0 + e * kDrawThreads;
+            for (int e = 0; e < kAtOnce; ++e) {
+                const int i = i0 + e * kDrawThreads + tid;
                 x[e] = i < end ? logit<DT>(pr, i) : -INFINITY;
                 y[e] = i < end ? logit<DT>(qr, i) : -INFINITY;
                 g[e] = i < end ? gr[i] : 0.f;
             }
+#pragma unroll 1
+            for (int e = 0; e < kAtOnce; ++e) {   // (one copy of the visit; what it needs moves down by one)
+                visit(x[0], y[0], g[0], i0 + e * kDrawThreads + tid);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) visit(x[e], y[e], g[e], i0 + e * kDrawThreads);
+                for (int r = 0; r + 1 < kAtOnce; ++r) { x[r] = x[r + 1]; y[r] = y[r + 1]; g[r] = g[r + 1]; }
+                more_near = wave_max(more_near);
+            }
+            any_near = wave_max(any_near);
         }
     } else if (piece == 0) {
         const uint2 *list = a.f.lists + (int64_t)row * a.f.chunks * kListCap;

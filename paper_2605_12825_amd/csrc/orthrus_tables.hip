@@ -11,6 +11,7 @@
 //                        kernel reads there is written by it.
 //   kv_store_kernel      grid (rows, layer): 16-byte chunks, four of K and of V in flight per thread.
 #include "orthrus_internal.h"
+#include "orthrus_lanes.h"
 
 namespace orthrus {
 
@@ -28,167 +29,310 @@ __device__ __forceinline__ EntryRange entry_range(const TablesArgs &a, int L, in
     return {L >> a.page_shift, n > 0 ? (L + n - 1) >> a.page_shift : (L >> a.page_shift) - 1};
 }
 
+// By `threads` threads of which this is the tid-th (a wave or a workgroup); `sum_up` makes what they found one.
+template <typename F> __device__ __forceinline__ void count_sequence(const TablesArgs &a, int b, int tid, int threads, F sum_up)
+{
+    const int L = a.seq_lens[b], n = a.new_lens[b];
+    bool bad = n >= 0 && (L < 0 || (int64_t)L + n > a.max_seq_len);
+    int count = 0, first = INT32_MAX, last = -1;
+    EntryRange r = {0, -1};
+    if (!bad) {
+        const int32_t *row = a.page_table + (int64_t)b * a.max_pages_per_seq;
+        r = entry_range(a, L, n);
+        // ended: mapped entries, else unmapped ones; four loads in flight
+        for (int e0 = r.first + tid; e0 <= r.last; e0 += 4 * threads) {
+            int page[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) page[u] = row[min(e0 + u * threads, r.last)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int e = e0 + u * threads;
+                if (e <= r.last && is_mapped(a, page[u]) == (n < 0)) { ++count; first = min(first, e); last = e; }
+            }
+        }
+    }
+    sum_up(count, first, last);
+    // the page of tokens that are cached already must be there
+    if (n > 0 && (L & ((1 << a.page_shift) - 1)) && first == r.first) bad = true;
+    if (tid == 0) {
+        a.need[b] = bad ? kBadSequence : n < 0 ? -1 - count : count;
+        // entry of the first; -1 - entry: those behind it are not all alike (up to the last new token's entry, where it grows)
+        const bool whole = last - first + 1 == count && (n < 0 || last == r.last);
+        a.first[b] = count == 0 ? INT32_MAX : whole ? first : -1 - first;
+    }
+}
+
+__device__ __forceinline__ void wave_sum_up(int &count, int &first, int &last)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        count += __shfl_xor(count, off);
+        first = min(first, __shfl_xor(first, off));
+        last = max(last, __shfl_xor(last, off));
+    }
+}
+
 __global__ void __launch_bounds__(256) tables_count_kernel(const TablesArgs a)
 {
-    const int b = blockIdx.x, tid = threadIdx.x;
-    const int L = a.seq_lens[b], n = a.new_lens[b];
+    const int tid = threadIdx.x;
     __shared__ int s_count, s_first, s_last;
     if (tid == 0) { s_count = 0; s_first = INT32_MAX; s_last = -1; }
     __syncthreads();
-    bool bad = n >= 0 && (L < 0 || (int64_t)L + n > a.max_seq_len);
-    if (!bad) {
-        const int32_t *row = a.page_table + (int64_t)b * a.max_pages_per_seq;
-        const EntryRange r = entry_range(a, L, n);
-        // ended: mapped entries, else unmapped ones
-        int count = 0, first = INT32_MAX, last = -1;
-        for (int e = r.first + tid; e <= r.last; e += blockDim.x)
-            if (is_mapped(a, row[e]) == (n < 0)) { ++count; first = min(first, e); last = e; }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-            count += __shfl_xor(count, off);
-            first = min(first, __shfl_xor(first, off));
-            last = max(last, __shfl_xor(last, off));
-        }
+    count_sequence(a, blockIdx.x, tid, blockDim.x, [&](int &count, int &first, int &last) __attribute__((always_inline)) {
+        wave_sum_up(count, first, last);
         if ((tid & 63) == 0 && count) { atomicAdd(&s_count, count); atomicMin(&s_first, first); atomicMax(&s_last, last); }
         __syncthreads();
-        // the page of tokens that are cached already must be there
-        if (n > 0 && (L & ((1 << a.page_shift) - 1)) && s_first == r.first) bad = true;
-    }
-    if (tid == 0) {
-        a.need[b] = bad ? kBadSequence : n < 0 ? -1 - s_count : s_count;
-        // entry of the first; -1 - entry: those behind it are not all alike (up to the last new token's entry, where it grows)
-        const bool whole = s_last - s_first + 1 == s_count && (n < 0 || s_last == entry_range(a, L, n).last);
-        a.first[b] = s_count == 0 ? INT32_MAX : whole ? s_first : -1 - s_first;
-    }
+        count = s_count; first = s_first; last = s_last;
+    });
 }
 
 constexpr int kScanThreads = 1024;
 
-// Inclusive sum over a workgroup, in thread order.  Contains barriers.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *sums, int tid)
+struct Pair {
+    int64_t a, b;
+};
+__device__ __forceinline__ int64_t last_lane(int64_t v)
 {
-    const int lane = tid & 63;
+    return (int64_t)lane_value((u64)v, 63);
+}
+// Running sums of two numbers over the threads, in their order: `up to` a thread and `all` of them.
+struct WaveSums {   // 64 threads
+    __device__ __forceinline__ void operator()(Pair v, Pair &upto, Pair &all)
+    {
+        upto = {(int64_t)wave_scan((u64)v.a), (int64_t)wave_scan((u64)v.b)};
+        all = {last_lane(upto.a), last_lane(upto.b)};
+    }
+    __device__ __forceinline__ int64_t most(int64_t v)
+    {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int64_t o = __shfl_up((long long)v, off);
-        if (lane >= off) v += o;
+        for (int off = 32; off >= 1; off >>= 1) v = max(v, (int64_t)__shfl_xor((long long)v, off));
+        return v;
     }
-    __syncthreads();
-    if (lane == 63) sums[tid >> 6] = v;
-    __syncthreads();
-    for (int w = 0; w < (tid >> 6); ++w) v += sums[w];
-    return v;
-}
+};
+struct BlockSums {   // kScanThreads of them; contains barriers
+    Pair *sums;
+    int64_t *top;
+    __device__ __forceinline__ void operator()(Pair v, Pair &upto, Pair &all)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        upto = {(int64_t)wave_scan((u64)v.a), (int64_t)wave_scan((u64)v.b)};
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        const Pair w = lane < kScanThreads / 64 ? sums[lane] : Pair{0, 0};
+        upto.a += (int64_t)wave_sum(lane < wave ? (u64)w.a : (u64)0);
+        upto.b += (int64_t)wave_sum(lane < wave ? (u64)w.b : (u64)0);
+        all = {(int64_t)wave_sum((u64)w.a), (int64_t)wave_sum((u64)w.b)};
+        __syncthreads();
+    }
+    __device__ __forceinline__ int64_t most(int64_t v)
+    {
+        if (threadIdx.x == 0) *top = 0;
+        __syncthreads();
+        if (v > 0) atomicMax((long long *)top, (long long)v);
+        __syncthreads();
+        return *top;
+    }
+};
 
-__global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(const TablesArgs a)
+// Who is granted what: a thread to a run of neighbouring sequences.  The pages that granted sequences take are those that
+// they and all before them want (a sequence that wants any is granted only if all of those are there).
+template <typename S> __device__ __forceinline__ void scan_sequences(const TablesArgs &a, int tid, int threads, S sums)
 {
-    const int tid = threadIdx.x;
-    __shared__ int64_t sums[kScanThreads / 64];
-    __shared__ int64_t s_carry[4];  // pages wanted, taken, returned; tokens
-    const int64_t N = a.num_pages;
-    const int64_t head = ((int64_t)a.free_state[0] % N + N) % N;
-    const int64_t free = min(max((int64_t)a.free_state[1], (int64_t)0), N);
-    if (tid < 4) s_carry[tid] = 0;
+    const int N = (int)a.num_pages;
+    int head = a.free_state[0];
+    if (head < 0 || head >= N) head = head % N + (head % N < 0 ? N : 0);
+    const int free = min(max(a.free_state[1], 0), N);
+    const int each = (a.batch + threads - 1) / threads;
+    const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
+    Pair sum = {0, 0}, run, all;   // pages wanted, returned
+    for (int b = b0; b < b1; ++b) {
+        const int need = a.need[b];
+        if (need >= 0) sum.a += need;
+        else if (need != kBadSequence) sum.b += -1 - (int64_t)need;
+    }
+    sums(sum, run, all);
+    const int64_t all_returned = all.b;
+    int64_t wanted = run.a - sum.a, returned = run.b - sum.b, tokens = 0, taken = 0;
     bool error = false;
-    for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
-        const int b = b0 + tid;
-        const int need = b < a.batch ? a.need[b] : 0, n = b < a.batch ? a.new_lens[b] : 0;
-        const bool bad = need == kBadSequence;
-        const int64_t lacks = bad || need < 0 ? 0 : need, back = bad || need >= 0 ? 0 : -1 - (int64_t)need;
-        __syncthreads();
-        const int64_t wanted0 = s_carry[0], taken0 = s_carry[1], back0 = s_carry[2], tokens0 = s_carry[3];
-        const int64_t wanted = wanted0 + block_scan(lacks, sums, tid);
-        const bool granted = n >= 0 && !bad && (lacks == 0 || wanted <= free);
-        const int64_t taken = taken0 + block_scan(granted ? lacks : 0, sums, tid);
-        const int64_t returned = back0 + block_scan(back, sums, tid);
-        const int64_t tokens = tokens0 + block_scan(granted ? n : 0, sums, tid);
-        error |= (n >= 0 && !granted && b < a.batch) || returned > N - free || tokens > a.max_tokens;
-        if (b < a.batch) {
-            a.granted[b] = granted ? n : 0;
-            a.token_starts[b] = (int32_t)min(tokens - (granted ? n : 0), (int64_t)INT32_MAX);
-            a.pages_before[b] = (int32_t)(need < 0 ? min(returned - back, (int64_t)INT32_MAX) : taken - (granted ? lacks : 0));
-        }
-        __syncthreads();
-        if (tid == kScanThreads - 1) { s_carry[0] = wanted; s_carry[1] = taken; s_carry[2] = returned; s_carry[3] = tokens; }
+    for (int b = b0; b < b1; ++b) {
+        const int need = a.need[b], n = a.new_lens[b];
+        if (need >= 0) wanted += need;
+        const bool granted = n >= 0 && need >= 0 && (need == 0 || wanted <= free);
+        if (granted && need > 0) taken = wanted;
+        error |= n >= 0 && !granted;
+        a.granted[b] = granted ? n : 0;
+        a.pages_before[b] = (int32_t)(need >= 0 ? min(wanted - need, (int64_t)INT32_MAX) : min(returned, (int64_t)INT32_MAX));
+        if (need < 0 && need != kBadSequence) returned += -1 - (int64_t)need;
+        tokens += granted ? n : 0;
     }
-    __syncthreads();
-    if (__syncthreads_or(error) && tid == 0) atomicExch(a.err_word, -4);
+    sums({tokens, 0}, run, all);
+    int64_t start = run.a - tokens;
+    for (int b = b0; b < b1; ++b) {
+        a.token_starts[b] = (int32_t)min(start, (int64_t)INT32_MAX);
+        start += a.granted[b];
+    }
+    taken = sums.most(taken);
+    error |= all_returned > N - free || all.a > a.max_tokens;
+    if (error) atomicExch(a.err_word, -4);
     if (tid == 0) {
-        a.token_starts[a.batch] = (int32_t)min(s_carry[3], (int64_t)INT32_MAX);
-        a.ring_before[0] = (int32_t)head;
-        a.ring_before[1] = (int32_t)free;
-        a.free_state[0] = (int32_t)((head + s_carry[1]) % N);
-        a.free_state[1] = (int32_t)(free - s_carry[1] + min(s_carry[2], N - free));
+        const int64_t next = head + taken;   // (at most `free` pages are taken)
+        a.token_starts[a.batch] = (int32_t)min(all.a, (int64_t)INT32_MAX);
+        a.ring_before[0] = head;
+        a.ring_before[1] = free;
+        a.free_state[0] = (int32_t)(next < N ? next : next - N);
+        a.free_state[1] = (int32_t)(free - taken + min(all_returned, (int64_t)(N - free)));
     }
 }
 
-// A range with holes, by one workgroup: entries in order, 256 at a time.
-__device__ __forceinline__ void apply_ordered(const TablesArgs &a, int b, int tid, int L, int n, int64_t head, int64_t free)
+// (WAVE: for a few hundred sequences one wave, which waits for nobody, is the faster.)
+template <bool WAVE> __global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(const TablesArgs a)
 {
-    __shared__ int s_wave[4];
-    int32_t *row = a.page_table + (int64_t)b * a.max_pages_per_seq;
-    const EntryRange r = entry_range(a, L, n);
-    int64_t before = a.pages_before[b];
-    for (int e0 = r.first; e0 <= r.last; e0 += 256) {
-        const int e = e0 + tid, page = e <= r.last ? row[e] : 0;
-        const bool hit = e <= r.last && is_mapped(a, page) == (n < 0);
-        const unsigned long long mask = __ballot(hit);
-        __syncthreads();
-        if ((tid & 63) == 0) s_wave[tid >> 6] = __popcll(mask);
-        __syncthreads();
-        int rank = __popcll(mask & ((1ull << (tid & 63)) - 1)), total = 0;
-        for (int w = 0; w < 4; ++w) { rank += w < (tid >> 6) ? s_wave[w] : 0; total += s_wave[w]; }
-        if (hit) {
-            const int64_t at = before + rank;
-            if (n >= 0) row[e] = a.free_pages[(head + at) % a.num_pages];
-            else {
-                if (at < a.num_pages - free) a.free_pages[(head + free + at) % a.num_pages] = page;
-                row[e] = -1;
-            }
-        }
-        before += total;
+    if constexpr (WAVE) {
+        scan_sequences(a, threadIdx.x, 64, WaveSums());
+    } else {
+        __shared__ Pair s_sums[kScanThreads / 64];
+        __shared__ int64_t s_top;
+        scan_sequences(a, threadIdx.x, kScanThreads, BlockSums{s_sums, &s_top});
     }
-    __syncthreads();  // (the entries are read below by other threads of this workgroup)
+}
+
+// What a sequence's entries and slots are made from.
+struct Sequence {
+    int32_t *row;
+    int L, n, need, first;
+    int64_t before;          // pages taken (returned) by the sequences before it
+    int head, free, pages;   // the ring before the call
+
+    __device__ __forceinline__ Sequence(const TablesArgs &a, int b)
+        : row(a.page_table + (int64_t)b * a.max_pages_per_seq), L(a.seq_lens[b]), n(a.new_lens[b]), need(a.need[b]), first(a.first[b]),
+          before(a.pages_before[b]), head(a.ring_before[0]), free(a.ring_before[1]), pages((int)a.num_pages)
+    {
+        if (need == kBadSequence) n = 0;
+        else if (n > 0) n = a.granted[b];
+    }
+    __device__ __forceinline__ bool holes() const { return first < 0; }
+    __device__ __forceinline__ int place(int64_t at) const   // at < 2 * pages - head
+    {
+        const int64_t p = head + at;
+        return (int)(p < pages ? p : p - pages);
+    }
+    __device__ __forceinline__ void give_back(const TablesArgs &a, int64_t at, int page) const
+    {
+        if (at < pages - free) a.free_pages[place(free + at)] = page;
+    }
+};
+
+// A range with holes, by one wave: entries in order, 64 at a time.
+__device__ __forceinline__ void apply_ordered(const TablesArgs &a, const Sequence &s, int lane)
+{
+    const EntryRange r = entry_range(a, s.L, s.n);
+    int64_t before = s.before;
+    for (int e0 = r.first; e0 <= r.last; e0 += 64) {
+        const int e = e0 + lane, page = e <= r.last ? s.row[e] : 0;
+        const bool hit = e <= r.last && is_mapped(a, page) == (s.n < 0);
+        const u64 hits = __ballot(hit);
+        if (hit) {
+            const int64_t at = before + __popcll(hits & ((1ull << lane) - 1));
+            if (s.n >= 0) s.row[e] = a.free_pages[s.place(at)];
+            else { s.give_back(a, at, page); s.row[e] = -1; }
+        }
+        before += __popcll(hits);
+    }
+}
+
+// Slot of token i of a granted sequence, and its entry where the token is the entry's first.  (Ranges with holes: the entries
+// are there.)
+__device__ __forceinline__ bool apply_token(const TablesArgs &a, const Sequence &s, int i, int64_t slot_at)
+{
+    const int pos = s.L + i, e = pos >> a.page_shift, off = pos & ((1 << a.page_shift) - 1);
+    int page;
+    if (!s.holes() && e >= s.first) {
+        page = a.free_pages[s.place(s.before + (e - s.first))];
+        if (off == 0) s.row[e] = page;
+    } else {
+        page = s.row[e];
+    }
+    const bool ok = is_mapped(a, page);   // (the ring may hold anything)
+    if (slot_at < a.max_tokens) a.slot_map[slot_at] = ok ? (page << a.page_shift) + off : -1;
+    return ok;
+}
+
+__device__ __forceinline__ void return_pages(const TablesArgs &a, const Sequence &s, int from, int step)
+{
+    const int count = -1 - s.need;
+    for (int i = from; i < count; i += step) {
+        s.give_back(a, s.before + i, s.row[s.first + i]);
+        s.row[s.first + i] = -1;
+    }
 }
 
 __global__ void __launch_bounds__(256) tables_apply_kernel(const TablesArgs a)
 {
     const int b = blockIdx.x, strip = blockIdx.y, strips = gridDim.y, tid = threadIdx.x;
-    const int need = a.need[b], L = a.seq_lens[b], first = a.first[b];
-    int n = a.new_lens[b];
-    if (need == kBadSequence) return;
-    const int64_t head = a.ring_before[0], free = a.ring_before[1], N = a.num_pages;
-    int32_t *row = a.page_table + (int64_t)b * a.max_pages_per_seq;
-    const bool holes = first < 0;
-    if (holes && strip > 0) return;
-    const int64_t before = a.pages_before[b];
-    if (n < 0) {
-        if (holes) { apply_ordered(a, b, tid, L, n, head, free); return; }
-        const int count = -1 - need;
-        for (int i = strip * 256 + tid; i < count; i += strips * 256) {
-            const int page = row[first + i];
-            if (before + i < N - free) a.free_pages[(head + free + before + i) % N] = page;
-            row[first + i] = -1;
-        }
+    const Sequence s(a, b);
+    if (s.n == 0 || (s.holes() && strip > 0)) return;
+    if (s.holes()) {
+        if (tid < 64) apply_ordered(a, s, tid);
+        __syncthreads();  // (the entries are read below by other threads of this workgroup)
+    }
+    if (s.n < 0) {
+        if (!s.holes()) return_pages(a, s, strip * 256 + tid, strips * 256);
         return;
     }
-    n = a.granted[b];
-    if (n == 0) return;
-    if (holes) apply_ordered(a, b, tid, L, n, head, free);
-    const int step = holes ? 256 : strips * 256, start = a.token_starts[b];
     bool error = false;
-    for (int i = (holes ? 0 : strip * 256) + tid; i < n; i += step) {
-        const int pos = L + i, e = pos >> a.page_shift, off = pos & ((1 << a.page_shift) - 1);
-        int page;
-        if (!holes && e >= first) {
-            page = a.free_pages[(head + before + (e - first)) % N];
-            if (off == 0 || i == 0) row[e] = page;
-        } else {
-            page = row[e];
+    const int step = s.holes() ? 256 : strips * 256;
+    const int64_t start = a.token_starts[b];
+    for (int i = strip * 256 + tid; i < s.n; i += step) error |= !apply_token(a, s, i, start + i);
+    if (error) atomicExch(a.err_word, -4);
+}
+
+// All three in one workgroup, for few sequences with few new tokens.  What the steps hand to each other stays in LDS; the
+// sequences are counted side by side, 1024 / batch threads to each.
+constexpr int kSmallBatch = 256, kSmallTokens = 4096, kSmallEntries = 65536;
+
+__global__ void __launch_bounds__(kScanThreads) tables_small_kernel(const TablesArgs g)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int s_len[kSmallBatch], s_new[kSmallBatch], s_need[kSmallBatch], s_first[kSmallBatch], s_before[kSmallBatch],
+        s_granted[kSmallBatch], s_start[kSmallBatch + 1], s_ring[2];
+    TablesArgs a = g;
+    a.seq_lens = s_len; a.new_lens = s_new;
+    a.need = s_need; a.first = s_first; a.pages_before = s_before; a.granted = s_granted; a.token_starts = s_start; a.ring_before = s_ring;
+    for (int b = tid; b < a.batch; b += kScanThreads) { s_len[b] = g.seq_lens[b]; s_new[b] = g.new_lens[b]; }
+    __syncthreads();
+    int threads = 64;
+    while (threads * a.batch > kScanThreads) threads >>= 1;
+    const int own = tid / threads, sub = tid & (threads - 1);
+    if (own < a.batch)
+        count_sequence(a, own, sub, threads, [&](int &count, int &first, int &last) __attribute__((always_inline)) {
+            for (int off = threads / 2; off >= 1; off >>= 1) {
+                count += __shfl_xor(count, off);
+                first = min(first, __shfl_xor(first, off));
+                last = max(last, __shfl_xor(last, off));
+            }
+        });
+    __syncthreads();
+    if (wave == 0) scan_sequences(a, lane, 64, WaveSums());
+    __syncthreads();
+    if (own < a.batch && s_first[own] >= 0 && s_new[own] < 0) return_pages(a, Sequence(a, own), sub, threads);
+    for (int b = wave; b < a.batch; b += kScanThreads / 64)
+        if (s_first[b] < 0) {
+            const Sequence s(a, b);
+            if (s.n != 0) apply_ordered(a, s, lane);
         }
-        const bool ok = is_mapped(a, page);   // (the ring may hold anything)
-        error |= !ok;
-        if ((int64_t)start + i < a.max_tokens) a.slot_map[start + i] = ok ? (page << a.page_shift) + off : -1;
+    for (int b = tid; b <= a.batch; b += kScanThreads) {
+        g.token_starts[b] = s_start[b];
+        if (b < a.batch) g.granted[b] = s_granted[b];
+    }
+    __syncthreads();
+    bool error = false;
+    for (int t = tid; t < s_start[a.batch]; t += kScanThreads) {
+        int b = 0;   // the last sequence that starts at t or before, which is the one that holds it
+#pragma unroll
+        for (int half = kSmallBatch / 2; half >= 1; half >>= 1)
+            if (b + half < a.batch && s_start[b + half] <= t) b += half;
+        const Sequence s(a, b);
+        error |= !apply_token(a, s, t - s_start[b], t);
     }
     if (error) atomicExch(a.err_word, -4);
 }
@@ -196,12 +340,18 @@ __global__ void __launch_bounds__(256) tables_apply_kernel(const TablesArgs a)
 hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream)
 {
     hipError_t e = hipSuccess;
+    if (a.batch > 0 && a.batch <= kSmallBatch && a.max_tokens <= kSmallTokens &&
+        (int64_t)a.batch * a.max_pages_per_seq <= kSmallEntries) {
+        hipLaunchKernelGGL(tables_small_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+        return hipGetLastError();
+    }
     if (a.batch > 0) {
         hipLaunchKernelGGL(tables_count_kernel, dim3(a.batch), dim3(a.batch > 1024 ? 64 : 256), 0, stream, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(tables_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+    if (a.batch <= kSmallBatch) hipLaunchKernelGGL((tables_scan_kernel<true>), dim3(1), dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((tables_scan_kernel<false>), dim3(1), dim3(kScanThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.batch == 0) return e;
     const int64_t most = a.max_tokens > a.max_pages_per_seq ? a.max_tokens : a.max_pages_per_seq;
