@@ -127,16 +127,25 @@ class DecodeStep:
                                       v_pool, page_table, seq_lens, out, self.prefill_ws, stream)
 
     def _workspace(self, name, need):
-        """The buffer kept for one kind of call (made on its first use, not inside a captured sequence)."""
+        """The buffer kept for one kind of call (made on its first use; ahead of a captured sequence by reserve)."""
         ws = getattr(self, name, None)
         if ws is None or ws.numel() < need:
             ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             setattr(self, name, ws)
         return ws
 
+    def reserve(self, sampling=False, tables=False) -> None:
+        """Makes the workspaces of sample_tokens and filtered_consensus_commit, or of update_page_tables, ahead of their first
+        call: a program that records calls into a graph does this before."""
+        if sampling:
+            self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
+            self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes(self.params))
+        if tables:
+            self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes(self.params))
+
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, logprobs=None, stream=None,
                       logits_stride_row=0):
-        """One token per logits row [batch, block_k, vocab] by each sequence's temperature, top-k, top-p and min-p (each of
+        """One token per logits row [batch, block_k, vocab] (float32, bfloat16 or float16) by each sequence's temperature, top-k, top-p and min-p (each of
         the last three a [batch] tensor or None) from the uniform numbers u [batch, block_k]."""
         ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
         return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits), logits, logits_stride_row, temperature,
@@ -200,7 +209,7 @@ class DecodeStack:
 
     def __init__(self, *, num_layers, batch, num_q_heads, num_kv_heads, head_dim, block_k, page_size,
                  k_pool, v_pool, page_table, seq_lens, max_seq_len, vocab, num_splits=0, temperature=0.0,
-                 diffusion_passes=1, device=0):
+                 diffusion_passes=1, device=0, filters=False, free_pages=None, free_state=None):
         if k_pool.dim() != 5 or k_pool.shape[0] != num_layers or not k_pool.is_contiguous():
             raise ValueError("pools must be contiguous [layers, pages, H_kv, P, d]")
         L, pages, H, P, d = k_pool.shape
@@ -232,6 +241,28 @@ class DecodeStack:
             self.accept_u = torch.zeros((batch, block_k), dtype=torch.float32, device=dev)
             self.gumbel = torch.zeros((batch, vocab), dtype=torch.float32, device=dev)
         i32 = dict(dtype=torch.int32, device=dev)
+        # filters: every request samples by its own `temperatures`, `top_k`, `top_p` and `min_p`; the cycle draws the drafts
+        # itself, from `diff_logits` by `draft_u`, and verifies them under the same filters
+        self.filters = bool(filters)
+        if self.filters:
+            f32 = dict(dtype=torch.float32, device=dev)
+            self.temperatures, self.top_p = torch.ones((batch,), **f32), torch.ones((batch,), **f32)
+            self.top_k, self.min_p = torch.zeros((batch,), **i32), torch.zeros((batch,), **f32)
+            self.diff_logits = torch.zeros_like(self.ar_logits)
+            self.draft_u, self.accept_u = torch.zeros((batch, block_k), **f32), torch.zeros((batch, block_k), **f32)
+            self.draft_logprobs = torch.zeros((batch, block_k), **f32)
+            self.gumbel = torch.zeros((batch, vocab), **f32)
+            self.step.reserve(sampling=True)
+        # a ring of free pages: the cycle first maps pages for `grow` tokens more per request (block_k each; a request that
+        # is over gets -1 there and its pages come back)
+        self.free_pages, self.free_state = free_pages, free_state
+        if free_pages is not None:
+            if free_pages.numel() != pages or free_state is None:
+                raise ValueError("free_pages holds num_pages entries and comes with free_state")
+            self.grow = torch.full((batch,), block_k, **i32)
+            self.granted, self.token_starts = torch.zeros((batch,), **i32), torch.zeros((batch + 1,), **i32)
+            self.slot_map = torch.zeros((batch * block_k,), **i32)
+            self.step.reserve(tables=True)
         self.accept_len, self.num_committed, self.next_anchor = (torch.zeros((batch,), **i32) for _ in range(3))
         self.out_tokens = torch.zeros((batch, block_k), **i32)
         self.graph = None
@@ -242,11 +273,22 @@ class DecodeStack:
         s = self.step
         diff = (0, self.q_diff, self.k_blk_diff, self.v_blk_diff, self.out_diff)
         ar = (1, self.q_ar, self.k_blk_ar, self.v_blk_ar, self.out_ar)
+        if self.free_pages is not None:
+            s.update_page_tables(self.seq_lens, self.grow, self.page_table, self.free_pages, self.free_state, self.granted,
+                                 self.token_starts, self.slot_map, stream)
         for view, q, kb, vb, out in (diff,) * self.diffusion_passes + (ar,):
+            if view == 1 and self.filters:
+                s.sample_tokens(self.diff_logits, self.temperatures, self.top_k, self.top_p, self.min_p, self.draft_u,
+                                self.draft_tokens, self.draft_logprobs, stream)
             for l in range(self.num_layers):
                 s.attn(view, q[l], kb[l], vb[l], self.k_pool[l], self.v_pool[l], self.page_table, self.seq_lens,
                        out[l], None, stream)
-        if self.temperature > 0:
+        if self.filters:
+            s.filtered_consensus_commit(self.ar_logits, self.diff_logits, self.temperatures, self.top_k, self.top_p,
+                                        self.min_p, self.draft_tokens, self.accept_u, self.gumbel, self.k_blk_ar,
+                                        self.v_blk_ar, self.k_pool, self.v_pool, self.page_table, self.seq_lens,
+                                        self.accept_len, self.num_committed, self.out_tokens, self.next_anchor, stream)
+        elif self.temperature > 0:
             s.sampling_consensus_commit(self.temperature, self.ar_logits, self.diff_logits, self.draft_tokens,
                                         self.accept_u, self.gumbel, self.k_blk_ar, self.v_blk_ar, self.k_pool,
                                         self.v_pool, self.page_table, self.seq_lens, self.accept_len,

@@ -1,0 +1,230 @@
+"""The sampling, page-table and store operators together, as a serving loop uses them: a stack whose cycle maps its own
+pages, draws its own drafts and verifies them under every request's filters (eager and as a replayed graph, each cycle
+against the oracle), and admission of prompts by slots followed by single-token decoding."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from orthrus_inputs import Workload, bf16_bits_to_f32, make_block
+
+pytestmark = pytest.mark.gpu
+
+MAX_ABS, MEAN_ABS = 2e-2, 2e-3   # attention tolerance of the path (bf16 in, fp32 accumulate)
+LAYERS, CYCLES, B, K, V, P, H, HQ, D = 2, 4, 5, 8, 4001, 16, 2, 8, 128
+FILTERS = [(0.8, 0, 0.95, 0.0), (0.7, 20, 0.9, 0.02), (0.0, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.0), (1.2, 0, 0.98, 0.05)]
+
+
+def _rt():
+    from paper_2605_12825_amd import runtime
+    return runtime
+
+
+def _bits(rng, *shape):
+    x = (rng.standard_normal(shape).astype(np.float32)).view(np.uint32)
+    return (x >> 16).astype(np.uint16)
+
+
+def _state(seed):
+    rng = np.random.default_rng(seed)
+    lens = np.array([0, 5, 37, 90, 64], np.int32)
+    width, pages = 12, 60
+    perm = rng.permutation(pages).astype(np.int32)
+    table, at = np.full((B, width), -1, np.int32), 0
+    for b in range(B):
+        n = (lens[b] + P - 1) // P
+        table[b, :n] = perm[at:at + n]
+        at += n
+    ring = np.full(pages, -1, np.int32)
+    head = 47
+    ring[(head + np.arange(pages - at)) % pages] = perm[at:]
+    kp, vp = _bits(rng, LAYERS, pages, H, P, D), _bits(rng, LAYERS, pages, H, P, D)
+    return dict(lens=lens, table=table, ring=ring, state=np.array([head, pages - at], np.int32), kp=kp, vp=vp)
+
+
+def _stack(st):
+    rt = _rt()
+    d = rt.to_device_bits
+    s = rt.DecodeStack(num_layers=LAYERS, batch=B, num_q_heads=HQ, num_kv_heads=H, head_dim=D, block_k=K, page_size=P,
+                       k_pool=d(st["kp"]), v_pool=d(st["vp"]), page_table=d(st["table"]), seq_lens=d(st["lens"]),
+                       max_seq_len=st["table"].shape[1] * P, vocab=V, filters=True, free_pages=d(st["ring"]),
+                       free_state=d(st["state"]))
+    for i, name in enumerate(("temperatures", "top_k", "top_p", "min_p")):
+        getattr(s, name).copy_(torch.tensor([f[i] for f in FILTERS]))
+    return s
+
+
+def _inputs(c):
+    rng = np.random.default_rng(100 + c)
+    x = dict(q_diff=_bits(rng, LAYERS, B, K, HQ, D), q_ar=_bits(rng, LAYERS, B, K, HQ, D))
+    for n in ("k_blk_diff", "v_blk_diff", "k_blk_ar", "v_blk_ar"):
+        x[n] = _bits(rng, LAYERS, B, K, H, D)
+    ar = rng.standard_normal((B, K, V)).astype(np.float32) * 2
+    ar[:, :, :40] += rng.uniform(6, 14, (B, K, 40)).astype(np.float32)
+    x["ar_logits"], x["diff_logits"] = ar, ar + 0.3 * rng.standard_normal(ar.shape).astype(np.float32)
+    x["draft_u"], x["accept_u"] = rng.random((B, K), dtype=np.float32), rng.random((B, K), dtype=np.float32)
+    x["gumbel"] = rng.gumbel(size=(B, V)).astype(np.float32)
+    grow = np.full(B, K, np.int32)
+    if c == 2:
+        grow[3] = -1       # a request ends and gives its pages back; its length is put to 0 by whoever ends it
+    x["grow"] = grow
+    return x
+
+
+def _close(got_bits, want):
+    err = np.abs(bf16_bits_to_f32(got_bits).astype(np.float64) - want)
+    assert np.all(np.isfinite(err)) and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS
+
+
+def test_cycles_that_map_their_pages_and_draw_their_drafts_eager_and_replayed():
+    rt = _rt()
+    st = _state(1)
+    ref = {k: v.copy() for k, v in st.items()}
+    eager, graph = _stack(st), _stack(st)
+    graph.capture()
+    f = [np.array([r[i] for r in FILTERS], t) for i, t in enumerate((np.float32, np.int32, np.float32, np.float32))]
+    for c in range(CYCLES):
+        x = _inputs(c)
+        slots = np.full(B * K, -9, np.int32)
+        granted, starts, status = oracle.page_tables_update(ref["lens"], x["grow"], ref["table"], ref["ring"], ref["state"], P,
+                                                            ref["table"].shape[1] * P, B * K, slots)
+        assert status == 0
+        if c == 2:
+            ref["lens"][3] = 0
+            x["grow"] = x["grow"].copy()
+        want_d, want_a = [[oracle.dual_view_attn(v, 1 / np.sqrt(D), x["q_" + t][l], x["k_blk_" + t][l], x["v_blk_" + t][l],
+                                                 ref["kp"][l], ref["vp"][l], ref["table"], ref["lens"]) for l in range(LAYERS)]
+                          for v, t in ((0, "diff"), (1, "ar"))]
+        drafts, lp, margin = oracle.sample_tokens(x["diff_logits"], *f, x["draft_u"])
+        want = oracle.filtered_consensus_commit(x["ar_logits"], x["diff_logits"], *f, drafts, x["accept_u"], x["gumbel"],
+                                                x["k_blk_ar"], x["v_blk_ar"], ref["kp"], ref["vp"], ref["table"], ref["lens"])
+        assert margin.min() > 1e-9 and want["margin"] > 1e-8
+        for s, run in ((eager, eager.cycle), (graph, graph.replay)):
+            for k, v in x.items():
+                getattr(s, k).copy_(rt.to_device_bits(v))
+            s.slot_map.fill_(-9)
+            if c == 2:     # the request that ends: its old length has no meaning for the rest of the cycle
+                s.seq_lens[3] = 0
+            torch.cuda.synchronize()
+            run()
+            torch.cuda.synchronize()
+            g = lambda n: rt.bits_to_numpy(getattr(s, n))  # noqa: E731
+            for n, w in (("granted", granted), ("token_starts", starts), ("page_table", ref["table"]), ("free_pages", ref["ring"]),
+                         ("free_state", ref["state"]), ("slot_map", slots), ("draft_tokens", drafts), ("seq_lens", ref["lens"]),
+                         ("k_pool", ref["kp"]), ("v_pool", ref["vp"]), ("accept_len", want["accept_len"]),
+                         ("num_committed", want["num_committed"]), ("out_tokens", want["out_tokens"]),
+                         ("next_anchor", want["next_anchor"])):
+                np.testing.assert_array_equal(g(n), w, err_msg="%s cycle %d" % (n, c))
+            _close(g("out_diff"), np.stack(want_d))
+            _close(g("out_ar"), np.stack(want_a))
+            assert np.all(np.abs(g("draft_logprobs") - lp) <= np.abs(lp) * 2.0 ** -24 + 1e-9)
+            assert s.step.device_error() == want["status"]
+    eager.close()
+    graph.close()
+
+
+@pytest.mark.parametrize("replays", [3])
+def test_a_captured_draw_replays_like_the_eager_one(replays):
+    """Rows of every kind (listed, wide, plain, empty) in one captured call, new inputs before each replay, eager work between."""
+    from paper_2605_12825_amd import binding as bd
+    rt = _rt()
+    Bn, Kn, Vn = 12, 2, 40001
+    step = rt.DecodeStep(batch=Bn, num_q_heads=2, num_kv_heads=2, head_dim=64, block_k=Kn, page_size=16, max_pages_per_seq=1,
+                         max_seq_len=16, num_pages=1, vocab=Vn)
+    step.reserve(sampling=True)
+    rows = [FILTERS[b % 5] if b < 10 else (1.4, 0, 0.97, 0.0) for b in range(Bn)]
+    f = [torch.tensor([r[i] for r in rows], dtype=t, device="cuda") for i, t in enumerate((torch.float32, torch.int32, torch.float32, torch.float32))]
+    logits, u = torch.zeros((Bn, Kn, Vn), device="cuda"), torch.zeros((Bn, Kn), device="cuda")
+    toks, lps = torch.zeros((Bn, Kn), dtype=torch.int32, device="cuda"), torch.zeros((Bn, Kn), device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    bd.orthrus_graph_begin(step.ctx, stream)
+    step.sample_tokens(logits, *f, u, toks, lps, stream=stream)
+    g = bd.orthrus_graph_end(step.ctx, stream)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for i in range(replays):
+        logits.copy_(torch.randn(logits.shape, generator=gen, device="cuda") * 2)
+        logits[:6, :, 100 * i:100 * i + 30] += 14
+        logits[i] = -float("inf")
+        u.copy_(torch.rand(u.shape, generator=gen, device="cuda"))
+        torch.cuda.synchronize()
+        bd.orthrus_graph_launch(g, stream)
+        torch.cuda.synchronize()
+        got, got_lp = toks.clone(), lps.clone()
+        step.sample_tokens(logits, *f, u, toks, lps)
+        torch.cuda.synchronize()
+        assert torch.equal(got, toks) and torch.equal(got_lp, lps) and (toks[i] == -1).all()
+        want, _, _ = oracle.sample_tokens(logits.cpu().numpy(), *[v.cpu().numpy() for v in f], u.cpu().numpy())
+        np.testing.assert_array_equal(got.cpu().numpy(), want)
+    bd.orthrus_graph_destroy(g)
+    step.close()
+
+
+def test_prompts_admitted_by_slots_then_decoded_token_by_token():
+    """Tables, store, single-token attention and draw, four steps, every tensor against the oracle."""
+    rt = _rt()
+    rng = np.random.default_rng(7)
+    Bn, width, pages = 4, 8, 40
+    table, ring, state = np.full((Bn, width), -1, np.int32), rng.permutation(pages).astype(np.int32), np.array([9, pages], np.int32)
+    kp, vp = _bits(rng, 1, pages, H, P, D), _bits(rng, 1, pages, H, P, D)
+    lens = np.zeros(Bn, np.int32)
+    d = rt.to_device_bits
+    mk = lambda bound: rt.DecodeStep(batch=Bn, num_q_heads=HQ, num_kv_heads=H, head_dim=D, block_k=1, page_size=P,  # noqa: E731
+                                     max_pages_per_seq=width, max_seq_len=bound, num_pages=pages, vocab=V)
+    step = mk(width * P)
+    t, r, s, kpd, vpd, ld = d(table), d(ring), d(state), d(kp), d(vp), d(lens)
+    granted_d, starts_d = torch.zeros(Bn, dtype=torch.int32, device="cuda"), torch.zeros(Bn + 1, dtype=torch.int32, device="cuda")
+    f = [np.array([x[i] for x in FILTERS[:Bn]], ty) for i, ty in enumerate((np.float32, np.int32, np.float32, np.float32))]
+    for i, new in enumerate([[37, 1, 60, 16], [1, 1, 1, 1], [1, 40, -1, 1], [1, 1, 20, 1]]):
+        new = np.array(new, np.int32)
+        cap = 128
+        k, v = _bits(rng, 1, cap, H, D), _bits(rng, 1, cap, H, D)
+        slots = np.full(cap, -1, np.int32)
+        granted, starts, status = oracle.page_tables_update(lens, new, table, ring, state, P, width * P, cap, slots)
+        assert status == 0 and oracle.kv_store(k, v, slots, kp, vp, starts[-1]) == 0
+        m = torch.full((cap,), -1, dtype=torch.int32, device="cuda")
+        step.update_page_tables(ld, d(new), t, r, s, granted_d, starts_d, m)
+        step.store_kv(d(k), d(v), m, kpd, vpd, num_valid=starts_d[Bn:])
+        lens = np.where(new < 0, 0, lens + granted).astype(np.int32)
+        ld.copy_(torch.where(d(new) < 0, 0, ld + granted_d))
+        q, kb, vb = _bits(rng, Bn, 1, HQ, D), _bits(rng, Bn, 1, H, D), _bits(rng, Bn, 1, H, D)
+        out = torch.zeros((Bn, 1, HQ, D), dtype=torch.int16, device="cuda")
+        step.attn(1, d(q), d(kb), d(vb), kpd[0], vpd[0], t, ld, out)
+        logits, u = rng.standard_normal((Bn, 1, V)).astype(np.float32) * 4, rng.random((Bn, 1), dtype=np.float32)
+        tokens = torch.zeros((Bn, 1), dtype=torch.int32, device="cuda")
+        step.sample_tokens(d(logits), *[d(x) for x in f], d(u), tokens)
+        torch.cuda.synchronize()
+        assert step.device_error() == 0
+        for got, want in ((t, table), (r, ring), (s, state), (m, slots), (ld, lens), (kpd, kp), (vpd, vp)):
+            np.testing.assert_array_equal(rt.bits_to_numpy(got), want)
+        _close(rt.bits_to_numpy(out), oracle.dual_view_attn(1, 1 / np.sqrt(D), q, kb, vb, kp[0], vp[0], table, lens))
+        np.testing.assert_array_equal(tokens.cpu().numpy(), oracle.sample_tokens(logits, *f, u)[0])
+    step.close()
+
+
+def test_calls_on_two_streams_with_a_workspace_each():
+    """Two steps' calls may overlap in time: every step has its own context and workspaces."""
+    rt = _rt()
+    Bn, Kn, Vn = 6, 4, 30011
+    steps = [rt.DecodeStep(batch=Bn, num_q_heads=2, num_kv_heads=2, head_dim=64, block_k=Kn, page_size=16, max_pages_per_seq=1,
+                           max_seq_len=16, num_pages=1, vocab=Vn) for _ in range(2)]
+    rng = np.random.default_rng(11)
+    f = [torch.tensor([FILTERS[b % 5][i] for b in range(Bn)], dtype=t, device="cuda")
+         for i, t in enumerate((torch.float32, torch.int32, torch.float32, torch.float32))]
+    xs = [(rng.standard_normal((Bn, Kn, Vn)) * 3).astype(np.float32) for _ in range(2)]
+    us = [rng.random((Bn, Kn), dtype=np.float32) for _ in range(2)]
+    dev = [(torch.from_numpy(x).cuda(), torch.from_numpy(u).cuda(), torch.zeros((Bn, Kn), dtype=torch.int32, device="cuda"))
+           for x, u in zip(xs, us)]
+    for s in steps:
+        s.reserve(sampling=True)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, st, (x, u, t) in zip(steps, streams, dev):
+            s.sample_tokens(x, *f, u, t, stream=st)
+    torch.cuda.synchronize()
+    for x, u, (_, _, t) in zip(xs, us, dev):
+        want, _, _ = oracle.sample_tokens(x, *[v.cpu().numpy() for v in f], u)
+        np.testing.assert_array_equal(t.cpu().numpy(), want)
+    for s in steps:
+        s.close()
