@@ -46,6 +46,15 @@ template <int DT> __device__ __forceinline__ const void *logit_row(const FilterA
     return (const char *)a.logits[side] + (int64_t)row * a.stride_row * (DT == 0 ? 4 : 2);
 }
 
+// The i-th of the rows that a launch is about: block rows first_k .. first_k + stage_k - 1 of every sequence and view.  -1: the
+// sequence has lost a draft already, its later rows are not asked for.
+__device__ __forceinline__ int stage_row(const FilterArgs &a, int i)
+{
+    const int side = i >= a.stage_rows, r = i - side * a.stage_rows, b = r / a.stage_k;
+    if (a.decided && a.decided[b] < a.first_k) return -1;
+    return side * a.rows + b * a.block_k + a.first_k + (r - b * a.stage_k);
+}
+
 // A whole number that orders like the logit.
 __device__ __forceinline__ uint32_t order_key(float x)
 {
@@ -276,9 +285,12 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
     const int lane = threadIdx.x & 63;
     const uint32_t item = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item == 0 && lane == 0) a.unresolved[0] = 0;
-    const int rr = (int)(item / (uint32_t)a.chunks), chunk = (int)(item - (uint32_t)rr * a.chunks);
-    if (rr >= a.all_rows) return;
+    const int nth = (int)(item / (uint32_t)a.chunks), chunk = (int)(item - (uint32_t)nth * a.chunks);
+    if (nth >= a.all_rows) return;
+    const int rr = stage_row(a, nth);
+    if (rr < 0) return;
     const int side = rr >= a.rows, row = rr - side * a.rows;
+    const int64_t place = (int64_t)rr * a.chunks + chunk;
     const void *logits = logit_row<DT>(a, side, row);
     const Chunk<DT> c = {logits, chunk * kChunk - row_skew<DT>(logits), a.vocab};
     float x[kEach];
@@ -328,7 +340,7 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
         }
     }
     if (n <= kListCap)
-        for (int i = lane; i < n; i += 64) a.lists[(int64_t)item * kListCap + i] = mine[i];
+        for (int i = lane; i < n; i += 64) a.lists[place * kListCap + i] = mine[i];
     // ---- the weights, relative to the chunk's maximum
     double sum = 0.0;
     if (top > -INFINITY) {
@@ -345,7 +357,7 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
         r.top = top;
         r.tau = n <= kListCap ? tau : INFINITY;   // more equal ones than the list holds: nothing is listed
         r.count = n <= kListCap ? n : 0;
-        a.stats[item] = r;
+        a.stats[place] = r;
     }
 }
 
@@ -407,7 +419,9 @@ struct PickShared {
 // SCANNED: the row's chunks have been listed; else it has at most kPickEntries logits and is read here.
 template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads, 4) filter_pick_kernel(const FilterArgs a)
 {
-    const int rr = blockIdx.x, side = rr >= a.rows, row = rr - side * a.rows, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int rr = stage_row(a, blockIdx.x), side = rr >= a.rows, row = rr - side * a.rows;
+    if (rr < 0) return;
     __shared__ PickShared s;
     const RowFilter f = row_filter(a, row / a.block_k);
     const void *logits = logit_row<DT>(a, side, row);
@@ -1125,21 +1139,40 @@ template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArg
     return hipGetLastError();
 }
 
-template <bool DRAW> static hipError_t launch_filters(FilterArgs &a, hipStream_t stream)
+template <bool DRAW> static hipError_t launch_filters(const FilterArgs &a, hipStream_t stream)
 {
-    a.all_rows = a.rows * (DRAW ? 1 : 2);
-    const FilterPlan p = filter_plan(a.all_rows, a.vocab);
-    char *ws = (char *)a.workspace;
-    a.stats = (ChunkStat *)(ws + p.stats);
-    a.lists = (uint2 *)(ws + p.lists);
-    a.unresolved = (int32_t *)(ws + p.unresolved);
-    a.chunks = p.chunks;
     if (a.dtype == 0) return launch_filters_of<0, DRAW>(a, stream);
     if (a.dtype == 1) return launch_filters_of<1, DRAW>(a, stream);
     return launch_filters_of<2, DRAW>(a, stream);
 }
 
-hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream) { return launch_filters<true>(a, stream); }
+// Lays out the workspace for all rows of `views` views.
+static void place_workspace(FilterArgs &a, int views)
+{
+    const FilterPlan p = filter_plan((int64_t)a.rows * views, a.vocab);
+    char *ws = (char *)a.workspace;
+    a.stats = (ChunkStat *)(ws + p.stats);
+    a.lists = (uint2 *)(ws + p.lists);
+    a.unresolved = (int32_t *)(ws + p.unresolved);
+    a.chunks = p.chunks;
+}
+
+// Block rows k0 .. k1-1 of every sequence and view.
+static void set_stage(FilterArgs &a, int views, int k0, int k1)
+{
+    a.first_k = k0;
+    a.stage_k = k1 - k0;
+    a.stage_rows = a.rows / a.block_k * a.stage_k;
+    a.all_rows = a.stage_rows * views;
+}
+
+hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream)
+{
+    place_workspace(a, 1);
+    set_stage(a, 1, 0, a.block_k);
+    a.decided = nullptr;
+    return launch_filters<true>(a, stream);
+}
 
 // ---- consensus
 
@@ -1162,6 +1195,26 @@ struct Candidate {
     }
 };
 
+template <int DT> __device__ __forceinline__ bool keeps_draft(const FilteredArgs &a, const Scale &t, int row)
+{
+    const int x = a.c.draft_tokens[row];
+    const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
+    const float u = a.accept_u[row];
+    if (x < 0 || x >= a.c.vocab) return false;
+    const float xp = logit<DT>(logit_row<DT>(a.f, 0, row), x), xq = logit<DT>(logit_row<DT>(a.f, 1, row), x);
+    return (double)u * kept_prob(cq, t, xq, x) < kept_prob(cp, t, xp, x);
+}
+
+// Between two stages: a wave per sequence, the leading drafts of the first `rows` that are kept.
+template <int DT> __global__ void __launch_bounds__(64) filtered_stage_kernel(const FilteredArgs a, int rows)
+{
+    const int b = blockIdx.x, k = threadIdx.x;
+    const Scale t = row_filter(a.f, b).t;
+    const bool keep = k >= rows || keeps_draft<DT>(a, t, b * a.c.block_k + k);
+    const u64 lost = ~__ballot(keep);
+    if (k == 0) a.c.decided[b] = lost ? __ffsll((long long)lost) - 1 : rows;
+}
+
 // Grid (piece, sequence).  Every workgroup repeats the keep decisions of its sequence (three dependent round trips), the first
 // records them.  The first rejected row's kept tokens are in the row's lists, which the first workgroup goes through, or
 // anywhere (no filter, a wide cut): then each goes through its piece of the row.
@@ -1172,17 +1225,8 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
     const Scale t = row_filter(a.f, b).t;
     __shared__ int s_keep[32];
     __shared__ Candidate s_best[2][kDrawThreads / 64];
-    if (tid < K) {
-        const int row = b * K + tid, x = a.c.draft_tokens[row];
-        const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
-        const float u = a.accept_u[row];
-        bool keep = false;
-        if (x >= 0 && x < V) {
-            const float xp = logit<DT>(logit_row<DT>(a.f, 0, row), x), xq = logit<DT>(logit_row<DT>(a.f, 1, row), x);
-            keep = (double)u * kept_prob(cq, t, xq, x) < kept_prob(cp, t, xp, x);
-        }
-        s_keep[tid] = keep;
-    }
+    // (rows behind a lost one may not have been looked at: what is found for them does not matter)
+    if (tid < K) s_keep[tid] = keeps_draft<DT>(a, t, b * K + tid);
     __syncthreads();
     const unsigned long long rej = ~__ballot(lane >= K || s_keep[lane < K ? lane : 0]);
     const int j = rej ? __ffsll((long long)rej) - 1 : K;
@@ -1315,19 +1359,46 @@ __global__ void __launch_bounds__(256) filtered_commit_kernel(const FilteredArgs
 
 int draw_pieces(int vocab) { return (vocab + kDrawPiece - 1) / kDrawPiece; }
 
-hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream)
+// Logits that take long to go through are gone through in two stages, the second for the sequences that kept every draft of the
+// first.  With a share r of drafts kept and 16 rows, 6 + 10 r^6 of them are read: 7 at r = 0.7, 10 at 0.85, 13 at 0.95; the second
+// stage's four launches take 12 us, what a third of kKeepBytes takes to read.  (64 x 16 rows of 151936, r about 0.9: 336 us in one
+// stage.)
+static int first_stage(const FilterArgs &a)
+{
+    const int64_t bytes = (int64_t)a.rows * 2 * a.vocab * (a.dtype == 0 ? 4 : 2);
+    return a.chunks > 0 && a.block_k >= 4 && bytes > kKeepBytes ? (3 * a.block_k + 7) / 8 : a.block_k;
+}
+
+template <int DT> static hipError_t launch_filtered_of(FilteredArgs &a, hipStream_t stream)
 {
     const ConsensusArgs &c = a.c;
-    hipError_t e = launch_filters<false>(a.f, stream);
+    const int k1 = first_stage(a.f);
+    set_stage(a.f, 2, 0, k1);
+    hipError_t e = launch_filters_of<DT, false>(a.f, stream);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)a.pieces, (unsigned)c.batch);
-    if (a.f.dtype == 0) hipLaunchKernelGGL((filtered_draw_kernel<0>), grid, dim3(kDrawThreads), 0, stream, a);
-    else if (a.f.dtype == 1) hipLaunchKernelGGL((filtered_draw_kernel<1>), grid, dim3(kDrawThreads), 0, stream, a);
-    else hipLaunchKernelGGL((filtered_draw_kernel<2>), grid, dim3(kDrawThreads), 0, stream, a);
+    if (k1 < c.block_k) {
+        hipLaunchKernelGGL((filtered_stage_kernel<DT>), dim3(c.batch), dim3(64), 0, stream, a, k1);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        set_stage(a.f, 2, k1, c.block_k);
+        a.f.decided = c.decided;
+        e = launch_filters_of<DT, false>(a.f, stream);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((filtered_draw_kernel<DT>), dim3((unsigned)a.pieces, (unsigned)c.batch), dim3(kDrawThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(filtered_commit_kernel, dim3(c.batch, c.do_commit ? c.num_layers : 1), dim3(256), 0, stream, a);
     return hipGetLastError();
+}
+
+hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream)
+{
+    place_workspace(a.f, 2);
+    a.f.decided = nullptr;
+    if (a.f.dtype == 0) return launch_filtered_of<0>(a, stream);
+    if (a.f.dtype == 1) return launch_filtered_of<1>(a, stream);
+    return launch_filtered_of<2>(a, stream);
 }
 
 }  // namespace orthrus

@@ -327,3 +327,25 @@ def test_without_filters_the_decisions_are_those_of_the_sampling_consensus():
     step.close()
     for k, v in (("accept_len", acc), ("num_committed", ncm), ("out_tokens", toks), ("next_anchor", anchor)):
         np.testing.assert_array_equal(got[k], v.cpu().numpy(), err_msg=k)
+
+
+@pytest.mark.parametrize("K,dtype", [(4, "f32"), (13, "f32"), (32, "bf16")])
+def test_consensus_in_two_stages(K, dtype):
+    """More logits than the last-level cache holds: the later rows are gone through only where the first drafts were all kept.
+    The rows behind a lost draft hold NaN, which nothing may read anything from."""
+    V = 151936 if dtype == "f32" else 160001
+    B = (220 << 20) // (2 * K * V * (4 if dtype == "f32" else 2)) + 1
+    rows = [FILTERS[b % len(FILTERS)] for b in range(B)]
+    c = _case(61 + K, B, K, V, rows, noise=0.25, dtype=dtype)
+    first = (3 * K + 7) // 8
+    c["draft"][1, first - 1] = -1       # lost at the last row of the first stage
+    if B > 2:
+        c["draft"][2, first:first + 1] = -1   # at the first of the second
+    got = _check_consensus(c)
+    for b in range(B):
+        c["ar"][b, got["accept_len"][b] + 1:] = float("nan")
+        c["df"][b, got["accept_len"][b] + 1:] = float("nan")
+    again, err = _consensus(c)
+    assert err == 0
+    for k in got:
+        np.testing.assert_array_equal(again[k], got[k], err_msg=k)
