@@ -312,7 +312,7 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
  *   logprobs     [dev] fp32 [B, K] or NULL written if given
  *   p            batch, block_k and vocab are used
  *   workspace/workspace_bytes: at least orthrus_sample_workspace_bytes(p)
- * Supported: V <= 1048576.
+ * Supported: V <= 1048576, B * K * ceil(V / 2048) below 3 * 10^7.
  */
 int64_t orthrus_sample_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
@@ -333,7 +333,7 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
  *   temperature, top_k, top_p, min_p as in orthrus_sample_tokens, applied to both views
  *   remaining arguments as in orthrus_sampling_consensus_commit
  *   workspace/workspace_bytes: at least orthrus_filtered_workspace_bytes(p)
- * Probabilities are formed in 64 bits.  Supported: V <= 1048576.
+ * Probabilities are formed in 64 bits.  Supported as in orthrus_sample_tokens.
  */
 int64_t orthrus_filtered_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,
@@ -356,7 +356,8 @@ orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus
  *   n < 0   the request is over: all its mapped entries go to the tail of the ring in order and become -1, granted[b] = 0.
  *           Pages that come back are handed out from the next call on.
  * token_starts[b] = sum of granted[0..b-1] (B+1 values); slot_map[token_starts[b] + i] = page * P + offset of token
- * position L + i for i < granted[b].  Slots behind the last token are left as they were.  seq_lens are not changed.
+ * position L + i for i < granted[b].  Slots behind the last token are left as they were.  seq_lens are not changed.  The
+ * arrays must not overlap.
  *
  *   seq_lens, new_lens [dev] int32 [B] (read only)
  *   page_table   [dev] int32 [B, max_pages_per_seq]; free_pages [dev] int32 [num_pages]; free_state [dev] int32 [2]

@@ -742,7 +742,6 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
     const size_t need = orthrus::filter_workspace_bytes(rows, p->vocab, 1);
     if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return ORTHRUS_EWORKSPACE;
     orthrus::FilterArgs a = filter_args(p, logits_type, logits, nullptr, logits_stride_row, temperature, top_k, top_p, min_p);
-    a.num_cus = plan_cus(ctx);
     a.u = u; a.tokens = tokens; a.logprobs = logprobs;
     a.workspace = workspace;
     return orthrus::launch_sample_tokens(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
@@ -807,7 +806,6 @@ orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus
     c.page_shift = do_commit ? log2_exact(p->page_size) : 0; c.max_pages_per_seq = p->max_pages_per_seq;
     c.chunks = 0; c.chunk_elems = 0; c.do_commit = do_commit ? 1 : 0;
     a.f = filter_args(p, logits_type, ar_logits, diff_logits, logits_stride_row, temperature, top_k, top_p, min_p);
-    a.f.num_cus = plan_cus(ctx);
     a.f.cuts = (orthrus::RowCut *)((char *)workspace + l.cuts);
     a.f.workspace = (char *)workspace + l.filter;
     a.accept_u = accept_u; a.gumbel = gumbel;

@@ -9,13 +9,19 @@
 // the weights are taken in 64 bits, because a token next to a cut or to the uniform number is decided by the last bits
 // of a sum over the vocabulary: with a sum good to 1e-7 one row in a few thousand would draw another token.
 //
-//   filter_scan_kernel     grid (row, chunk): the one pass over the logits.  Leaves per chunk its maximum, the sum of its
-//                          weights and a list of its largest logits, some hundred of them.
-//   filter_pick_kernel     one workgroup per row (and view): cuts and token from the lists of its chunks, which hold every
-//                          logit down to the least that one of them lists; a row without filters from the chunks' sums and
-//                          one chunk read again.  A row whose cut lies below the lists goes to the next kernel.
-//   filter_wide_kernel     one workgroup per such row, several passes over it.
-//   filtered_draw_kernel   one workgroup per sequence: keep decisions, the replacement drawn from the first rejected row.
+//   filter_scan_kernel     a wave to a chunk of 2048 logits, the one pass over them: the chunk's maximum, the sum of its weights
+//                          and a list of its largest logits, some thirty.  Bound by the vector unit where weights are summed
+//                          (18 instructions each, 64 bits at full rate), else near the stream: 1024 rows of 151936, 622 MB,
+//                          104 us without the weights of any row, 156 with those of all, 94 for the plain argmax scan.
+//   filter_pick_kernel     a workgroup to a row: cuts and token from the lists of its chunks, which together hold every logit down to
+//                          the highest of their thresholds (some thousand); what the first cut leaves is ranked in the lanes of a
+//                          wave.  A row without filters: from the chunks' sums, and one chunk read again.  A row whose cut lies
+//                          below the lists goes to the next kernel.  Rows of at most 1792 logits come here at once.  Bound by
+//                          its chain of memory and LDS round trips, 7 to 12 us; 1024 rows 37 us.
+//   filter_wide_kernel     a workgroup to such a row: a histogram pass and a pass that gathers the step of the cut; bound by the
+//                          weights of both passes (256 rows of 151936, nuclei of tens of thousands: 126 us).
+//   filtered_stage_kernel  keep decisions between the consensus's two stages.
+//   filtered_draw_kernel   grid (piece, sequence): keep decisions, the replacement drawn from the first rejected row.
 //   filtered_commit_kernel grid (sequence, layer): outputs and the commit, as sample_commit_kernel does it.
 #include "orthrus_internal.h"
 #include "orthrus_lanes.h"
@@ -278,8 +284,8 @@ struct Least {
 
 // A wave to a chunk, without a word to the others: waves that wait for their loads then run beside waves that compute.
 // The list's threshold is the third least of the maxima of sixteen groups of four lanes (of those that hold anything): 30
-// logits +- 10 reach it in a row without order.  (The least one of all leaves 38 more with a tail that overruns a list of
-// 128 in one chunk of 200.)  NT: the logits are more than the last-level cache holds.
+// logits +- 10 reach it in a row without order.  (The least one of all leaves 54, with a tail that overruns a list of 128
+// in one chunk of 200.)  NT: the logits are more than the last-level cache holds.
 template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filter_scan_kernel(const FilterArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -754,11 +760,14 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
 
 // ---- rows whose cut lies below the lists
 
+// (A workgroup to each such row, the others leave at once: with a loop over the rows the compiler kept 80 registers more alive,
+// for half the waves.)
+
 // A whole row in the hands of a workgroup, read in blocks: a wave takes a block of 512 vectors, eight loads at a time, so
 // that a block's sum is one reduction.  Cuts are found by a histogram over 4096 steps of the logit (a hundredth of a
 // binade of the weight each) and then among the logits of one step, gathered in the second pass, which also sums what lies
 // above them; steps that hold more logits than the gather has room for (rows of equal logits) go digit by digit.
-constexpr int kWideThreads = 512, kWideWaves = kWideThreads / 64;
+constexpr int kWideThreads = 1024, kWideWaves = kWideThreads / 64;
 constexpr int kWideEntries = 4096;
 constexpr int kSteps = 4096, kMaxBlocks = 520;   // of 2048 logits (or 4096): 2^20 and what a row's start takes
 
@@ -1013,83 +1022,81 @@ template <int DT> struct WideRow {
 
 };
 
-template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads, 2) filter_wide_kernel(const FilterArgs a)
+template <int DT, bool DRAW> __global__ void __launch_bounds__(kWideThreads, 4) filter_wide_kernel(const FilterArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, count = a.unresolved[0];
+    if ((int)blockIdx.x >= count) return;
     __shared__ WideShared s;
     s.bins.clear(tid);
     s.steps.clear(tid);
-    for (int at = blockIdx.x; at < count; at += gridDim.x) {
-        const int rr = a.unresolved[1 + at], side = rr >= a.rows, row = rr - side * a.rows;
-        const RowFilter f = row_filter(a, row / a.block_k);
-        const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
-        float top = -INFINITY, tau = INFINITY;
-        for (int c = tid; c < a.chunks; c += kWideThreads) { top = fmaxf(top, stats[c].top); tau = fminf(tau, stats[c].tau); }
+    const int rr = a.unresolved[1 + blockIdx.x], side = rr >= a.rows, row = rr - side * a.rows;
+    const RowFilter f = row_filter(a, row / a.block_k);
+    const ChunkStat *stats = a.stats + (int64_t)rr * a.chunks;
+    float top = -INFINITY, tau = INFINITY;
+    for (int c = tid; c < a.chunks; c += kWideThreads) { top = fmaxf(top, stats[c].top); tau = fminf(tau, stats[c].tau); }
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) { top = fmaxf(top, __shfl_xor(top, off)); tau = fminf(tau, __shfl_xor(tau, off)); }
-        if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
-        __syncthreads();
-        for (int w = 0; w < kWideWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fminf(tau, s.tau[w]); }
-        double z = 0.0;
-        for (int c = tid; c < a.chunks; c += kWideThreads) z += stats[c].sum * weight(stats[c].top, top, f.t);
+    for (int off = 32; off >= 1; off >>= 1) { top = fmaxf(top, __shfl_xor(top, off)); tau = fminf(tau, __shfl_xor(tau, off)); }
+    if (lane == 0) { s.top[wave] = top; s.tau[wave] = tau; }
+    __syncthreads();
+    for (int w = 0; w < kWideWaves; ++w) { top = fmaxf(top, s.top[w]); tau = fminf(tau, s.tau[w]); }
+    double z = 0.0;
+    for (int c = tid; c < a.chunks; c += kWideThreads) z += stats[c].sum * weight(stats[c].top, top, f.t);
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
-        if (lane == 0) s.z[wave] = z;
+    for (int off = 32; off >= 1; off >>= 1) z += __shfl_xor(z, off);
+    if (lane == 0) s.z[wave] = z;
+    __syncthreads();
+    z = 0.0;
+    for (int w = 0; w < kWideWaves; ++w) z += s.z[w];
+    const void *logits = logit_row<DT>(a, side, row);
+    const int skew = row_skew<DT>(logits);
+    // fixed point: the sum of all weights (at most one each) stays below 2^61
+    const double unit = uniform(exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab))));
+    top = uniform(top);
+    WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
+                     uniform((float)(f.t.scale * (kSteps / 40.0))), {uniform(f.t.scale), uniform(f.t.floor)}, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0}};
+    bool summed = false;
+    u64 z1 = 0;
+    if (f.top_k > 0) {
+        // steps that reach well below the lists' logits, whatever the temperature
+        const float by_weight = r.step_scale;
+        if (top - tau > 0.f && top - tau < INFINITY) r.step_scale = kSteps / (8.f * (top - tau));
+        z1 = r.template cut_at<false>((u64)f.top_k, summed);
+        r.step_scale = by_weight;
+    } else if (f.top_p < 1.0) {
+        z1 = (u64)(z * unit);
+    }
+    if (f.top_p < 1.0) {
+        const float min_w = r.cut.min_w;
+        if (z1 == 0) {
+            r.cut.min_w = 0.f;
+            z1 = r.sum_blocks([&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); });
+            r.cut.min_w = min_w;
+        }
+        r.template cut_at<true>(max((u64)1, (u64)ceil(f.top_p * (double)z1)), summed);
+    }
+    auto amount = [&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); };
+    u64 total;
+    if (summed) {
         __syncthreads();
-        z = 0.0;
-        for (int w = 0; w < kWideWaves; ++w) z += s.z[w];
-        const void *logits = logit_row<DT>(a, side, row);
-        const int skew = row_skew<DT>(logits);
-        // fixed point: the sum of all weights (at most one each) stays below 2^61
-        const double unit = uniform(exp2((double)min(50, z >= 1.0 ? 60 - ilogb(z) : 60 - bits_of((uint32_t)a.vocab))));
-        top = uniform(top);
-        WideRow<DT> r = {s, logits, a.vocab, skew, (a.vocab + skew + WideRow<DT>::kBlock - 1) / WideRow<DT>::kBlock, tid, top,
-                         uniform((float)(f.t.scale * (kSteps / 40.0))), {uniform(f.t.scale), uniform(f.t.floor)}, unit, {0.0, top, (float)f.min_p, 0u, 0x7fffffff, 0}};
-        bool summed = false;
-        u64 z1 = 0;
-        if (f.top_k > 0) {
-            // steps that reach well below the lists' logits, whatever the temperature
-            const float by_weight = r.step_scale;
-            if (top - tau > 0.f && top - tau < INFINITY) r.step_scale = kSteps / (8.f * (top - tau));
-            z1 = r.template cut_at<false>((u64)f.top_k, summed);
-            r.step_scale = by_weight;
-        } else if (f.top_p < 1.0) {
-            z1 = (u64)(z * unit);
-        }
-        if (f.top_p < 1.0) {
-            const float min_w = r.cut.min_w;
-            if (z1 == 0) {
-                r.cut.min_w = 0.f;
-                z1 = r.sum_blocks([&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); });
-                r.cut.min_w = min_w;
-            }
-            r.template cut_at<true>(max((u64)1, (u64)ceil(f.top_p * (double)z1)), summed);
-        }
-        auto amount = [&](float x, int i) __attribute__((always_inline)) { return r.kept_mass(x, i); };
-        u64 total;
-        if (summed) {
-            __syncthreads();
-            u64 part = 0;
-            for (int blk = tid; blk < r.blocks; blk += kWideThreads) part += s.block[blk];
-            total = s.bins.sum_of(tid, part);
-        } else {
-            total = r.sum_blocks(amount);
-        }
-        r.cut.z = (double)total / unit;
-        int token = -1;
+        u64 part = 0;
+        for (int blk = tid; blk < r.blocks; blk += kWideThreads) part += s.block[blk];
+        total = s.bins.sum_of(tid, part);
+    } else {
+        total = r.sum_blocks(amount);
+    }
+    r.cut.z = (double)total / unit;
+    int token = -1;
+    if (DRAW) {
+        const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
+        token = r.find_in_blocks((u64)((double)u * (double)total) + 1, amount);
+    }
+    if (tid == 0) {
         if (DRAW) {
-            const float u = fminf(fmaxf(a.u[row], 0.f), 0x1.fffffep-1f);
-            token = r.find_in_blocks((u64)((double)u * (double)total) + 1, amount);
+            a.tokens[row] = token;
+            if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(r.weight_of(logit<DT>(logits, token)) / r.cut.z);
+        } else {
+            a.cuts[rr] = r.cut;
         }
-        if (tid == 0) {
-            if (DRAW) {
-                a.tokens[row] = token;
-                if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(r.weight_of(logit<DT>(logits, token)) / r.cut.z);
-            } else {
-                a.cuts[rr] = r.cut;
-            }
-        }
-        __syncthreads();
     }
 }
 
@@ -1112,8 +1119,12 @@ static FilterPlan filter_plan(int64_t rows, int vocab)   // rows of all views
     return p;
 }
 
-// Chunks are counted in 32 bits.
-bool filter_fits(int64_t rows, int vocab, int views) { return rows * views * filter_plan(1, vocab).chunks < 0x7fffffff; }
+// A launch counts its threads in 32 bits.
+bool filter_fits(int64_t rows, int vocab, int views)
+{
+    const int64_t all = rows * views;
+    return all * kWideThreads < 0xffffffffll && (all * filter_plan(1, vocab).chunks + 4) * 64 < 0xffffffffll;
+}
 size_t filter_workspace_bytes(int64_t rows, int vocab, int views) { return filter_plan(rows * views, vocab).total; }
 
 // Logits of more than this leave nothing behind in the last-level cache that a later kernel of the call would find.
@@ -1135,7 +1146,7 @@ template <int DT, bool DRAW> static hipError_t launch_filters_of(const FilterArg
     hipLaunchKernelGGL((filter_pick_kernel<DT, true, DRAW>), dim3(a.all_rows), dim3(kPickThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(a.all_rows < a.num_cus ? a.all_rows : a.num_cus), dim3(kWideThreads), 0, stream, a);
+    hipLaunchKernelGGL((filter_wide_kernel<DT, DRAW>), dim3(a.all_rows), dim3(kWideThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -1179,11 +1190,11 @@ hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream)
 constexpr int kDrawThreads = 512, kDrawPiece = 8192;
 
 // Probability that a row's filters leave a token (0: cut, or an empty row).
-__device__ __forceinline__ double kept_prob(const RowCut &c, const Scale &t, float x, int i)
+__device__ __forceinline__ double kept_prob(const RowCut &c, double inv_z, const Scale &t, float x, int i)
 {
     if (!kept(c, x, i)) return 0.0;
     const double d = (double)x - (double)c.top, w = d <= t.floor ? 0.0 : weight(d, t);
-    return w >= (double)c.min_w ? w / c.z : 0.0;
+    return w >= (double)c.min_w ? w * inv_z : 0.0;
 }
 
 struct Candidate {
@@ -1202,7 +1213,7 @@ template <int DT> __device__ __forceinline__ bool keeps_draft(const FilteredArgs
     const float u = a.accept_u[row];
     if (x < 0 || x >= a.c.vocab) return false;
     const float xp = logit<DT>(logit_row<DT>(a.f, 0, row), x), xq = logit<DT>(logit_row<DT>(a.f, 1, row), x);
-    return (double)u * kept_prob(cq, t, xq, x) < kept_prob(cp, t, xp, x);
+    return (double)u * kept_prob(cq, 1.0 / cq.z, t, xq, x) < kept_prob(cp, 1.0 / cp.z, t, xp, x);
 }
 
 // Between two stages: a wave per sequence, the leading drafts of the first `rows` that are kept.
@@ -1239,12 +1250,13 @@ template <int DT> __global__ void __launch_bounds__(kDrawThreads) filtered_draw_
     const void *pr = logit_row<DT>(a.f, 0, row), *qr = logit_row<DT>(a.f, 1, row);
     const RowCut cp = a.f.cuts[row], cq = a.f.cuts[a.f.rows + row];
     const float *gr = a.gumbel + (int64_t)b * V;
+    const double inv_p = 1.0 / cp.z, inv_q = 1.0 / cq.z;
     Candidate more = {-INFINITY, 0x7fffffff}, any = {-INFINITY, 0x7fffffff};  // best among p > q, best of p
     float more_near = -INFINITY, any_near = -INFINITY;   // single precision: the full logarithm only for what comes near the best
     auto visit = [&](float xp, float xq, float g, int i) __attribute__((always_inline)) {
-        const double p = kept_prob(cp, t, xp, i);
+        const double p = kept_prob(cp, inv_p, t, xp, i);
         if (p > 0.0) {
-            const double q = kept_prob(cq, t, xq, i), r = p - q;
+            const double q = kept_prob(cq, inv_q, t, xq, i), r = p - q;
             auto consider = [&](double v, float &near, Candidate &best) __attribute__((always_inline)) {
                 const float f = (float)v, score = __logf(f) + g;
                 if (!(score < near - 0.01f) || f < 1e-30f) {

@@ -111,7 +111,7 @@ struct FilterArgs {
     ChunkStat *stats;        // [view][row][chunk]
     uint2 *lists;            // [view][row][chunk][128]: (logit, index); consensus: then the row's kept tokens, packed
     int32_t *unresolved;     // [0]: count, then rows (view * rows + row)
-    int chunks, num_cus;
+    int chunks;
     // rows of the launch: block rows first_k .. first_k + stage_k - 1 of every sequence (stage_rows a view, all_rows in all); with
     // `decided` [B] only of sequences whose first first_k drafts are kept
     int first_k, stage_k, stage_rows, all_rows;

@@ -42,6 +42,7 @@ def _sample(p=None, ctx=CTX, logits_type=0, stride=0, ws=None, **kw):
     (dict(logits=A + 2), B.ORTHRUS_EINVAL), (dict(logits=A + 1, logits_type=1), B.ORTHRUS_EINVAL),
     (dict(u=A + 2), B.ORTHRUS_EINVAL), (dict(logprobs=A + 1), B.ORTHRUS_EINVAL), (dict(top_k=A + 3), B.ORTHRUS_EINVAL),
     (dict(p=_params(vocab=0)), B.ORTHRUS_EINVAL), (dict(p=_params(vocab=(1 << 20) + 1)), B.ORTHRUS_EUNSUPPORTED),
+    (dict(p=_params(batch=65535, block_k=32, vocab=1 << 20)), B.ORTHRUS_EUNSUPPORTED),   # more than a launch counts
     (dict(p=_params(block_k=33)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(block_k=0)), B.ORTHRUS_EINVAL),
     (dict(p=_params(batch=-1)), B.ORTHRUS_EINVAL), (dict(p=_params(batch=70000)), B.ORTHRUS_EUNSUPPORTED),
     (dict(p=_params(batch=0)), B.ORTHRUS_OK),
