@@ -368,7 +368,7 @@ orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus
  * short, because L < 0 or L + n > max_seq_len, or because L is inside a page that is not mapped; slots at and
  * behind max_tokens (not written); a page id outside [0, num_pages) taken from the ring (slot -1); more pages coming back
  * than the ring has room for (a page mapped twice; the last ones are dropped).  Nothing is written out of bounds.
- * Supported: num_pages * page_size < 2^31.
+ * Supported: num_pages * page_size < 2^31, max_tokens < 2^31.
  */
 int64_t orthrus_page_tables_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_page_tables_update(orthrus_ctx *ctx, const orthrus_params *p, const int32_t *seq_lens,
@@ -432,7 +432,7 @@ orthrus_status orthrus_prefill_attn(orthrus_ctx *ctx, const orthrus_params *p, i
  * of short launches whose arguments do not change from cycle to cycle when the caller reuses its
  * buffers; replaying them as a graph removes the per-launch host cost and most of the gaps between
  * kernels.  Usage: orthrus_graph_begin(ctx, stream); any number of orthrus_dual_view_attn /
- * orthrus_consensus_commit / orthrus_sampling_consensus_commit calls on that same stream (nothing
+ * orthrus_consensus_commit / orthrus_sampling_consensus_commit and other compute calls on that same stream (nothing
  * runs, the launches are recorded; the entry points launch kernels only, so all of them may be
  * recorded); orthrus_graph_end(ctx, stream, &g); then orthrus_graph_launch(g, stream) once per cycle.
  *   - `stream` must be a created stream (not NULL).  The calling thread must not allocate or free

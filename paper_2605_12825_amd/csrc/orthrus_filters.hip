@@ -17,9 +17,9 @@
 //                          the highest of their thresholds (some thousand); what the first cut leaves is ranked in the lanes of a
 //                          wave.  A row without filters: from the chunks' sums, and one chunk read again.  A row whose cut lies
 //                          below the lists goes to the next kernel.  Rows of at most 1792 logits come here at once.  Bound by
-//                          its chain of memory and LDS round trips, 7 to 12 us; 1024 rows 37 us.
+//                          its chain of memory and LDS round trips, 7 to 19 us; 1024 rows 35 us.
 //   filter_wide_kernel     a workgroup to such a row: a histogram pass and a pass that gathers the step of the cut; bound by the
-//                          weights of both passes (256 rows of 151936, nuclei of tens of thousands: 126 us).
+//                          weights of both passes (256 rows of 151936, nuclei of tens of thousands: 128 us).
 //   filtered_stage_kernel  keep decisions between the consensus's two stages.
 //   filtered_draw_kernel   grid (piece, sequence): keep decisions, the replacement drawn from the first rejected row.
 //   filtered_commit_kernel grid (sequence, layer): outputs and the commit, as sample_commit_kernel does it.
