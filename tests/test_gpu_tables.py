@@ -220,3 +220,27 @@ def test_store_with_bad_slots_and_counts():
         np.testing.assert_array_equal(_rt().bits_to_numpy(dkp), kp)
         np.testing.assert_array_equal(_rt().bits_to_numpy(dvp), vp)
     step.close()
+
+
+def test_store_of_no_rows():
+    step = _step(num_q_heads=2, num_kv_heads=2, head_dim=64, num_pages=2)
+    none = torch.empty((1, 0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    pool = torch.full((1, 2, 2, 16, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    step.store_kv(none, none, torch.empty((0,), dtype=torch.int32, device="cuda"), pool, pool)
+    torch.cuda.synchronize()
+    assert step.device_error() == 0 and bool((pool == 3.0).all())
+    step.close()
+
+
+def test_store_to_pages_behind_the_first_2_to_the_31_elements():
+    H, d, P, pages = 16, 128, 16, 70000
+    step = _step(num_q_heads=H, num_kv_heads=H, head_dim=d, page_size=P, num_pages=pages)
+    kp, vp = (torch.empty((pages, H, P, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    slots = np.array([(pages - 1) * P + 15, 65536 * P, 65535 * P + 15, 3], np.int32)
+    k, v = (torch.randn((1, slots.size, H, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    step.store_kv(k, v, _dev(slots), kp, vp)
+    torch.cuda.synchronize()
+    assert step.device_error() == 0
+    for t, s in enumerate(slots.tolist()):
+        assert torch.equal(kp[s // P, :, s % P], k[0, t]) and torch.equal(vp[s // P, :, s % P], v[0, t])
+    step.close()

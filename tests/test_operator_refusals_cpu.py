@@ -103,6 +103,7 @@ def test_page_tables(kw, status):
     (dict(slots=A + 2), B.ORTHRUS_EINVAL), (dict(count=A + 1), B.ORTHRUS_EINVAL), (dict(p=_params(num_layers=0)), B.ORTHRUS_EINVAL),
     (dict(p=_params(num_pages=1 << 27)), B.ORTHRUS_EUNSUPPORTED), (dict(p=_params(head_dim=96)), B.ORTHRUS_EUNSUPPORTED),
     (dict(p=_params(blk_stride_row=100)), B.ORTHRUS_EUNSUPPORTED), (dict(n=0), B.ORTHRUS_OK),
+    (dict(n=0, k=None, v=None, slots=None), B.ORTHRUS_OK), (dict(n=0, kp=None), B.ORTHRUS_EINVAL),
 ])
 def test_kv_store(kw, status):
     a = dict(ctx=CTX, p=_params(), n=5, k=A, v=A, slots=A, count=None, kp=A, vp=A)
