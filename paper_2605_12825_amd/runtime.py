@@ -131,6 +131,9 @@ class DecodeStep:
         ws = getattr(self, name, None)
         if ws is None or ws.numel() < need:
             ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            with torch.cuda.device(self.device):
+                if not torch.cuda.is_current_stream_capturing():   # the call may be on another stream than what used this memory before
+                    torch.cuda.current_stream().synchronize()
             setattr(self, name, ws)
         return ws
 
@@ -145,8 +148,9 @@ class DecodeStep:
 
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, logprobs=None, stream=None,
                       logits_stride_row=0):
-        """One token per logits row [batch, block_k, vocab] (float32, bfloat16 or float16) by each sequence's temperature, top-k, top-p and min-p (each of
-        the last three a [batch] tensor or None) from the uniform numbers u [batch, block_k]."""
+        """One token per logits row [batch, block_k, vocab] (float32, bfloat16 or float16; rows dense or logits_stride_row
+        elements apart) by each sequence's temperature, top-k, top-p and min-p (each of the last three a [batch] tensor or None)
+        from the uniform numbers u [batch, block_k]."""
         ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
         return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits), logits, logits_stride_row, temperature,
                                        top_k, top_p, min_p, u, tokens, logprobs, ws, stream)

@@ -199,6 +199,54 @@ def test_the_same_call_twice_and_rows_alone_or_together():
         assert c[0, 0] == a[i, 3] and lc[0, 0] == la[i, 3]
 
 
+@pytest.mark.parametrize("vocab,dtype,off", [(1 << 20, "f32", 3), (1 << 20, "bf16", 7), (300007, "f16", 1)])
+@pytest.mark.parametrize("kind", ["peaked", "flat"])
+def test_the_largest_vocabularies(vocab, dtype, off, kind):
+    x = torch.from_numpy(_logits(41, len(FILTERS), 1, vocab, kind)).to(TYPES[dtype])
+    u = np.random.default_rng(42).random((len(FILTERS), 1)).astype(np.float32)
+    _check(x, _filters(FILTERS), u, off=off)
+
+
+@pytest.mark.parametrize("batch,vocab", [(65535, 40), (20000, 1801)])
+def test_as_many_sequences_as_a_call_takes(batch, vocab):
+    """Sequence b repeats sequence b mod 52: the oracle answers for those."""
+    few = 52
+    rows = [FILTERS[b % len(FILTERS)] for b in range(few)]
+    x = torch.from_numpy(_logits(43, few, 1, vocab))
+    u = np.random.default_rng(44).random((few, 1)).astype(np.float32)
+    f = _filters(rows)
+    want, _, _ = oracle.sample_tokens(x.numpy(), *f, u)
+    again = np.arange(batch) % few
+    tokens, _ = _sample(x[torch.from_numpy(again)], [v[again] for v in f], u[again])
+    np.testing.assert_array_equal(tokens, want[again])
+    c = _case(45, few, 1, vocab, rows)
+    want = oracle.filtered_consensus_commit(c["ar"].numpy(), c["df"].numpy(), *c["f"], c["draft"], c["u"], c["gumbel"])
+    assert want["margin"] > 1e-8
+    many = {k: c[k][again] for k in ("draft", "u", "gumbel")}
+    many.update(ar=c["ar"][torch.from_numpy(again)], df=c["df"][torch.from_numpy(again)], f=[v[again] for v in c["f"]])
+    got, err = _consensus(many)
+    assert err == 0
+    for k in ("accept_len", "num_committed", "out_tokens", "next_anchor"):
+        np.testing.assert_array_equal(got[k], want[k][again], err_msg=k)
+
+
+def test_rows_farther_apart_than_32_bits_count():
+    B, K, V, stride = 2, 10, 40001, (1 << 27) + 8
+    x = torch.from_numpy(_logits(46, B, K, V)).to(torch.bfloat16)
+    u = np.random.default_rng(47).random((B, K)).astype(np.float32)
+    f = _filters([FILTERS[1], FILTERS[0]])
+    want, _ = _sample(x, f, u)
+    buf = torch.empty((B * K - 1) * stride + V, dtype=torch.bfloat16, device="cuda")
+    for r in range(B * K):
+        buf[r * stride:r * stride + V] = x.view(B * K, V)[r].cuda()
+    step = _step(B, K, V)
+    tokens = torch.full((B, K), -7, dtype=torch.int32, device="cuda")
+    step.sample_tokens(buf, *[_dev(v) for v in f], _dev(u), tokens, None, logits_stride_row=stride)
+    torch.cuda.synchronize()
+    step.close()
+    np.testing.assert_array_equal(tokens.cpu().numpy(), want)
+
+
 # ---- the consensus
 
 def _case(seed, B, K, V, rows, kind="peaked", noise=0.4, dtype="f32"):
@@ -327,6 +375,10 @@ def test_without_filters_the_decisions_are_those_of_the_sampling_consensus():
     step.close()
     for k, v in (("accept_len", acc), ("num_committed", ncm), ("out_tokens", toks), ("next_anchor", anchor)):
         np.testing.assert_array_equal(got[k], v.cpu().numpy(), err_msg=k)
+
+
+def test_consensus_of_the_largest_vocabulary():
+    _check_consensus(_case(48, 4, 2, 1 << 20, [FILTERS[0], FILTERS[1], FILTERS[4], FILTERS[2]]))
 
 
 @pytest.mark.parametrize("K,dtype", [(4, "f32"), (13, "f32"), (32, "bf16")])
