@@ -28,11 +28,13 @@ def bits_to_numpy(t: torch.Tensor) -> np.ndarray:
 _LOGITS_TYPES = {torch.float32: B.ORTHRUS_F32, torch.bfloat16: B.ORTHRUS_BF16, torch.float16: B.ORTHRUS_F16}
 
 
-def _logits_type(*logits) -> int:
-    """The ABI's name of the logits' type; every tensor of a call has the same."""
+def _logits_type(stride_row, *logits) -> int:
+    """The ABI's name of the logits' type; every tensor of a call has the same.  A view of padded rows comes with its stride."""
     t = _LOGITS_TYPES.get(logits[0].dtype)
     if t is None or any(x.dtype != logits[0].dtype for x in logits):
         raise ValueError("logits must be float32, bfloat16 or float16, all of one type")
+    if stride_row == 0 and not all(x.is_contiguous() for x in logits):
+        raise ValueError("logits whose rows are not dense need logits_stride_row")
     return t
 
 
@@ -126,11 +128,11 @@ class DecodeStep:
         return B.orthrus_prefill_attn(self.ctx, self.params, max_new_tokens, q, k_new, v_new, new_lens, k_pool,
                                       v_pool, page_table, seq_lens, out, self.prefill_ws, stream)
 
-    def _workspace(self, name, need):
+    def _workspace(self, name, query):
         """The buffer kept for one kind of call (made on its first use; ahead of a captured sequence by reserve)."""
         ws = getattr(self, name, None)
-        if ws is None or ws.numel() < need:
-            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        if ws is None:
+            ws = torch.empty(max(query(self.params), 256), dtype=torch.uint8, device=self.device)
             with torch.cuda.device(self.device):
                 if not torch.cuda.is_current_stream_capturing():   # the call may be on another stream than what used this memory before
                     torch.cuda.current_stream().synchronize()
@@ -141,27 +143,27 @@ class DecodeStep:
         """Makes the workspaces of sample_tokens and filtered_consensus_commit, or of update_page_tables, ahead of their first
         call: a program that records calls into a graph does this before."""
         if sampling:
-            self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
-            self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes(self.params))
+            self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
+            self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
         if tables:
-            self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes(self.params))
+            self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes)
 
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, logprobs=None, stream=None,
                       logits_stride_row=0):
         """One token per logits row [batch, block_k, vocab] (float32, bfloat16 or float16; rows dense or logits_stride_row
         elements apart) by each sequence's temperature, top-k, top-p and min-p (each of the last three a [batch] tensor or None)
         from the uniform numbers u [batch, block_k]."""
-        ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes(self.params))
-        return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits), logits, logits_stride_row, temperature,
-                                       top_k, top_p, min_p, u, tokens, logprobs, ws, stream)
+        ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
+        return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits_stride_row, logits), logits,
+                                       logits_stride_row, temperature, top_k, top_p, min_p, u, tokens, logprobs, ws, stream)
 
     def filtered_consensus_commit(self, ar_logits, diff_logits, temperature, top_k, top_p, min_p, draft_tokens, accept_u,
                                   gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
                                   num_committed, out_tokens, next_anchor, stream=None, logits_stride_row=0):
         """sampling_consensus_commit where both views' distributions are filtered as in sample_tokens."""
-        ws = self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes(self.params))
-        return B.orthrus_filtered_consensus_commit(self.ctx, self.params, _logits_type(ar_logits, diff_logits), ar_logits,
-                                                   diff_logits, logits_stride_row, temperature, top_k, top_p, min_p,
+        ws = self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
+        return B.orthrus_filtered_consensus_commit(self.ctx, self.params, _logits_type(logits_stride_row, ar_logits, diff_logits),
+                                                   ar_logits, diff_logits, logits_stride_row, temperature, top_k, top_p, min_p,
                                                    draft_tokens, accept_u, gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool,
                                                    page_table, seq_lens, accept_len, num_committed, out_tokens,
                                                    next_anchor, ws, stream)
@@ -170,7 +172,7 @@ class DecodeStep:
                            stream=None):
         """Pages for the sequences that grow by new_lens tokens, pages back from those with new_lens < 0, and the slots of
         the new tokens (packed; slot_map's length is the bound on their number)."""
-        ws = self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes(self.params))
+        ws = self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes)
         return B.orthrus_page_tables_update(self.ctx, self.params, seq_lens, new_lens, page_table, free_pages, free_state,
                                             granted, token_starts, slot_map, 0 if slot_map is None else slot_map.numel(),
                                             ws, stream)

@@ -3,6 +3,7 @@ are checked here with addresses that are never read (a call that were not refuse
 import ctypes
 
 import pytest
+import torch
 
 import paper_2605_12825_amd as orthrus
 from paper_2605_12825_amd import binding as B
@@ -110,6 +111,15 @@ def test_kv_store(kw, status):
     a.update(kw)
     assert orthrus.orthrus_kv_store(a["ctx"], a["p"], a["n"], a["k"], a["v"], a["slots"], a["count"], a["kp"], a["vp"], 0,
                                     check=False) == status
+
+
+def test_logits_tensors():
+    from paper_2605_12825_amd import runtime
+    x = torch.zeros((2, 3, 8))
+    assert runtime._logits_type(0, x) == B.ORTHRUS_F32 and runtime._logits_type(8, x[..., :5].bfloat16(), x.bfloat16()) == B.ORTHRUS_BF16
+    for bad in ((0, x.double()), (0, x, x.half()), (0, x[..., :5]), (0, x, x.transpose(1, 2))):
+        with pytest.raises(ValueError):
+            runtime._logits_type(*bad)
 
 
 def test_workspace_queries():
