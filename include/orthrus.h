@@ -301,7 +301,8 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
  * log-probability 0.  A NaN logit counts as -inf, +inf as the largest float; a row of nothing but -inf has token -1 and
  * log-probability -inf.  u outside [0, 1) counts as the nearest float in it, NaN as 0.
  * The result is a deterministic function of the inputs: sums run over whole numbers (fixed point of 39 bits or more
- * below the largest weight), weights are formed in 64 bits.
+ * below the largest weight; a token that weighs less than half of the last of them is never drawn, also at u = 0), weights are
+ * formed in 64 bits.
  *
  *   logits       [dev] [B, K, V] of logits_type, any alignment of the type's own; row (b, k) starts at element
  *                (b*K + k) * logits_stride_row (0: dense, = V), so that the padding of an output head can stay

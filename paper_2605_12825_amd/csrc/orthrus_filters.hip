@@ -492,7 +492,9 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
                 u64 sum = 0;
 #pragma unroll
                 for (int i = 0; i < kChunksEach; ++i) {
-                    const u64 m = to_fixed(part[i], unit);
+                    // (A chunk none of whose logits has an amount of its own has none, whatever the sum of its weights:
+                    // the chunk that the target falls into always holds a token to draw.)
+                    const u64 m = to_fixed(weight(st[i].top, top, f.t), unit) ? to_fixed(part[i], unit) : 0;
                     s.bins.amount[i * kPickThreads + tid] = m;
                     sum += m;
                 }
@@ -521,7 +523,7 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
                 __syncthreads();
                 atomicMax(&s.count, last);
                 __syncthreads();
-                if (in.bin < 0) {   // the chunk's sum was rounded apart from its parts': its last token that weighs anything
+                if (in.bin < 0) {   // the chunk's sum, rounded once, is more than that of its parts: its last token with an amount
                     token = s.count;
                 } else {
 #pragma unroll

@@ -144,6 +144,34 @@ def test_uniform_numbers_at_and_outside_their_ends():
     _check(x, _filters(FILTERS), np.tile(np.array(us, np.float32), (B, 1)))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("gap,T", [(18.5, 0.3), (22.0, 0.5), (45.0, 1.0)])
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_unfiltered_draws_next_to_chunks_that_weigh_next_to_nothing(dtype, gap, T, off):
+    """Every logit but the planted ones is 40 T to 41 T below the largest (0.2 T more or less for the types' rounding): e^-39.8 < 2^-57,
+    so none has an amount in a fixed point of 50 bits, though 2048 of them together have, e^-41.2 * 2048 > 2^-49.  What is drawn is
+    a planted token, wherever in the row it stands and however small the uniform number."""
+    V, rng = 40001, np.random.default_rng(int(gap) + off)
+    x = (gap - rng.uniform(40, 41, (5, 1, V)) * T).astype(np.float32)
+    x[0, 0, 20007] = gap
+    x[1, 0, :3 * 2048] = -np.inf                     # masked, then next to nothing, then the token
+    x[1, 0, 39000] = gap
+    x[2, 0, [100, 30000]] = gap                      # half of the sum at either, stretches of next to nothing between them
+    x[3, 0, V - 1] = gap
+    x[4, 0, :] = -np.inf
+    x[4, 0, :2048] = gap - 40 * T                    # one stretch of next to nothing, the token at the end of the next
+    x[4, 0, 4000] = gap
+    us = np.array([0.0, -1.0, np.nan, 2.0 ** -149, 2.0 ** -50, 0.25, 0.5, 1.0], np.float32)
+    f = [np.full(5, T, np.float32), None, None, None]
+    t = torch.from_numpy(np.repeat(x, us.size, axis=1)).to(TYPES[dtype])
+    tokens, lp = _sample(t, f, np.tile(us, (5, 1)), off=off)
+    want = np.tile(np.array([20007, 39000, 100, V - 1, 4000], np.int32)[:, None], (1, us.size))
+    want[2, us >= 0.5] = 30000
+    np.testing.assert_array_equal(tokens, want)
+    half = np.log(0.5)
+    assert np.all(np.abs(lp[[0, 1, 3, 4]]) <= 1e-9) and np.all(np.abs(lp[2] - half) <= -half * 2.0 ** -24 + 1e-9)
+
+
 @pytest.mark.parametrize("vocab", [1, 64, 1024, 9001, 65536])
 @pytest.mark.parametrize("value", [0.0, -3.25, np.finfo(np.float32).min, np.inf])
 def test_rows_of_equal_logits(vocab, value):
