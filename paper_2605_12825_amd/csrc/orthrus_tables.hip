@@ -253,8 +253,16 @@ __device__ __forceinline__ bool apply_token(const TablesArgs &a, const Sequence 
         page = s.row[e];
     }
     const bool ok = is_mapped(a, page);   // (the ring may hold anything)
-    if (slot_at < a.max_tokens) a.slot_map[slot_at] = ok ? (page << a.page_shift) + off : -1;
+    a.slot_map[slot_at] = ok ? (page << a.page_shift) + off : -1;
     return ok;
+}
+
+// The entries that a granted sequence without holes lacked: for calls whose tokens do not all have a slot.
+__device__ __forceinline__ void apply_entries(const TablesArgs &a, const Sequence &s, int from, int step)
+{
+    const int last = (s.L + s.n - 1) >> a.page_shift;
+    if (s.need > 0 && !s.holes())
+        for (int e = s.first + from; e <= last; e += step) s.row[e] = a.free_pages[s.place(s.before + (e - s.first))];
 }
 
 __device__ __forceinline__ void return_pages(const TablesArgs &a, const Sequence &s, int from, int step)
@@ -281,8 +289,11 @@ __global__ void __launch_bounds__(256) tables_apply_kernel(const TablesArgs a)
     }
     bool error = false;
     const int step = s.holes() ? 256 : strips * 256;
-    const int64_t start = a.token_starts[b];
-    for (int i = strip * 256 + tid; i < s.n; i += step) error |= !apply_token(a, s, i, start + i);
+    // Tokens behind the last slot are not gone through (there may be 2^31 of them): their entries are, and the scan has
+    // reported them.
+    const int64_t start = a.token_starts[b], slots = min((int64_t)s.n, a.max_tokens - start);
+    if (slots < s.n) apply_entries(a, s, strip * 256 + tid, strips * 256);
+    for (int64_t i = strip * 256 + tid; i < slots; i += step) error |= !apply_token(a, s, (int)i, start + i);
     if (error) atomicExch(a.err_word, -4);
 }
 
@@ -326,7 +337,13 @@ __global__ void __launch_bounds__(kScanThreads) tables_small_kernel(const Tables
     }
     __syncthreads();
     bool error = false;
-    for (int t = tid; t < s_start[a.batch]; t += kScanThreads) {
+    const int tokens = (int)min((int64_t)s_start[a.batch], a.max_tokens);   // (as in tables_apply_kernel)
+    if (tokens < s_start[a.batch])
+        for (int b = wave; b < a.batch; b += kScanThreads / 64) {
+            const Sequence s(a, b);
+            if (s.n > 0) apply_entries(a, s, lane, 64);
+        }
+    for (int t = tid; t < tokens; t += kScanThreads) {
         int b = 0;   // the last sequence that starts at t or before, which is the one that holds it
 #pragma unroll
         for (int half = kSmallBatch / 2; half >= 1; half >>= 1)

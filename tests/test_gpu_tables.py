@@ -147,6 +147,46 @@ def test_pages_come_back_once_too_often():
     _check([48, 48, 0], [-1, -1, 20], table, ring, state, 16, 48, np.full(30, -9, np.int32))
 
 
+def test_as_many_tokens_as_a_length_counts():
+    """2^31 - 4096 tokens of one sequence, of which 5000 have a slot: every entry is mapped, and nothing else is written."""
+    P, N = 4096, (1 << 19) - 1
+    rng = np.random.default_rng(5)
+    ring, head, n = rng.permutation(N).astype(np.int32), 77777, N * 4096
+    step = _step(page_size=P, max_pages_per_seq=N, max_seq_len=n, num_pages=N)
+    slots = np.full(5000 + 64, -9, np.int32)
+    t, r, s, m = _dev(np.full((1, N), -1, np.int32)), _dev(ring), _dev(np.array([head, N], np.int32)), _dev(slots)
+    granted, starts = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    step.update_page_tables(_dev(np.zeros(1, np.int32)), _dev(np.array([n], np.int32)), t, r, s, granted, starts, m[:5000])
+    torch.cuda.synchronize()
+    assert step.device_error() == -4     # slots behind the last one
+    step.close()
+    pages = np.roll(ring, -head)
+    np.testing.assert_array_equal(t.cpu().numpy()[0], pages)
+    np.testing.assert_array_equal(r.cpu().numpy(), ring)
+    i = np.arange(5000)
+    slots[:5000] = pages[i // P] * P + i % P
+    np.testing.assert_array_equal(m.cpu().numpy(), slots)
+    assert granted.tolist() == [n] and starts.tolist() == [0, n] and s.tolist() == [head, 0]
+
+
+def test_more_tokens_together_than_32_bits_count():
+    """Two sequences on the same pages (one's last is still to be mapped), 2^31 - 65536 tokens each, few slots: one launch."""
+    P, N = 65536, 32767
+    n = N * P
+    ring = np.full(N, -1, np.int32)
+    ring[9] = N - 1
+    table = np.tile(np.arange(N, dtype=np.int32), (2, 1))
+    table[0, N - 1], table[1, N - 1] = -1, 5
+    step = _step(batch=2, page_size=P, max_pages_per_seq=N, max_seq_len=n, num_pages=N)
+    (granted, starts, t, r, s, m), err = _update(step, np.zeros(2, np.int32), np.full(2, n, np.int32), table, ring,
+                                                 np.array([9, 1], np.int32), np.full(100, -9, np.int32))
+    step.close()
+    table[0, N - 1] = N - 1
+    np.testing.assert_array_equal(t, table)
+    np.testing.assert_array_equal(m, np.arange(100))
+    assert err == -4 and granted.tolist() == [n, n] and starts.tolist() == [0, n, 2 ** 31 - 1] and s.tolist() == [10, 0]
+
+
 def test_steps_in_a_row_keep_every_page():
     rng = np.random.default_rng(6)
     B, width, P, N = 24, 20, 16, 300
