@@ -392,6 +392,7 @@ orthrus_status orthrus_page_tables_update(orthrus_ctx *ctx, const orthrus_params
  *   k_pool, v_pool [dev] bf16, updated in place, strides in params
  * Device-side error: a slot at or behind num_pages * P is not written and sets the context's error word
  * (ORTHRUS_ECAPACITY).  Rows are copied bit for bit.
+ * Supported: num_pages * page_size < 2^31, num_layers < 65536, N / max(1, floor(8192 / (H_kv * d))) below 2^24.
  */
 orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32_t num_rows, const void *k_new,
                                 const void *v_new, const int32_t *slot_map, const int32_t *num_valid, void *k_pool,

@@ -860,6 +860,7 @@ orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32
     if (num_rows < 0 || p->num_layers <= 0 || !k_pool || !v_pool) return ORTHRUS_EINVAL;
     if (num_rows > 0 && (!k_new || !v_new || !slot_map)) return ORTHRUS_EINVAL;   // (arrays of nothing may have no address)
     if (p->num_layers > 65535 || p->num_pages > 0x7fffffff / p->page_size) return ORTHRUS_EUNSUPPORTED;
+    if (!orthrus::kv_store_fits(num_rows, p->num_kv_heads, p->head_dim)) return ORTHRUS_EUNSUPPORTED;
     if (((uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) return ORTHRUS_EINVAL;
     if (((uintptr_t)slot_map | (uintptr_t)num_valid) & 3) return ORTHRUS_EINVAL;
     if (num_rows == 0) return ORTHRUS_OK;

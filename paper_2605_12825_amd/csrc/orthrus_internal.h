@@ -285,6 +285,7 @@ hipError_t launch_sample_tokens(FilterArgs a, hipStream_t stream);
 int draw_pieces(int vocab);
 hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream);
 hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream);
+bool kv_store_fits(int rows, int num_kv_heads, int head_dim);
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
 int consensus_chunk_elems();
 int draw_chunk_elems();

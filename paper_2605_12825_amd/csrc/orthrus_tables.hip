@@ -422,10 +422,22 @@ __global__ void __launch_bounds__(256) kv_store_kernel(const StoreArgs a, int ro
     if (error) atomicExch(a.err_word, -4);
 }
 
+static int store_rows_per_wg(int num_kv_heads, int head_dim)
+{
+    const int per_tok = num_kv_heads * (head_dim / 8);
+    return per_tok >= kStoreChunks ? 1 : kStoreChunks / per_tok;
+}
+
+// A launch counts its threads in 32 bits.
+bool kv_store_fits(int rows, int num_kv_heads, int head_dim)
+{
+    const int rows_per_wg = store_rows_per_wg(num_kv_heads, head_dim);
+    return ((int64_t)rows + rows_per_wg - 1) / rows_per_wg * 256 < 0xffffffffll;
+}
+
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream)
 {
-    const int per_tok = a.num_kv_heads * (a.head_dim / 8);
-    const int rows_per_wg = per_tok >= kStoreChunks ? 1 : kStoreChunks / per_tok;
+    const int rows_per_wg = store_rows_per_wg(a.num_kv_heads, a.head_dim);
     const dim3 grid((unsigned)(((int64_t)a.rows + rows_per_wg - 1) / rows_per_wg), (unsigned)a.num_layers);
     hipLaunchKernelGGL(kv_store_kernel, grid, dim3(256), 0, stream, a, rows_per_wg);
     return hipGetLastError();

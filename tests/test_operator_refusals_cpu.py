@@ -113,6 +113,14 @@ def test_kv_store(kw, status):
                                     check=False) == status
 
 
+def test_kv_store_of_more_rows_than_a_launch_counts():
+    """A workgroup of 256 threads to a row of 8192 elements and more, 32 bits for the threads of a launch."""
+    def store(n, heads):
+        return orthrus.orthrus_kv_store(CTX, _params(num_q_heads=heads, num_kv_heads=heads), n, A, A, A, None, A, A, 0, check=False)
+    assert store(1 << 24, 64) == store(2 ** 31 - 1, 64) == store(2 ** 31 - 1, 1000) == store(2 ** 31 - 1, 8) == B.ORTHRUS_EUNSUPPORTED
+    # (what is not refused gets as far as the launch, which finds no device here)
+
+
 def test_logits_tensors():
     from paper_2605_12825_amd import runtime
     x = torch.zeros((2, 3, 8))
