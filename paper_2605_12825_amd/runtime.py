@@ -242,17 +242,19 @@ class DecodeStack:
         self.out_diff, self.out_ar = torch.zeros(qs, **i16), torch.zeros(qs, **i16)
         self.ar_logits = torch.zeros((batch, block_k, vocab), dtype=torch.float32, device=dev)
         self.draft_tokens = torch.zeros((batch, block_k), dtype=torch.int32, device=dev)
-        if self.temperature > 0:
+        self.filters = bool(filters)
+        if self.temperature > 0 and not self.filters:
             self.diff_logits = torch.zeros_like(self.ar_logits)
             self.accept_u = torch.zeros((batch, block_k), dtype=torch.float32, device=dev)
             self.gumbel = torch.zeros((batch, vocab), dtype=torch.float32, device=dev)
         i32 = dict(dtype=torch.int32, device=dev)
         # filters: every request samples by its own `temperatures`, `top_k`, `top_p` and `min_p`; the cycle draws the drafts
-        # itself, from `diff_logits` by `draft_u`, and verifies them under the same filters
-        self.filters = bool(filters)
+        # itself, from `diff_logits` by `draft_u`, and verifies them under the same filters.  `temperatures` start at
+        # `temperature`, at 1 where none is given.
         if self.filters:
             f32 = dict(dtype=torch.float32, device=dev)
-            self.temperatures, self.top_p = torch.ones((batch,), **f32), torch.ones((batch,), **f32)
+            self.temperatures = torch.full((batch,), self.temperature if self.temperature > 0 else 1.0, **f32)
+            self.top_p = torch.ones((batch,), **f32)
             self.top_k, self.min_p = torch.zeros((batch,), **i32), torch.zeros((batch,), **f32)
             self.diff_logits = torch.zeros_like(self.ar_logits)
             self.draft_u, self.accept_u = torch.zeros((batch, block_k), **f32), torch.zeros((batch, block_k), **f32)

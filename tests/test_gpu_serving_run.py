@@ -123,6 +123,20 @@ def test_cycles_that_map_their_pages_and_draw_their_drafts_eager_and_replayed():
     graph.close()
 
 
+def _small_stack(**kw):
+    pool = torch.zeros((1, 2, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+    return _rt().DecodeStack(num_layers=1, batch=3, num_q_heads=1, num_kv_heads=1, head_dim=64, block_k=2, page_size=16,
+                             k_pool=pool, v_pool=pool.clone(), page_table=torch.zeros((3, 1), dtype=torch.int32, device="cuda"),
+                             seq_lens=torch.zeros(3, dtype=torch.int32, device="cuda"), max_seq_len=16, vocab=40, **kw)
+
+
+@pytest.mark.parametrize("kw,want", [({}, 1.0), (dict(temperature=0.75), 0.75)])
+def test_a_stack_with_filters_starts_at_its_temperature(kw, want):
+    s = _small_stack(filters=True, **kw)
+    assert s.temperatures.tolist() == [want] * 3
+    s.close()
+
+
 @pytest.mark.parametrize("replays", [3])
 def test_a_captured_draw_replays_like_the_eager_one(replays):
     """Rows of every kind (listed, wide, plain, empty) in one captured call, new inputs before each replay, eager work between."""
