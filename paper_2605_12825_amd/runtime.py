@@ -261,8 +261,12 @@ class DecodeStack:
             self.draft_logprobs = torch.zeros((batch, block_k), **f32)
             self.gumbel = torch.zeros((batch, vocab), **f32)
             self.step.reserve(sampling=True)
-        # a ring of free pages: the cycle first maps pages for `grow` tokens more per request (block_k each; a request that
-        # is over gets -1 there and its pages come back)
+        # a ring of free pages: the cycle first maps pages for `grow` tokens more per request, block_k each.  A request that
+        # is not granted them (`granted` is 0) sets the error word (ORTHRUS_ECAPACITY) as every page that is missing does; it is
+        # decoded all the same, and where its kept rows do not fit into the pages that it has, none is committed (`num_committed`
+        # is 0) and it goes on in a later cycle.  end() takes the pages of requests that are over between two cycles, without an error.  -1 in `grow` takes
+        # them within one: put the length to 0 before it (the cycle decodes all slots, and tokens behind cleared entries are read
+        # from page 0), and note that the commit finds no page for that slot and reports it.
         self.free_pages, self.free_state = free_pages, free_state
         if free_pages is not None:
             if free_pages.numel() != pages or free_state is None:
@@ -305,6 +309,20 @@ class DecodeStack:
             s.consensus_commit(self.ar_logits, self.draft_tokens, self.k_blk_ar, self.v_blk_ar, self.k_pool,
                                self.v_pool, self.page_table, self.seq_lens, self.accept_len, self.num_committed,
                                self.out_tokens, self.next_anchor, stream)
+
+    def end(self, ended) -> None:
+        """Requests that are over, between two cycles: the pages of those that `ended` ([batch], bool) marks go back to the ring,
+        their lengths to 0.  Runs on the current stream; `granted` and `token_starts` are afterwards those of this call.
+
+        With `grow` left at block_k the slots stay in the cycles, each with a block's pages, until the next requests take them;
+        put their lengths to 0 before every cycle, or what they commit lets them grow.
+        """
+        if self.free_pages is None:
+            raise ValueError("end() is for stacks with free_pages")
+        new_lens = ended.to(torch.int32).neg_()
+        self.step.update_page_tables(self.seq_lens, new_lens, self.page_table, self.free_pages, self.free_state, self.granted,
+                                     self.token_starts, self.slot_map)
+        self.seq_lens.masked_fill_(ended, 0)
 
     def capture(self) -> None:
         """Records one cycle into a HIP graph (on a stream of its own, default priority)."""

@@ -123,6 +123,47 @@ def test_cycles_that_map_their_pages_and_draw_their_drafts_eager_and_replayed():
     graph.close()
 
 
+def test_requests_that_end_between_cycles_report_no_error():
+    """Their pages are in the ring for the cycle that follows, their slots idle at length 0 or take the next request."""
+    rt = _rt()
+    st = _state(2)
+    ref = {k: v.copy() for k, v in st.items()}
+    eager, graph = _stack(st), _stack(st)
+    graph.capture()
+    f = [np.array([r[i] for r in FILTERS], t) for i, t in enumerate((np.float32, np.int32, np.float32, np.float32))]
+    for c, over in enumerate([[], [3], [0, 3, 4], [3]]):
+        x = _inputs(c + 10)
+        mask = np.isin(np.arange(B), over)
+        starts = granted = None
+        for new in (np.where(mask, -1, 0), x["grow"]):
+            slots = np.full(B * K, -9, np.int32)
+            granted, starts, status = oracle.page_tables_update(ref["lens"], new, ref["table"], ref["ring"], ref["state"], P,
+                                                                ref["table"].shape[1] * P, B * K, slots)
+            assert status == 0
+            ref["lens"][mask] = 0
+        drafts, _, _ = oracle.sample_tokens(x["diff_logits"], *f, x["draft_u"])
+        want = oracle.filtered_consensus_commit(x["ar_logits"], x["diff_logits"], *f, drafts, x["accept_u"], x["gumbel"],
+                                                x["k_blk_ar"], x["v_blk_ar"], ref["kp"], ref["vp"], ref["table"], ref["lens"])
+        assert want["status"] == 0 and want["margin"] > 1e-8
+        for s, run in ((eager, eager.cycle), (graph, graph.replay)):
+            for k, v in x.items():
+                getattr(s, k).copy_(rt.to_device_bits(v))
+            s.slot_map.fill_(-9)
+            s.end(torch.from_numpy(mask).cuda())
+            torch.cuda.synchronize()
+            assert (s.seq_lens.cpu().numpy()[mask] == 0).all() and (s.page_table.cpu().numpy()[mask] == -1).all()
+            run()
+            torch.cuda.synchronize()
+            assert s.step.device_error() == 0
+            g = lambda n: rt.bits_to_numpy(getattr(s, n))  # noqa: E731
+            for n, w in (("granted", granted), ("token_starts", starts), ("page_table", ref["table"]), ("free_pages", ref["ring"]),
+                         ("free_state", ref["state"]), ("slot_map", slots), ("seq_lens", ref["lens"]), ("k_pool", ref["kp"]),
+                         ("v_pool", ref["vp"]), ("num_committed", want["num_committed"]), ("out_tokens", want["out_tokens"])):
+                np.testing.assert_array_equal(g(n), w, err_msg="%s cycle %d" % (n, c))
+    eager.close()
+    graph.close()
+
+
 def _small_stack(**kw):
     pool = torch.zeros((1, 2, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
     return _rt().DecodeStack(num_layers=1, batch=3, num_q_heads=1, num_kv_heads=1, head_dim=64, block_k=2, page_size=16,
@@ -134,6 +175,8 @@ def _small_stack(**kw):
 def test_a_stack_with_filters_starts_at_its_temperature(kw, want):
     s = _small_stack(filters=True, **kw)
     assert s.temperatures.tolist() == [want] * 3
+    with pytest.raises(ValueError):
+        s.end(torch.zeros(3, dtype=torch.bool, device="cuda"))     # no pages of its own
     s.close()
 
 
