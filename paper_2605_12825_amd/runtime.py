@@ -30,12 +30,38 @@ _LOGITS_TYPES = {torch.float32: B.ORTHRUS_F32, torch.bfloat16: B.ORTHRUS_BF16, t
 
 def _logits_type(stride_row, *logits) -> int:
     """The ABI's name of the logits' type; every tensor of a call has the same.  A view of padded rows comes with its stride."""
-    t = _LOGITS_TYPES.get(logits[0].dtype)
-    if t is None or any(x.dtype != logits[0].dtype for x in logits):
-        raise ValueError("logits must be float32, bfloat16 or float16, all of one type")
-    if stride_row == 0 and not all(x.is_contiguous() for x in logits):
-        raise ValueError("logits whose rows are not dense need logits_stride_row")
+    dtype = logits[0].dtype
+    t = _LOGITS_TYPES.get(dtype)
+    for x in logits:
+        if t is None or x.dtype is not dtype:
+            raise ValueError("logits must be float32, bfloat16 or float16, all of one type")
+        if stride_row == 0 and not x.is_contiguous():
+            raise ValueError("logits whose rows are not dense need logits_stride_row")
     return t
+
+
+_F32, _I32 = torch.float32, torch.int32
+
+
+def _check_operands(*operands) -> None:
+    """(name, tensor, type, elements): what is of another type (torch makes whole numbers 64 bits wide), too short, or a column of
+    something larger would be read as what it is not.  None and addresses stand for themselves."""
+    for name, t, dtype, count in operands:
+        if t is not None and t.__class__ is not int and (t.dtype is not dtype or t.numel() < count or not t.is_contiguous()):
+            raise ValueError("%s must hold %d dense elements of %s, not %s of %s with strides %s"
+                             % (name, count, dtype, tuple(t.shape), t.dtype, t.stride()))
+
+
+def _check_filters(batch, temperature, top_k, top_p, min_p) -> None:
+    # (The smallest calls take as long as the host needs for them, and the types say all there is to say of one element: 0.5 us, the
+    # whole check 1.5.)
+    if batch == 1 and (temperature is None or temperature.__class__ is int or temperature.dtype is _F32) and \
+            (top_k is None or top_k.__class__ is int or top_k.dtype is _I32) and \
+            (top_p is None or top_p.__class__ is int or top_p.dtype is _F32) and \
+            (min_p is None or min_p.__class__ is int or min_p.dtype is _F32):
+        return
+    _check_operands(("temperature", temperature, _F32, batch), ("top_k", top_k, _I32, batch), ("top_p", top_p, _F32, batch),
+                    ("min_p", min_p, _F32, batch))
 
 
 class DecodeStep:
@@ -153,6 +179,7 @@ class DecodeStep:
         """One token per logits row [batch, block_k, vocab] (float32, bfloat16 or float16; rows dense or logits_stride_row
         elements apart) by each sequence's temperature, top-k, top-p and min-p (each of the last three a [batch] tensor or None)
         from the uniform numbers u [batch, block_k]."""
+        _check_filters(self.params.batch, temperature, top_k, top_p, min_p)
         ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
         return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits_stride_row, logits), logits,
                                        logits_stride_row, temperature, top_k, top_p, min_p, u, tokens, logprobs, ws, stream)
@@ -161,6 +188,7 @@ class DecodeStep:
                                   gumbel, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
                                   num_committed, out_tokens, next_anchor, stream=None, logits_stride_row=0):
         """sampling_consensus_commit where both views' distributions are filtered as in sample_tokens."""
+        _check_filters(self.params.batch, temperature, top_k, top_p, min_p)
         ws = self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
         return B.orthrus_filtered_consensus_commit(self.ctx, self.params, _logits_type(logits_stride_row, ar_logits, diff_logits),
                                                    ar_logits, diff_logits, logits_stride_row, temperature, top_k, top_p, min_p,
@@ -172,6 +200,10 @@ class DecodeStep:
                            stream=None):
         """Pages for the sequences that grow by new_lens tokens, pages back from those with new_lens < 0, and the slots of
         the new tokens (packed; slot_map's length is the bound on their number)."""
+        # (what a program makes anew for every step, and the ring, whose length it does not pass)
+        if new_lens is not None and new_lens.__class__ is not int and new_lens.dtype is not _I32 or \
+                free_pages is not None and free_pages.__class__ is not int and free_pages.numel() < self.params.num_pages:
+            _check_operands(("new_lens", new_lens, _I32, self.params.batch), ("free_pages", free_pages, _I32, self.params.num_pages))
         ws = self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes)
         return B.orthrus_page_tables_update(self.ctx, self.params, seq_lens, new_lens, page_table, free_pages, free_state,
                                             granted, token_starts, slot_map, 0 if slot_map is None else slot_map.numel(),

@@ -130,6 +130,36 @@ def test_logits_tensors():
             runtime._logits_type(*bad)
 
 
+def test_filter_tensors():
+    from paper_2605_12825_amd import runtime
+    for n in (1, 2):
+        t, k = torch.zeros(n), torch.zeros(n, dtype=torch.int32)
+        runtime._check_filters(n, t, k, t, t)
+        runtime._check_filters(n, t, None, None, None)
+        runtime._check_filters(n, A, A, A, A)
+        runtime._check_filters(n, None, k, t, t)       # (refused by the library)
+        bad = [(t, k.long(), t, t), (t.double(), k, t, t), (t, k, t.half(), t), (t, k, t, k), (k, k, t, t), (t, t, t, t)]
+        if n == 2:
+            bad += [(t[:1], k, t, t), (t, k[:1], t, t), (t, k, torch.zeros(2, 4)[:, 0], t), (t, k, t, t[:1].expand(2))]
+        for f in bad:
+            with pytest.raises(ValueError):
+                runtime._check_filters(n, *f)
+
+
+def test_page_table_tensors():
+    from paper_2605_12825_amd import runtime
+    step = object.__new__(runtime.DecodeStep)
+    step.params, step.ctx, step.tables_ws = _params(), CTX, _Space(8)     # (a workspace that is too small: nothing is launched)
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    good = [i32(3), i32(3), i32(3, 9), i32(50), i32(2), i32(3), i32(4), i32(10)]
+    with pytest.raises(orthrus.OrthrusError):
+        step.update_page_tables(*good, stream=0)
+    for i, x in ((1, good[1].long()), (1, good[1].float()), (3, good[3][1:])):
+        with pytest.raises(ValueError):
+            step.update_page_tables(*good[:i], x, *good[i + 1:], stream=0)
+    step.ctx = None
+
+
 def test_workspace_queries():
     for f in (orthrus.orthrus_sample_workspace_bytes, orthrus.orthrus_filtered_workspace_bytes):
         assert f(_params()) >= 0 and f(_params(batch=0)) >= 0
