@@ -5,6 +5,7 @@ computation happens inside liborthrus.so.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional
 
 import numpy as np
@@ -85,6 +86,11 @@ class DecodeStep:
                                     max_pages_per_seq=max_pages_per_seq, max_seq_len=max_seq_len,
                                     num_pages=num_pages, num_splits=num_splits, num_layers=num_layers,
                                     vocab=vocab, sm_scale=sm_scale, **kw)
+        # store_kv: how rows lie that the parameters describe; for the last number of them, their strides and elements
+        p = self.params
+        self._row_strides = (p.blk_stride_row or num_kv_heads * head_dim, p.blk_stride_head or head_dim, 1)
+        self._row_elements = num_layers * num_kv_heads * head_dim
+        self._layout = (-1, None, 0)
         self.ctx = B.orthrus_create(device)
         # plans and sizes for the device the context lives on
         self.num_splits = B.orthrus_attn_num_splits_on(self.ctx, self.params)
@@ -210,9 +216,43 @@ class DecodeStep:
                                             ws, stream)
 
     def store_kv(self, k_new, v_new, slot_map, k_pool, v_pool, num_valid=None, stream=None):
-        """Copies packed K/V rows [num_layers, N, H_kv, d] (N = slot_map's length) to their slots in every layer's cache."""
-        return B.orthrus_kv_store(self.ctx, self.params, slot_map.numel(), k_new, v_new, slot_map, num_valid, k_pool,
-                                  v_pool, stream)
+        """Copies packed K/V rows [num_layers, N, H_kv, d] (N = slot_map's length) to their slots in every layer's cache.  The rows
+        are read where k_new and v_new have them (views of a fused projection's output, say), laid out alike; given as
+        addresses, by the step's block strides."""
+        rows = slot_map.numel()
+        if k_new.__class__ is int:
+            return B.orthrus_kv_store(self.ctx, self.params, rows, k_new, v_new, slot_map, num_valid, k_pool, v_pool, stream)
+        p = self.params
+        known, strides, elements = self._layout
+        if known != rows:
+            strides, elements = (p.blk_stride_layer or rows * self._row_strides[0],) + self._row_strides, rows * self._row_elements
+            self._layout = (rows, strides, elements)
+        if k_new.stride() != strides or v_new.stride() != strides or k_new.numel() != elements or v_new.numel() != elements or \
+                k_new.element_size() != 2:
+            p = self._params_for_rows(k_new, v_new, rows)
+        # (straight to the library: a call of few rows takes as long as the host needs for it)
+        st = B._lib.orthrus_kv_store(self.ctx, ctypes.byref(p), rows, k_new.data_ptr(), v_new.data_ptr(), slot_map.data_ptr(),
+                                     B._ptr(num_valid), B._ptr(k_pool), B._ptr(v_pool), B._stream_handle(stream))
+        if st != B.ORTHRUS_OK:
+            raise B.OrthrusError(st, "orthrus_kv_store")
+        return st
+
+    def _params_for_rows(self, k_new, v_new, rows):
+        """The step's parameters with the strides of these rows."""
+        p, shape = self.params, (self.params.num_layers, rows, self.params.num_kv_heads, self.params.head_dim)
+        if k_new.shape != shape or v_new.shape != shape or k_new.element_size() != 2 or v_new.element_size() != 2:
+            raise ValueError("k_new and v_new must be [num_layers, slots, H_kv, d] = %s of 16 bits, not %s and %s of %s"
+                             % (shape, tuple(k_new.shape), tuple(v_new.shape), k_new.dtype))
+        strides = [0, 0, 0, 0]   # (0 is the library's word for dense; the stride of an axis of one element means nothing)
+        if rows > 0:
+            for i, (n, s, t) in enumerate(zip(shape, k_new.stride(), v_new.stride())):
+                if n > 1 and (s != t or s == 0 or i == 3 and s != 1):
+                    raise ValueError("k_new and v_new must be laid out alike, rows of dense elements, none of them twice: strides %s and %s"
+                                     % (k_new.stride(), v_new.stride()))
+                strides[i] = s if n > 1 else 0
+        q = B.orthrus_params.from_buffer_copy(p)
+        q.blk_stride_layer, q.blk_stride_row, q.blk_stride_head = strides[:3]
+        return q
 
     def attn_timing(self, enable: bool) -> None:
         """Attach HIP events to the attention kernels of the following attn() calls (or stop doing so)."""

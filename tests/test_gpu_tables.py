@@ -244,6 +244,34 @@ def test_store(layers, N, H, d, P, fused):
     step.close()
 
 
+@pytest.mark.parametrize("layers,N,H", [(1, 40, 2), (3, 40, 2), (2, 1, 2), (2, 40, 1), (1, 7, 1)])
+@pytest.mark.parametrize("step_strides", [False, True])
+def test_store_reads_rows_where_the_tensors_have_them(layers, N, H, step_strides):
+    """A step whose block lies in a fused projection stores dense rows, one of dense blocks the rows of such a projection, and
+    either takes rows in another order of axes: whatever number they have."""
+    d, P, pages = 64, 16, 6
+    rng = np.random.default_rng(N + H + layers)
+    bits = lambda *s: rng.integers(0, 1 << 16, s, dtype=np.uint16)  # noqa: E731
+    kp, vp = bits(layers, pages, H, P, d), bits(layers, pages, H, P, d)
+    slots = rng.permutation(pages * P)[:N].astype(np.int32)
+    D = _rt().to_device_bits
+    row = (4 + 2 * H) * d
+    kw = dict(block_strides=(row, d, row, d, 5 * row)) if step_strides else {}
+    step = _step(num_q_heads=H, num_kv_heads=H, head_dim=d, num_pages=pages, num_layers=layers, block_k=5,
+                 pool_strides=(pages * H * P * d, H * P * d, P * d, d), **kw)
+    dkp, dvp = D(kp), D(vp)
+    x, y, z = bits(layers, N, 4 + 2 * H, d), bits(2, layers, N, H, d), bits(N, 2, H, layers, d)
+    dx, dy, dz = D(x), D(y), D(z)
+    for (k, v), (dk, dv) in (((x[:, :, 4:4 + H], x[:, :, 4 + H:]), (dx[:, :, 4:4 + H], dx[:, :, 4 + H:])), (y, dy),
+                             ([z[:, i].transpose(2, 0, 1, 3) for i in (0, 1)], [dz[:, i].permute(2, 0, 1, 3) for i in (0, 1)])):
+        step.store_kv(dk, dv, _dev(slots), dkp, dvp)
+        torch.cuda.synchronize()
+        assert oracle.kv_store(k, v, slots, kp, vp) == 0 == step.device_error()
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dkp), kp)
+        np.testing.assert_array_equal(_rt().bits_to_numpy(dvp), vp)
+    step.close()
+
+
 def test_store_with_bad_slots_and_counts():
     H, d, P, pages, N = 2, 64, 16, 4, 9
     rng = np.random.default_rng(9)

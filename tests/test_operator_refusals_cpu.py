@@ -160,6 +160,30 @@ def test_page_table_tensors():
     step.ctx = None
 
 
+@pytest.mark.parametrize("explicit", [False, True])
+def test_rows_of_a_store(explicit):
+    from paper_2605_12825_amd import runtime
+    step = object.__new__(runtime.DecodeStep)
+    step.ctx = None
+    step.params = _params(num_layers=2, **(dict(blk_stride_row=20 * 128, blk_stride_head=128, blk_stride_layer=7 * 20 * 128) if explicit else {}))
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    x, k = z(2, 30, 20, 128), z(2, 30, 2, 128)
+    p = step._params_for_rows(x[:, :, :2], x[:, :, 2:4], 30)
+    assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (30 * 20 * 128, 20 * 128, 128)
+    p = step._params_for_rows(k, k, 30)
+    assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (30 * 256, 256, 128) and p.num_pages == 50
+    p = step._params_for_rows(z(2, 1, 2, 128), x[:, :1, :2].contiguous(), 1)
+    assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (256, 0, 128)
+    p = step._params_for_rows(z(2, 0, 2, 128), z(2, 0, 2, 128), 0)
+    assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (0, 0, 0)
+    wide = z(2, 30, 2, 256)[..., ::2]
+    for a, b, n in ((k, k, 31), (k[:, :29], k, 30), (k, k[:1], 30), (k[0], k[0], 30), (k.float(), k.float(), 30), (k, k.float(), 30),
+                    (k, x[:, :, :2], 30), (wide, wide, 30), (k[:1].expand(2, -1, -1, -1), k, 30), (k.transpose(1, 2), k.transpose(1, 2), 30),
+                    (k[:, :1].expand(-1, 30, -1, -1),) * 2 + (30,)):
+        with pytest.raises(ValueError):
+            step._params_for_rows(a, b, n)
+
+
 def test_workspace_queries():
     for f in (orthrus.orthrus_sample_workspace_bytes, orthrus.orthrus_filtered_workspace_bytes):
         assert f(_params()) >= 0 and f(_params(batch=0)) >= 0
