@@ -727,7 +727,8 @@ template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPi
                         }
                         total = s.bins.sum_of(tid, sum);
                         cut.z = (double)total / kUnit;
-                        cut.key = cut_fall == 0xffffffffu ? 0u : top_key - cut_fall;
+                        // (no cut among the listed ones, of which top-k may keep all: nothing below them is kept)
+                        cut.key = cut_fall != 0xffffffffu ? top_key - cut_fall : whole ? 0u : order_key(tau + 0.f);
                         cut.tie = cut_tie;
                         if constexpr (DRAW) {
                             token = (int)search_entries(s.bins, tid, kPickThreads, n, index_bits, (u64)((double)u * (double)total) + 1,

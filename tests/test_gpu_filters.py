@@ -345,6 +345,27 @@ def test_consensus_of_half_types(dtype, K):
     _check_consensus(_case(K, len(FILTERS), K, 2003, FILTERS, dtype=dtype), stride=2008)
 
 
+@pytest.mark.parametrize("vocab", [4526, 9001, 40001, 151936])
+def test_consensus_where_top_k_is_all_that_stands_above_a_level(vocab):
+    """Eight rows of logits in steps and, for every level with 65 to 1790 logits at and above it, a sequence whose top-k is that number:
+    whatever level a row's lists go down to, one sequence keeps exactly what they hold.  Its draft, a token below, is never kept."""
+    rng = np.random.default_rng(vocab)
+    rows, top_k, draft = [], [], []
+    for row in np.floor(rng.exponential(size=(8, vocab)) * 4).astype(np.float32):
+        counts = [(t, int((row >= t).sum())) for t in range(1, int(row.max()))]
+        for t, n in counts:
+            if 65 <= n <= 1790:
+                rows.append(row)
+                top_k.append(n)
+                draft.append(np.flatnonzero(row == t - 1)[0])
+    B = len(rows)
+    ar = torch.from_numpy(np.stack(rows)[:, None])
+    c = dict(ar=ar, df=ar, f=[np.full(B, 20.0, np.float32), np.array(top_k, np.int32), None, None], draft=np.array(draft, np.int32)[:, None],
+             u=np.full((B, 1), 0.25, np.float32), gumbel=rng.gumbel(size=(B, vocab)).astype(np.float32))
+    got = _check_consensus(c)
+    assert B >= 80 and (got["accept_len"] == 0).all()
+
+
 def test_consensus_of_equal_views_keeps_every_draft():
     c = _case(41, len(FILTERS), 6, 3000, FILTERS, noise=0.0)
     got = _check_consensus(c)
