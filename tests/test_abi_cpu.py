@@ -123,6 +123,33 @@ def test_consensus_workspaces_do_not_grow(batch, K, vocab, greedy, sampling):
     assert orthrus.orthrus_sampling_workspace_bytes(p) == sampling
 
 
+@pytest.mark.parametrize("batch,K,vocab,sample,filtered", [
+    (1, 1, 1, 0, 768), (3, 4, 1792, 0, 1280), (3, 4, 1793, 13056, 26880), (1, 16, 128256, 1056768, 2114816),
+    (64, 16, 151936, 80490752, 161076480), (2, 3, 1 << 20, 3226112, 6458880), (0, 1, 5000, 256, 256)])
+def test_filter_workspaces_do_not_grow(batch, K, vocab, sample, filtered):
+    """As many bytes as these: per row (consensus: and view) and 2048 logits 24 bytes and a list of 128 pairs, a number per row; nothing
+    of these up to 1792 logits.  The consensus adds 32 bytes per row and view, two words per sequence, 24 bytes per sequence
+    and 8192 logits.  Each part padded to 256 bytes."""
+    p = _good()
+    p.batch, p.block_k, p.vocab = batch, K, vocab
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    rows, chunks = batch * K, (vocab + 7 + 2047) // 2048
+
+    def plan(n):
+        return up(n * chunks * 24) + up(n * chunks * 1024) + up((n + 1) * 4) if vocab > 1792 else 0
+    assert orthrus.orthrus_sample_workspace_bytes(p) == plan(rows) == sample
+    whole = up(2 * rows * 32) + up(batch * 8) + up(batch * ((vocab + 8191) // 8192) * 24) + plan(2 * rows)
+    assert orthrus.orthrus_filtered_workspace_bytes(p) == whole == filtered
+
+
+@pytest.mark.parametrize("batch,want", [(0, 256), (1, 256), (20, 256), (21, 512), (4096, 49408)])
+def test_page_table_workspace_does_not_grow(batch, want):
+    """Three words per sequence, two for the ring."""
+    p = _good()
+    p.batch = batch
+    assert orthrus.orthrus_page_tables_workspace_bytes(p) == ((3 * batch + 2) * 4 + 255) // 256 * 256 == want
+
+
 @pytest.mark.parametrize("batch,q_heads,kv_heads,d,K,max_seq_len,splits,workspace", [
     (1, 32, 8, 128, 16, 4112, 13, 3461120), (1, 32, 8, 128, 16, 8000, 21, 5591040), (1, 32, 8, 128, 1, 2000, 11, 1464320),
     (1, 32, 8, 128, 32, 40000, 30, 15974400), (4, 32, 8, 128, 16, 32768, 8, 8519680), (4, 32, 8, 128, 8, 1000, 4, 2129920),

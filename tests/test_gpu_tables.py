@@ -208,6 +208,31 @@ def test_steps_in_a_row_keep_every_page():
         assert (table[b, :(L + P - 1) // P] >= 0).all()
 
 
+def test_steps_in_a_row_report_what_the_oracle_does():
+    """Fifty steps on the same tables, a ring that is short now and then, every result and the error word of each step."""
+    rng = np.random.default_rng(8)
+    B, width, P, N = 24, 20, 16, 60
+    step = _step(batch=B, max_pages_per_seq=width, max_seq_len=width * P, num_pages=N)
+    table, ring, state = np.full((B, width), -1, np.int32), rng.permutation(N).astype(np.int32), np.array([41, N], np.int32)
+    t, r, s, lens = _dev(table), _dev(ring), _dev(state), np.zeros(B, np.int32)
+    granted, starts = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    statuses = []
+    for _ in range(50):
+        new = np.where(rng.random(B) < 0.1, -1, rng.integers(0, 20, B)).astype(np.int32)
+        slots = np.full(800, -9, np.int32)
+        m = _dev(slots)
+        step.update_page_tables(_dev(lens), _dev(new), t, r, s, granted, starts, m)
+        torch.cuda.synchronize()
+        want = oracle.page_tables_update(lens, new, table, ring, state, P, width * P, 800, slots)
+        for got, w in ((granted, want[0]), (starts, want[1]), (t, table), (r, ring), (s, state), (m, slots)):
+            np.testing.assert_array_equal(got.cpu().numpy(), w)
+        assert step.device_error() == want[2]
+        statuses.append(want[2])
+        lens = np.where(new < 0, 0, lens + want[0]).astype(np.int32)
+    assert set(statuses) == {0, -4}
+    step.close()
+
+
 # ---- the store
 
 @pytest.mark.parametrize("layers,N,H,d,P", [(1, 1, 8, 128, 16), (3, 37, 2, 64, 16), (2, 700, 4, 128, 32), (1, 3001, 1, 64, 64),
