@@ -300,9 +300,10 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
  * kept weights; its log-probability is ln(w_v / that sum).  T_b <= 0 or NaN: the largest logit (smallest index on ties),
  * log-probability 0.  A NaN logit counts as -inf, +inf as the largest float; a row of nothing but -inf has token -1 and
  * log-probability -inf.  u outside [0, 1) counts as the nearest float in it, NaN as 0.
- * The result is a deterministic function of the inputs: sums run over whole numbers (fixed point of 39 bits or more
- * below the largest weight; a token that weighs less than half of the last of them is never drawn, also at u = 0), weights are
- * formed in 64 bits.
+ * The result is a deterministic function of the inputs and the rows' alignment to 16 bytes: running sums are of whole numbers
+ * (fixed point of 39 bits or more below the largest weight; a token that weighs less than half of the last of them is never
+ * drawn, also at u = 0), weights and the sums of whole rows are formed in 64 bits.  A copy of a row at another alignment can differ
+ * in the last bits of such a sum.
  *
  *   logits       [dev] [B, K, V] of logits_type, any alignment of the type's own; row (b, k) starts at element
  *                (b*K + k) * logits_stride_row (0: dense, = V), so that the padding of an output head can stay
@@ -312,7 +313,8 @@ orthrus_status orthrus_sampling_consensus_commit(orthrus_ctx *ctx, const orthrus
  *   tokens       [dev] int32 [B, K]        written
  *   logprobs     [dev] fp32 [B, K] or NULL written if given
  *   p            batch, block_k and vocab are used
- *   workspace/workspace_bytes: at least orthrus_sample_workspace_bytes(p)
+ *   workspace/workspace_bytes: at least orthrus_sample_workspace_bytes(p): none for V <= 1792, else about 1 KB per row and 2048
+ *                logits (80 MB for 64 x 16 rows of 151936).  Calls that overlap in time need a workspace each.
  * Supported: V <= 1048576, B * K * ceil(V / 2048) below 3 * 10^7.
  */
 int64_t orthrus_sample_workspace_bytes(const orthrus_params *p);
@@ -333,8 +335,9 @@ orthrus_status orthrus_sample_tokens(orthrus_ctx *ctx, const orthrus_params *p, 
  *   ar_logits, diff_logits [dev] [B, K, V] of logits_type, both with logits_stride_row as in orthrus_sample_tokens
  *   temperature, top_k, top_p, min_p as in orthrus_sample_tokens, applied to both views
  *   remaining arguments as in orthrus_sampling_consensus_commit
- *   workspace/workspace_bytes: at least orthrus_filtered_workspace_bytes(p)
- * Probabilities are formed in 64 bits.  Supported as in orthrus_sample_tokens.
+ *   workspace/workspace_bytes: at least orthrus_filtered_workspace_bytes(p): of both views' rows as in orthrus_sample_tokens, and
+ *                32 bytes for each (161 MB for 64 x 16 rows of 151936)
+ * Probabilities are formed in 64 bits; a weight below 2^-1000 of the largest counts as none.  Supported as in orthrus_sample_tokens.
  */
 int64_t orthrus_filtered_workspace_bytes(const orthrus_params *p);
 orthrus_status orthrus_filtered_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,

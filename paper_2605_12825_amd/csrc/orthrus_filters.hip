@@ -4,10 +4,12 @@
 // With M the row's maximum and w_v = exp((x_v - M) / T), the filters cut the tokens ordered by (logit falling, index
 // rising): the first top_k; of those the shortest prefix that holds top_p of their weight; of those the ones with
 // w >= min_p.  The token is the first one in index order at which the running sum of the kept weights exceeds u times
-// their sum.  Every step is "find where a running sum over an order crosses a target".  The sums are whole numbers (weights
+// their sum.  Every step is "find where a running sum over an order crosses a target".  Running sums are of whole numbers (weights
 // in fixed point, scaled so that the row's sum fills 61 bits), so they do not depend on the order in which they are taken;
 // the weights are taken in 64 bits, because a token next to a cut or to the uniform number is decided by the last bits
-// of a sum over the vocabulary: with a sum good to 1e-7 one row in a few thousand would draw another token.
+// of a sum over the vocabulary: with a sum good to 1e-7 one row in a few thousand would draw another token.  The sum of a whole row
+// that the scan leaves (top-p's target, an unfiltered row's chunks) is one of 64-bit floats over chunks that begin at 16-byte
+// boundaries: always the same for a row, but a copy of it at another alignment may differ in the last bits.
 //
 //   filter_scan_kernel     a wave to a chunk of 2048 logits, the one pass over them: the chunk's maximum, the sum of its weights
 //                          and a list of its largest logits, some thirty.  Bound by the vector unit where weights are summed
@@ -19,7 +21,7 @@
 //                          below the lists goes to the next kernel.  Rows of at most 1792 logits come here at once.  Bound by
 //                          its chain of memory and LDS round trips, 7 to 19 us; 1024 rows 35 us.
 //   filter_wide_kernel     a workgroup to such a row: a histogram pass and a pass that gathers the step of the cut; bound by the
-//                          weights of both passes (256 rows of 151936, nuclei of tens of thousands: 128 us).
+//                          weights of both passes (256 rows of 151936, nuclei of tens of thousands: 124 us).
 //   filtered_stage_kernel  keep decisions between the consensus's two stages.
 //   filtered_draw_kernel   grid (piece, sequence): keep decisions, the replacement drawn from the first rejected row.
 //   filtered_commit_kernel grid (sequence, layer): outputs and the commit, as sample_commit_kernel does it.
@@ -370,7 +372,10 @@ template <int DT, bool NT> __global__ void __launch_bounds__(kScanThreads) filte
 // ---- cuts and token from the lists
 
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
-constexpr int kPickEntries = 1792;   // logits of a row's lists that are looked at
+// Logits of a row's lists that are looked at, and of a row that has no scan: as many as leave room for four workgroups (all the waves
+// a CU holds) in its LDS.  A row of 1792: 7.3 us in this one launch, 14.7 with a scan; 1024 such rows 23.6 and 50.8.  With room for
+// 3584 (two workgroups) 1024 rows of 1792 take 28.1, 256 rows of 151936 113.2 instead of 112.6; with room for 1024 those take 119.
+constexpr int kPickEntries = 1792;
 constexpr int kMaxChunks = 1024, kChunksEach = kMaxChunks / kPickThreads;
 
 __device__ __forceinline__ float key_logit(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
@@ -421,6 +426,8 @@ struct PickShared {
     int rank[kFew];
     int count, few_count;
 };
+
+static_assert(sizeof(PickShared) <= 160 * 1024 / 4, "four workgroups to a CU");
 
 // SCANNED: the row's chunks have been listed; else it has at most kPickEntries logits and is read here.
 template <int DT, bool SCANNED, bool DRAW> __global__ void __launch_bounds__(kPickThreads, 4) filter_pick_kernel(const FilterArgs a)

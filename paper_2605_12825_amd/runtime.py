@@ -173,7 +173,8 @@ class DecodeStep:
 
     def reserve(self, sampling=False, tables=False) -> None:
         """Makes the workspaces of sample_tokens and filtered_consensus_commit, or of update_page_tables, ahead of their first
-        call: a program that records calls into a graph does this before."""
+        call: a program that records calls into a graph does this before.  Calls that overlap in time, in replays of two graphs as on
+        two streams, need a step each."""
         if sampling:
             self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
             self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
@@ -336,9 +337,9 @@ class DecodeStack:
         # a ring of free pages: the cycle first maps pages for `grow` tokens more per request, block_k each.  A request that
         # is not granted them (`granted` is 0) sets the error word (ORTHRUS_ECAPACITY) as every page that is missing does; it is
         # decoded all the same, and where its kept rows do not fit into the pages that it has, none is committed (`num_committed`
-        # is 0) and it goes on in a later cycle.  end() takes the pages of requests that are over between two cycles, without an error.  -1 in `grow` takes
-        # them within one: put the length to 0 before it (the cycle decodes all slots, and tokens behind cleared entries are read
-        # from page 0), and note that the commit finds no page for that slot and reports it.
+        # is 0) and it goes on in a later cycle.  end() takes the pages of requests that are over between two cycles, without an
+        # error.  -1 in `grow` takes them within one: put the length to 0 before it (the cycle decodes all slots, and tokens
+        # behind cleared entries are read from page 0), and note that the commit finds no page for that slot and reports it.
         self.free_pages, self.free_state = free_pages, free_state
         if free_pages is not None:
             if free_pages.numel() != pages or free_state is None:
