@@ -86,7 +86,7 @@ class DecodeStep:
                                     max_pages_per_seq=max_pages_per_seq, max_seq_len=max_seq_len,
                                     num_pages=num_pages, num_splits=num_splits, num_layers=num_layers,
                                     vocab=vocab, sm_scale=sm_scale, **kw)
-        # store_kv: how rows lie that the parameters describe; for the last number of them, their strides and elements
+        # store_kv: how rows lie that the parameters describe; for the last number of them, their strides and bytes
         p = self.params
         self._row_strides = (p.blk_stride_row or num_kv_heads * head_dim, p.blk_stride_head or head_dim, 1)
         self._row_elements = num_layers * num_kv_heads * head_dim
@@ -221,15 +221,16 @@ class DecodeStep:
         are read where k_new and v_new have them (views of a fused projection's output, say), laid out alike; given as
         addresses, by the step's block strides."""
         rows = slot_map.numel()
+        if slot_map.dtype is not _I32:   # (64-bit slots would be read as twice as many, every other one slot 0)
+            raise ValueError("slot_map must be of torch.int32, not %s" % slot_map.dtype)
         if k_new.__class__ is int:
             return B.orthrus_kv_store(self.ctx, self.params, rows, k_new, v_new, slot_map, num_valid, k_pool, v_pool, stream)
         p = self.params
-        known, strides, elements = self._layout
+        known, strides, size = self._layout
         if known != rows:
-            strides, elements = (p.blk_stride_layer or rows * self._row_strides[0],) + self._row_strides, rows * self._row_elements
-            self._layout = (rows, strides, elements)
-        if k_new.stride() != strides or v_new.stride() != strides or k_new.numel() != elements or v_new.numel() != elements or \
-                k_new.element_size() != 2:
+            strides, size = (p.blk_stride_layer or rows * self._row_strides[0],) + self._row_strides, 2 * rows * self._row_elements
+            self._layout = (rows, strides, size)
+        if k_new.stride() != strides or v_new.stride() != strides or k_new.nbytes != size or v_new.nbytes != size:
             p = self._params_for_rows(k_new, v_new, rows)
         # (straight to the library: a call of few rows takes as long as the host needs for it)
         st = B._lib.orthrus_kv_store(self.ctx, ctypes.byref(p), rows, k_new.data_ptr(), v_new.data_ptr(), slot_map.data_ptr(),

@@ -176,6 +176,8 @@ def test_rows_of_a_store(explicit):
     assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (256, 0, 128)
     p = step._params_for_rows(z(2, 0, 2, 128), z(2, 0, 2, 128), 0)
     assert (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head) == (0, 0, 0)
+    with pytest.raises(ValueError):
+        step.store_kv(k, k, torch.zeros(30, dtype=torch.int64), A, A)
     wide = z(2, 30, 2, 256)[..., ::2]
     for a, b, n in ((k, k, 31), (k[:, :29], k, 30), (k, k[:1], 30), (k[0], k[0], 30), (k.float(), k.float(), 30), (k, k.float(), 30),
                     (k, x[:, :, :2], 30), (wide, wide, 30), (k[:1].expand(2, -1, -1, -1), k, 30), (k.transpose(1, 2), k.transpose(1, 2), 30),
