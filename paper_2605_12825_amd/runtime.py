@@ -53,6 +53,11 @@ def _check_operands(*operands) -> None:
                              % (name, count, dtype, tuple(t.shape), t.dtype, t.stride()))
 
 
+def _check_type(name, t, dtype) -> None:
+    if t is not None and t.__class__ is not int and t.dtype is not dtype:
+        raise ValueError("%s must be of %s, not %s" % (name, dtype, t.dtype))
+
+
 def _check_filters(batch, temperature, top_k, top_p, min_p) -> None:
     # (The smallest calls take as long as the host needs for them, and the types say all there is to say of one element: 0.5 us, the
     # whole check 1.5.)
@@ -187,6 +192,8 @@ class DecodeStep:
         elements apart) by each sequence's temperature, top-k, top-p and min-p (each of the last three a [batch] tensor or None)
         from the uniform numbers u [batch, block_k]."""
         _check_filters(self.params.batch, temperature, top_k, top_p, min_p)
+        _check_type("u", u, _F32)
+        _check_type("tokens", tokens, _I32)
         ws = self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
         return B.orthrus_sample_tokens(self.ctx, self.params, _logits_type(logits_stride_row, logits), logits,
                                        logits_stride_row, temperature, top_k, top_p, min_p, u, tokens, logprobs, ws, stream)
@@ -196,6 +203,10 @@ class DecodeStep:
                                   num_committed, out_tokens, next_anchor, stream=None, logits_stride_row=0):
         """sampling_consensus_commit where both views' distributions are filtered as in sample_tokens."""
         _check_filters(self.params.batch, temperature, top_k, top_p, min_p)
+        _check_type("draft_tokens", draft_tokens, _I32)
+        _check_type("accept_u", accept_u, _F32)
+        _check_type("gumbel", gumbel, _F32)
+        _check_type("out_tokens", out_tokens, _I32)
         ws = self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
         return B.orthrus_filtered_consensus_commit(self.ctx, self.params, _logits_type(logits_stride_row, ar_logits, diff_logits),
                                                    ar_logits, diff_logits, logits_stride_row, temperature, top_k, top_p, min_p,
@@ -222,19 +233,21 @@ class DecodeStep:
         addresses, by the step's block strides."""
         rows = slot_map.numel()
         if slot_map.dtype is not _I32:   # (64-bit slots would be read as twice as many, every other one slot 0)
-            raise ValueError("slot_map must be of torch.int32, not %s" % slot_map.dtype)
-        if k_new.__class__ is int:
-            return B.orthrus_kv_store(self.ctx, self.params, rows, k_new, v_new, slot_map, num_valid, k_pool, v_pool, stream)
+            _check_type("slot_map", slot_map, _I32)
         p = self.params
-        known, strides, size = self._layout
-        if known != rows:
-            strides, size = (p.blk_stride_layer or rows * self._row_strides[0],) + self._row_strides, 2 * rows * self._row_elements
-            self._layout = (rows, strides, size)
-        if k_new.stride() != strides or v_new.stride() != strides or k_new.nbytes != size or v_new.nbytes != size:
-            p = self._params_for_rows(k_new, v_new, rows)
-        # (straight to the library: a call of few rows takes as long as the host needs for it)
-        st = B._lib.orthrus_kv_store(self.ctx, ctypes.byref(p), rows, k_new.data_ptr(), v_new.data_ptr(), slot_map.data_ptr(),
-                                     B._ptr(num_valid), B._ptr(k_pool), B._ptr(v_pool), B._stream_handle(stream))
+        if k_new.__class__ is not int and v_new.__class__ is not int:
+            known, strides, size = self._layout
+            if known != rows:
+                strides, size = (p.blk_stride_layer or rows * self._row_strides[0],) + self._row_strides, 2 * rows * self._row_elements
+                self._layout = (rows, strides, size)
+            if k_new.stride() != strides or v_new.stride() != strides or k_new.nbytes != size or v_new.nbytes != size:
+                p = self._params_for_rows(k_new, v_new, rows)
+        try:   # straight to the library: a call of few rows takes as long as the host needs for it
+            st = B._lib.orthrus_kv_store(self.ctx, ctypes.byref(p), rows, k_new.data_ptr(), v_new.data_ptr(), slot_map.data_ptr(),
+                                         None if num_valid is None else num_valid.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                         B._stream_handle(stream))
+        except AttributeError:   # (addresses among the operands)
+            return B.orthrus_kv_store(self.ctx, p, rows, k_new, v_new, slot_map, num_valid, k_pool, v_pool, stream)
         if st != B.ORTHRUS_OK:
             raise B.OrthrusError(st, "orthrus_kv_store")
         return st

@@ -315,6 +315,25 @@ def test_store_with_bad_slots_and_counts():
     step.close()
 
 
+@pytest.mark.parametrize("named", [(), (0, 1), (2, 3), (4,), (0, 1, 2, 3, 4), (1, 3)])
+def test_store_of_operands_by_address(named):
+    H, d, P, pages, N = 2, 64, 16, 3, 20
+    rng = np.random.default_rng(12)
+    bits = lambda *s: rng.integers(0, 1 << 16, s, dtype=np.uint16)  # noqa: E731
+    kp, vp, k, v = bits(1, pages, H, P, d), bits(1, pages, H, P, d), bits(1, N, H, d), bits(1, N, H, d)
+    slots = rng.permutation(pages * P)[:N].astype(np.int32)
+    D = _rt().to_device_bits
+    step = _step(num_q_heads=H, num_kv_heads=H, head_dim=d, num_pages=pages)
+    t = [D(k), D(v), D(kp), D(vp), _dev(np.array([N - 3], np.int32))]
+    a = [x.data_ptr() if i in named else x for i, x in enumerate(t)]
+    step.store_kv(a[0], a[1], _dev(slots), a[2], a[3], a[4])
+    torch.cuda.synchronize()
+    assert oracle.kv_store(k, v, slots, kp, vp, N - 3) == 0 == step.device_error()
+    np.testing.assert_array_equal(_rt().bits_to_numpy(t[2]), kp)
+    np.testing.assert_array_equal(_rt().bits_to_numpy(t[3]), vp)
+    step.close()
+
+
 def test_store_of_no_rows():
     step = _step(num_q_heads=2, num_kv_heads=2, head_dim=64, num_pages=2)
     none = torch.empty((1, 0, 2, 64), dtype=torch.bfloat16, device="cuda")

@@ -146,6 +146,25 @@ def test_filter_tensors():
                 runtime._check_filters(n, *f)
 
 
+def test_tokens_and_random_numbers_of_another_type():
+    from paper_2605_12825_amd import runtime
+    step = object.__new__(runtime.DecodeStep)
+    step.params, step.ctx, step.sample_ws, step.filtered_ws = _params(batch=1), CTX, _Space(8), _Space(8)   # (too small: nothing is launched)
+    x, t, u, i = torch.zeros(1, 4, 1000), torch.zeros(1), torch.zeros(1, 4), torch.zeros(1, 4, dtype=torch.int32)
+    n, gumbel = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1000)
+    verify = [i, u, gumbel] + [None] * 6 + [n, n, i, n]
+    step.params.vocab = 5000
+    for f, args, names in ((step.sample_tokens, [u, i], (0, 1)), (step.filtered_consensus_commit, verify, (0, 1, 2, 11))):
+        logits = [x] if f == step.sample_tokens else [x, x]
+        with pytest.raises(orthrus.OrthrusError):
+            f(*logits, t, None, None, None, *args, stream=0)
+        for k in names:
+            for bad in (args[k].double(), args[k].long()):
+                with pytest.raises(ValueError):
+                    f(*logits, t, None, None, None, *args[:k], bad, *args[k + 1:], stream=0)
+    step.ctx = None
+
+
 def test_page_table_tensors():
     from paper_2605_12825_amd import runtime
     step = object.__new__(runtime.DecodeStep)
