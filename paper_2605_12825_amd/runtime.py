@@ -406,6 +406,8 @@ class DecodeStack:
         """
         if self.free_pages is None:
             raise ValueError("end() is for stacks with free_pages")
+        if ended.dtype is not torch.bool or ended.shape != self.seq_lens.shape:
+            raise ValueError("ended must be [batch] of torch.bool, not %s of %s" % (tuple(ended.shape), ended.dtype))
         new_lens = ended.to(torch.int32).neg_()
         self.step.update_page_tables(self.seq_lens, new_lens, self.page_table, self.free_pages, self.free_state, self.granted,
                                      self.token_starts, self.slot_map)

@@ -160,6 +160,9 @@ def test_requests_that_end_between_cycles_report_no_error():
                          ("free_state", ref["state"]), ("slot_map", slots), ("seq_lens", ref["lens"]), ("k_pool", ref["kp"]),
                          ("v_pool", ref["vp"]), ("num_committed", want["num_committed"]), ("out_tokens", want["out_tokens"])):
                 np.testing.assert_array_equal(g(n), w, err_msg="%s cycle %d" % (n, c))
+    for bad in (mask.astype(np.int32), mask[:B - 1], mask[None]):
+        with pytest.raises(ValueError):
+            eager.end(torch.from_numpy(bad).cuda())
     eager.close()
     graph.close()
 
