@@ -8,7 +8,8 @@ A case is a dict of plain values.  `kind` names the operator:
   walk     from the root down to the child that holds the node's greedy token; the path's K/V rows enter the cache
   logits   repetition, presence and frequency penalties by a request's history and a node's path, biases, allowed tokens
 
-A tree is given by parents[b][i]: the node that node i follows, -1 for the root (node 0, the anchor) and for unused nodes.
+A tree is given by parents[b][i]: the node that node i follows, -1 for the root (node 0, the anchor) and for unused nodes, which
+see and follow the root alone.
 `own` false: `run` computes in elementary torch operations; true: it calls the framework.  The consensus changes lengths:
 it gets those of before the call back first, so that every pass is the same one.
 """
@@ -321,13 +322,14 @@ def run(s):
 
 
 def _ancestors(parents):
-    """[B, N, N]: whether node j is on the path from the root to node i, i itself included."""
+    """[B, N, N]: whether node j is on the path from the root to node i, i itself included; for unused nodes the root alone."""
     B, N = parents.shape
     i = torch.arange(N, device=parents.device)
     up = parents.long()
     up = torch.where((up >= 0) & (up < i[None]), up, -1)
     step = (up[:, :, None] == i) | (i[:, None] == i)
-    return torch.linalg.matrix_power(step.double(), max(N - 1, 1)) > 0
+    on = torch.linalg.matrix_power(step.double(), max(N - 1, 1)) > 0
+    return torch.where(on[:, :, :1], on, i == 0)
 
 
 def _plain_attn(s, c):
@@ -363,7 +365,7 @@ def _plain_walk(s, c):
     right[:, 0] = True
     on = _ancestors(s["parents"])
     level = on.sum(2) - 1
-    kept = ~(on & ~right[:, None, :]).any(2) & on[:, :, 0] & (level < c["depth"])
+    kept = ~(on & ~right[:, None, :]).any(2) & on[:, i, i] & (level < c["depth"])
     m = kept.sum(1)
     at = torch.where(kept, level, N)
     put = lambda x: torch.full((B, N + 1), -1, dtype=torch.long, device=DEV).scatter_(1, at, x)[:, :N]  # noqa: E731
@@ -427,11 +429,11 @@ def exact(case, seed):
 
 
 def _path(up, i):
-    """The nodes from the root, or from an unused node, down to i."""
+    """The nodes from the root down to i; of an unused node the root."""
     path = [i]
     while 0 <= up[path[-1]] < path[-1]:
         path.append(int(up[path[-1]]))
-    return path[::-1]
+    return path[::-1] if path[-1] == 0 else [0]
 
 
 def _exact_attn(c, h):
