@@ -402,6 +402,108 @@ orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32
                                 void *v_pool, void *stream);
 
 /*
+ * Attention of a tree of drafted tokens over the shared cache: the verification pass where a position has several drafts.  Node 0
+ * is the anchor (the root); parents[b][i] is the node that node i follows, an earlier one.  A parent outside [0, i) is none, and
+ * nodes that do not come from the root are unused (the padding of a sequence with fewer of them, -1, say).  With A(i) the nodes
+ * from the root down to node i, both included, and the root alone for an unused node:
+ *   out[b][i][h] = Softmax(q[b][i][h] [K_cache || K_A(i)]^T * sm_scale) [V_cache || V_A(i)]
+ * K/V rows of unused nodes are not read.  (A value of a used node that is not finite reaches the rows of all nodes.)
+ * A chain (parents[b][i] = i - 1) is the AR view of orthrus_dual_view_attn.  A node's position in the text is that of the anchor
+ * plus its depth; positions are the caller's (queries and keys come post-RoPE).
+ *
+ *   num_nodes    [host] N, 1 <= N <= 64; the block size of this call (block_k of the params is not used)
+ *   parents      [dev] int32 [B, N]
+ *   q            [dev] bf16 [B, N, H_q, d]; k_blk, v_blk [dev] bf16 [B, N, H_kv, d] (dense, or strided as in orthrus_dual_view_attn,
+ *                row (b, i) being row b*N + i); out [dev] bf16 [B, N, H_q, d]; lse [dev] fp32 [B, H_q, N] or NULL
+ *   remaining arguments, num_splits (also ORTHRUS_SPLITS_BALANCED), arithmetic and device-side errors as in orthrus_dual_view_attn;
+ *   its per-kernel timing does not cover this call
+ *   workspace/workspace_bytes: at least orthrus_tree_attn_workspace_bytes(ctx, p, num_nodes); ctx NULL: for the full 256-CU part
+ * Supported: (num_q_heads / num_kv_heads) * N <= 512.
+ */
+int64_t orthrus_tree_attn_workspace_bytes(const orthrus_ctx *ctx, const orthrus_params *p, int32_t num_nodes);
+orthrus_status orthrus_tree_attn(orthrus_ctx *ctx, const orthrus_params *p, int32_t num_nodes, const int32_t *parents,
+                                 const void *q, const void *k_blk, const void *v_blk, const void *k_pool, const void *v_pool,
+                                 const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+/*
+ * Greedy consensus of a tree of drafts and commit: orthrus_consensus_commit with several drafts for a position.  The path starts
+ * at node 0; at each of its nodes the token is the row's largest logit (smallest index on ties, NaN ranks above all numbers), and
+ * it goes on to the child that holds this token (parents[b][i] = the node, node_tokens[b][i] = the token; of several the lowest i).
+ * It ends where no child does, or after max_path nodes.  With m nodes on the path and L = seq_lens[b] on entry:
+ *   accept_len[b] = m - 1 (drafts kept), num_committed[b] = m; path_nodes[b][0..m-1] = the nodes, -1 behind them;
+ *   out_tokens[b][0..m-1] = the tokens (the kept drafts, then the correction), -1 behind them; next_anchor[b] = the last of them;
+ *   the path's rows of k_blk_ar / v_blk_ar go to token positions L..L+m-1 of every layer's pool; seq_lens[b] = L + m.
+ *
+ *   num_nodes    [host] N, 1 <= N <= 64; max_path [host] >= 1 (more than N counts as N): where the depth of the trees is known, it
+ *                bounds the number of launches
+ *   parents      [dev] int32 [B, N] as in orthrus_tree_attn (unused nodes are on no path); node_tokens [dev] int32 [B, N]: the token
+ *                of every node (that of node 0 is not looked at); a value outside [0, V) never matches
+ *   ar_logits    [dev] [B, N, V] of logits_type, with logits_stride_row as in orthrus_sample_tokens; row i follows node i
+ *   k_blk_ar, v_blk_ar [dev] bf16 [num_layers, B, N, H_kv, d] (dense, or strided by blk_stride_*), or both NULL: consensus only
+ *   accept_len, num_committed, next_anchor [dev] int32 [B]; path_nodes, out_tokens [dev] int32 [B, N], neither of them parents or
+ *                node_tokens (nor parts of them)
+ *   k_pool, v_pool, page_table, seq_lens and the capacity error as in orthrus_consensus_commit
+ *   workspace/workspace_bytes: at least orthrus_tree_consensus_workspace_bytes(p, num_nodes)
+ * Supported: V <= 1048576.  Results are exact.
+ */
+int64_t orthrus_tree_consensus_workspace_bytes(const orthrus_params *p, int32_t num_nodes);
+orthrus_status orthrus_tree_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,
+                                             const void *ar_logits, int64_t logits_stride_row, int32_t num_nodes, int32_t max_path,
+                                             const int32_t *parents, const int32_t *node_tokens, const void *k_blk_ar,
+                                             const void *v_blk_ar, void *k_pool, void *v_pool, const int32_t *page_table,
+                                             int32_t *seq_lens, int32_t *accept_len, int32_t *num_committed, int32_t *path_nodes,
+                                             int32_t *out_tokens, int32_t *next_anchor, void *workspace, size_t workspace_bytes,
+                                             void *stream);
+
+/*
+ * The rules that requests bring along for their tokens.  Every pointer is [dev]; a rule whose pointers are NULL is off.
+ */
+typedef struct {
+    const int32_t *history;      /* [B, history_stride]: the tokens before the anchor, prompt first; values outside [0, V) count for nothing */
+    const int32_t *history_lens; /* [B]: tokens in it, clamped to [0, history_stride] */
+    const int32_t *prompt_lens;  /* [B] or NULL (0): how many of them the request has not written itself, clamped to [0, history_lens] */
+    int64_t history_stride;      /* [host] elements between sequences */
+    const float *repetition;     /* [B] or NULL: off at 1, and where it is not a positive number */
+    const float *presence;       /* [B] or NULL: off at 0, and where it is no finite number */
+    const float *frequency;      /* [B] or NULL: likewise */
+    const int32_t *bias_starts;  /* [B + 1] or NULL: entries bias_starts[b] .. bias_starts[b+1]-1 are sequence b's, those outside [0, num_biases) none's */
+    const int32_t *bias_tokens;  /* [num_biases]; of entries with the same token the last one counts, a token outside [0, V) for nothing */
+    const float *bias_values;    /* [num_biases] */
+    int64_t num_biases;          /* [host] */
+    const uint32_t *masks;       /* [num_masks, mask_stride]: bit v % 32 of word v / 32 is set where token v is allowed */
+    const int32_t *mask_rows;    /* [B, num_rows]: the row's mask; outside [0, num_masks): every token is allowed */
+    int64_t num_masks;           /* [host] */
+    int64_t mask_stride;         /* [host] words between masks, 0: ceil(V / 32) */
+} orthrus_logit_rules;
+
+/*
+ * Puts logits through their requests' rules: what orthrus_sample_tokens or a consensus then takes tokens from.  For row r of
+ * sequence b and token v, with n the number of times v stands in history[b] behind the prompt and on the row's path, and "seen"
+ * where n > 0 or v stands in the prompt:
+ *   x = logits[b][r][v];   x = seen ? (x > 0 ? x / repetition[b] : x * repetition[b]) : x
+ *   x = x - frequency[b] * n - (n > 0 ? presence[b] : 0);   x = x + bias;   out[b][r][v] = allowed ? x : -inf
+ * The path is what the row follows of this step's own block: the tokens of nodes A(r) of the tree that `parents` describes (as in
+ * orthrus_tree_attn; node r is row r), the anchor's among them; without `parents` those of rows 0..r (a chain: the anchor and the
+ * drafts fed before and at row r; a plain decoding step has one row); without `tokens` nothing.
+ * A row that its mask leaves nothing of is -inf throughout (orthrus_sample_tokens gives token -1 for it).  Logits that no rule
+ * touches keep their bits; a NaN stays NaN unless its token is not allowed.
+ *
+ *   num_rows     [host] R, 1 <= R <= 64
+ *   logits       [dev] [B, R, V] of logits_type, any alignment of the type's own, row (b, r) at element (b*R + r) * logits_stride_row
+ *                (0: dense)
+ *   tokens       [dev] int32 [B, R] or NULL, values outside [0, V) count for nothing; parents [dev] int32 [B, R] or NULL
+ *   rules        [host]
+ *   out          [dev] like logits with out_stride_row: logits itself (with the same stride; only what changes is written), or memory
+ *                apart from it
+ * Arithmetic is fp32, every operation rounded once (frequency * n is subtracted in one), and rounded to the type at the end.
+ * Supported: V <= 1048576.  Needs no workspace.
+ */
+orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
+                                      int64_t logits_stride_row, int32_t num_rows, const int32_t *tokens, const int32_t *parents,
+                                      const orthrus_logit_rules *rules, void *out, int64_t out_stride_row, void *stream);
+
+/*
  * AR-view prefill attention of one layer — Section 3.1 (first paragraph) and Section 3.3: the frozen AR
  * view processes the context with its ordinary causal self-attention, and the K/V it produces is the
  * cache both views share afterwards.  Per sequence b with L = seq_lens[b] cached tokens and

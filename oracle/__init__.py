@@ -474,3 +474,122 @@ def kv_store(k_new, v_new, slot_map, k_pool, v_pool, num_valid=None):
             k_pool[:, s // P, :, s % P] = k_new[:, t]
             v_pool[:, s // P, :, s % P] = v_new[:, t]
     return status
+
+
+# ---- drafts that branch, rules on logits: plain numpy, fp64, one row or request after another
+
+def tree_path(parents, i: int):
+    """Nodes from the root (node 0) of one sequence's tree down to node i; the root alone for an unused node."""
+    path = [int(i)]
+    while 0 <= int(parents[path[-1]]) < path[-1]:
+        path.append(int(parents[path[-1]]))
+    return path[::-1] if path[-1] == 0 else [0]
+
+
+def tree_attn(sm_scale: float, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens):
+    """Attention of every node to the cache and to its path: float arrays q [B,N,Hq,d], k_blk / v_blk [B,N,H,d], pools
+    [pages,H,P,d].  Returns the output, the same weights over the values' magnitudes (what rounding the weights can move) and the
+    log of the sum of exponentials [B,Hq,N]."""
+    B, N, Hq, d = q.shape
+    H, P = k_pool.shape[1], k_pool.shape[2]
+    G = Hq // H
+    out, size, lse = np.zeros((B, N, Hq, d)), np.zeros((B, N, Hq, d)), np.zeros((B, Hq, N))
+    for b in range(B):
+        at = np.arange(int(seq_lens[b]))
+        pages = page_table[b, at // P]
+        for g in range(H):
+            kc, vc = (pool[pages, g, at % P].astype(np.float64).reshape(at.size, d) for pool in (k_pool, v_pool))
+            for i in range(N):
+                path = tree_path(parents[b], i)
+                k, v = np.concatenate([kc, k_blk[b, path, g]]), np.concatenate([vc, v_blk[b, path, g]])
+                for h in range(g * G, (g + 1) * G):
+                    x = k @ q[b, i, h].astype(np.float64) * sm_scale
+                    w = np.exp(x - x.max())
+                    out[b, i, h], size[b, i, h] = w @ v / w.sum(), w @ np.abs(v) / w.sum()
+                    lse[b, h, i] = x.max() + np.log(w.sum())
+    return out, size, lse
+
+
+def _first_largest(x):
+    x = np.asarray(x, dtype=np.float64)
+    nan = np.flatnonzero(np.isnan(x))
+    return int(nan[0]) if nan.size else int(np.argmax(x))
+
+
+def tree_consensus_commit(ar_logits, parents, node_tokens, max_path: int, k_blk_ar=None, v_blk_ar=None, k_pool=None, v_pool=None,
+                          page_table=None, seq_lens=None):
+    """From node 0 to the first child that holds the node's largest logit, and the path's rows into the pools
+    [layers,pages,H,P,d] (in place, as ``seq_lens``)."""
+    B, N, V = ar_logits.shape
+    r = {n: np.zeros(B, np.int32) for n in ("accept_len", "num_committed", "next_anchor")}
+    r.update({n: np.full((B, N), -1, np.int32) for n in ("path_nodes", "out_tokens")})
+    r["status"] = 0
+    for b in range(B):
+        path, tokens = [0], []
+        while True:
+            tokens.append(_first_largest(ar_logits[b, path[-1]]))
+            below = [i for i in range(path[-1] + 1, N) if parents[b, i] == path[-1] and node_tokens[b, i] == tokens[-1]]
+            if not below or len(path) == max_path:
+                break
+            path.append(below[0])
+        m = len(path)
+        r["path_nodes"][b, :m], r["out_tokens"][b, :m] = path, tokens
+        r["accept_len"][b], r["num_committed"][b], r["next_anchor"][b] = m - 1, m, tokens[-1]
+        if k_blk_ar is None:
+            continue
+        P, L = k_pool.shape[3], int(seq_lens[b])
+        slots = [(L + i) // P for i in range(m)]
+        pages = [int(page_table[b, s]) if 0 <= L and s < page_table.shape[1] else -1 for s in slots]
+        if any(not 0 <= g < k_pool.shape[1] for g in pages):
+            r["num_committed"][b], r["status"] = 0, -4
+            continue
+        for i, g in enumerate(pages):
+            k_pool[:, g, :, (L + i) % P] = k_blk_ar[:, b, path[i]]
+            v_pool[:, g, :, (L + i) % P] = v_blk_ar[:, b, path[i]]
+        seq_lens[b] = L + m
+    return r
+
+
+def process_logits(logits, tokens=None, parents=None, history=None, history_lens=None, prompt_lens=None, repetition=None,
+                   presence=None, frequency=None, bias_starts=None, bias_tokens=None, bias_values=None, masks=None, mask_rows=None):
+    """Logits [B,R,V] through their requests' rules, one logit after another.  Also returns the magnitudes that its roundings are of:
+    the sum over the steps of the size of what each of them leaves."""
+    B, R, V = logits.shape
+    out, size = logits.astype(np.float64), np.zeros((B, R, V))
+    finite = lambda a, b, other: other if a is None or not np.isfinite(a[b]) else float(a[b])  # noqa: E731
+    for b in range(B):
+        rep = finite(repetition, b, 1.0)
+        rep = rep if rep > 0 else 1.0
+        pres, freq = finite(presence, b, 0.0), finite(frequency, b, 0.0)
+        text = [] if history is None else [int(t) for t in history[b][:max(0, min(int(history_lens[b]), history.shape[1]))]]
+        n0 = 0 if prompt_lens is None else max(0, min(int(prompt_lens[b]), len(text)))
+        bias = {}
+        if bias_starts is not None:
+            for i in range(max(0, int(bias_starts[b])), min(int(bias_starts[b + 1]), len(bias_tokens))):
+                bias[int(bias_tokens[i])] = float(bias_values[i])
+        for r in range(R):
+            path = [] if tokens is None else range(r + 1) if parents is None else tree_path(parents[b], r)
+            written = text[n0:] + [int(tokens[b, i]) for i in path]
+            seen = set(text[:n0]) | set(written)
+            off = (rep, pres, freq) == (1.0, 0.0, 0.0)
+            for v in (set() if off else seen) | set(bias):
+                if not 0 <= v < V:
+                    continue
+                x, n = out[b, r, v], written.count(v)
+                if v in seen and not off:
+                    x = x / rep if x > 0 else x * rep
+                    size[b, r, v] += abs(x)
+                    if n:
+                        x -= freq * n
+                        size[b, r, v] += abs(x)
+                        x -= pres
+                        size[b, r, v] += abs(x)
+                if v in bias:
+                    x += bias[v]
+                    size[b, r, v] += abs(x)
+                out[b, r, v] = x
+            if masks is not None and 0 <= mask_rows.reshape(B, R)[b, r] < len(masks):
+                words = np.ascontiguousarray(masks[mask_rows.reshape(B, R)[b, r]])
+                gone = np.unpackbits(words.view(np.uint8), bitorder="little")[:V] == 0
+                out[b, r, gone], size[b, r, gone] = -np.inf, 0.0
+    return out, size

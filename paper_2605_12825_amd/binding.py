@@ -39,6 +39,8 @@ EXPORTED = [
     "orthrus_sample_workspace_bytes", "orthrus_sample_tokens", "orthrus_filtered_workspace_bytes",
     "orthrus_filtered_consensus_commit", "orthrus_page_tables_workspace_bytes", "orthrus_page_tables_update",
     "orthrus_kv_store",
+    "orthrus_tree_attn_workspace_bytes", "orthrus_tree_attn", "orthrus_tree_consensus_workspace_bytes",
+    "orthrus_tree_consensus_commit", "orthrus_logits_process",
 ]
 
 
@@ -54,6 +56,17 @@ class orthrus_params(ctypes.Structure):
         ("pool_stride_head", ctypes.c_int64), ("pool_stride_tok", ctypes.c_int64),
         ("q_stride_row", ctypes.c_int64), ("q_stride_head", ctypes.c_int64), ("blk_stride_row", ctypes.c_int64),
         ("blk_stride_head", ctypes.c_int64), ("blk_stride_layer", ctypes.c_int64),
+    ]
+
+
+class orthrus_logit_rules(ctypes.Structure):
+    """Mirror of the C struct orthrus_logit_rules (device addresses and host numbers)."""
+    _fields_ = [
+        ("history", ctypes.c_void_p), ("history_lens", ctypes.c_void_p), ("prompt_lens", ctypes.c_void_p),
+        ("history_stride", ctypes.c_int64), ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+        ("frequency", ctypes.c_void_p), ("bias_starts", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p),
+        ("bias_values", ctypes.c_void_p), ("num_biases", ctypes.c_int64), ("masks", ctypes.c_void_p),
+        ("mask_rows", ctypes.c_void_p), ("num_masks", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
     ]
 
 
@@ -160,6 +173,19 @@ def _load() -> ctypes.CDLL:
                                                ctypes.c_size_t, vp]
     lib.orthrus_kv_store.restype = ctypes.c_int
     lib.orthrus_kv_store.argtypes = [vp, pp, ctypes.c_int32, vp, vp, i32p, i32p, vp, vp, vp]
+    i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    lib.orthrus_tree_attn_workspace_bytes.restype = i64
+    lib.orthrus_tree_attn_workspace_bytes.argtypes = [vp, pp, i32]
+    lib.orthrus_tree_attn.restype = ctypes.c_int
+    lib.orthrus_tree_attn.argtypes = [vp, pp, i32, i32p, vp, vp, vp, vp, vp, i32p, i32p, vp, vp, vp, size, vp]
+    lib.orthrus_tree_consensus_workspace_bytes.restype = i64
+    lib.orthrus_tree_consensus_workspace_bytes.argtypes = [pp, i32]
+    lib.orthrus_tree_consensus_commit.restype = ctypes.c_int
+    lib.orthrus_tree_consensus_commit.argtypes = [vp, pp, ctypes.c_int, vp, i64, i32, i32, i32p, i32p, vp, vp, vp, vp, i32p, i32p,
+                                                  i32p, i32p, i32p, i32p, i32p, vp, size, vp]
+    lib.orthrus_logits_process.restype = ctypes.c_int
+    lib.orthrus_logits_process.argtypes = [vp, pp, ctypes.c_int, vp, i64, i32, i32p, i32p, ctypes.POINTER(orthrus_logit_rules), vp,
+                                           i64, vp]
     lib.orthrus_kv_stream_probe.restype = ctypes.c_int
     lib.orthrus_kv_stream_probe.argtypes = [vp, pp, vp, vp, i32p, i32p, vp]
     return lib
@@ -417,6 +443,54 @@ def orthrus_kv_store(ctx, p: orthrus_params, num_rows: int, k_new, v_new, slot_m
                                _ptr(num_valid), _ptr(k_pool), _ptr(v_pool), _stream_handle(stream))
     if check and st != ORTHRUS_OK:
         raise OrthrusError(st, "orthrus_kv_store")
+    return st
+
+
+def orthrus_tree_attn_workspace_bytes(ctx, p: orthrus_params, num_nodes: int) -> int:
+    n = _lib.orthrus_tree_attn_workspace_bytes(ctx, ctypes.byref(p), int(num_nodes))
+    if n < 0:
+        raise OrthrusError(int(n), "orthrus_tree_attn_workspace_bytes")
+    return int(n)
+
+
+def orthrus_tree_attn(ctx, p: orthrus_params, num_nodes: int, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out,
+                      lse=None, workspace=None, stream=None, check: bool = True) -> int:
+    st = _lib.orthrus_tree_attn(ctx, ctypes.byref(p), int(num_nodes), _ptr(parents), _ptr(q), _ptr(k_blk), _ptr(v_blk),
+                                _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(seq_lens), _ptr(out), _ptr(lse),
+                                _ptr(workspace), _nbytes(workspace), _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_tree_attn")
+    return st
+
+
+def orthrus_tree_consensus_workspace_bytes(p: orthrus_params, num_nodes: int) -> int:
+    n = _lib.orthrus_tree_consensus_workspace_bytes(ctypes.byref(p), int(num_nodes))
+    if n < 0:
+        raise OrthrusError(int(n), "orthrus_tree_consensus_workspace_bytes")
+    return int(n)
+
+
+def orthrus_tree_consensus_commit(ctx, p: orthrus_params, logits_type: int, ar_logits, logits_stride_row: int, num_nodes: int,
+                                  max_path: int, parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens,
+                                  accept_len, num_committed, path_nodes, out_tokens, next_anchor, workspace=None, stream=None,
+                                  check: bool = True) -> int:
+    st = _lib.orthrus_tree_consensus_commit(
+        ctx, ctypes.byref(p), int(logits_type), _ptr(ar_logits), int(logits_stride_row), int(num_nodes), int(max_path),
+        _ptr(parents), _ptr(node_tokens), _ptr(k_blk_ar), _ptr(v_blk_ar), _ptr(k_pool), _ptr(v_pool), _ptr(page_table),
+        _ptr(seq_lens), _ptr(accept_len), _ptr(num_committed), _ptr(path_nodes), _ptr(out_tokens), _ptr(next_anchor),
+        _ptr(workspace), _nbytes(workspace), _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_tree_consensus_commit")
+    return st
+
+
+def orthrus_logits_process(ctx, p: orthrus_params, logits_type: int, logits, logits_stride_row: int, num_rows: int, tokens, parents,
+                           rules: orthrus_logit_rules, out, out_stride_row: int = 0, stream=None, check: bool = True) -> int:
+    st = _lib.orthrus_logits_process(ctx, ctypes.byref(p), int(logits_type), _ptr(logits), int(logits_stride_row), int(num_rows),
+                                     _ptr(tokens), _ptr(parents), None if rules is None else ctypes.byref(rules), _ptr(out),
+                                     int(out_stride_row), _stream_handle(stream))
+    if check and st != ORTHRUS_OK:
+        raise OrthrusError(st, "orthrus_logits_process")
     return st
 
 

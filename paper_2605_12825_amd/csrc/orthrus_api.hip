@@ -197,6 +197,74 @@ orthrus_status check_table_params(const orthrus_params *p)
     return p->num_pages > 0x7fffffff / p->page_size ? ORTHRUS_EUNSUPPORTED : ORTHRUS_OK;
 }
 
+// ---- trees of drafts, rules on logits
+
+struct TreePlan {
+    orthrus::AttnPlan plan;
+    int row_groups;
+};
+orthrus_status make_tree_plan(const orthrus_params *p, int num_nodes, int num_cus, TreePlan *t)
+{
+    if (!p || num_nodes < 1) return ORTHRUS_EINVAL;
+    orthrus_params one = *p;  // the block's size is the call's
+    one.block_k = 1;
+    const orthrus_status s = check_params(&one, true, false, true);
+    if (s != ORTHRUS_OK) return s;
+    const int group = p->num_q_heads / p->num_kv_heads;
+    if (num_nodes > orthrus::kMaxNodes || (int64_t)group * num_nodes > 512) return ORTHRUS_EUNSUPPORTED;
+    orthrus::plan_tree_attn(p->head_dim, group, num_nodes, p->batch, p->num_kv_heads, p->max_seq_len, p->num_splits, num_cus,
+                            p->num_layers, (double)p->num_pages * p->page_size, &t->plan, &t->row_groups);
+    const int64_t units = (int64_t)p->batch * p->num_kv_heads * t->row_groups;
+    if (t->plan.num_splits > 65535 * 16 || units * t->plan.num_splits * t->plan.waves * 4 > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
+    // the balanced partition counts one head's tiles in a 32-bit int
+    if (t->plan.bal_wgs > 0 && (int64_t)p->batch * (p->max_seq_len / 32 + 3) > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
+    return ORTHRUS_OK;
+}
+
+orthrus_status check_tree_consensus(const orthrus_params *p, int num_nodes, bool do_commit)
+{
+    if (!p || num_nodes < 1) return ORTHRUS_EINVAL;
+    orthrus_params one = *p;
+    one.block_k = 1;
+    const orthrus_status s = check_params(&one, false, true, do_commit);
+    if (s != ORTHRUS_OK) return s;
+    return num_nodes > orthrus::kMaxNodes || p->vocab > (1 << 20) ||
+                   orthrus::tree_best_bytes(p->batch, num_nodes, p->vocab) / sizeof(unsigned long long) > 0x7fffffff
+               ? ORTHRUS_EUNSUPPORTED
+               : ORTHRUS_OK;
+}
+
+// Workspace of the tree's consensus: byte offsets behind the chunk maxima.
+struct TreeLayout {
+    size_t nodes, tokens, lens, total;
+};
+TreeLayout tree_layout(const orthrus_params *p, int num_nodes)
+{
+    const size_t levels = align_up((size_t)p->batch * orthrus::kMaxNodes * sizeof(int32_t), 256);
+    TreeLayout l;
+    l.nodes = align_up(orthrus::tree_best_bytes(p->batch, num_nodes, p->vocab), 256);
+    l.tokens = l.nodes + levels;
+    l.lens = l.tokens + levels;
+    l.total = l.lens + align_up((size_t)p->batch * sizeof(int32_t), 256);
+    return l;
+}
+
+// The context's device as the current one while a call launches: its tensors and stream are there, whatever device the calling
+// thread works on.
+struct OnDevice {
+    int before = -1;
+    bool ok, moved = false;
+    explicit OnDevice(int device)
+    {
+        ok = hipGetDevice(&before) == hipSuccess;
+        if (ok && before != device) ok = moved = hipSetDevice(device) == hipSuccess;
+    }
+    ~OnDevice()
+    {
+        if (moved) (void)hipSetDevice(before);
+    }
+};
+
 }  // namespace
 
 // Kernel arguments of a decode-mode attention launch for `plan`.
@@ -877,6 +945,145 @@ orthrus_status orthrus_kv_store(orthrus_ctx *ctx, const orthrus_params *p, int32
     a.rows = num_rows; a.num_layers = p->num_layers; a.num_kv_heads = p->num_kv_heads; a.head_dim = p->head_dim;
     a.page_shift = log2_exact(p->page_size);
     return orthrus::launch_kv_store(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+int64_t orthrus_tree_attn_workspace_bytes(const orthrus_ctx *ctx, const orthrus_params *p, int32_t num_nodes)
+{
+    TreePlan t;
+    const orthrus_status s = make_tree_plan(p, num_nodes, plan_cus(ctx), &t);
+    return s != ORTHRUS_OK ? (int64_t)s : (int64_t)(align_up(t.plan.part_o_bytes, 256) + align_up(t.plan.part_ml_bytes, 256));
+}
+
+orthrus_status orthrus_tree_attn(orthrus_ctx *ctx, const orthrus_params *p, int32_t num_nodes, const int32_t *parents,
+                                 const void *q, const void *k_blk, const void *v_blk, const void *k_pool, const void *v_pool,
+                                 const int32_t *page_table, const int32_t *seq_lens, void *out, float *lse, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    TreePlan t;
+    const orthrus_status s = make_tree_plan(p, num_nodes, plan_cus(ctx), &t);
+    if (s != ORTHRUS_OK) return s;
+    if (!parents || !q || !k_blk || !v_blk || !k_pool || !v_pool || !page_table || !seq_lens || !out) return ORTHRUS_EINVAL;
+    const uintptr_t al = (uintptr_t)q | (uintptr_t)k_blk | (uintptr_t)v_blk | (uintptr_t)k_pool | (uintptr_t)v_pool | (uintptr_t)out;
+    if ((al & 15) || (((uintptr_t)parents | (uintptr_t)page_table | (uintptr_t)seq_lens | (uintptr_t)lse) & 3)) return ORTHRUS_EINVAL;
+    if (p->batch == 0) return ORTHRUS_OK;
+    const size_t need = align_up(t.plan.part_o_bytes, 256) + align_up(t.plan.part_ml_bytes, 256);
+    if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return ORTHRUS_EWORKSPACE;
+    orthrus::AttnArgs a = decode_attn_args(ctx, p, t.plan, 0, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, workspace);
+    a.parents = parents;
+    a.block_k = num_nodes;
+    a.rows = a.group * num_nodes;
+    a.num_kv_heads = p->num_kv_heads * t.row_groups;
+    a.row_groups = t.row_groups;
+    const OnDevice on(ctx->device);
+    if (!on.ok) return ORTHRUS_EHIP;
+    return orthrus::launch_tree_attn(a, t.plan, p->head_dim, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+int64_t orthrus_tree_consensus_workspace_bytes(const orthrus_params *p, int32_t num_nodes)
+{
+    const orthrus_status s = check_tree_consensus(p, num_nodes, false);
+    return s != ORTHRUS_OK ? (int64_t)s : (int64_t)tree_layout(p, num_nodes).total;
+}
+
+orthrus_status orthrus_tree_consensus_commit(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type,
+                                             const void *ar_logits, int64_t logits_stride_row, int32_t num_nodes, int32_t max_path,
+                                             const int32_t *parents, const int32_t *node_tokens, const void *k_blk_ar,
+                                             const void *v_blk_ar, void *k_pool, void *v_pool, const int32_t *page_table,
+                                             int32_t *seq_lens, int32_t *accept_len, int32_t *num_committed, int32_t *path_nodes,
+                                             int32_t *out_tokens, int32_t *next_anchor, void *workspace, size_t workspace_bytes,
+                                             void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    if ((k_blk_ar == nullptr) != (v_blk_ar == nullptr) || max_path < 1) return ORTHRUS_EINVAL;
+    const bool do_commit = k_blk_ar != nullptr;
+    orthrus_status s = check_tree_consensus(p, num_nodes, do_commit);
+    if (s != ORTHRUS_OK) return s;
+    if (!ar_logits || !parents || !node_tokens || !accept_len || !num_committed || !path_nodes || !out_tokens || !next_anchor)
+        return ORTHRUS_EINVAL;
+    if (out_tokens == node_tokens || out_tokens == parents || path_nodes == node_tokens || path_nodes == parents || path_nodes == out_tokens)
+        return ORTHRUS_EINVAL;
+    s = check_logits(p, logits_type, (uintptr_t)ar_logits, logits_stride_row,
+                     (uintptr_t)parents | (uintptr_t)node_tokens | (uintptr_t)accept_len | (uintptr_t)num_committed |
+                         (uintptr_t)path_nodes | (uintptr_t)out_tokens | (uintptr_t)next_anchor);
+    if (s != ORTHRUS_OK) return s;
+    if (do_commit) {
+        if (!k_pool || !v_pool || !page_table || !seq_lens || p->num_layers <= 0) return ORTHRUS_EINVAL;
+        if (p->num_layers > 65535) return ORTHRUS_EUNSUPPORTED;
+        const uintptr_t al = (uintptr_t)k_blk_ar | (uintptr_t)v_blk_ar | (uintptr_t)k_pool | (uintptr_t)v_pool;
+        if ((al & 15) || (((uintptr_t)page_table | (uintptr_t)seq_lens) & 3)) return ORTHRUS_EINVAL;
+    }
+    if (p->batch == 0) return ORTHRUS_OK;
+    const TreeLayout l = tree_layout(p, num_nodes);
+    if (!workspace || workspace_bytes < l.total || ((uintptr_t)workspace & 255)) return ORTHRUS_EWORKSPACE;
+
+    orthrus::TreeArgs a = {};
+    a.logits = ar_logits; a.stride_row = logits_stride_row ? logits_stride_row : p->vocab;
+    a.parents = parents; a.tokens = node_tokens;
+    a.k_blk_ar = (const uint16_t *)k_blk_ar; a.v_blk_ar = (const uint16_t *)v_blk_ar;
+    a.k_pool = (uint16_t *)k_pool; a.v_pool = (uint16_t *)v_pool;
+    a.page_table = page_table; a.seq_lens = seq_lens;
+    a.accept_len = accept_len; a.num_committed = num_committed; a.path_nodes = path_nodes; a.out_tokens = out_tokens;
+    a.next_anchor = next_anchor;
+    a.best = (unsigned long long *)workspace;
+    a.level_node = (int32_t *)((char *)workspace + l.nodes);
+    a.level_token = (int32_t *)((char *)workspace + l.tokens);
+    a.old_lens = (int32_t *)((char *)workspace + l.lens);
+    a.err_word = ctx->err_word;
+    a.stride_layer = p->pool_stride_layer; a.stride_page = p->pool_stride_page;
+    a.stride_head = p->pool_stride_head; a.stride_tok = p->pool_stride_tok; a.num_pages = p->num_pages;
+    a.blk_stride_head = p->blk_stride_head ? p->blk_stride_head : p->head_dim;
+    a.blk_stride_row = p->blk_stride_row ? p->blk_stride_row : (int64_t)p->num_kv_heads * p->head_dim;
+    a.blk_stride_layer = p->blk_stride_layer ? p->blk_stride_layer : (int64_t)p->batch * num_nodes * a.blk_stride_row;
+    a.batch = p->batch; a.nodes = num_nodes; a.max_path = max_path; a.vocab = p->vocab; a.dtype = (int)logits_type;
+    a.num_layers = p->num_layers; a.num_kv_heads = p->num_kv_heads; a.head_dim = p->head_dim;
+    a.page_shift = do_commit ? log2_exact(p->page_size) : 0; a.max_pages_per_seq = p->max_pages_per_seq;
+    a.do_commit = do_commit ? 1 : 0;
+    const OnDevice on(ctx->device);
+    if (!on.ok) return ORTHRUS_EHIP;
+    return orthrus::launch_tree_consensus(a, (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
+}
+
+orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
+                                      int64_t logits_stride_row, int32_t num_rows, const int32_t *tokens, const int32_t *parents,
+                                      const orthrus_logit_rules *rules, void *out, int64_t out_stride_row, void *stream)
+{
+    if (!ctx) return ORTHRUS_EINVAL;
+    orthrus_status s = check_params(p, false, true, false);
+    if (s != ORTHRUS_OK) return s;
+    if (!logits || !out || !rules || num_rows < 1 || (parents && !tokens)) return ORTHRUS_EINVAL;
+    const orthrus_logit_rules &r = *rules;
+    if ((r.history == nullptr) != (r.history_lens == nullptr) || (r.prompt_lens && !r.history) || (r.history && r.history_stride < 1))
+        return ORTHRUS_EINVAL;
+    if (r.num_biases < 0 || (r.bias_starts ? r.num_biases > 0 && (!r.bias_tokens || !r.bias_values) : r.bias_tokens || r.bias_values))
+        return ORTHRUS_EINVAL;
+    const int64_t words = ((int64_t)p->vocab + 31) / 32;
+    if ((r.masks == nullptr) != (r.mask_rows == nullptr) || r.num_masks < 0 || r.mask_stride < 0 || (r.mask_stride && r.mask_stride < words))
+        return ORTHRUS_EINVAL;
+    s = check_logits(p, logits_type, (uintptr_t)logits, logits_stride_row,
+                     (uintptr_t)tokens | (uintptr_t)parents | (uintptr_t)r.history | (uintptr_t)r.history_lens | (uintptr_t)r.prompt_lens |
+                         (uintptr_t)r.repetition | (uintptr_t)r.presence | (uintptr_t)r.frequency | (uintptr_t)r.bias_starts |
+                         (uintptr_t)r.bias_tokens | (uintptr_t)r.bias_values | (uintptr_t)r.masks | (uintptr_t)r.mask_rows);
+    if (s == ORTHRUS_OK) s = check_logits(p, logits_type, (uintptr_t)out, out_stride_row, 0);
+    if (s != ORTHRUS_OK) return s;
+    if (num_rows > orthrus::kMaxNodes || p->vocab > (1 << 20)) return ORTHRUS_EUNSUPPORTED;
+
+    orthrus::RulesArgs a = {};
+    a.logits = logits; a.out = out;
+    a.stride_row = logits_stride_row ? logits_stride_row : p->vocab;
+    a.out_stride_row = out_stride_row ? out_stride_row : p->vocab;
+    a.in_place = logits == out ? 1 : 0;
+    if (a.in_place && a.stride_row != a.out_stride_row) return ORTHRUS_EINVAL;
+    if (p->batch == 0) return ORTHRUS_OK;
+    a.tokens = tokens; a.parents = parents;
+    a.history = r.history; a.history_lens = r.history_lens; a.prompt_lens = r.prompt_lens; a.history_stride = r.history_stride;
+    a.repetition = r.repetition; a.presence = r.presence; a.frequency = r.frequency;
+    a.bias_starts = r.bias_starts; a.bias_tokens = r.bias_tokens; a.bias_values = r.bias_values; a.num_biases = r.num_biases;
+    a.masks = r.masks; a.mask_rows = r.mask_rows; a.num_masks = r.num_masks; a.mask_stride = r.mask_stride ? r.mask_stride : words;
+    a.batch = p->batch; a.rows = num_rows; a.vocab = p->vocab; a.dtype = (int)logits_type;
+    const OnDevice on(ctx->device);
+    if (!on.ok) return ORTHRUS_EHIP;
+    return orthrus::launch_logits_process(a, plan_cus(ctx), (hipStream_t)stream) == hipSuccess ? ORTHRUS_OK : ORTHRUS_EHIP;
 }
 
 orthrus_status orthrus_last_device_error(orthrus_ctx *ctx, void *stream, int32_t *code)

@@ -81,6 +81,7 @@ template <int D, int W, int NS, int MODE, int NT, int PROBE = 0>
 __global__ void __launch_bounds__(64 * (W + 1), 3) attn_split_kernel(ATTN_FIRST_PARAMS, const AttnArgs rest)
 {
     constexpr int ROWS = 32;
+    constexpr bool TREE = false;
 #include "orthrus_attn_split.inc"
 }
 
@@ -295,13 +296,13 @@ int decode_direction_on_host(const int *lens, int batch, bool small_counts)
 }
 
 hipError_t plan_attn(int head_dim, int group, int block_k, int batch, int num_kv_heads, int max_seq_len,
-                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan)
+                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan, bool may_be_wide)
 {
     const int R = group * block_k;
     plan->rows = R;
     const int blocks = R > 32 ? (R + 31) / 32 : 1;
     const int64_t units = (int64_t)batch * num_kv_heads;
-    plan->wide = requested_splits >= 0 && requested_splits <= 1 && attn_wide_pays(head_dim, R, max_seq_len, units, num_cus);
+    plan->wide = may_be_wide && requested_splits >= 0 && requested_splits <= 1 && attn_wide_pays(head_dim, R, max_seq_len, units, num_cus);
     const int W = plan->wide ? (R > 128 ? 4 : 2) : blocks;
     plan->waves = W;
     plan->rows_padded = blocks * 32;

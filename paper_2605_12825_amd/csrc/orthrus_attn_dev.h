@@ -20,6 +20,9 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
 typedef __attribute__((address_space(4))) int32_t const_i32;
 
 union Frag {
@@ -152,9 +155,9 @@ struct SplitCut {
     int count;  // tiles in it, the in-block tile included if it is the unit's last piece
     int live;   // pieces of this unit that have any tile
 };
-__host__ __device__ __forceinline__ SplitCut split_cut(int L, int splits, int split)
+__host__ __device__ __forceinline__ SplitCut split_cut(int L, int splits, int split, int blk_tiles = 1)
 {
-    const int total = ((L + 31) >> 5) + 1;  // cache tiles + the in-block tile
+    const int total = ((L + 31) >> 5) + blk_tiles;  // cache tiles + the in-block tile (a tree of more than 32 nodes has two)
     const int per = total / splits, rem = total - per * splits;
     SplitCut c;
     c.first = split * per + (split < rem ? split : rem);
@@ -487,7 +490,9 @@ constexpr int kNtAsked = 2;
 #endif
 constexpr int kStages = ORTHRUS_ATTN_STAGES;  // LDS ring depth of these kernels (2..4)
 
-template <int MODE>
+// TREE: the block is a tree of up to 64 nodes (attn_tree_kernel) in one or two tiles, and a unit is one of the row groups of a
+// (sequence, KV head): g counts all of them, a head's next to each other.
+template <int MODE, bool TREE = false>
 struct WorkItems {
     int b, g;
     int t_begin, t_end, n_cache, n_tiles;  // cache tokens [t_begin, t_end) in n_cache tiles; n_tiles adds the in-block tile
@@ -498,6 +503,24 @@ struct WorkItems {
     const const_i32 *pt_row;
     int64_t head_off;
     int bal_b, bal_g, bal_o, bal_left;  // balanced form: position in the launch's tile sequence
+    int blk0;                           // tree: which of the block's tiles is the item's first one
+
+    static __device__ __forceinline__ int blk_tiles(const AttnArgs &a)
+    {
+        if constexpr (TREE) return (a.block_k + 31) >> 5;
+        else return 1;
+    }
+    __device__ __forceinline__ int kv_head(const AttnArgs &a) const
+    {
+        if constexpr (TREE) return (int)((unsigned)g / (unsigned)a.row_groups);
+        else return g;
+    }
+    // the item's first query row, of groups of `rows`
+    __device__ __forceinline__ int first_row(const AttnArgs &a, int rows) const
+    {
+        if constexpr (TREE) return (int)((unsigned)g % (unsigned)a.row_groups) * rows;
+        else return 0;
+    }
 
     // validated length of sequence x (scalar)
     __device__ __forceinline__ int seq_len(const AttnArgs &a, int x) { return checked_len(a, ((const const_i32 *)a.seq_lens)[x]); }
@@ -525,7 +548,7 @@ struct WorkItems {
                 if (x >= a.batch) return 0;
                 int L = a.seq_lens[x];
                 L = L < 0 ? 0 : (L > a.max_seq_len ? a.max_seq_len : L);
-                return ((L + 31) >> 5) + 1;
+                return ((L + 31) >> 5) + blk_tiles(a);
             };
             int per_head = 0;  // tiles of one head's units
             for (int x0 = 0; x0 < a.batch; x0 += 64) {
@@ -611,12 +634,16 @@ struct WorkItems {
             g = bal_g;
             const int L = seq_len(a, b);
             const int nc = (L + 31) >> 5;                    // cache tiles of the unit; the in-block tile is tile nc
-            const int take = min(nc + 1 - bal_o, bal_left);  // tiles of this segment
-            const bool has_blk = bal_o + take == nc + 1;
+            const int take = min(nc + blk_tiles(a) - bal_o, bal_left);  // tiles of this segment
+            const bool has_blk = bal_o + take == nc + blk_tiles(a);
             // (everything here is wave-uniform; readfirstlane keeps it in scalar registers)
             n_tiles = __builtin_amdgcn_readfirstlane(take);
-            n_cache = has_blk ? n_tiles - 1 : n_tiles;
-            t_begin = __builtin_amdgcn_readfirstlane(bal_o * 32);
+            if constexpr (TREE) {
+                cut_block(bal_o, nc);
+            } else {
+                n_cache = has_blk ? n_tiles - 1 : n_tiles;
+                t_begin = __builtin_amdgcn_readfirstlane(bal_o * 32);
+            }
             t_end = min(L, t_begin + n_cache * 32);
             final_out = bal_o == 0 && has_blk;
             part_slot = (size_t)(blockIdx.x * 2u + (bal_o == 0 ? 1u : 0u));
@@ -701,11 +728,15 @@ struct WorkItems {
         // The sequence's own length, not the host's bound on it, is cut into num_splits pieces:
         // they stay equal however loose the bound is (it only sized the grid), e.g. when a
         // decode loop bumps it by K per step without reading back.
-        const SplitCut cut = split_cut(L, a.num_splits, split);
+        const SplitCut cut = split_cut(L, a.num_splits, split, blk_tiles(a));
         if (cut.count == 0) return false;  // fewer tiles than splits: nothing falls in this one
         n_tiles = __builtin_amdgcn_readfirstlane(cut.count);
-        n_cache = split == cut.live - 1 ? n_tiles - 1 : n_tiles;  // the last piece ends with the in-block tile
-        t_begin = __builtin_amdgcn_readfirstlane(cut.first * 32);
+        if constexpr (TREE) {
+            cut_block(cut.first, (L + 31) >> 5);
+        } else {
+            n_cache = split == cut.live - 1 ? n_tiles - 1 : n_tiles;  // the last piece ends with the in-block tile
+            t_begin = __builtin_amdgcn_readfirstlane(cut.first * 32);
+        }
         t_end = min(L, t_begin + n_cache * 32);
         final_out = a.num_splits == 1;
         part_slot = ((size_t)b * a.num_kv_heads + g) * a.num_splits + split;
@@ -713,12 +744,47 @@ struct WorkItems {
         return true;
     }
 
+    // Tree: of the item's n_tiles tiles from `first` on, which are the cache's (of its `nc`) and which the block's.
+    __device__ __forceinline__ void cut_block(int first, int nc)
+    {
+        n_cache = __builtin_amdgcn_readfirstlane(max(min(nc - first, n_tiles), 0));
+        blk0 = __builtin_amdgcn_readfirstlane(max(first - nc, 0));
+        t_begin = __builtin_amdgcn_readfirstlane(min(first, nc) * 32);
+    }
+
     __device__ __forceinline__ void point(const AttnArgs &a)
     {
         pt_row = (const const_i32 *)(a.page_table + (int64_t)b * a.max_pages_per_seq);
-        head_off = (int64_t)g * a.stride_head;
+        head_off = (int64_t)kv_head(a) * a.stride_head;
     }
 };
+
+// The nodes on the way from the root (node 0) of a tree to node `lane`, both included, a bit each: of 64 in (x, y).  `parents`
+// holds the node that each of the N <= 64 follows; what is not an earlier node is none, and a node whose way does not come from
+// the root is unused: its way is the root alone.  A whole wave takes part: lane i starts as node i that knows itself, and in each
+// of six steps asks the node it points to for what that one has seen and where it points, so that the way doubles.
+__device__ __forceinline__ uint2 tree_path(const int32_t *parents, int N)
+{
+    const int lane = threadIdx.x & 63;
+    const int up = lane < N ? parents[lane] : -1;
+    int at = up >= 0 && up < lane ? up : lane;
+    uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
+#pragma unroll
+    for (int s = 0; s < 6; ++s) {
+        lo |= (uint32_t)__shfl((int)lo, at);
+        hi |= (uint32_t)__shfl((int)hi, at);
+        at = __shfl(at, at);
+    }
+    const bool used = lo & 1u;
+    return make_uint2(used ? lo : 1u, used ? hi : 0u);
+}
+// Which nodes are used: those that are on their own way.
+__device__ __forceinline__ uint64_t tree_used(uint32_t lo, uint32_t hi)
+{
+    const int lane = threadIdx.x & 63;
+    return __ballot((lane < 32 ? lo >> lane : hi >> (lane - 32)) & 1u);
+}
+constexpr int kTreePathBytes = 64 * 8;
 
 // Launch of one of a call's two kernels (kind 0: split, 1: combine), with its timing events attached when wanted.
 template <class Kern>

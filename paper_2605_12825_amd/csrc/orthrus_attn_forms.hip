@@ -148,6 +148,7 @@ template <int D, int W, int NS, int NT>
 __global__ void __launch_bounds__(64 * (W + 1), 3) attn_by_size_kernel(ATTN_FIRST_PARAMS, const AttnArgs rest)
 {
     constexpr int MODE = kItemsBySize, PROBE = 0, ROWS = 32;
+    constexpr bool TREE = false;
 #include "orthrus_attn_split.inc"
 }
 
@@ -156,6 +157,7 @@ template <int D, int NS, int MODE, int NT>
 __global__ void __launch_bounds__(128, 3) attn_thin_kernel(ATTN_FIRST_PARAMS, const AttnArgs rest)
 {
     constexpr int W = 1, PROBE = 0, ROWS = 16;
+    constexpr bool TREE = false;
 #include "orthrus_attn_split.inc"
 }
 

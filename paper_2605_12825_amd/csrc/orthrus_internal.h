@@ -33,7 +33,11 @@ struct AttnArgs {
     float *part_ml;  // [p][wave][32 rows] float2: running max (log2 domain) and sum
     int32_t *err_word;
     // prefill only: lengths before the call and validated new-token counts [B] (workspace), the lengths to bump, row stride T
-    const int32_t *old_lens, *new_lens;
+    union {
+        const int32_t *old_lens;
+        const int32_t *parents;  // tree only: [B, block_k], the node that a node follows
+    };
+    const int32_t *new_lens;
     int32_t *seq_lens_out;
     int max_new;
     int64_t stride_page, stride_head, stride_tok, num_pages;
@@ -41,7 +45,11 @@ struct AttnArgs {
     // (prefill: of q and of the new K/V rows, always dense)
     int64_t q_stride_row, q_stride_head, blk_stride_row, blk_stride_head;
     int batch, num_q_heads, num_kv_heads, group, block_k, rows;
-    int page_shift, max_pages_per_seq, max_seq_len, chunk_tokens, num_splits, view;
+    int page_shift, max_pages_per_seq, max_seq_len, chunk_tokens, num_splits;
+    union {
+        int view;
+        int row_groups;  // tree only: workgroups that share a (sequence, KV head)'s rows; num_kv_heads counts each of them
+    };
     int bal_wgs;  // balanced partition: workgroups of the split launch (0 otherwise)
     union {
         int ranked;  // prefill: chunks start longest first over all sequences (prefill_ranked)
@@ -159,6 +167,44 @@ struct StoreArgs {
     int rows, num_layers, num_kv_heads, head_dim, page_shift;
 };
 
+constexpr int kMaxNodes = 64;  // of a tree: a lane to a node
+
+struct TreeArgs {
+    const void *logits;
+    int64_t stride_row;          // elements between rows
+    const int32_t *parents, *tokens;  // [B][nodes]
+    const uint16_t *k_blk_ar, *v_blk_ar;
+    uint16_t *k_pool, *v_pool;
+    const int32_t *page_table;
+    int32_t *seq_lens, *accept_len, *num_committed, *path_nodes, *out_tokens, *next_anchor;
+    // workspace: the largest logit of every chunk (argmax_key), [row][chunk], or where the path is walked [level & 1][b][chunk]; the
+    // node and the token of every level of a path [b][kMaxNodes]; the lengths before the step
+    unsigned long long *best;
+    int32_t *level_node, *level_token, *old_lens;
+    int32_t *err_word;
+    int64_t stride_layer, stride_page, stride_head, stride_tok, num_pages;
+    int64_t blk_stride_layer, blk_stride_row, blk_stride_head;
+    int batch, nodes, max_path, vocab, dtype, num_layers, num_kv_heads, head_dim;
+    int page_shift, max_pages_per_seq, chunks, do_commit;
+    int walk;                    // 1: level by level, 0: every row is scanned
+};
+
+struct RulesArgs {
+    const void *logits;
+    void *out;
+    int64_t stride_row, out_stride_row;  // elements between rows
+    const int32_t *tokens, *parents;     // [B][rows] or NULL
+    const int32_t *history, *history_lens, *prompt_lens;
+    int64_t history_stride;
+    const float *repetition, *presence, *frequency;  // [B] or NULL
+    const int32_t *bias_starts, *bias_tokens;
+    const float *bias_values;
+    const uint32_t *masks;
+    const int32_t *mask_rows;
+    int64_t num_biases, num_masks, mask_stride;
+    int batch, rows, rows_per_wg, vocab, dtype, in_place;
+};
+
 // ---- commit helpers shared by the greedy and the sampling consensus kernels (device code)
 #if defined(__HIPCC__)
 // Copy rows 0..m-1 of the AR view's block K/V of (sequence b, layer) to token positions L..L+m-1 of the
@@ -253,7 +299,8 @@ struct AttnLaunchEvents {
 
 // Host-side launchers (defined next to the kernels).  Return hipSuccess or the launch error.
 hipError_t plan_attn(int head_dim, int group, int block_k, int batch, int num_kv_heads, int max_seq_len,
-                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan);
+                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan,
+                     bool may_be_wide = true);
 // Whether the items of a fixed-split launch start longest first; `items` workgroups of which per_cu are resident on a CU at once.
 bool decode_by_size(int batch, int64_t items, int per_cu, int num_cus);
 // What the kernels make of a batch's lengths: 0 to be ranked, 1 alike, 2 rising, 3 falling.  `small_counts`: the 64-row kernel.
@@ -276,6 +323,10 @@ hipError_t launch_attn_wide(const AttnArgs &a, const AttnPlan &plan, int head_di
 hipError_t launch_attn_thin(const AttnArgs &a, const AttnPlan &plan, int head_dim, dim3 grid, hipStream_t stream, AttnLaunchEvents *events);
 hipError_t launch_attn_by_size(const AttnArgs &a, const AttnPlan &plan, int head_dim, dim3 grid, hipStream_t stream, AttnLaunchEvents *events);
 hipError_t launch_prefill_attn(const AttnArgs &a, int head_dim, int num_cus, hipStream_t stream);
+// Attention of a tree of drafts: the plan, whose rows are those of one of `row_groups` workgroups of a (sequence, KV head), and the launch.
+hipError_t plan_tree_attn(int head_dim, int group, int nodes, int batch, int num_kv_heads, int max_seq_len, int requested_splits,
+                          int num_cus, int num_layers, double pool_tokens, AttnPlan *plan, int *row_groups);
+hipError_t launch_tree_attn(const AttnArgs &a, const AttnPlan &plan, int head_dim, hipStream_t stream);
 hipError_t launch_prefill_split(const AttnArgs &a, int head_dim, int num_cus, hipStream_t stream);
 hipError_t launch_consensus(ConsensusArgs a, hipStream_t stream);
 hipError_t launch_sampling_consensus(const SamplingArgs &a, hipStream_t stream);
@@ -287,6 +338,9 @@ hipError_t launch_filtered_consensus(FilteredArgs a, hipStream_t stream);
 hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream);
 bool kv_store_fits(int rows, int num_kv_heads, int head_dim);
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
+size_t tree_best_bytes(int batch, int nodes, int vocab);
+hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream);
+hipError_t launch_logits_process(RulesArgs a, int num_cus, hipStream_t stream);
 int consensus_chunk_elems();
 int draw_chunk_elems();
 // Static device scratch of the allocation-free consensus entry point: looked up once per device (with

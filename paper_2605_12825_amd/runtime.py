@@ -70,6 +70,73 @@ def _check_filters(batch, temperature, top_k, top_p, min_p) -> None:
                     ("min_p", min_p, _F32, batch))
 
 
+def _check_rows(name, t, elements, dense) -> None:
+    if t.__class__ is not int and (t.element_size() != 2 or t.numel() != elements or dense and not t.is_contiguous()):
+        raise ValueError("%s must hold %d elements of 16 bits%s, not %s of %s with strides %s"
+                         % (name, elements, " without gaps" if dense else "", tuple(t.shape), t.dtype, t.stride()))
+
+
+def _check_logits_rows(name, t, rows, vocab, stride_row) -> None:
+    """The memory behind a tensor of logits, or a view of one, holds that many rows so far apart."""
+    behind = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    if rows > 0 and behind < (rows - 1) * (stride_row or vocab) + vocab or stride_row == 0 and t.numel() != rows * vocab:
+        raise ValueError("%s must hold %d rows of %d logits, %d apart, not %s" % (name, rows, vocab, stride_row or vocab, tuple(t.shape)))
+
+
+class LogitRules:
+    """What requests ask of their tokens, for DecodeStep.process_logits: tensors on the device, one entry a request.  What is None
+    is off.  The tensors' contents may change from call to call.
+
+    history [batch, most tokens] and history_lens: the tokens before the anchor, the prompt's (prompt_lens of them) first;
+    repetition, presence, frequency: penalties for tokens that are in it or on the row's path; bias_starts [batch + 1], bias_tokens
+    and bias_values: entries bias_starts[b] .. bias_starts[b + 1] - 1 are request b's, the last of a token counts; masks
+    [number, words of 32 tokens] with a bit set for every token allowed and mask_rows [batch, rows] that names each row's, -1 for none.
+    """
+
+    def __init__(self, *, history=None, history_lens=None, prompt_lens=None, repetition=None, presence=None, frequency=None,
+                 bias_starts=None, bias_tokens=None, bias_values=None, masks=None, mask_rows=None):
+        for name, t, dims, dtype in (("history", history, 2, _I32), ("history_lens", history_lens, 1, _I32), ("prompt_lens", prompt_lens, 1, _I32),
+                                     ("repetition", repetition, 1, _F32), ("presence", presence, 1, _F32), ("frequency", frequency, 1, _F32),
+                                     ("bias_starts", bias_starts, 1, _I32), ("bias_tokens", bias_tokens, 1, _I32),
+                                     ("bias_values", bias_values, 1, _F32), ("masks", masks, 2, _I32), ("mask_rows", mask_rows, None, _I32)):
+            if t is not None and (t.dtype is not dtype or dims is not None and t.dim() != dims or not t.is_contiguous()):
+                raise ValueError("%s must be dense, of %s%s, not %s of %s" % (name, dtype, "" if dims is None else " and %d dimensions" % dims,
+                                                                              tuple(t.shape), t.dtype))
+        for a, b, both in ((history, history_lens, "history and history_lens"), (masks, mask_rows, "masks and mask_rows"),
+                           (bias_starts, bias_tokens, "bias_starts and bias_tokens"), (bias_tokens, bias_values, "bias_tokens and bias_values")):
+            if (a is None) != (b is None):
+                raise ValueError("%s come together" % both)
+        if prompt_lens is not None and history is None:
+            raise ValueError("prompt_lens comes with history")
+        if bias_tokens is not None and bias_tokens.numel() != bias_values.numel():
+            raise ValueError("bias_tokens and bias_values have as many entries")
+        self.history, self.history_lens, self.prompt_lens = history, history_lens, prompt_lens
+        self.repetition, self.presence, self.frequency = repetition, presence, frequency
+        self.bias_starts, self.bias_tokens, self.bias_values = bias_starts, bias_tokens, bias_values
+        self.masks, self.mask_rows = masks, mask_rows
+        r = self.c = B.orthrus_logit_rules()
+        for name in ("history", "history_lens", "prompt_lens", "repetition", "presence", "frequency", "bias_starts", "bias_tokens",
+                     "bias_values", "masks", "mask_rows"):
+            setattr(r, name, B._ptr(getattr(self, name)))
+        if history is not None and history.shape[1] == 0:   # nothing can stand in it
+            r.history = r.history_lens = r.prompt_lens = None
+        r.history_stride = 0 if history is None else history.shape[1]
+        r.num_biases = 0 if bias_tokens is None else bias_tokens.numel()
+        r.num_masks, r.mask_stride = (0, 0) if masks is None else masks.shape
+
+    def check(self, batch, rows, vocab) -> None:
+        """Refuses rules of another batch, block or vocabulary."""
+        _check_operands(*((name, getattr(self, name), dtype, batch) for name, dtype in
+                          (("history_lens", _I32), ("prompt_lens", _I32), ("repetition", _F32), ("presence", _F32), ("frequency", _F32))),
+                        ("bias_starts", self.bias_starts, _I32, batch + 1), ("mask_rows", self.mask_rows, _I32, batch * rows))
+        if self.history is not None and self.history.shape[0] != batch:
+            raise ValueError("history must have a row for each of %d requests, not %s" % (batch, tuple(self.history.shape)))
+        if self.mask_rows is not None and self.mask_rows.numel() != batch * rows:
+            raise ValueError("mask_rows must name a mask for each of %d x %d rows, not %s" % (batch, rows, tuple(self.mask_rows.shape)))
+        if self.masks is not None and self.masks.shape[1] < (vocab + 31) // 32:
+            raise ValueError("masks must have %d words for %d tokens, not %d" % ((vocab + 31) // 32, vocab, self.masks.shape[1]))
+
+
 class DecodeStep:
     """Owns an orthrus context plus the attention / consensus workspaces for fixed shapes."""
 
@@ -176,15 +243,19 @@ class DecodeStep:
             setattr(self, name, ws)
         return ws
 
-    def reserve(self, sampling=False, tables=False) -> None:
-        """Makes the workspaces of sample_tokens and filtered_consensus_commit, or of update_page_tables, ahead of their first
-        call: a program that records calls into a graph does this before.  Calls that overlap in time, in replays of two graphs as on
+    def reserve(self, sampling=False, tables=False, tree_nodes=0) -> None:
+        """Makes the workspaces of sample_tokens and filtered_consensus_commit, of update_page_tables, or of tree_attn and
+        tree_consensus_commit for trees of so many nodes (under the present max_seq_len), ahead of their first call: a program that records calls into a graph does this before.  Calls that overlap in time, in replays of two graphs as on
         two streams, need a step each."""
         if sampling:
             self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
             self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
         if tables:
             self._workspace("tables_ws", B.orthrus_page_tables_workspace_bytes)
+        if tree_nodes:
+            self._tree_attn_ws(tree_nodes)
+            if self.params.vocab > 0:
+                self._tree_consensus_ws(tree_nodes)
 
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, logprobs=None, stream=None,
                       logits_stride_row=0):
@@ -269,6 +340,84 @@ class DecodeStep:
         q.blk_stride_layer, q.blk_stride_row, q.blk_stride_head = strides[:3]
         return q
 
+    def _stream(self, stream):
+        """The caller's stream, or the current one of the step's device."""
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def _sized_workspace(self, name, need):
+        """The buffer of a kind of call whose size goes by its arguments; a larger one takes its place (never inside a captured
+        sequence: reserve comes before)."""
+        ws = getattr(self, name, None)
+        if ws is None or ws.numel() < need:
+            with torch.cuda.device(self.device):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("reserve() comes before a call is recorded")
+                ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+                torch.cuda.current_stream().synchronize()   # the call may be on another stream than what used this memory before
+            setattr(self, name, ws)
+        return ws
+
+    def _tree_attn_ws(self, nodes):
+        return self._sized_workspace("tree_attn_ws", B.orthrus_tree_attn_workspace_bytes(self.ctx, self.params, nodes))
+
+    def _tree_consensus_ws(self, nodes):
+        return self._sized_workspace("tree_consensus_ws", B.orthrus_tree_consensus_workspace_bytes(self.params, nodes))
+
+    def tree_attn(self, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse=None, stream=None):
+        """Attention of a tree of drafts per sequence: parents [batch, nodes] (at most 64) names the node that each follows, -1 for
+        node 0 and for unused ones; every node sees the cache, the nodes above it and itself.  Block tensors are [batch, nodes, ...]."""
+        p, nodes = self.params, parents.shape[1]
+        rows = p.batch * nodes
+        _check_operands(("parents", parents, _I32, rows))
+        _check_rows("q", q, rows * p.num_q_heads * p.head_dim, p.q_stride_row == 0 and p.q_stride_head == 0)
+        dense = p.blk_stride_row == 0 and p.blk_stride_head == 0
+        _check_rows("k_blk", k_blk, rows * p.num_kv_heads * p.head_dim, dense)
+        _check_rows("v_blk", v_blk, rows * p.num_kv_heads * p.head_dim, dense)
+        _check_rows("out", out, rows * p.num_q_heads * p.head_dim, True)
+        _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
+        return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse,
+                                   self._tree_attn_ws(nodes), self._stream(stream))
+
+    def tree_consensus_commit(self, ar_logits, parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens,
+                              accept_len, num_committed, path_nodes, out_tokens, next_anchor, max_path=None, stream=None,
+                              logits_stride_row=0):
+        """Greedy consensus of a tree of drafts: from node 0 on to the child that holds the node's greedy token, for as long as there
+        is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed."""
+        p, nodes = self.params, parents.shape[1]
+        rows = p.batch * nodes
+        _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
+                        ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, p.batch),
+                        ("num_committed", num_committed, _I32, p.batch), ("next_anchor", next_anchor, _I32, p.batch))
+        kind = _logits_type(logits_stride_row, ar_logits)
+        _check_logits_rows("ar_logits", ar_logits, rows, p.vocab, logits_stride_row)
+        if k_blk_ar is not None and v_blk_ar is not None:
+            size, dense = p.num_layers * rows * p.num_kv_heads * p.head_dim, p.blk_stride_row == 0 and p.blk_stride_head == 0 and p.blk_stride_layer == 0
+            _check_rows("k_blk_ar", k_blk_ar, size, dense)
+            _check_rows("v_blk_ar", v_blk_ar, size, dense)
+        return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, nodes if max_path is None else max_path,
+                                               parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
+                                               num_committed, path_nodes, out_tokens, next_anchor, self._tree_consensus_ws(nodes),
+                                               self._stream(stream))
+
+    def process_logits(self, logits, rules, tokens=None, parents=None, out=None, stream=None, logits_stride_row=0, out_stride_row=0):
+        """Puts logits [batch, rows, vocab] (or [batch, vocab]) through their requests' LogitRules: in place, or into `out`.  tokens
+        [batch, rows] are those fed at the rows and parents [batch, rows] the row that each follows (None: the one before it); they
+        count as written on the way to a row.  Rows are dense or the given numbers of elements apart."""
+        p, rows = self.params, 1 if logits.dim() == 2 else logits.shape[1]
+        if logits.shape[0] != p.batch or logits.dim() not in (2, 3):
+            raise ValueError("logits must be [batch, rows, vocab] or [batch, vocab], not %s" % (tuple(logits.shape),))
+        if out is None:
+            out, out_stride_row = logits, logits_stride_row
+        kind = _logits_type(logits_stride_row, logits)
+        if _logits_type(out_stride_row, out) != kind:
+            raise ValueError("out must be of the logits' type")
+        _check_logits_rows("logits", logits, p.batch * rows, p.vocab, logits_stride_row)
+        _check_logits_rows("out", out, p.batch * rows, p.vocab, out_stride_row)
+        _check_operands(("tokens", tokens, _I32, p.batch * rows), ("parents", parents, _I32, p.batch * rows))
+        rules.check(p.batch, rows, p.vocab)
+        return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row,
+                                        self._stream(stream))
+
     def attn_timing(self, enable: bool) -> None:
         """Attach HIP events to the attention kernels of the following attn() calls (or stop doing so)."""
         B.orthrus_attn_timing(self.ctx, enable)
@@ -302,7 +451,8 @@ class DecodeStack:
 
     def __init__(self, *, num_layers, batch, num_q_heads, num_kv_heads, head_dim, block_k, page_size,
                  k_pool, v_pool, page_table, seq_lens, max_seq_len, vocab, num_splits=0, temperature=0.0,
-                 diffusion_passes=1, device=0, filters=False, free_pages=None, free_state=None):
+                 diffusion_passes=1, device=0, filters=False, free_pages=None, free_state=None, tree_nodes=0, tree_depth=0,
+                 rules=None):
         if k_pool.dim() != 5 or k_pool.shape[0] != num_layers or not k_pool.is_contiguous():
             raise ValueError("pools must be contiguous [layers, pages, H_kv, P, d]")
         L, pages, H, P, d = k_pool.shape
@@ -320,14 +470,26 @@ class DecodeStack:
                                num_splits=num_splits, device=device,
                                pool_strides=(pages * H * P * d, H * P * d, P * d, d))
         dev = self.step.device
-        blk = (num_layers, batch, block_k, num_kv_heads, head_dim)
-        qs = (num_layers, batch, block_k, num_q_heads, head_dim)
+        # tree_nodes: the AR view verifies a tree of so many drafts per sequence (node 0 is the anchor) of at most tree_depth levels,
+        # greedily: the program writes `parents` and `node_tokens` and the tree's rows into `q_ar`, `k_blk_ar`, `v_blk_ar` and
+        # `ar_logits`; the cycle leaves the path in `path_nodes`.  `rules` (LogitRules): `ar_logits` go through them, in place, each
+        # node by its own path.  Their history is the program's to extend between two cycles, by the path's node_tokens.
+        self.tree_nodes, self.rules = int(tree_nodes), rules
+        self.tree_depth = int(tree_depth) if tree_depth else self.tree_nodes
+        if self.tree_nodes and (self.temperature > 0 or filters):
+            raise ValueError("trees are verified greedily: no temperature, no filters")
+        if (tree_depth or rules is not None) and not self.tree_nodes or self.tree_depth < 0 or self.tree_nodes < 0:
+            raise ValueError("tree_depth and rules are for stacks with tree_nodes")
+        verified = self.tree_nodes or block_k
         i16 = dict(dtype=torch.int16, device=dev)
-        self.q_diff, self.q_ar = torch.zeros(qs, **i16), torch.zeros(qs, **i16)
-        self.k_blk_diff, self.v_blk_diff = torch.zeros(blk, **i16), torch.zeros(blk, **i16)
-        self.k_blk_ar, self.v_blk_ar = torch.zeros(blk, **i16), torch.zeros(blk, **i16)
-        self.out_diff, self.out_ar = torch.zeros(qs, **i16), torch.zeros(qs, **i16)
-        self.ar_logits = torch.zeros((batch, block_k, vocab), dtype=torch.float32, device=dev)
+
+        def block(rows, heads):
+            return torch.zeros((num_layers, batch, rows, heads, head_dim), **i16)
+        self.q_diff, self.q_ar = block(block_k, num_q_heads), block(verified, num_q_heads)
+        self.k_blk_diff, self.v_blk_diff = block(block_k, num_kv_heads), block(block_k, num_kv_heads)
+        self.k_blk_ar, self.v_blk_ar = block(verified, num_kv_heads), block(verified, num_kv_heads)
+        self.out_diff, self.out_ar = block(block_k, num_q_heads), block(verified, num_q_heads)
+        self.ar_logits = torch.zeros((batch, verified, vocab), dtype=torch.float32, device=dev)
         self.draft_tokens = torch.zeros((batch, block_k), dtype=torch.int32, device=dev)
         self.filters = bool(filters)
         if self.temperature > 0 and not self.filters:
@@ -348,7 +510,7 @@ class DecodeStack:
             self.draft_logprobs = torch.zeros((batch, block_k), **f32)
             self.gumbel = torch.zeros((batch, vocab), **f32)
             self.step.reserve(sampling=True)
-        # a ring of free pages: the cycle first maps pages for `grow` tokens more per request, block_k each.  A request that
+        # a ring of free pages: the cycle first maps pages for `grow` tokens more per request, block_k each (tree_depth for trees).  A request that
         # is not granted them (`granted` is 0) sets the error word (ORTHRUS_ECAPACITY) as every page that is missing does; it is
         # decoded all the same, and where its kept rows do not fit into the pages that it has, none is committed (`num_committed`
         # is 0) and it goes on in a later cycle.  end() takes the pages of requests that are over between two cycles, without an
@@ -358,12 +520,19 @@ class DecodeStack:
         if free_pages is not None:
             if free_pages.numel() != pages or free_state is None:
                 raise ValueError("free_pages holds num_pages entries and comes with free_state")
-            self.grow = torch.full((batch,), block_k, **i32)
+            most = min(self.tree_depth, self.tree_nodes) if self.tree_nodes else block_k   # tokens that a cycle may commit
+            self.grow = torch.full((batch,), most, **i32)
             self.granted, self.token_starts = torch.zeros((batch,), **i32), torch.zeros((batch + 1,), **i32)
-            self.slot_map = torch.zeros((batch * block_k,), **i32)
+            self.slot_map = torch.zeros((batch * most,), **i32)
             self.step.reserve(tables=True)
         self.accept_len, self.num_committed, self.next_anchor = (torch.zeros((batch,), **i32) for _ in range(3))
-        self.out_tokens = torch.zeros((batch, block_k), **i32)
+        self.out_tokens = torch.zeros((batch, verified), **i32)
+        if self.tree_nodes:
+            self.parents = torch.arange(-1, verified - 1, **i32).repeat(batch, 1)   # a chain
+            self.node_tokens, self.path_nodes = torch.zeros_like(self.out_tokens), torch.zeros_like(self.out_tokens)
+            self.step.reserve(tree_nodes=verified)
+            if rules is not None:
+                rules.check(batch, verified, vocab)
         self.graph = None
         self.graph_stream = None
 
@@ -380,9 +549,19 @@ class DecodeStack:
                 s.sample_tokens(self.diff_logits, self.temperatures, self.top_k, self.top_p, self.min_p, self.draft_u,
                                 self.draft_tokens, self.draft_logprobs, stream)
             for l in range(self.num_layers):
+                if view == 1 and self.tree_nodes:
+                    s.tree_attn(self.parents, q[l], kb[l], vb[l], self.k_pool[l], self.v_pool[l], self.page_table, self.seq_lens,
+                                out[l], None, stream)
+                    continue
                 s.attn(view, q[l], kb[l], vb[l], self.k_pool[l], self.v_pool[l], self.page_table, self.seq_lens,
                        out[l], None, stream)
-        if self.filters:
+        if self.tree_nodes:
+            if self.rules is not None:
+                s.process_logits(self.ar_logits, self.rules, self.node_tokens, self.parents, stream=stream)
+            s.tree_consensus_commit(self.ar_logits, self.parents, self.node_tokens, self.k_blk_ar, self.v_blk_ar, self.k_pool,
+                                    self.v_pool, self.page_table, self.seq_lens, self.accept_len, self.num_committed,
+                                    self.path_nodes, self.out_tokens, self.next_anchor, self.tree_depth, stream)
+        elif self.filters:
             s.filtered_consensus_commit(self.ar_logits, self.diff_logits, self.temperatures, self.top_k, self.top_p,
                                         self.min_p, self.draft_tokens, self.accept_u, self.gumbel, self.k_blk_ar,
                                         self.v_blk_ar, self.k_pool, self.v_pool, self.page_table, self.seq_lens,
