@@ -1051,7 +1051,7 @@ orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p,
     if (!ctx) return ORTHRUS_EINVAL;
     orthrus_status s = check_params(p, false, true, false);
     if (s != ORTHRUS_OK) return s;
-    if (!logits || !out || !rules || num_rows < 1 || (parents && !tokens)) return ORTHRUS_EINVAL;
+    if (!logits || !out || !rules || num_rows < 1) return ORTHRUS_EINVAL;
     const orthrus_logit_rules &r = *rules;
     if ((r.history == nullptr) != (r.history_lens == nullptr) || (r.prompt_lens && !r.history) || (r.history && r.history_stride < 1))
         return ORTHRUS_EINVAL;

@@ -42,6 +42,7 @@ def _logits_type(stride_row, *logits) -> int:
 
 
 _F32, _I32 = torch.float32, torch.int32
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _check_operands(*operands) -> None:
@@ -78,6 +79,8 @@ def _check_rows(name, t, elements, dense) -> None:
 
 def _check_logits_rows(name, t, rows, vocab, stride_row) -> None:
     """The memory behind a tensor of logits, or a view of one, holds that many rows so far apart."""
+    if t.numel() == rows * (stride_row or vocab) and stride_row >= 0:
+        return
     behind = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
     if rows > 0 and behind < (rows - 1) * (stride_row or vocab) + vocab or stride_row == 0 and t.numel() != rows * vocab:
         raise ValueError("%s must hold %d rows of %d logits, %d apart, not %s" % (name, rows, vocab, stride_row or vocab, tuple(t.shape)))
@@ -123,6 +126,7 @@ class LogitRules:
         r.history_stride = 0 if history is None else history.shape[1]
         r.num_biases = 0 if bias_tokens is None else bias_tokens.numel()
         r.num_masks, r.mask_stride = (0, 0) if masks is None else masks.shape
+        self.checked = None   # the batch, rows and vocabulary that they are known to fit
 
     def check(self, batch, rows, vocab) -> None:
         """Refuses rules of another batch, block or vocabulary."""
@@ -135,6 +139,7 @@ class LogitRules:
             raise ValueError("mask_rows must name a mask for each of %d x %d rows, not %s" % (batch, rows, tuple(self.mask_rows.shape)))
         if self.masks is not None and self.masks.shape[1] < (vocab + 31) // 32:
             raise ValueError("masks must have %d words for %d tokens, not %d" % ((vocab + 31) // 32, vocab, self.masks.shape[1]))
+        self.checked = (batch, rows, vocab)
 
 
 class DecodeStep:
@@ -173,6 +178,7 @@ class DecodeStep:
             self.params.max_seq_len = bound
             n = max(n, B.orthrus_attn_workspace_bytes_on(self.ctx, self.params))
         self.params.max_seq_len = max_seq_len
+        self._tree_attn_key = self._tree_consensus_key = (None, None)   # what their workspaces are made for, and these
         self.attn_ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
         self.cons_ws = None
         if vocab > 0:
@@ -341,8 +347,10 @@ class DecodeStep:
         return q
 
     def _stream(self, stream):
-        """The caller's stream, or the current one of the step's device."""
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+        """The caller's stream, or the current one of the step's device (a torch Stream object for it would take 2.9 us)."""
+        if stream is not None:
+            return stream
+        return torch.cuda.current_stream(self.device) if _raw_stream is None else _raw_stream(self.device.index)
 
     def _sized_workspace(self, name, need):
         """The buffer of a kind of call whose size goes by its arguments; a larger one takes its place (never inside a captured
@@ -358,23 +366,40 @@ class DecodeStep:
         return ws
 
     def _tree_attn_ws(self, nodes):
-        return self._sized_workspace("tree_attn_ws", B.orthrus_tree_attn_workspace_bytes(self.ctx, self.params, nodes))
+        key, ws = self._tree_attn_key
+        if key != (nodes, self.params.max_seq_len):   # (a query is a call into the library)
+            ws = self._sized_workspace("tree_attn_ws", B.orthrus_tree_attn_workspace_bytes(self.ctx, self.params, nodes))
+            self._tree_attn_key = (nodes, self.params.max_seq_len), ws
+        return ws
 
     def _tree_consensus_ws(self, nodes):
-        return self._sized_workspace("tree_consensus_ws", B.orthrus_tree_consensus_workspace_bytes(self.params, nodes))
+        key, ws = self._tree_consensus_key
+        if key != nodes:
+            ws = self._sized_workspace("tree_consensus_ws", B.orthrus_tree_consensus_workspace_bytes(self.params, nodes))
+            self._tree_consensus_key = nodes, ws
+        return ws
 
     def tree_attn(self, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse=None, stream=None):
         """Attention of a tree of drafts per sequence: parents [batch, nodes] (at most 64) names the node that each follows, -1 for
         node 0 and for unused ones; every node sees the cache, the nodes above it and itself.  Block tensors are [batch, nodes, ...]."""
         p, nodes = self.params, parents.shape[1]
-        rows = p.batch * nodes
-        _check_operands(("parents", parents, _I32, rows))
-        _check_rows("q", q, rows * p.num_q_heads * p.head_dim, p.q_stride_row == 0 and p.q_stride_head == 0)
-        dense = p.blk_stride_row == 0 and p.blk_stride_head == 0
-        _check_rows("k_blk", k_blk, rows * p.num_kv_heads * p.head_dim, dense)
-        _check_rows("v_blk", v_blk, rows * p.num_kv_heads * p.head_dim, dense)
-        _check_rows("out", out, rows * p.num_q_heads * p.head_dim, True)
-        _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
+        rows, d = p.batch * nodes, p.head_dim
+        queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
+        dense_q, dense = p.q_stride_row == 0 and p.q_stride_head == 0, p.blk_stride_row == 0 and p.blk_stride_head == 0
+        try:   # (what the calls below look at one after the other takes 3 us here)
+            fine = parents.dtype is _I32 and parents.numel() == rows and parents.is_contiguous() and \
+                q.nbytes == out.nbytes == 2 * queries and k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and \
+                (not dense_q or q.is_contiguous()) and (not dense or k_blk.is_contiguous() and v_blk.is_contiguous())
+        except AttributeError:   # (addresses)
+            fine = False
+        if not fine:
+            _check_operands(("parents", parents, _I32, rows))
+            _check_rows("q", q, queries, dense_q)
+            _check_rows("k_blk", k_blk, keys, dense)
+            _check_rows("v_blk", v_blk, keys, dense)
+            _check_rows("out", out, queries, True)
+        if lse is not None:
+            _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
         return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse,
                                    self._tree_attn_ws(nodes), self._stream(stream))
 
@@ -384,10 +409,20 @@ class DecodeStep:
         """Greedy consensus of a tree of drafts: from node 0 on to the child that holds the node's greedy token, for as long as there
         is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed."""
         p, nodes = self.params, parents.shape[1]
-        rows = p.batch * nodes
-        _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
-                        ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, p.batch),
-                        ("num_committed", num_committed, _I32, p.batch), ("next_anchor", next_anchor, _I32, p.batch))
+        rows, batch = p.batch * nodes, p.batch
+        try:
+            fine = parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
+                parents.numel() == node_tokens.numel() == path_nodes.numel() == out_tokens.numel() == rows and \
+                accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
+                accept_len.numel() == num_committed.numel() == next_anchor.numel() == batch and parents.is_contiguous() and \
+                node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and \
+                accept_len.is_contiguous() and num_committed.is_contiguous() and next_anchor.is_contiguous()
+        except AttributeError:   # (addresses)
+            fine = False
+        if not fine:
+            _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
+                            ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, batch),
+                            ("num_committed", num_committed, _I32, batch), ("next_anchor", next_anchor, _I32, batch))
         kind = _logits_type(logits_stride_row, ar_logits)
         _check_logits_rows("ar_logits", ar_logits, rows, p.vocab, logits_stride_row)
         if k_blk_ar is not None and v_blk_ar is not None:
@@ -403,18 +438,22 @@ class DecodeStep:
         """Puts logits [batch, rows, vocab] (or [batch, vocab]) through their requests' LogitRules: in place, or into `out`.  tokens
         [batch, rows] are those fed at the rows and parents [batch, rows] the row that each follows (None: the one before it); they
         count as written on the way to a row.  Rows are dense or the given numbers of elements apart."""
-        p, rows = self.params, 1 if logits.dim() == 2 else logits.shape[1]
-        if logits.shape[0] != p.batch or logits.dim() not in (2, 3):
-            raise ValueError("logits must be [batch, rows, vocab] or [batch, vocab], not %s" % (tuple(logits.shape),))
-        if out is None:
-            out, out_stride_row = logits, logits_stride_row
+        p, shape = self.params, logits.shape
+        batch, rows = p.batch, 1 if len(shape) == 2 else shape[1]
+        if shape[0] != batch or len(shape) not in (2, 3):
+            raise ValueError("logits must be [batch, rows, vocab] or [batch, vocab], not %s" % (tuple(shape),))
         kind = _logits_type(logits_stride_row, logits)
-        if _logits_type(out_stride_row, out) != kind:
-            raise ValueError("out must be of the logits' type")
-        _check_logits_rows("logits", logits, p.batch * rows, p.vocab, logits_stride_row)
-        _check_logits_rows("out", out, p.batch * rows, p.vocab, out_stride_row)
-        _check_operands(("tokens", tokens, _I32, p.batch * rows), ("parents", parents, _I32, p.batch * rows))
-        rules.check(p.batch, rows, p.vocab)
+        _check_logits_rows("logits", logits, batch * rows, p.vocab, logits_stride_row)
+        if out is None or out is logits:
+            out, out_stride_row = logits, out_stride_row if out is logits else logits_stride_row
+        else:
+            if _logits_type(out_stride_row, out) != kind:
+                raise ValueError("out must be of the logits' type")
+            _check_logits_rows("out", out, batch * rows, p.vocab, out_stride_row)
+        if tokens is not None or parents is not None:
+            _check_operands(("tokens", tokens, _I32, batch * rows), ("parents", parents, _I32, batch * rows))
+        if rules.checked != (batch, rows, p.vocab):
+            rules.check(batch, rows, p.vocab)
         return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row,
                                         self._stream(stream))
 
