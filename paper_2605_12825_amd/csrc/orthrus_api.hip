@@ -1080,6 +1080,7 @@ orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p,
     a.repetition = r.repetition; a.presence = r.presence; a.frequency = r.frequency;
     a.bias_starts = r.bias_starts; a.bias_tokens = r.bias_tokens; a.bias_values = r.bias_values; a.num_biases = r.num_biases;
     a.masks = r.masks; a.mask_rows = r.mask_rows; a.num_masks = r.num_masks; a.mask_stride = r.mask_stride ? r.mask_stride : words;
+    a.err_word = ctx->err_word;
     a.batch = p->batch; a.rows = num_rows; a.vocab = p->vocab; a.dtype = (int)logits_type;
     const OnDevice on(ctx->device);
     if (!on.ok) return ORTHRUS_EHIP;

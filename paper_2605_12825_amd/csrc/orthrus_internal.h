@@ -201,6 +201,7 @@ struct RulesArgs {
     const float *bias_values;
     const uint32_t *masks;
     const int32_t *mask_rows;
+    const int32_t *err_word;  // (four readable bytes)
     int64_t num_biases, num_masks, mask_stride;
     int batch, rows, rows_per_wg, vocab, dtype, in_place;
 };
@@ -340,7 +341,7 @@ bool kv_store_fits(int rows, int num_kv_heads, int head_dim);
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
 size_t tree_best_bytes(int batch, int nodes, int vocab);
 hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream);
-hipError_t launch_logits_process(RulesArgs a, int num_cus, hipStream_t stream);
+hipError_t launch_logits_process(const RulesArgs &a, int num_cus, hipStream_t stream);
 int consensus_chunk_elems();
 int draw_chunk_elems();
 // Static device scratch of the allocation-free consensus entry point: looked up once per device (with
