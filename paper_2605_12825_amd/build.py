@@ -15,7 +15,7 @@ LIB = os.path.join(_HERE, "liborthrus.so")
 LIB_HOST_UBSAN = os.path.join(_HERE, "liborthrus_hostubsan.so")
 HOST_UBSAN_FLAGS = ["-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fsanitize-trap=undefined",
                     "-Xarch_host", "-fno-omit-frame-pointer"]
-SOURCES = ["orthrus_api.hip", "orthrus_attn.hip", "orthrus_attn_forms.hip", "orthrus_attn_wide.hip", "orthrus_attn_tree.hip",
+SOURCES = ["orthrus_api.hip", "orthrus_attn.hip", "orthrus_attn_forms.hip", "orthrus_attn_wide.hip", "orthrus_attn_tree.hip", "orthrus_attn_tree_wide.hip",
            "orthrus_consensus.hip",
            "orthrus_sampling.hip", "orthrus_prefill.hip", "orthrus_filters.hip", "orthrus_tables.hip",
            "orthrus_tree.hip", "orthrus_rules.hip"]
@@ -33,7 +33,8 @@ HIPCC_FLAGS = [
 # Per-source additions.  attn_wide: the matrix products of that kernel keep scores and accumulators in plain vector
 # registers (the default moves every product's result to the accumulation file and copies the scores back: 32 extra
 # instructions per tile).
-SOURCE_FLAGS = {"orthrus_attn_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+SOURCE_FLAGS = {"orthrus_attn_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+                "orthrus_attn_tree_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc_path() -> str:

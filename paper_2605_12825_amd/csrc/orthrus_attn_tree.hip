@@ -8,6 +8,8 @@
 //     16 bit tests; the cache's tiles cost nothing more than a chain's;
 //   - up to 64 nodes, in one or two tiles behind the cache's;
 //   - more than 256 query rows (group x nodes) in two workgroups that each stream the cache.
+// Launches with rows and units enough to be bound by the products run the 64-row kernel (orthrus_attn_tree_wide.hip), by the rule
+// of the chains (attn_wide_pays).
 #include "orthrus_attn_dev.h"
 
 namespace orthrus {
@@ -136,16 +138,16 @@ hipError_t plan_tree_attn(int head_dim, int group, int nodes, int batch, int num
     const int blocks = (group * nodes + 31) / 32;
     const int most = tree_blocks(requested_splits < 0);
     const int groups = (blocks + most - 1) / most;
-    const int rows = 32 * ((blocks + groups - 1) / groups);    // of one of them
+    const int rows = groups == 1 ? group * nodes : 32 * ((blocks + groups - 1) / groups);  // of one of them
     *row_groups = groups;
     const hipError_t e = plan_attn(head_dim, 1, rows, batch, num_kv_heads * groups, max_seq_len, requested_splits, num_cus,
-                                   num_layers, pool_tokens, plan, false);
-    plan->lds_bytes += kTreePathBytes;
+                                   num_layers, pool_tokens, plan);
+    if (!plan->wide) plan->lds_bytes += kTreePathBytes;
     if (plan->bal_wgs > 0) {  // resident at once, two partial slots each
         const int by_waves = 4 * tree_waves(kItemsBalanced) / (plan->waves + 1), by_lds = (int)(160 * 1024 / plan->lds_bytes);
         plan->bal_wgs = num_cus * (by_waves < by_lds ? by_waves : by_lds);
-        plan->part_o_bytes = (size_t)plan->bal_wgs * 2 * rows * head_dim * sizeof(float);
-        plan->part_ml_bytes = (size_t)plan->bal_wgs * 2 * rows * 2 * sizeof(float);
+        plan->part_o_bytes = (size_t)plan->bal_wgs * 2 * plan->rows_padded * head_dim * sizeof(float);
+        plan->part_ml_bytes = (size_t)plan->bal_wgs * 2 * plan->rows_padded * 2 * sizeof(float);
     }
     if (groups > 1) plan->kv_nt = 0;  // the cache's rows are read again by the next group of a head
     return e;
@@ -170,6 +172,7 @@ static hipError_t launch_tree_d(const AttnArgs &a, const AttnPlan &plan, hipStre
     const bool bal = plan.bal_wgs > 0;
     const unsigned units = (unsigned)a.batch * (unsigned)a.num_kv_heads;
     const dim3 grid(bal ? (unsigned)plan.bal_wgs : units * (unsigned)plan.num_splits);
+    if (plan.wide) return launch_tree_wide(a, plan, D, grid, stream);  // (never split)
     hipError_t e = hipErrorInvalidValue;
     switch (plan.waves) {
     case 1: e = launch_tree_w<D, 1>(a, plan, grid, stream); break;

@@ -24,433 +24,21 @@
 // 478 -> 456; ragged prefill at 28/4 heads 325 -> 300; training mask 623 -> 598.  (attn_split_kernel's form: 675, 400 and 864
 // for the last three.  With the chunks ranked over all sequences the ragged prefill takes 250 to 280 by the order of the
 // lengths, with 16-byte stores the mask 570 to 602 from one card to another.)
-#include "orthrus_attn_dev.h"
-
-#include <utility>
+#include "orthrus_attn_wide_dev.h"
 
 namespace orthrus {
-
-template <int... S, class F>
-__device__ __forceinline__ void for_each_stage(std::integer_sequence<int, S...>, F &&f)
-{
-    (f(std::integral_constant<int, S>{}), ...);
-}
 
 // D head_dim, W waves of 64 query rows, NS LDS stages, MODE the work items (not kItemsBalanced), NT the
 // non-temporal form of the tile loads.
 template <int D, int W, int NS, int MODE, int NT = 0>
 __global__ void __launch_bounds__(64 * W, 1) attn_wide_kernel(ATTN_FIRST_PARAMS, const AttnArgs rest)
 {
-    const AttnArgs a = with_first(rest, first_lens, first_batch);
-    using Gm = AttnGeom<D>;
-    constexpr int CH = Gm::CH, ROWB = Gm::ROWB, RPI = Gm::RPI, NI = Gm::NI, GS = Gm::GS;
-    constexpr int TILE_B = Gm::TILE_B, STAGE_B = Gm::STAGE_B, KSTEPS = Gm::KSTEPS, DBLK = Gm::DBLK;
-    constexpr int LPW = 2 * NI / W;  // load instructions per tile and wave
-    static_assert(2 * NI % W == 0, "the waves share a tile's loads evenly");
-    constexpr int PG = 4 / W;  // of a tile's four 16-token halves (K, K, V, V), how many a wave loads
-    static_assert(W == 2 || W == 4, "a wave's halves stay within one operand");
-    static_assert(NS >= 4 && (NS - 3) * LPW < 64, "stage count");
-    static_assert(MODE != kItemsBalanced, "one work item per workgroup");
-    constexpr bool PREFILL = MODE == kItemsPrefill;
-    using NtTag = std::integral_constant<bool, NT != 0>;
-
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, h = lane >> 5;
-    const int K = a.block_k, G = a.group;
-    const int P = 1 << a.page_shift;
-    const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
-
-    WorkItems<MODE> w;
-    w.start(a);
-    if (!w.open(a, true)) return;
-
-    // ---- tile loads: a tile is four 16-token halves (K, K, V, V) and a wave loads PG of them, both of one operand
-    const int ld_tok = lane / CH;  // this lane's row inside one wave-wide load, and the byte offset of its chunk in that row
-    const uint32_t ld_swz = (uint32_t)(((lane % CH) ^ xm<CH>(ld_tok)) << 4);
-    HalfLoads<D> half(a, lane);
-    const int my_half = wave * PG % 2;
-    const bool my_v = wave * PG >= 2;
-    const uint32_t my_dst = (my_v ? TILE_B : 0) + my_half * half.GPH * GS;
-    const uint32_t dst_first = smem_lds + my_dst, dst_end = dst_first + NS * STAGE_B;
-    const uint16_t *my_operand = (my_v ? a.v_pool : a.k_pool) + w.head_off;
-    const char *my_pool = half.lowered(my_operand);
-    uint32_t worst = 0;  // largest page id that this lane has fetched
-    const int n_whole = half.usable ? min(w.n_cache, (w.t_end - w.t_begin) >> 5) : 0;  // tiles loaded a half at a time
-    uint32_t dst = dst_first;                                     // where the next tile to be issued goes
-    uint32_t page_at = (uint32_t)(w.t_begin + my_half * 16);      // token position of this wave's first half of that tile
-    auto advance = [&]() __attribute__((always_inline)) {
-        dst = dst + STAGE_B == dst_end ? dst_first : dst + STAGE_B;
-        page_at += 32;
-    };
-    // Where the halves of 64 whole tiles start in memory, a tile to a lane: one vector load and a few vector
-    // instructions for 64 tiles, and two lane reads for a half when it is issued.  (A scalar load of the page id and the
-    // address arithmetic on it were 24 of the ~105 instructions that a tile costs next to its products and softmax.)
-    uint32_t at_lo[PG], at_hi[PG];
-    int win = 0;  // tile of lane 0
-    auto open_window = [&](int t) __attribute__((always_inline)) {
-        win = t;
-        const uint32_t tok = (uint32_t)(w.t_begin + min(t + lane, n_whole - 1) * 32 + my_half * 16);
-        uint32_t id[PG];
-#pragma unroll
-        for (int u = 0; u < PG; ++u) id[u] = (uint32_t)((const int32_t *)w.pt_row)[(tok + u * 16u) >> a.page_shift];
-        // one wait for all of them: the compiler's wait for an id counts its own loads only, so that one behind a tile
-        // load would wait for the tile as well
-        if constexpr (PG == 2) asm volatile("" : "+v"(id[0]), "+v"(id[PG - 1]));
-#pragma unroll
-        for (int u = 0; u < PG; ++u) {
-            worst = max(worst, id[u]);
-            const uint64_t at = (uint64_t)(uintptr_t)my_pool + (uint64_t)(id[u] < half.num_pages ? id[u] : 0u) * half.page_bytes +
-                                ((tok + u * 16u) & half.page_mask) * half.tok_bytes;
-            at_lo[u] = (uint32_t)at;
-            at_hi[u] = (uint32_t)(at >> 32);
-        }
-    };
-    auto half_base = [&](int u, int t) __attribute__((always_inline)) {
-        return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_lo[u], t - win) |
-                              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi[u], t - win) << 32);
-    };
-    // any tile t, outside the main loop
-    auto issue_tile = [&](int t) __attribute__((always_inline)) {
-        if (t < n_whole) {
-            int page[PG];
-#pragma unroll
-            for (int u = 0; u < PG; ++u) page[u] = w.pt_row[(page_at + u * 16u) >> a.page_shift];
-#pragma unroll
-            for (int u = 0; u < PG; ++u)
-                half.issue(NtTag{}, my_pool + half.offset(page[u], page_at + u * 16u), dst + u * half.GPH * GS);
-        } else if (PREFILL || t < w.n_cache) {
-            // the last, ragged cache tile: rows past the end repeat the last valid row (finite data, masked later), so
-            // nothing is fetched through an unmapped page and no LDS row is left undefined
-#pragma unroll 1
-            for (int e = 0; e < PG * half.GPH; ++e) {
-                const int tg = min((int)page_at + e * RPI + ld_tok, w.t_end - 1);
-                const int first = min((int)page_at + e * RPI / 16 * 16, w.t_end - 1);
-                const uint32_t id = (uint32_t)w.pt_row[first >> a.page_shift];  // (a load's rows lie in one page)
-                half.worst = max(half.worst, id);
-                const int64_t off = (int64_t)(id < half.num_pages ? id : 0u) * a.stride_page + (int64_t)(tg & (P - 1)) * a.stride_tok;
-                dma16(NtTag{}, my_operand + off + (ld_swz >> 1), dst + e * GS);
-            }
-        } else {
-            // the in-block tile; rows past the block repeat its last row
-            const uint16_t *blk = (my_v ? a.v_blk : a.k_blk) + (int64_t)w.b * K * a.blk_stride_row + (int64_t)w.g * a.blk_stride_head;
-#pragma unroll 1
-            for (int e = 0; e < PG * half.GPH; ++e)
-                dma16(NtTag{}, blk + (int64_t)min(my_half * 16 + e * RPI + ld_tok, K - 1) * a.blk_stride_row + (ld_swz >> 1), dst + e * GS);
-        }
-        advance();
-    };
-
-    // ---- lane-invariant LDS read offsets inside one stage
-    int kb[KSTEPS / 2];
-    {
-        const int r = col % RPI;
-#pragma unroll
-        for (int q = 0; q < KSTEPS / 2; ++q)
-            kb[q] = (col / RPI) * GS + r * ROWB + ((q ^ (xm<CH>(r) >> 2)) << 6) + (h << 4);
-    }
-    int vb[DBLK];
-    {
-        const int tok0 = 4 * h + ((lane & 15) >> 2);
-        const int r = tok0 % RPI;
-        const int tr_ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-        for (int db = 0; db < DBLK; ++db)
-            vb[db] = TILE_B + (tok0 / RPI) * GS + r * ROWB + ((db ^ (xm<CH>(r) >> 2)) << 6) + (tr_ch << 4) + ((lane & 1) << 3);
-    }
-    const float c = a.scale_log2e;
-    // ---- pipeline fill (the page ids of the whole fill in one round trip)
-    if (n_whole >= NS - 1) {
-        open_window(0);
-#pragma unroll
-        for (int t = 0; t < NS - 1; ++t) {
-#pragma unroll
-            for (int u = 0; u < PG; ++u) half.issue(NtTag{}, half_base(u, t), dst + u * half.GPH * GS);
-            advance();
-        }
-    } else {
-#pragma unroll 1
-        for (int t = 0; t < NS - 1; ++t)
-            if (t < w.n_tiles) issue_tile(t);
-    }
-
-    // ---- queries: block x holds rows wave*64 + 32*x + col
-    Frag qf[2][KSTEPS];
-    int irow[2];
-    bool row_ok[2];
-    const int64_t row_base = PREFILL ? (int64_t)w.b * a.max_new + w.row0 : (int64_t)w.b * K;
-    const int rows = w.rows_live * G;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int ridx = wave * 64 + x * 32 + col;
-        row_ok[x] = ridx < rows;
-        const int i = ridx / G, hl = ridx - i * G;
-        irow[x] = row_ok[x] ? i : w.rows_live - 1;
-        if (row_ok[x]) {
-            const uint16_t *qp = a.q + (row_base + i) * a.q_stride_row + ((int64_t)w.g * G + hl) * a.q_stride_head;
-#pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) qf[x][kk].u = *(const uint4 *)(qp + kk * 16 + h * 8);
-        } else {
-#pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) qf[x][kk].u = make_uint4(0, 0, 0, 0);
-        }
-    }
-    // tiles of this wave: n_full that every row sees whole, n_mine that any row sees
-    int n_full, n_mine;
-    if constexpr (PREFILL) {
-        const int i0 = wave * 64 / G;
-        const int i1 = min((wave * 64 + 63) / G, w.rows_live - 1);
-        n_full = i0 < w.rows_live ? (w.pos0 + i0 + 1) >> 5 : 0;
-        n_mine = i0 < w.rows_live ? ((w.pos0 + i1) >> 5) + 1 : 0;
-    } else {
-        n_full = (w.t_end - w.t_begin) >> 5;
-        n_mine = w.n_tiles;
-    }
-    auto limit = [&](int x, int i) __attribute__((always_inline)) -> int {
-        if constexpr (PREFILL) return w.pos0 + irow[x] + 1 - i * 32;
-        if (i < w.n_cache) return w.t_end - (w.t_begin + i * 32);
-        return a.view == 0 ? K : min(K, irow[x] + 1);
-    };
-
-    f32x16 o[2][DBLK], s[2];
-    float m[2], l[2];
-    Frag kf[KSTEPS], vf[DBLK][2], p[2][2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        m[x] = kNegBig;
-        l[x] = 0.f;
-        p[x][0].u = p[x][1].u = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[x][r] = -INFINITY;
-#pragma unroll
-        for (int db = 0; db < DBLK; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[x][db][r] = 0.f;
-    }
-    // LDS reads at a stage that is known when the kernel is compiled (S >= 0): the stage is part of the instruction's
-    // 16-bit offset, from one of two bases; at any other stage: an add per base.
-    constexpr int SPB = 3;  // stages behind one base
-    static_assert(NS <= 2 * SPB && SPB * STAGE_B <= 65536, "");
-    uint32_t ka[2][KSTEPS / 2], va[2][DBLK];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-        for (int q = 0; q < KSTEPS / 2; ++q) {
-            ka[u][q] = smem_lds + u * SPB * STAGE_B + kb[q];
-            asm("" : "+v"(ka[u][q]));
-        }
-#pragma unroll
-        for (int db = 0; db < DBLK; ++db) {
-            va[u][db] = smem_lds + u * SPB * STAGE_B + vb[db];
-            asm("" : "+v"(va[u][db]));
-        }
-    }
-    auto read_k = [&](auto stage, uint32_t st, int kk) __attribute__((always_inline)) {
-        constexpr int S = decltype(stage)::value;
-        uint32_t ad;
-        if constexpr (S >= 0) {
-            ad = ka[S / SPB][kk >> 1] + S % SPB * STAGE_B;
-        } else {
-            ad = st + kb[kk >> 1];
-            asm("" : "+v"(ad));
-        }
-        kf[kk].n = *(const lds_u32x4 *)(uintptr_t)(ad + ((kk & 1) << 5));
-    };
-    auto read_v = [&](auto stage, uint32_t st, int db, int q2) __attribute__((always_inline)) {
-        constexpr int S = decltype(stage)::value;
-        uint32_t ad;
-        if constexpr (S >= 0) {
-            ad = va[S / SPB][db] + S % SPB * STAGE_B;
-        } else {
-            ad = st + vb[db];
-            asm("" : "+v"(ad));
-        }
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-            vf[db][q2].h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4 *)(uintptr_t)(ad + (2 * q2 + q) * (8 / RPI) * GS));
-    };
-    using AnyStage = std::integral_constant<int, -1>;
-    constexpr int NCH = KSTEPS + 2 * DBLK;  // products of a slot
-    constexpr int VPC = 16 / NCH;           // softmax values handled next to each of them
-    // One slot: the matrix work of block C (scores of tile i, values of tile i-1) next to the softmax of the other
-    // block's last scores, one product and VPC values at a time.  `extra(j, after)` adds the waits that
-    // go in front of product j (after = false) and the loads that go behind it (after = true).
-    auto slot = [&](auto cb, auto masked, int lim, auto &&extra) __attribute__((always_inline)) {
-        constexpr int C = decltype(cb)::value, X = 1 - C;
-        f32x16 z;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) z[r] = 0.f;
-        float e[16], sum = 0.f;
-        f32x16 t;
-        uint32_t pk[8];
-        const float mref = m[X];
-#pragma unroll
-        for (int j = 0; j < NCH; ++j) {
-            extra(j, std::integral_constant<bool, false>{});
-            if (j < KSTEPS) {
-                z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j].v, qf[C][j].v, z, 0, 0, 0);
-            } else {
-                const int db = (j - KSTEPS) % DBLK, q2 = (j - KSTEPS) / DBLK;
-                o[C][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db][q2].v, p[C][q2].v, o[C][db], 0, 0, 0);
-            }
-            extra(j, std::integral_constant<bool, true>{});
-#pragma unroll
-            for (int v = 0; v < VPC; ++v) {
-                const int r = j * VPC + v;
-                t[r] = s[X][r];
-                if constexpr (decltype(masked)::value) {
-                    const int tok = 8 * (r >> 2) + 4 * h + (r & 3);
-                    t[r] = tok >= lim ? -INFINITY : t[r];
-                }
-                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[r], c, -mref));
-                if (r == 1) sum = e[0];
-                else if (r > 1) sum += e[r - 1];
-                if ((r & 1) && r >= 3) pk[(r - 3) / 2] = pack_bf16(e[r - 3], e[r - 2]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        sum += e[15];
-        pk[7] = pack_bf16(e[14], e[15]);
-        asm volatile("" : "+v"(sum), "+v"(pk[0]), "+v"(pk[1]), "+v"(pk[2]), "+v"(pk[3]), "+v"(pk[4]), "+v"(pk[5]), "+v"(pk[6]), "+v"(pk[7]));
-        float alpha;
-        if (__builtin_expect(may_outgrow(sum), 0) && move_reference(t, c, m[X], e, sum, alpha)) {
-            l[X] *= alpha;
-#pragma unroll
-            for (int db = 0; db < DBLK; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[X][db][r] *= alpha;
-#pragma unroll
-            for (int r = 1; r < 16; r += 2) pk[r / 2] = pack_bf16(e[r - 1], e[r]);
-        }
-        l[X] += sum;
-        p[X][0].u = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-        p[X][1].u = make_uint4(pk[4], pk[5], pk[6], pk[7]);
-        s[C] = z;
-    };
-    // The barrier inside tile i's step: tile i+1 has landed, the stage of tile i-1 is free and takes tile i+NS-1.
-    auto step_barrier = [&](int i) __attribute__((always_inline)) {
-        const int ahead = min(NS - 3, w.n_tiles - 2 - i);
-        if (ahead >= 3) wait_vmcnt<3 * LPW>();
-        else if (ahead == 2) wait_vmcnt<2 * LPW>();
-        else if (ahead == 1) wait_vmcnt<LPW>();
-        else wait_vmcnt<0>();
-        wg_barrier();
-        if (i + NS - 1 < w.n_tiles) issue_tile(i + NS - 1);
-    };
-    // The pipeline's first pass multiplies zero weights, where an infinite V would make NaN of the sums: it reads the V
-    // half of the last stage, which holds zeros until the barrier of the first step lets a tile into it.
-    const uint32_t last_v = smem_lds + (NS - 1) * STAGE_B + TILE_B;
-    for (int x = tid * 16; x < TILE_B; x += 64 * W * 16) *(lds_u32x4 *)(uintptr_t)(last_v + x) = u32x4{0, 0, 0, 0};
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    // tile 0 has landed
-    {
-        const int ahead = min(NS - 2, w.n_tiles - 1);
-        if (ahead >= 3) wait_vmcnt<3 * LPW>();
-        else if (ahead == 2) wait_vmcnt<2 * LPW>();
-        else if (ahead == 1) wait_vmcnt<LPW>();
-        else wait_vmcnt<0>();
-        wg_barrier();
-    }
-    uint32_t st = smem_lds, sv = smem_lds + (NS - 1) * STAGE_B;  // stages of tiles i and i-1
-    auto next = [&](uint32_t x) __attribute__((always_inline)) { return x + STAGE_B == smem_lds + NS * STAGE_B ? smem_lds : x + STAGE_B; };
-#pragma unroll
-    for (int kk = 0; kk < KSTEPS; ++kk) read_k(std::integral_constant<int, 0>{}, st, kk);
-#pragma unroll
-    for (int db = 0; db < DBLK; ++db) vf[db][0].u = make_uint4(0, 0, 0, 0);
-    // One tile step.  The reads of a step go out well before their products, in two groups with one wait each (a wait in
-    // front of every product costs an issue slot each): next tile's keys as soon as this tile's last product with them is
-    // out, the first half of this tile's values (for the next step) behind them, the second half when the next step
-    // starts.  S >= 0: the ring stage of tile i, and the step issues the whole tile i+NS-1.
-    auto tile = [&](auto stage, auto masked, int i) __attribute__((always_inline)) {
-        constexpr int S = decltype(stage)::value;
-        constexpr bool FAST = S >= 0;
-        using Prev = std::integral_constant<int, FAST ? (S + NS - 1) % NS : -1>;
-        using Next = std::integral_constant<int, FAST ? (S + 1) % NS : -1>;
-        constexpr int JK = NCH == 16 ? 4 : 2;  // the first read of the next tile's keys
-        slot(std::integral_constant<int, 0>{}, masked, limit(1, i - 1), [&](int j, auto after) __attribute__((always_inline)) {
-            if constexpr (!decltype(after)::value) {
-                if (j == 0) __builtin_amdgcn_s_waitcnt(0xc07f | 2 * DBLK << 8);  // lgkmcnt: all but the values behind the keys
-                if (j == KSTEPS) __builtin_amdgcn_s_waitcnt(0xc07f);             // lgkmcnt(0)
-            } else if (j < DBLK) {
-                read_v(Prev{}, sv, j, 1);
-            }
-        });
-        uint64_t base[PG];
-        slot(std::integral_constant<int, 1>{}, masked, limit(0, i), [&](int j, auto after) __attribute__((always_inline)) {
-            if constexpr (!decltype(after)::value) return;
-            if constexpr (FAST) {
-                if (j == 0) {
-                    wait_vmcnt<(NS - 3) * LPW>();
-                    wg_barrier();
-#pragma unroll
-                    for (int u = 0; u < PG; ++u) {
-                        base[u] = (uint64_t)(uintptr_t)half_base(u, i + NS - 1);
-                        asm volatile("" : "+s"(base[u]));
-                    }
-                }
-                // the base was read from a lane two products ago, and nothing passes the scheduling barriers between
-                // them, so the load does without its own wait (training mask 593.3 -> 589.7 us, 8192 new tokens
-                // 455.6 -> 454.6)
-#pragma unroll
-                for (int u = 0; u < PG; ++u)
-                    if (j == 2 + u)
-                        half.template issue<true>(NtTag{}, (const char *)base[u], dst_first + Prev::value * STAGE_B + u * half.GPH * GS);
-            } else if (j == 0) {
-                step_barrier(i);
-                sv = st;
-                st = next(st);
-            }
-            if (j >= JK && j < JK + KSTEPS) read_k(Next{}, st, j - JK);
-            if (j >= NCH - DBLK) read_v(stage, sv, j - (NCH - DBLK), 0);
-        });
-    };
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0), lgkmcnt(0): queries and keys are in registers before the loop starts
-    int i = 0;
-    // steps that issue a whole tile and whose rows see all of theirs, a turn of the ring at a time
-    const int n_fast = min(n_full, n_whole - (NS - 1)) / NS * NS;
-    while (i < n_fast) {
-        if (i + 2 * NS - 2 - win >= 64) open_window(i + NS - 1);
-        for_each_stage(std::make_integer_sequence<int, NS>{},
-                       [&](auto stage) __attribute__((always_inline)) { tile(stage, std::false_type{}, i + decltype(stage)::value); });
-        i += NS;
-        page_at += 32 * NS;
-    }
-    for (; i < n_full; ++i) tile(AnyStage{}, std::false_type{}, i);
-    for (; i < n_mine; ++i) tile(AnyStage{}, std::true_type{}, i);
-    // drain: the last tile's value products (its second block's softmax in between)
-#pragma unroll
-    for (int db = 0; db < DBLK; ++db) read_v(AnyStage{}, sv, db, 1);
-    slot(std::integral_constant<int, 0>{}, std::true_type{}, limit(1, n_mine - 1), [](int, auto) {});
-#pragma unroll
-    for (int q2 = 0; q2 < 2; ++q2)
-#pragma unroll
-        for (int db = 0; db < DBLK; ++db)
-            o[1][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db][q2].v, p[1][q2].v, o[1][db], 0, 0, 0);
-    for (; i < w.n_tiles; ++i) step_barrier(i);
-
-    // ---- write-out (every workgroup holds all of its rows' keys)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const float lt = sum_with_other_half(l[x]);
-        if (!row_ok[x]) continue;
-        const int hl = wave * 64 + x * 32 + col - irow[x] * G;
-        const float inv = lt > 0.f ? 1.f / lt : 0.f;
-        uint16_t *op = a.out + ((row_base + irow[x]) * a.num_q_heads + (int64_t)w.g * G + hl) * D;
-        store_row<DBLK>(op, o[x], inv, h);
-        if (!PREFILL && a.lse && h == 0)
-            a.lse[((int64_t)w.b * a.num_q_heads + (int64_t)w.g * G + hl) * K + irow[x]] =
-                (m[x] + __builtin_amdgcn_logf(lt)) * 0.6931471805599453f;
-    }
-    if (max(worst, half.worst) >= half.num_pages) atomicExch(a.err_word, -4);
+    constexpr bool TREE = false;
+#include "orthrus_attn_wide.inc"
 }
 
 // ---------------------------------------------------------------------------------------------
 // host side
-
-// LDS ring stages: four waves have the CU's LDS to themselves, two workgroups of two waves share it
-constexpr int wide_stages(int W) { return W == 4 ? 6 : 4; }
 
 int attn_wide_per_cu(int waves) { return 4 / waves; }  // one wave per SIMD
 

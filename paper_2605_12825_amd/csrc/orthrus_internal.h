@@ -300,8 +300,7 @@ struct AttnLaunchEvents {
 
 // Host-side launchers (defined next to the kernels).  Return hipSuccess or the launch error.
 hipError_t plan_attn(int head_dim, int group, int block_k, int batch, int num_kv_heads, int max_seq_len,
-                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan,
-                     bool may_be_wide = true);
+                     int requested_splits, int num_cus, int num_layers, double pool_tokens, AttnPlan *plan);
 // Whether the items of a fixed-split launch start longest first; `items` workgroups of which per_cu are resident on a CU at once.
 bool decode_by_size(int batch, int64_t items, int per_cu, int num_cus);
 // What the kernels make of a batch's lengths: 0 to be ranked, 1 alike, 2 rising, 3 falling.  `small_counts`: the 64-row kernel.
@@ -327,6 +326,7 @@ hipError_t launch_prefill_attn(const AttnArgs &a, int head_dim, int num_cus, hip
 // Attention of a tree of drafts: the plan, whose rows are those of one of `row_groups` workgroups of a (sequence, KV head), and the launch.
 hipError_t plan_tree_attn(int head_dim, int group, int nodes, int batch, int num_kv_heads, int max_seq_len, int requested_splits,
                           int num_cus, int num_layers, double pool_tokens, AttnPlan *plan, int *row_groups);
+hipError_t launch_tree_wide(const AttnArgs &a, const AttnPlan &plan, int head_dim, dim3 grid, hipStream_t stream);
 hipError_t launch_tree_attn(const AttnArgs &a, const AttnPlan &plan, int head_dim, hipStream_t stream);
 hipError_t launch_prefill_split(const AttnArgs &a, int head_dim, int num_cus, hipStream_t stream);
 hipError_t launch_consensus(ConsensusArgs a, hipStream_t stream);

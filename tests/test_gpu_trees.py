@@ -320,3 +320,33 @@ def test_the_path_enters_every_layers_cache(layers, B, N, depth, V):
     got = _walk(x, parents, tokens, depth, kv=kv, table=table, lens=bad, P=P, layers=layers)
     want = _check_walk(x, parents, tokens, depth, got, kv, table, bad)
     assert want["status"] == -4 and want["num_committed"][0] == 0 and want["num_committed"][1] == 0
+
+
+@pytest.mark.parametrize("Hq,H,d,N,B,lo,hi", [(2, 2, 128, 56, 300, 128, 140), (2, 1, 128, 64, 520, 128, 170), (4, 1, 128, 64, 257, 1920, 1930),
+                                              (8, 1, 64, 32, 320, 520, 540), (4, 1, 64, 63, 257, 890, 920), (2, 1, 64, 64, 704, 250, 260),
+                                              (8, 1, 64, 64, 160, 512, 560)])
+def test_the_64_row_kernel(Hq, H, d, N, B, lo, hi):
+    """Launches that take it (units over CUs, rows that fill its waves, lengths from its rule on), both sides of its limits; a few of the
+    sequences, with lengths from none on, against the oracle, the other ones against the 32-row kernel at two splits."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(lo, hi + 1, B).astype(np.int32)
+    some = [0, 1, 7, B // 2, B - 1]
+    lens[some[:4]] = [0, 1, 33, 64]
+    pages = 400
+    x = dict(q=_bits(rng, B, N, Hq, d), k=_bits(rng, B, N, H, d), v=_bits(rng, B, N, H, d), kp=_bits(rng, pages, H, 16, d),
+             vp=_bits(rng, pages, H, 16, d), table=rng.integers(0, pages, (B, (hi + 15) // 16)).astype(np.int32), lens=lens)
+    parents = np.array([_tree(rng, N, 9, 0.1) for _ in range(B)], np.int64).astype(np.int32)
+    bad = x["v"].copy()
+    for b in range(0, B, 9):
+        for i in range(1, N):
+            if i not in oracle.tree_path(parents[b], i):
+                bad[b, i] = 0x7fc0
+    got, lse, err, step = _attn(dict(x, v=bad), parents, 0, 16, bound=hi)
+    assert err == 0
+    step.close()
+    part = {k: v if k in ("kp", "vp") else v[some] for k, v in x.items()}
+    _check_attn(part, parents[some], got[some], lse[some])
+    other, lse2, _, step = _attn(x, parents, 2, 16, bound=hi)
+    step.close()
+    # two roundings of each, of weights and outputs of order one
+    assert np.abs(got - other).max() <= 4 * U * max(1.0, np.abs(other).max()) and np.abs(lse - lse2).max() <= 2 * LSE_TOL
