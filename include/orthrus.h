@@ -497,7 +497,7 @@ typedef struct {
  *   out          [dev] like logits with out_stride_row: logits itself (with the same stride; only what changes is written), or memory
  *                apart from it
  * Arithmetic is fp32, every operation rounded once (frequency * n is subtracted in one), and rounded to the type at the end.
- * Supported: V <= 1048576.  Needs no workspace.
+ * Supported: V <= 1048576, B * R * ceil(V / 4096) below 2^24.  Needs no workspace.
  */
 orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p, orthrus_dtype logits_type, const void *logits,
                                       int64_t logits_stride_row, int32_t num_rows, const int32_t *tokens, const int32_t *parents,

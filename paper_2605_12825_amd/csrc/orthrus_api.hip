@@ -215,7 +215,9 @@ orthrus_status make_tree_plan(const orthrus_params *p, int num_nodes, int num_cu
     orthrus::plan_tree_attn(p->head_dim, group, num_nodes, p->batch, p->num_kv_heads, p->max_seq_len, p->num_splits, num_cus,
                             p->num_layers, (double)p->num_pages * p->page_size, &t->plan, &t->row_groups);
     const int64_t units = (int64_t)p->batch * p->num_kv_heads * t->row_groups;
-    if (t->plan.num_splits > 65535 * 16 || units * t->plan.num_splits * t->plan.waves * 4 > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
+    // a launch counts its threads in 32 bits
+    if (units * t->plan.num_splits * 64 * (t->plan.waves + 1) > 0xffffffffll || units * t->plan.waves * (p->head_dim / 32) * 256 > 0xffffffffll)
+        return ORTHRUS_EUNSUPPORTED;
     // the balanced partition counts one head's tiles in a 32-bit int
     if (t->plan.bal_wgs > 0 && (int64_t)p->batch * (p->max_seq_len / 32 + 3) > 0x7fffffff) return ORTHRUS_EUNSUPPORTED;
     return ORTHRUS_OK;
@@ -1067,6 +1069,7 @@ orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p,
     if (s == ORTHRUS_OK) s = check_logits(p, logits_type, (uintptr_t)out, out_stride_row, 0);
     if (s != ORTHRUS_OK) return s;
     if (num_rows > orthrus::kMaxNodes || p->vocab > (1 << 20)) return ORTHRUS_EUNSUPPORTED;
+    if ((int64_t)p->batch * num_rows * (((int64_t)p->vocab + 4095) / 4096) >= 1 << 24) return ORTHRUS_EUNSUPPORTED;  // what a launch counts
 
     orthrus::RulesArgs a = {};
     a.logits = logits; a.out = out;

@@ -309,7 +309,7 @@ hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream)
     if (a.max_path > a.nodes) a.max_path = a.nodes;
     const double bytes = (double)a.vocab * (a.dtype == 0 ? 4 : 2) * a.batch;
     const double all = a.nodes * bytes / 6.5e6, level = bytes / 6.5e6;  // us
-    a.walk = all > a.max_path * (level + 5.0);
+    a.walk = all > a.max_path * (level + 5.0);  // (more than the 2^24 workgroups that a launch counts would take 20 ms and are walked)
     return a.dtype == 0 ? launch_tree_sized<0>(a, stream) : a.dtype == 1 ? launch_tree_sized<1>(a, stream) : launch_tree_sized<2>(a, stream);
 }
 

@@ -439,9 +439,9 @@ class DecodeStep:
         [batch, rows] are those fed at the rows and parents [batch, rows] the row that each follows (None: the one before it); they
         count as written on the way to a row.  Rows are dense or the given numbers of elements apart."""
         p, shape = self.params, logits.shape
-        batch, rows = p.batch, 1 if len(shape) == 2 else shape[1]
-        if shape[0] != batch or len(shape) not in (2, 3):
+        if len(shape) not in (2, 3) or shape[0] != p.batch:
             raise ValueError("logits must be [batch, rows, vocab] or [batch, vocab], not %s" % (tuple(shape),))
+        batch, rows = p.batch, 1 if len(shape) == 2 else shape[1]
         kind = _logits_type(logits_stride_row, logits)
         _check_logits_rows("logits", logits, batch * rows, p.vocab, logits_stride_row)
         if out is None or out is logits:
