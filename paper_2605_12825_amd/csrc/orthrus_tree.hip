@@ -134,11 +134,12 @@ __global__ void __launch_bounds__(256) tree_level_kernel(const TreeArgs a, int l
     const int64_t half = (int64_t)a.batch * a.chunks;
     int node = 0;
     if (level > 0) {  // every wave finds it for itself
+        // (the maxima are read whether or not the path came to this level, so that all loads go out together)
         const Node mine(a, b);
+        const int t = key_index(row_max(a.best + ((level - 1) & 1) * half + (int64_t)b * a.chunks, a.chunks));
         const int before = __builtin_amdgcn_readfirstlane(a.level_node[(int64_t)b * kMaxNodes + level - 1]);
         node = -1;
         if (before >= 0) {
-            const int t = key_index(row_max(a.best + ((level - 1) & 1) * half + (int64_t)b * a.chunks, a.chunks));
             node = mine.child(before, t);
             if (chunk == 0 && tid == 0) a.level_token[(int64_t)b * kMaxNodes + level - 1] = t;
         }
@@ -167,7 +168,8 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
     const int b = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ int s_am[kMaxNodes], s_src[kMaxNodes], s_pg[kMaxNodes];
     __shared__ int s_m;
-    // loads that do not depend on the path go out first: the length, then the page ids of the positions that may be appended
+    // loads that do not depend on the path go out first: the tree, the length, then the page ids of the positions that may be appended
+    const Node mine(a, b);
     int L = 0, pg = -1;
     if (a.do_commit) {
         L = a.old_lens[b];
@@ -175,9 +177,23 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
         if (wave == 0 && lane < a.max_path && L >= 0 && slot < (uint32_t)a.max_pages_per_seq) pg = a.page_table[(int64_t)b * a.max_pages_per_seq + slot];
     }
     if (!a.walk) {
-        for (int i = wave; i < a.nodes; i += 4) {
-            const int t = key_index(row_max(a.best + ((int64_t)b * a.nodes + i) * a.chunks, a.chunks));
-            if (lane == 0) s_am[i] = t;
+        // wave w finishes rows w, w + 4, ..; every row's chunks are on their way before the first is looked at
+        constexpr int ROWS = kMaxNodes / 4;
+        unsigned long long key[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int i = wave + 4 * u;
+            key[u] = i < a.nodes && lane < a.chunks ? a.best[((int64_t)b * a.nodes + i) * a.chunks + lane] : 0ull;
+        }
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int i = wave + 4 * u;
+            if (i < a.nodes) {
+                const unsigned long long *row = a.best + ((int64_t)b * a.nodes + i) * a.chunks;
+                for (int c = lane + 64; c < a.chunks; c += 64) key[u] = key[u] > row[c] ? key[u] : row[c];
+                const int t = key_index(wave_max(key[u]));
+                if (lane == 0) s_am[i] = t;
+            }
         }
     }
     __syncthreads();
@@ -195,7 +211,6 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
             }
             if (lane >= m) token = -1;
         } else {
-            const Node mine(a, b);
             int node = 0;
             while (node >= 0 && m < a.max_path) {
                 const int t = s_am[node];

@@ -386,20 +386,26 @@ class DecodeStep:
         rows, d = p.batch * nodes, p.head_dim
         queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
         dense_q, dense = p.q_stride_row == 0 and p.q_stride_head == 0, p.blk_stride_row == 0 and p.blk_stride_head == 0
-        try:   # (what the calls below look at one after the other takes 3 us here)
-            fine = parents.dtype is _I32 and parents.numel() == rows and parents.is_contiguous() and \
-                q.nbytes == out.nbytes == 2 * queries and k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and \
-                (not dense_q or q.is_contiguous()) and (not dense or k_blk.is_contiguous() and v_blk.is_contiguous())
-        except AttributeError:   # (addresses)
-            fine = False
-        if not fine:
-            _check_operands(("parents", parents, _I32, rows))
-            _check_rows("q", q, queries, dense_q)
-            _check_rows("k_blk", k_blk, keys, dense)
-            _check_rows("v_blk", v_blk, keys, dense)
-            _check_rows("out", out, queries, True)
-        if lse is not None:
-            _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
+        try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
+            if parents.dtype is _I32 and parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
+                    k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and (not dense_q or q.is_contiguous()) and \
+                    (not dense or k_blk.is_contiguous() and v_blk.is_contiguous()) and \
+                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous()):
+                ws = self._tree_attn_ws(nodes)
+                st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
+                                              k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(),
+                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, B._stream_handle(self._stream(stream)))
+                if st != B.ORTHRUS_OK:
+                    raise B.OrthrusError(st, "orthrus_tree_attn")
+                return st
+        except AttributeError:   # (addresses among the operands)
+            pass
+        _check_operands(("parents", parents, _I32, rows))
+        _check_rows("q", q, queries, dense_q)
+        _check_rows("k_blk", k_blk, keys, dense)
+        _check_rows("v_blk", v_blk, keys, dense)
+        _check_rows("out", out, queries, True)
+        _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
         return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse,
                                    self._tree_attn_ws(nodes), self._stream(stream))
 
@@ -409,30 +415,40 @@ class DecodeStep:
         """Greedy consensus of a tree of drafts: from node 0 on to the child that holds the node's greedy token, for as long as there
         is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed."""
         p, nodes = self.params, parents.shape[1]
-        rows, batch = p.batch * nodes, p.batch
-        try:
-            fine = parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
-                parents.numel() == node_tokens.numel() == path_nodes.numel() == out_tokens.numel() == rows and \
-                accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
-                accept_len.numel() == num_committed.numel() == next_anchor.numel() == batch and parents.is_contiguous() and \
-                node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and \
-                accept_len.is_contiguous() and num_committed.is_contiguous() and next_anchor.is_contiguous()
-        except AttributeError:   # (addresses)
-            fine = False
-        if not fine:
-            _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
-                            ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, batch),
-                            ("num_committed", num_committed, _I32, batch), ("next_anchor", next_anchor, _I32, batch))
+        batch = p.batch
+        rows = batch * nodes
         kind = _logits_type(logits_stride_row, ar_logits)
         _check_logits_rows("ar_logits", ar_logits, rows, p.vocab, logits_stride_row)
+        size, dense = p.num_layers * rows * p.num_kv_heads * p.head_dim, p.blk_stride_row == 0 and p.blk_stride_head == 0 and p.blk_stride_layer == 0
+        longest = nodes if max_path is None else max_path
+        try:
+            if parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
+                    accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
+                    parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == 4 * rows and \
+                    accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and parents.is_contiguous() and \
+                    node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and accept_len.is_contiguous() and \
+                    num_committed.is_contiguous() and next_anchor.is_contiguous() and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * size and \
+                    (not dense or k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous()):
+                ws = self._tree_consensus_ws(nodes)
+                st = B._lib.orthrus_tree_consensus_commit(
+                    self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(), node_tokens.data_ptr(),
+                    k_blk_ar.data_ptr(), v_blk_ar.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
+                    accept_len.data_ptr(), num_committed.data_ptr(), path_nodes.data_ptr(), out_tokens.data_ptr(), next_anchor.data_ptr(),
+                    ws.data_ptr(), ws.nbytes, B._stream_handle(self._stream(stream)))
+                if st != B.ORTHRUS_OK:
+                    raise B.OrthrusError(st, "orthrus_tree_consensus_commit")
+                return st
+        except AttributeError:   # (addresses among the operands, or no rows to commit)
+            pass
+        _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
+                        ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, batch),
+                        ("num_committed", num_committed, _I32, batch), ("next_anchor", next_anchor, _I32, batch))
         if k_blk_ar is not None and v_blk_ar is not None:
-            size, dense = p.num_layers * rows * p.num_kv_heads * p.head_dim, p.blk_stride_row == 0 and p.blk_stride_head == 0 and p.blk_stride_layer == 0
             _check_rows("k_blk_ar", k_blk_ar, size, dense)
             _check_rows("v_blk_ar", v_blk_ar, size, dense)
-        return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, nodes if max_path is None else max_path,
-                                               parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len,
-                                               num_committed, path_nodes, out_tokens, next_anchor, self._tree_consensus_ws(nodes),
-                                               self._stream(stream))
+        return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
+                                               v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
+                                               next_anchor, self._tree_consensus_ws(nodes), self._stream(stream))
 
     def process_logits(self, logits, rules, tokens=None, parents=None, out=None, stream=None, logits_stride_row=0, out_stride_row=0):
         """Puts logits [batch, rows, vocab] (or [batch, vocab]) through their requests' LogitRules: in place, or into `out`.  tokens
@@ -450,7 +466,8 @@ class DecodeStep:
             if _logits_type(out_stride_row, out) != kind:
                 raise ValueError("out must be of the logits' type")
             _check_logits_rows("out", out, batch * rows, p.vocab, out_stride_row)
-        if tokens is not None or parents is not None:
+        if not (tokens is None or tokens.__class__ is not int and tokens.dtype is _I32 and tokens.nbytes == 4 * batch * rows and tokens.is_contiguous()) \
+                or parents is not None:
             _check_operands(("tokens", tokens, _I32, batch * rows), ("parents", parents, _I32, batch * rows))
         if rules.checked != (batch, rows, p.vocab):
             rules.check(batch, rows, p.vocab)
