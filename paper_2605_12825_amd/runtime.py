@@ -121,15 +121,22 @@ class LogitRules:
         for name in ("history", "history_lens", "prompt_lens", "repetition", "presence", "frequency", "bias_starts", "bias_tokens",
                      "bias_values", "masks", "mask_rows"):
             setattr(r, name, B._ptr(getattr(self, name)))
-        if history is not None and history.shape[1] == 0:   # nothing can stand in it
+        if history is not None and history.numel() == 0:   # nothing can stand in it
             r.history = r.history_lens = r.prompt_lens = None
+        if masks is not None and (masks.numel() == 0 or mask_rows.numel() == 0):   # no row has one
+            r.masks = r.mask_rows = None
         r.history_stride = 0 if history is None else history.shape[1]
         r.num_biases = 0 if bias_tokens is None else bias_tokens.numel()
-        r.num_masks, r.mask_stride = (0, 0) if masks is None else masks.shape
-        self.checked = None   # the batch, rows and vocabulary that they are known to fit
+        r.num_masks, r.mask_stride = masks.shape if r.masks else (0, 0)
+        self.checked = None   # the batch, rows, vocabulary and device that they are known to fit
 
-    def check(self, batch, rows, vocab) -> None:
-        """Refuses rules of another batch, block or vocabulary."""
+    def check(self, batch, rows, vocab, device=None) -> None:
+        """Refuses rules of another batch, block or vocabulary, or on another device."""
+        for name in ("history", "history_lens", "prompt_lens", "repetition", "presence", "frequency", "bias_starts", "bias_tokens",
+                     "bias_values", "masks", "mask_rows"):
+            t = getattr(self, name)
+            if t is not None and device is not None and t.device != device:
+                raise ValueError("%s must be on %s, not on %s" % (name, device, t.device))
         _check_operands(*((name, getattr(self, name), dtype, batch) for name, dtype in
                           (("history_lens", _I32), ("prompt_lens", _I32), ("repetition", _F32), ("presence", _F32), ("frequency", _F32))),
                         ("bias_starts", self.bias_starts, _I32, batch + 1), ("mask_rows", self.mask_rows, _I32, batch * rows))
@@ -139,7 +146,7 @@ class LogitRules:
             raise ValueError("mask_rows must name a mask for each of %d x %d rows, not %s" % (batch, rows, tuple(self.mask_rows.shape)))
         if self.masks is not None and self.masks.shape[1] < (vocab + 31) // 32:
             raise ValueError("masks must have %d words for %d tokens, not %d" % ((vocab + 31) // 32, vocab, self.masks.shape[1]))
-        self.checked = (batch, rows, vocab)
+        self.checked = (batch, rows, vocab, device)
 
 
 class DecodeStep:
@@ -469,8 +476,8 @@ class DecodeStep:
         if not (tokens is None or tokens.__class__ is not int and tokens.dtype is _I32 and tokens.nbytes == 4 * batch * rows and tokens.is_contiguous()) \
                 or parents is not None:
             _check_operands(("tokens", tokens, _I32, batch * rows), ("parents", parents, _I32, batch * rows))
-        if rules.checked != (batch, rows, p.vocab):
-            rules.check(batch, rows, p.vocab)
+        if rules.checked != (batch, rows, p.vocab, logits.device):
+            rules.check(batch, rows, p.vocab, logits.device)
         return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row,
                                         self._stream(stream))
 
@@ -588,7 +595,7 @@ class DecodeStack:
             self.node_tokens, self.path_nodes = torch.zeros_like(self.out_tokens), torch.zeros_like(self.out_tokens)
             self.step.reserve(tree_nodes=verified)
             if rules is not None:
-                rules.check(batch, verified, vocab)
+                rules.check(batch, verified, vocab, self.ar_logits.device)
         self.graph = None
         self.graph_stream = None
 

@@ -157,6 +157,58 @@ def test_biases_outside_the_list():
     _check(x, _run(x, rules, None, None, "f32"), "f32", rules, None, None)
 
 
+def test_long_texts_and_many_biases():
+    """Texts whose tokens may stand there more often than 15 bits count, and more biases than 16 bits number: two words a token."""
+    rng = np.random.default_rng(10)
+    B, V, hist = 3, 9000, 40000
+    x = torch.from_numpy(rng.standard_normal((B, 2, V)).astype(np.float32))
+    rules = _rules(rng, B, 2, V, hist=hist, bias=False)
+    rules["history"][0] = 8999
+    rules["history_lens"], rules["prompt_lens"] = np.array([hist, hist, 33000], np.int32), np.array([100, 39000, 0], np.int32)
+    rules["frequency"][:], rules["repetition"][:], rules["presence"][:] = 0.001, 1.2, 0.1
+    rules["mask_rows"][:] = -1
+    tokens = rng.integers(0, V, (B, 2)).astype(np.int32)
+    for biases in (False, True):
+        if biases:
+            rules["bias_starts"] = np.array([0, 66000, 66000, 70000], np.int32)
+            rules["bias_tokens"] = rng.integers(0, V, 70000).astype(np.int32)
+            rules["bias_values"] = rng.standard_normal(70000).astype(np.float32)
+        for in_place in (False, True):
+            want = _check(x, _run(x, rules, tokens, None, "f32", in_place=in_place), "f32", rules, tokens, None)
+    short = {k: v for k, v in rules.items() if k not in ("history", "history_lens", "prompt_lens")}   # biases alone ask for them too
+    _check(x, _run(x, short, tokens, None, "f32"), "f32", short, tokens, None)
+    assert want[0, 0, 8999] < -35
+
+
+@pytest.mark.parametrize("kind,in_place,pad", [("f32", False, 0), ("f32", True, 3), ("bf16", False, 1)])
+def test_more_logits_than_the_last_level_cache_holds(kind, in_place, pad):
+    """Several rows to a workgroup and accesses that go past the caches: the bits of the same sequences in small calls."""
+    rt = _rt()
+    rng = np.random.default_rng(11)
+    B, R, V = 32, 32, 150001
+    rules, tokens = _rules(rng, B, R, V, hist=500), rng.integers(0, V, (B, R)).astype(np.int32)
+    parents = np.array([[-1] + [int(rng.integers(0, i)) for i in range(1, R)] for _ in range(B)], np.int32)
+    make = lambda n: rt.DecodeStep(batch=n, num_q_heads=1, num_kv_heads=1, head_dim=64, block_k=1, page_size=16, max_pages_per_seq=1,  # noqa: E731
+                                   max_seq_len=0, num_pages=1, vocab=V)
+    x = torch.randn((B, R, V + pad), generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(_TYPES[kind][0])
+    part, big, small = {}, make(B), make(2)
+    for b in (0, 6, 30):
+        r = {k: v[b:b + 2] if k not in ("bias_starts", "bias_tokens", "bias_values", "masks") else v for k, v in rules.items()}
+        r["bias_starts"] = rules["bias_starts"][b:b + 3]
+        part[b] = torch.zeros((2, R, V + pad), dtype=x.dtype, device="cuda")
+        small.process_logits(x[b:b + 2], rt.LogitRules(**{k: _dev(v) for k, v in r.items()}), _dev(tokens[b:b + 2]), _dev(parents[b:b + 2]),
+                             out=part[b], logits_stride_row=V + pad, out_stride_row=V + pad)
+    out = None if in_place else torch.zeros_like(x)
+    big.process_logits(x, rt.LogitRules(**{k: _dev(v) for k, v in rules.items()}), _dev(tokens), _dev(parents), out=out, logits_stride_row=V + pad,
+                       out_stride_row=V + pad)
+    torch.cuda.synchronize()
+    words = torch.int32 if kind == "f32" else torch.int16
+    for b, want in part.items():
+        assert torch.equal((x if in_place else out)[b:b + 2, :, :V].view(words), want[..., :V].view(words)), b
+    big.close()
+    small.close()
+
+
 def test_many_rows_and_rules_on_two_streams_and_replayed():
     """Two calls at once, each in place on logits of its own, with tensors of rules shared; then the same from a graph, five times
     with eager work in between."""

@@ -128,6 +128,17 @@ def test_long_and_ragged_batches():
         step.close()
 
 
+def test_empty_caches():
+    for N in (1, 33, 64):
+        rng, x = _inputs(12, N, 4, 2, 64, [0, 0], 16)
+        parents = [_tree(rng, N) for _ in range(2)]
+        for splits in (0, 2, -1):
+            got, lse, err, step = _attn(x, parents, splits, 16)
+            assert err == 0
+            _check_attn(x, parents, got, lse)
+            step.close()
+
+
 def test_many_short_sequences_start_by_size():
     rng, x = _inputs(13, 8, 2, 2, 64, list(np.random.default_rng(3).integers(0, 60, 500)), 16)
     parents = [_tree(rng, 8, 4, 0.2) for _ in range(500)]

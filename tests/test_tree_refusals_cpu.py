@@ -1,6 +1,8 @@
 """Refusals of the tree and logit-rule entry points: found on the host before anything touches a device, so they are checked here with
 addresses that are never read (a call that were not refused would end in ORTHRUS_EHIP)."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -126,6 +128,17 @@ def test_logits_process(kw, status):
     assert _process(**kw) == status
 
 
+def test_rules_struct_matches_the_header():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "orthrus.h")).read()
+    end = text.index("} orthrus_logit_rules;")
+    body = re.sub(r"/\*.*?\*/", "", text[text.rindex("typedef struct {", 0, end):end], flags=re.S)
+    fields = re.findall(r"\b((?:const )?\w+) \*?([a-z_]+)\s*;", body)
+    assert [f[1] for f in fields] == [f[0] for f in B.orthrus_logit_rules._fields_]
+    for (kind, name), (_, ctype) in zip(fields, B.orthrus_logit_rules._fields_):
+        assert ctype is (ctypes.c_void_p if kind.startswith("const") else ctypes.c_int64), name
+
+
 def test_rules_of_the_wrong_kind_are_refused():
     i32, f32 = torch.zeros(4, dtype=torch.int32), torch.zeros(4)
     h = torch.zeros((4, 9), dtype=torch.int32)
@@ -140,7 +153,14 @@ def test_rules_of_the_wrong_kind_are_refused():
                      (dict(bias_starts=i32, bias_tokens=i32, bias_values=f32), (4, 1, 30))):
         with pytest.raises(ValueError):
             rt.LogitRules(**kw).check(*call)
+    with pytest.raises(ValueError):   # on another device than the logits
+        rt.LogitRules(repetition=f32).check(4, 1, 30, torch.device("cuda", 0))
+    rt.LogitRules(repetition=f32).check(4, 1, 30, f32.device)
     rt.LogitRules(masks=h, mask_rows=i32.view(2, 2)).check(2, 2, 288)
+    none = rt.LogitRules(history=h[:, :0].contiguous(), history_lens=i32, prompt_lens=i32, masks=h[:0], mask_rows=i32, bias_starts=i32,
+                         bias_tokens=i32[:0], bias_values=f32[:0])   # nothing in them: the same as without
+    assert not none.c.history and not none.c.history_lens and not none.c.prompt_lens and not none.c.masks and not none.c.mask_rows
+    assert _process(rules=none.c, p=_params(batch=0)) == B.ORTHRUS_OK
     rt.LogitRules(bias_starts=i32, bias_tokens=i32, bias_values=f32).check(3, 7, 30)
 
 
