@@ -7,6 +7,7 @@
 //   all    one launch over every node's row, where that is less than a launch per level.
 //   commit grid (sequence, layer): finishes the path, writes tokens and lengths (layer 0) and copies its rows' K/V.
 #include "orthrus_internal.h"
+#include "orthrus_lanes.h"
 
 #include <type_traits>
 
@@ -16,23 +17,24 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 // A logit and its place as one number whose order is that of the candidates: NaN above everything, then by value (both zeros
 // alike), among equals the lower index.  0 stands for no candidate.
-__device__ __forceinline__ unsigned long long argmax_key(float v, int index)
+__device__ __forceinline__ u64 argmax_key(float v, int index)
 {
     uint32_t u = __float_as_uint(v);
     u = u == 0x80000000u ? 0u : u;
     u = v != v ? 0xffffffffu : (u >> 31) ? ~u : u | 0x80000000u;
-    return (unsigned long long)u << 32 | (uint32_t)~index;
+    return (u64)u << 32 | (uint32_t)~index;
 }
-__device__ __forceinline__ int key_index(unsigned long long key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ int key_index(u64 key) { return (int)~(uint32_t)key; }
 
-__device__ __forceinline__ unsigned long long wave_max(unsigned long long x)
+__device__ __forceinline__ u64 larger(u64 x, u64 y) { return x > y ? x : y; }
+__device__ __forceinline__ u64 wave_largest(u64 x)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const unsigned long long y = __shfl_xor(x, off);
-        x = x > y ? x : y;
-    }
-    return x;
+    x = larger(x, swap_u64<kSwap1>(x));
+    x = larger(x, swap_u64<kSwap2>(x));
+    x = larger(x, swap_u64<kMirror8>(x));
+    x = larger(x, swap_u64<kMirror16>(x));
+    x = larger(x, __shfl_xor(x, 16));
+    return larger(x, __shfl_xor(x, 32));
 }
 
 template <int DTYPE>
@@ -45,7 +47,7 @@ __device__ __forceinline__ float logit_of(uint32_t bits)
 
 // The largest logit of elements [begin, begin + CE) of a row of V, as every thread of the workgroup's first wave has it.
 template <int DTYPE, int CE>
-__device__ __forceinline__ unsigned long long chunk_max(const void *row, int begin, int V)
+__device__ __forceinline__ u64 chunk_max(const void *row, int begin, int V)
 {
     using T = std::conditional_t<DTYPE == 0, uint32_t, uint16_t>;
     constexpr int VEC = 16 / sizeof(T), NL = CE / (256 * VEC);
@@ -64,7 +66,7 @@ __device__ __forceinline__ unsigned long long chunk_max(const void *row, int beg
             x[u] = __builtin_nontemporal_load((const u32x4_t *)(base + mid) + u * 256 + tid);
     }
     const int edge = tid < VEC ? (tid < head ? begin + tid : end) : tid < 2 * VEC ? tail + tid - VEC : end;
-    unsigned long long best = edge < end ? argmax_key(logit_of<DTYPE>(base[edge]), edge) : 0ull;
+    u64 best = edge < end ? argmax_key(logit_of<DTYPE>(base[edge]), edge) : 0ull;
     // a thread's own candidates come in the order of their index: a later one only wins by more, and nothing wins over a NaN
     // (nor does the -inf behind the end win over the first)
     float bv = 0.f;
@@ -85,24 +87,24 @@ __device__ __forceinline__ unsigned long long chunk_max(const void *row, int beg
         }
     }
     if (bi >= 0) {
-        const unsigned long long key = argmax_key(bv, bi);
-        best = best > key ? best : key;
+        const u64 key = argmax_key(bv, bi);
+        best = larger(best, key);
     }
-    best = wave_max(best);
-    __shared__ unsigned long long part[4];
+    best = wave_largest(best);
+    __shared__ u64 part[4];
     if ((tid & 63) == 0) part[tid >> 6] = best;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) best = best > part[w] ? best : part[w];
+    for (int w = 0; w < 4; ++w) best = larger(best, part[w]);
     return best;
 }
 
 // The maximum over a row's chunks, in every lane.
-__device__ __forceinline__ unsigned long long row_max(const unsigned long long *best, int chunks)
+__device__ __forceinline__ u64 row_max(const u64 *best, int chunks)
 {
-    unsigned long long key = 0;
-    for (int c = threadIdx.x & 63; c < chunks; c += 64) key = key > best[c] ? key : best[c];
-    return wave_max(key);
+    u64 key = 0;
+    for (int c = threadIdx.x & 63; c < chunks; c += 64) key = larger(key, best[c]);
+    return wave_largest(key);
 }
 
 // What lane i knows of node i: the node that it follows (-1: none) and its token.
@@ -121,7 +123,7 @@ struct Node {
     // the first child of `node` with that token, -1: none
     __device__ __forceinline__ int child(int node, int t) const
     {
-        const unsigned long long hit = __ballot(up == node && token == t);
+        const u64 hit = __ballot(up == node && token == t);
         return hit ? __builtin_ctzll(hit) : -1;
     }
 };
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(256) tree_level_kernel(const TreeArgs a, int l
     if (chunk == 0 && tid == 0) a.level_node[(int64_t)b * kMaxNodes + level] = node;
     if (node < 0) return;
     const char *row = (const char *)a.logits + ((int64_t)b * a.nodes + node) * a.stride_row * (DTYPE == 0 ? 4 : 2);
-    const unsigned long long best = chunk_max<DTYPE, CE>(row, chunk * CE, a.vocab);
+    const u64 best = chunk_max<DTYPE, CE>(row, chunk * CE, a.vocab);
     if (tid == 0) a.best[(level & 1) * half + (int64_t)b * a.chunks + chunk] = best;
 }
 
@@ -159,7 +161,7 @@ __global__ void __launch_bounds__(256) tree_scan_kernel(const TreeArgs a)
 {
     const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
     if (a.do_commit && threadIdx.x == 0 && chunk == 0 && row % a.nodes == 0) a.old_lens[row / a.nodes] = a.seq_lens[row / a.nodes];
-    const unsigned long long best = chunk_max<DTYPE, CE>((const char *)a.logits + (int64_t)row * a.stride_row * (DTYPE == 0 ? 4 : 2), chunk * CE, a.vocab);
+    const u64 best = chunk_max<DTYPE, CE>((const char *)a.logits + (int64_t)row * a.stride_row * (DTYPE == 0 ? 4 : 2), chunk * CE, a.vocab);
     if (threadIdx.x == 0) a.best[(int64_t)row * a.chunks + chunk] = best;
 }
 
@@ -179,7 +181,7 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
     if (!a.walk) {
         // wave w finishes rows w, w + 4, ..; every row's chunks are on their way before the first is looked at
         constexpr int ROWS = kMaxNodes / 4;
-        unsigned long long key[ROWS];
+        u64 key[ROWS];
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
             const int i = wave + 4 * u;
@@ -189,9 +191,9 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
         for (int u = 0; u < ROWS; ++u) {
             const int i = wave + 4 * u;
             if (i < a.nodes) {
-                const unsigned long long *row = a.best + ((int64_t)b * a.nodes + i) * a.chunks;
-                for (int c = lane + 64; c < a.chunks; c += 64) key[u] = key[u] > row[c] ? key[u] : row[c];
-                const int t = key_index(wave_max(key[u]));
+                const u64 *row = a.best + ((int64_t)b * a.nodes + i) * a.chunks;
+                for (int c = lane + 64; c < a.chunks; c += 64) key[u] = larger(key[u], row[c]);
+                const int t = key_index(wave_largest(key[u]));
                 if (lane == 0) s_am[i] = t;
             }
         }
@@ -289,7 +291,7 @@ constexpr int kTreeChunk = 8192, kTreeChunkFew = 2048;
 size_t tree_best_bytes(int batch, int nodes, int vocab)
 {
     const size_t rows = (size_t)batch * (nodes < 2 ? 2 : nodes);  // the walk has two levels
-    return rows * (((size_t)vocab + kTreeChunkFew - 1) / kTreeChunkFew) * sizeof(unsigned long long);
+    return rows * (((size_t)vocab + kTreeChunkFew - 1) / kTreeChunkFew) * sizeof(u64);
 }
 
 template <int DTYPE, int CE>
