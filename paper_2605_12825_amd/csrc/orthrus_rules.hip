@@ -150,9 +150,8 @@ __global__ void __launch_bounds__(256) logits_mask_kernel(const RulesArgs a)
     using T = typename Value<DTYPE>::T;
     constexpr int VEC = 16 / sizeof(T), U = 4;
     constexpr uint32_t kAll = (1u << VEC) - 1u;
-    const int parts = (a.vocab + 256 * VEC * U - 1) / (256 * VEC * U);
-    const int64_t row = blockIdx.x / (unsigned)parts;
-    const int first = (int)(blockIdx.x % (unsigned)parts) * (256 * VEC * U) + threadIdx.x * VEC, V = a.vocab;
+    const int64_t row = (int64_t)blockIdx.z * a.rows + blockIdx.y;
+    const int first = (int)blockIdx.x * (256 * VEC * U) + threadIdx.x * VEC, V = a.vocab;
     auto at = [&](int u) __attribute__((always_inline)) { return first + u * 256 * VEC; };
     uint32_t bits[U];
     if (!allowed_of<VEC>(a, row, V, bits, at) && IN_PLACE) return;
@@ -188,8 +187,15 @@ __global__ void __launch_bounds__(kRulesThreads, 8) logits_rules_kernel(const Ru
     uint32_t *biases = (uint32_t *)(s_path + kMaxNodes); // [kStretch], not PACKED and with biases: 1 + the entry's place in the list
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned stretches = (unsigned)(a.vocab + kStretch - 1) / kStretch, groups = (unsigned)(a.rows + a.rows_per_wg - 1) / (unsigned)a.rows_per_wg;
-    const int stretch = (int)(blockIdx.x % stretches), group = (int)(blockIdx.x / stretches % groups), b = (int)(blockIdx.x / (stretches * groups));
+    // The launch has an axis for each of these: divisions by their sizes are a tenth of a small workgroup's instructions (256 rows in bf16
+    // 48.0 -> 46.3 us).  In fp32 one axis: with three the compiler spills eight registers (1024 rows 222 -> 236 us).
+    int stretch = (int)blockIdx.x, group = (int)blockIdx.y, b = (int)blockIdx.z;
+    if constexpr (DTYPE == 0) {
+        const unsigned stretches = (unsigned)(a.vocab + kStretch - 1) / kStretch, groups = (unsigned)(a.rows + a.rows_per_wg - 1) / (unsigned)a.rows_per_wg;
+        stretch = (int)(blockIdx.x % stretches);
+        group = (int)(blockIdx.x / stretches % groups);
+        b = (int)(blockIdx.x / (stretches * groups));
+    }
     const int v0 = stretch * kStretch, v1 = min(a.vocab, v0 + kStretch);
     const int r0 = group * a.rows_per_wg, r1 = min(a.rows, r0 + a.rows_per_wg);
     const int64_t row0 = (int64_t)b * a.rows;
@@ -380,7 +386,7 @@ static hipError_t launch_rules(RulesArgs a, int num_cus, hipStream_t stream)
 {
     if (!a.repetition && !a.presence && !a.frequency && !a.bias_starts) {
         constexpr int PART = 256 * 4 * (DTYPE == 0 ? 4 : 8);
-        const dim3 grid((unsigned)(a.batch * a.rows) * (unsigned)((a.vocab + PART - 1) / PART));
+        const dim3 grid((unsigned)((a.vocab + PART - 1) / PART), (unsigned)a.rows, (unsigned)a.batch);
         hipLaunchKernelGGL((mask_kernel<DTYPE, NT>(a.in_place)), grid, dim3(256), 0, stream, a);
         return hipGetLastError();
     }
@@ -391,7 +397,7 @@ static hipError_t launch_rules(RulesArgs a, int num_cus, hipStream_t stream)
     while (a.rows_per_wg > 1 && (int64_t)a.batch * stretches * ((a.rows + a.rows_per_wg - 1) / a.rows_per_wg) < 32ll * num_cus)
         a.rows_per_wg = (a.rows_per_wg + 1) / 2;
     const unsigned groups = (unsigned)((a.rows + a.rows_per_wg - 1) / a.rows_per_wg);
-    const dim3 grid((unsigned)a.batch * (unsigned)stretches * groups);
+    const dim3 grid = DTYPE == 0 ? dim3((unsigned)stretches * groups * (unsigned)a.batch) : dim3((unsigned)stretches, groups, (unsigned)a.batch);
     const bool packed = (!a.history || a.history_stride < 0x8000) && a.num_biases < 0x10000;
     const size_t lds = (kStretch + 64) * 4 + kMaxNodes * 12 + (!packed && a.bias_starts ? kStretch * 4 : 0);
     hipLaunchKernelGGL((rules_kernel<DTYPE, NT>(packed, a.in_place)), grid, dim3(kRulesThreads), lds, stream, a);

@@ -132,7 +132,7 @@ struct Node {
 template <int DTYPE, int CE>
 __global__ void __launch_bounds__(256) tree_level_kernel(const TreeArgs a, int level)
 {
-    const int b = blockIdx.x / a.chunks, chunk = blockIdx.x - b * a.chunks, tid = threadIdx.x;
+    const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int64_t half = (int64_t)a.batch * a.chunks;
     int node = 0;
     if (level > 0) {  // every wave finds it for itself
@@ -159,10 +159,11 @@ __global__ void __launch_bounds__(256) tree_level_kernel(const TreeArgs a, int l
 template <int DTYPE, int CE>
 __global__ void __launch_bounds__(256) tree_scan_kernel(const TreeArgs a)
 {
-    const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
-    if (a.do_commit && threadIdx.x == 0 && chunk == 0 && row % a.nodes == 0) a.old_lens[row / a.nodes] = a.seq_lens[row / a.nodes];
-    const u64 best = chunk_max<DTYPE, CE>((const char *)a.logits + (int64_t)row * a.stride_row * (DTYPE == 0 ? 4 : 2), chunk * CE, a.vocab);
-    if (threadIdx.x == 0) a.best[(int64_t)row * a.chunks + chunk] = best;
+    const int chunk = blockIdx.x, b = blockIdx.z;
+    const int64_t row = (int64_t)b * a.nodes + blockIdx.y;
+    if (a.do_commit && threadIdx.x == 0 && chunk == 0 && blockIdx.y == 0) a.old_lens[b] = a.seq_lens[b];
+    const u64 best = chunk_max<DTYPE, CE>((const char *)a.logits + row * a.stride_row * (DTYPE == 0 ? 4 : 2), chunk * CE, a.vocab);
+    if (threadIdx.x == 0) a.best[row * a.chunks + chunk] = best;
 }
 
 __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
@@ -300,12 +301,12 @@ static hipError_t launch_tree(TreeArgs a, hipStream_t stream)
     a.chunks = (a.vocab + CE - 1) / CE;
     if (a.walk) {
         for (int level = 0; level < a.max_path; ++level) {
-            hipLaunchKernelGGL((tree_level_kernel<DTYPE, CE>), dim3((unsigned)a.batch * (unsigned)a.chunks), dim3(256), 0, stream, a, level);
+            hipLaunchKernelGGL((tree_level_kernel<DTYPE, CE>), dim3((unsigned)a.chunks, (unsigned)a.batch), dim3(256), 0, stream, a, level);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     } else {
-        hipLaunchKernelGGL((tree_scan_kernel<DTYPE, CE>), dim3((unsigned)(a.batch * a.nodes) * (unsigned)a.chunks), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((tree_scan_kernel<DTYPE, CE>), dim3((unsigned)a.chunks, (unsigned)a.nodes, (unsigned)a.batch), dim3(256), 0, stream, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
