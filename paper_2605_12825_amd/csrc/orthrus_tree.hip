@@ -6,6 +6,8 @@
 //          level before, the children and their tokens, and takes the maximum of its own chunk of that node's row.
 //   all    one launch over every node's row, where that is less than a launch per level.
 //   commit grid (sequence, layer): finishes the path, writes tokens and lengths (layer 0) and copies its rows' K/V.
+// What bounds it: 64 sequences the logits of their paths (177 MB, 25 us at the memory's rate; 50 with eight levels of 2.6 us that have
+// nothing to read when they are over, up to 12 for the first), fewer of them the chain of launches (batch 1: scan 4, commit 6).
 #include "orthrus_internal.h"
 #include "orthrus_lanes.h"
 
@@ -287,6 +289,9 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
 // ---------------------------------------------------------------------------------------------
 // host side
 
+// Logits of a workgroup: the fewer where that brings more of them to the memory at once than it costs launches of workgroups (8192 ->
+// 2048 a workgroup, fp32, vocabulary 151936; walked, 8 levels: 8 sequences 37.0 -> 33.1 us, 16 39.1 -> 36.7, 64 50.9 -> 64.2; every row
+// scanned: 1 x 32 rows 15.0 -> 13.7, 4 x 16 15.2 -> 14.0, 16 x 16 31.4 -> 30.7, 4 x 64 33.4 -> 34.1, 8 x 48 in bf16 27.9 -> 34.1).
 constexpr int kTreeChunk = 8192, kTreeChunkFew = 2048;
 
 size_t tree_best_bytes(int batch, int nodes, int vocab)
@@ -317,17 +322,20 @@ static hipError_t launch_tree(TreeArgs a, hipStream_t stream)
 template <int DTYPE>
 static hipError_t launch_tree_sized(const TreeArgs &a, hipStream_t stream)
 {
-    const int64_t rows = a.walk ? a.batch : (int64_t)a.batch * a.nodes;
-    return rows * a.vocab < (int64_t)256 * kTreeChunk ? launch_tree<DTYPE, kTreeChunkFew>(a, stream) : launch_tree<DTYPE, kTreeChunk>(a, stream);
+    const int64_t logits = (a.walk ? a.batch : (int64_t)a.batch * a.nodes) * a.vocab;
+    return logits < (int64_t)(a.walk ? 512 : 4096) * kTreeChunk ? launch_tree<DTYPE, kTreeChunkFew>(a, stream) : launch_tree<DTYPE, kTreeChunk>(a, stream);
 }
 
 hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream)
 {
     if (a.batch == 0) return hipSuccess;
     if (a.max_path > a.nodes) a.max_path = a.nodes;
+    // Every row at once runs at 6.2 to 6.6 TB/s, a level costs some 4 us and its rows' share of that (fp32, vocabulary 151936, walked ->
+    // every row: 64 sequences of 64 nodes, 8 levels 51 -> 375 us, 16 39 -> 101, 8 37 -> 56, 4 37.9 -> 33.4, 4 of 16 37.5 -> 15, 16 of 16
+    // 39 -> 31, 16 of 32 with 5 levels 30 -> 54).  (More rows than the 2^24 workgroups that a launch counts are walked: 20 ms.)
     const double bytes = (double)a.vocab * (a.dtype == 0 ? 4 : 2) * a.batch;
     const double all = a.nodes * bytes / 6.5e6, level = bytes / 6.5e6;  // us
-    a.walk = all > a.max_path * (level + 5.0);  // (more than the 2^24 workgroups that a launch counts would take 20 ms and are walked)
+    a.walk = all > a.max_path * (level + 4.5);
     return a.dtype == 0 ? launch_tree_sized<0>(a, stream) : a.dtype == 1 ? launch_tree_sized<1>(a, stream) : launch_tree_sized<2>(a, stream);
 }
 
