@@ -185,6 +185,7 @@ class DecodeStep:
             self.params.max_seq_len = bound
             n = max(n, B.orthrus_attn_workspace_bytes_on(self.ctx, self.params))
         self.params.max_seq_len = max_seq_len
+        self._outgrown = []
         self._tree_attn_key = self._tree_consensus_key = (None, None)   # what their workspaces are made for, and these
         self.attn_ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
         self.cons_ws = None
@@ -258,8 +259,9 @@ class DecodeStep:
 
     def reserve(self, sampling=False, tables=False, tree_nodes=0) -> None:
         """Makes the workspaces of sample_tokens and filtered_consensus_commit, of update_page_tables, or of tree_attn and
-        tree_consensus_commit for trees of so many nodes (under the present max_seq_len), ahead of their first call: a program that records calls into a graph does this before.  Calls that overlap in time, in replays of two graphs as on
-        two streams, need a step each."""
+        tree_consensus_commit for trees of so many nodes (under the present max_seq_len), ahead of their first call: a program that
+        records calls into a graph does this before.  Calls that overlap in time, in replays of two graphs as on two streams, need a
+        step each."""
         if sampling:
             self._workspace("sample_ws", B.orthrus_sample_workspace_bytes)
             self._workspace("filtered_ws", B.orthrus_filtered_workspace_bytes)
@@ -361,7 +363,7 @@ class DecodeStep:
 
     def _sized_workspace(self, name, need):
         """The buffer of a kind of call whose size goes by its arguments; a larger one takes its place (never inside a captured
-        sequence: reserve comes before)."""
+        sequence: reserve comes before).  The smaller one stays: graphs and other streams may have it."""
         ws = getattr(self, name, None)
         if ws is None or ws.numel() < need:
             with torch.cuda.device(self.device):
@@ -369,6 +371,7 @@ class DecodeStep:
                     raise RuntimeError("reserve() comes before a call is recorded")
                 ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
                 torch.cuda.current_stream().synchronize()   # the call may be on another stream than what used this memory before
+            self._outgrown.append(getattr(self, name, None))
             setattr(self, name, ws)
         return ws
 
@@ -470,8 +473,8 @@ class DecodeStep:
         if out is None or out is logits:
             out, out_stride_row = logits, out_stride_row if out is logits else logits_stride_row
         else:
-            if _logits_type(out_stride_row, out) != kind:
-                raise ValueError("out must be of the logits' type")
+            if _logits_type(out_stride_row, out) != kind or out.device != logits.device:
+                raise ValueError("out must be of the logits' type, on their device")
             _check_logits_rows("out", out, batch * rows, p.vocab, out_stride_row)
         if not (tokens is None or tokens.__class__ is not int and tokens.dtype is _I32 and tokens.nbytes == 4 * batch * rows and tokens.is_contiguous()) \
                 or parents is not None:
@@ -643,7 +646,7 @@ class DecodeStack:
         """Requests that are over, between two cycles: the pages of those that `ended` ([batch], bool) marks go back to the ring,
         their lengths to 0.  Runs on the current stream; `granted` and `token_starts` are afterwards those of this call.
 
-        With `grow` left at block_k the slots stay in the cycles, each with a block's pages, until the next requests take them;
+        With `grow` left as it is made the slots stay in the cycles, each with a block's pages, until the next requests take them;
         put their lengths to 0 before every cycle, or what they commit lets them grow.
         """
         if self.free_pages is None:

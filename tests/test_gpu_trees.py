@@ -361,3 +361,66 @@ def test_the_64_row_kernel(Hq, H, d, N, B, lo, hi):
     step.close()
     # two roundings of each, of weights and outputs of order one
     assert np.abs(got - other).max() <= 4 * U * max(1.0, np.abs(other).max()) and np.abs(lse - lse2).max() <= 2 * LSE_TOL
+
+
+@pytest.mark.parametrize("over", [-64, 64])
+def test_rows_of_the_block_gigabytes_apart(over):
+    """Offsets of the last rows on both sides of 31 bits."""
+    N, Hq, H, d, P = 64, 3, 1, 64, 16
+    rng, x = _inputs(61, N, Hq, H, d, [37], P)
+    parents = [_tree(rng, N)]
+    rt, row = _rt(), (1 << 24) + over
+    step = rt.DecodeStep(batch=1, num_q_heads=Hq, num_kv_heads=H, head_dim=d, block_k=1, page_size=P, max_pages_per_seq=x["table"].shape[1],
+                         max_seq_len=37, num_pages=x["kp"].shape[0], block_strides=(0, 0, row, d, 0))
+    dv = {k: rt.to_device_bits(v) for k, v in x.items()}
+    far = torch.empty(N * row, dtype=torch.int16, device="cuda")
+    k, v = (far[at:].as_strided((1, N, H, d), (N * row, row, d, 1)) for at in (0, 1024))
+    k.copy_(dv["k"].view(torch.int16))
+    v.copy_(dv["v"].view(torch.int16))
+    out = torch.zeros((1, N, Hq, d), dtype=torch.int16, device="cuda")
+    step.tree_attn(rt.to_device_bits(np.asarray(parents, np.int32)), dv["q"], k, v, dv["kp"], dv["vp"], dv["table"], dv["lens"], out)
+    torch.cuda.synchronize()
+    assert step.device_error() == 0
+    _check_attn(x, parents, _f(rt.bits_to_numpy(out)).astype(np.float64), None)
+    step.close()
+
+
+def test_a_recorded_call_keeps_its_workspace_when_a_larger_one_is_made():
+    rt = _rt()
+    from paper_2605_12825_amd import binding as B_
+    rng, x = _inputs(71, 8, 4, 2, 128, [300, 900], 16)
+    parents = [_tree(rng, 8) for _ in range(2)]
+    step = rt.DecodeStep(batch=2, num_q_heads=4, num_kv_heads=2, head_dim=128, block_k=1, page_size=16, max_pages_per_seq=x["table"].shape[1],
+                         max_seq_len=900, num_pages=x["kp"].shape[0], num_splits=4)
+    dv = {k: rt.to_device_bits(v) for k, v in x.items()}
+    up = rt.to_device_bits(np.asarray(parents, np.int32))
+    out = torch.zeros((2, 8, 4, 128), dtype=torch.int16, device="cuda")
+    step.reserve(tree_nodes=8)
+    stream = torch.cuda.Stream()
+    args = (up, dv["q"], dv["k"], dv["v"], dv["kp"], dv["vp"], dv["table"], dv["lens"], out)
+    step.tree_attn(*args)
+    torch.cuda.synchronize()
+    want = out.clone()
+    torch.cuda.synchronize()
+    B_.orthrus_graph_begin(step.ctx, stream)
+    step.tree_attn(*args, stream=stream)
+    g = B_.orthrus_graph_end(step.ctx, stream)
+    first = step.tree_attn_ws
+    place, size = first.data_ptr(), first.numel()
+    del first
+    for N in (40, 64):   # each larger than the one before
+        _, y = _inputs(N, N, 4, 2, 128, [300, 900], 16)
+        dy = {k: rt.to_device_bits(y[k]) for k in ("q", "k", "v")}
+        step.tree_attn(rt.to_device_bits(np.asarray([_tree(rng, N)] * 2, np.int32)), dy["q"], dy["k"], dy["v"], dv["kp"], dv["vp"], dv["table"], dv["lens"],
+                       torch.zeros((2, N, 4, 128), dtype=torch.int16, device="cuda"))
+    torch.cuda.synchronize()
+    others = [torch.full((size,), 77, dtype=torch.uint8, device="cuda") for _ in range(6)]
+    assert not any(t.data_ptr() < place + size and place < t.data_ptr() + t.numel() for t in others)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        B_.orthrus_graph_launch(g, stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(bool((t == 77).all()) for t in others)
+    B_.orthrus_graph_destroy(g)
+    step.close()

@@ -212,3 +212,8 @@ def test_operands_of_another_type_or_size_are_refused():
     for kw in (dict(logits=x, rules=r), dict(logits=x[:, 0].contiguous(), rules=r, tokens=i(3, 1)), dict(logits=x, rules=r, out=torch.zeros((3, N, 1003)), out_stride_row=1003)):
         with pytest.raises(AssertionError):
             s.process_logits(**kw)
+
+
+def test_logits_do_not_go_from_one_device_to_another():
+    with pytest.raises(ValueError):
+        _Step().process_logits(torch.zeros((3, 5, 1000)), rt.LogitRules(), out=torch.zeros((3, 5, 1000), device="meta"))
