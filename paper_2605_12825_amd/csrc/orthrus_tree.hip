@@ -332,7 +332,7 @@ hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream)
     if (a.max_path > a.nodes) a.max_path = a.nodes;
     // Every row at once runs at 6.2 to 6.6 TB/s, a level costs some 4 us and its rows' share of that (fp32, vocabulary 151936, walked ->
     // every row: 64 sequences of 64 nodes, 8 levels 51 -> 375 us, 16 39 -> 101, 8 37 -> 56, 4 37.9 -> 33.4, 4 of 16 37.5 -> 15, 16 of 16
-    // 39 -> 31, 16 of 32 with 5 levels 30 -> 54).  (More rows than the 2^24 workgroups that a launch counts are walked: 20 ms.)
+    // 39 -> 31, 16 of 32 with 5 levels 30 -> 54).
     const double bytes = (double)a.vocab * (a.dtype == 0 ? 4 : 2) * a.batch;
     const double all = a.nodes * bytes / 6.5e6, level = bytes / 6.5e6;  // us
     a.walk = all > a.max_path * (level + 4.5);
