@@ -32,13 +32,21 @@ __global__ void __launch_bounds__(64 * (W + 1), tree_waves(MODE)) attn_tree_kern
 #include "orthrus_attn_split.inc"
 }
 
+// x / y rounded down, 0 <= x, y < 2^53: one division in 64-bit floating point and a step of correction, where one of integers is
+// some 150 instructions.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
+{
+    const int64_t q = (int64_t)((double)x / (double)y), rest = x - q * y;
+    return rest < 0 ? q - 1 : rest >= y ? q + 1 : q;
+}
+
 // The pieces of a row group's units merged in their order, as attn_combine_kernel does: one workgroup per (unit, 32-row block,
 // 32-wide d block), a wave to four d values, a lane reads the float4 that it would hold in the accumulator.
 template <int D, int BALANCED>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(ATTN_FIRST_PARAMS, const AttnArgs rest, int W)
 {
     const AttnArgs a = with_first(rest, first_lens, first_batch);
-    constexpr int DBLK = D / 32, CHUNK = 8;
+    constexpr int DBLK = D / 32, CHUNK = BALANCED ? 8 : 16;
     const int lane = threadIdx.x & 63, r4 = threadIdx.x >> 6, col = lane & 31, h = lane >> 5;
     const int db = (int)(blockIdx.x % DBLK);
     const int wave = (int)(blockIdx.x / DBLK % (unsigned)W);
@@ -73,8 +81,8 @@ __global__ void __launch_bounds__(256) attn_tree_merge_kernel(ATTN_FIRST_PARAMS,
         const int64_t nwg = total < (int64_t)a.bal_wgs ? total : (int64_t)a.bal_wgs;
         const int64_t U0 = (int64_t)g * per_head + before, U1 = U0 + mine;
         // workgroup w starts at tile floor(w * total / nwg): the last one that starts at or before U0, and before U1
-        const int64_t w_lo = ((U0 + 1) * nwg + total - 1) / total - 1;
-        const int64_t w_hi = (U1 * nwg + total - 1) / total - 1;
+        const int64_t w_lo = quotient((U0 + 1) * nwg + total - 1, total) - 1;
+        const int64_t w_hi = quotient(U1 * nwg + total - 1, total) - 1;
         if (w_lo == w_hi) return;  // one workgroup held the whole unit and wrote its rows
         live = (int)(w_hi - w_lo + 1);
         first_slot = (size_t)w_lo * 2 + 1;
@@ -87,37 +95,42 @@ __global__ void __launch_bounds__(256) attn_tree_merge_kernel(ATTN_FIRST_PARAMS,
         first_slot = rest_slot = (size_t)unit * a.num_splits;
         slot_step = 1;
     }
+    // Every piece's rows and their (m, l) are on their way before the first is looked at, of a fixed count before the length is known:
+    // what a shorter sequence's last slots hold is dropped (one of 4096 tokens, 13 pieces 16.5 -> 16.0 us a call).
+    const int slots = BALANCED ? live : a.num_splits;
     auto slot_of = [&](int s) __attribute__((always_inline)) {
         return (s == 0 ? first_slot : rest_slot + (size_t)s * slot_step) * W + wave;
     };
     float M = kNegBig;
-    for (int s0 = 0; s0 < live; s0 += CHUNK) {
-        float m[CHUNK];
-#pragma unroll
-        for (int u = 0; u < CHUNK; ++u) m[u] = s0 + u < live ? ((const float2 *)a.part_ml)[slot_of(s0 + u) * 32 + col].x : kNegBig;
-#pragma unroll
-        for (int u = 0; u < CHUNK; ++u) M = fmaxf(M, m[u]);
-    }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float lsum = 0.f;
-    for (int s0 = 0; s0 < live; s0 += CHUNK) {
+    for (int s0 = 0; s0 < slots; s0 += CHUNK) {
         float4 v[CHUNK];
         float2 e[CHUNK];
 #pragma unroll
         for (int u = 0; u < CHUNK; ++u) {
             v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
             e[u] = make_float2(kNegBig, 0.f);
-            if (s0 + u < live) {
+            if (s0 + u < slots) {
                 const size_t slot = slot_of(s0 + u);
                 v[u] = ((const float4 *)a.part_o)[slot * (DBLK * 4 * 64) + (size_t)(db * 4 + r4) * 64 + lane];
                 e[u] = ((const float2 *)a.part_ml)[slot * 32 + col];
             }
         }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < CHUNK; ++u) top = s0 + u < live ? fmaxf(top, e[u].x) : top;
+        const float before = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        lsum *= before;
+        acc.x *= before; acc.y *= before; acc.z *= before; acc.w *= before;
 #pragma unroll
         for (int u = 0; u < CHUNK; ++u) {  // fixed order: the result does not depend on timing
-            const float sc = __builtin_amdgcn_exp2f(e[u].x - M);
-            lsum += sc * e[u].y;
-            acc.x += sc * v[u].x; acc.y += sc * v[u].y; acc.z += sc * v[u].z; acc.w += sc * v[u].w;
+            if (s0 + u < live) {
+                const float sc = __builtin_amdgcn_exp2f(e[u].x - M);
+                lsum += sc * e[u].y;
+                acc.x += sc * v[u].x; acc.y += sc * v[u].y; acc.z += sc * v[u].z; acc.w += sc * v[u].w;
+            }
         }
     }
     if (ridx >= a.rows) return;

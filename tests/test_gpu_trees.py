@@ -424,3 +424,16 @@ def test_a_recorded_call_keeps_its_workspace_when_a_larger_one_is_made():
         assert torch.equal(out, want) and all(bool((t == 77).all()) for t in others)
     B_.orthrus_graph_destroy(g)
     step.close()
+
+
+@pytest.mark.parametrize("splits", [16, 17, 40, -1])
+def test_more_pieces_than_are_merged_at_once(splits):
+    _, x = _inputs(81, 20, 2, 1, 128, [3000, 0, 100, 1, 1500], 16)
+    parents = [list(range(-1, 19))] * 5
+    for b in range(5) if splits < 0 else [None]:
+        y = x if b is None else {k: v if k in ("kp", "vp") else v[b:b + 1] for k, v in x.items()}
+        up = parents if b is None else parents[:1]
+        got, lse, err, step = _attn(y, up, splits, 16, bound=3000)
+        assert err == 0
+        _check_attn(y, up, got, lse)
+        step.close()
