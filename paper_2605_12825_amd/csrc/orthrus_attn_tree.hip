@@ -11,8 +11,8 @@
 // Launches with rows and units enough to be bound by the products run the 64-row kernel (orthrus_attn_tree_wide.hip), by the rule
 // of the chains (attn_wide_pays).
 // What bounds it, as it does the chains: 4 x 32768 tokens, 16 nodes (32/8 heads, 64 rows) 86.6 us a call, 6.2 TB/s of the cache; one
-// sequence of 4096, 32 nodes 16.4 us, the chain of tiles, partials and merge; 16 of 512..8192 tokens, 32 nodes at 28/4 heads, shared out
-// evenly, 59 us. Short calls of one block of rows 8 us, 5 of them the kernel.
+// sequence of 4096, 32 nodes 15.9 us, the chain of tiles, partials and merge; 16 of 512..8192 tokens, 32 nodes at 28/4 heads, shared out
+// evenly, 56 to 60 us.  Short calls of one block of rows 8 us, 5 of them the kernel.
 // (The rest that rounding the weights to bf16 leaves, as a second value product, takes the error from 0.0024 to the output's own 0.0017
 // of its size and costs 4 x 32768 tokens, 8 nodes 85.7 -> 96.3 us, one of 4096 13.3 -> 15.1: not in the library.)
 #include "orthrus_attn_dev.h"

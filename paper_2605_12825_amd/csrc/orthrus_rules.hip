@@ -12,10 +12,10 @@
 // What bounds it.  1024 rows of 151936 in fp32 with every rule: 222 us, where streaming them alone takes 198 (the touched ones are 11);
 // 256 rows of 151669 in bf16, histories of 50..8000 (4000 on average): 46 us, of which the stream 29, filling and clearing the counters
 // with their two barriers 6, the history, which each of 19 stretches reads, 2.5 per thousand tokens.  Tried: 16384 tokens a workgroup 50
-// and 375 us (two workgroups to a CU); with half a word a token, so that there are four again, 55 (spills); 256 threads 49 and 283;
-// 4096 tokens and 256 threads 48 and 270; the touched logits listed and written over the stream by gathers and stores of their own 58
-// and 334; a bit map of the touched tokens and jumps around what is of another stretch 47 and 250; whole sequences to an XCD, so that one
-// L2 sees a history, 45.8 and 226 but one sequence of 64 rows 25 -> 119.
+// and 375 us (two workgroups to a CU), with 1024 threads 46 and 240, with half a word a token, so that there are four again, 55 (spills);
+// 256 threads 49 and 283; 4096 tokens and 256 threads 48 and 270; the touched logits listed and written over the stream by gathers and
+// stores of their own 58 and 334; a bit map of the touched tokens and jumps around what is of another stretch 47 and 250; whole
+// sequences to an XCD, so that one L2 sees a history, 45.8 and 226 but one sequence of 64 rows 25 -> 119.
 #include "orthrus_attn_dev.h"
 
 namespace orthrus {

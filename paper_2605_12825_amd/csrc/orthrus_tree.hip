@@ -6,8 +6,8 @@
 //          level before, the children and their tokens, and takes the maximum of its own chunk of that node's row.
 //   all    one launch over every node's row, where that is less than a launch per level.
 //   commit grid (sequence, layer): finishes the path, writes tokens and lengths (layer 0) and copies its rows' K/V.
-// What bounds it: 64 sequences the logits of their paths (177 MB, 25 us at the memory's rate; 50 with eight levels of 2.6 us that have
-// nothing to read when they are over, up to 12 for the first), fewer of them the chain of launches (batch 1: scan 4, commit 6).
+// What bounds it: 64 sequences the logits of their paths (177 MB, 25 us at the memory's rate; 51 with eight levels, 7 to 9 us where
+// rows are read and 3 where every path is over), fewer of them the chain of launches (batch 1: scan 4, commit 6).
 #include "orthrus_internal.h"
 #include "orthrus_lanes.h"
 
