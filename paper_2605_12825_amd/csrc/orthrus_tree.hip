@@ -291,8 +291,10 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
 
 // Logits of a workgroup: the fewer where that brings more of them to the memory at once than it costs launches of workgroups (8192 ->
 // 2048 a workgroup, fp32, vocabulary 151936; walked, 8 levels: 8 sequences 37.0 -> 33.1 us, 16 39.1 -> 36.7, 64 50.9 -> 64.2; every row
-// scanned: 1 x 32 rows 15.0 -> 13.7, 4 x 16 15.2 -> 14.0, 16 x 16 31.4 -> 30.7, 4 x 64 33.4 -> 34.1, 8 x 48 in bf16 27.9 -> 34.1).
-constexpr int kTreeChunk = 8192, kTreeChunkFew = 2048;
+// scanned: 1 x 32 rows 15.0 -> 13.7, 4 x 16 15.2 -> 14.0, 16 x 16 31.4 -> 30.7, 4 x 64 33.4 -> 34.1, 8 x 48 in bf16 27.9 -> 34.1).  Many
+// rows of 16 bits, every row scanned, lie between: a thread has twice the comparisons behind its loads (8192 -> 4096: 8 x 48 28.1 -> 27.0,
+// 24 x 64 82.7 -> 77.9, 64 x 64 214 -> 206; fp32 8 x 48 31.6 both, 64 x 64 391 -> 399).
+constexpr int kTreeChunk = 8192, kTreeChunkFew = 2048, kTreeChunk16 = 4096;
 
 size_t tree_best_bytes(int batch, int nodes, int vocab)
 {
@@ -300,11 +302,11 @@ size_t tree_best_bytes(int batch, int nodes, int vocab)
     return rows * (((size_t)vocab + kTreeChunkFew - 1) / kTreeChunkFew) * sizeof(u64);
 }
 
-template <int DTYPE, int CE>
+template <int DTYPE, int CE, bool WALK>
 static hipError_t launch_tree(TreeArgs a, hipStream_t stream)
 {
     a.chunks = (a.vocab + CE - 1) / CE;
-    if (a.walk) {
+    if constexpr (WALK) {
         for (int level = 0; level < a.max_path; ++level) {
             hipLaunchKernelGGL((tree_level_kernel<DTYPE, CE>), dim3((unsigned)a.chunks, (unsigned)a.batch), dim3(256), 0, stream, a, level);
             const hipError_t e = hipGetLastError();
@@ -323,7 +325,9 @@ template <int DTYPE>
 static hipError_t launch_tree_sized(const TreeArgs &a, hipStream_t stream)
 {
     const int64_t logits = (a.walk ? a.batch : (int64_t)a.batch * a.nodes) * a.vocab;
-    return logits < (int64_t)(a.walk ? 512 : 4096) * kTreeChunk ? launch_tree<DTYPE, kTreeChunkFew>(a, stream) : launch_tree<DTYPE, kTreeChunk>(a, stream);
+    const bool few = logits < (int64_t)(a.walk ? 512 : 4096) * kTreeChunk;
+    if (a.walk) return few ? launch_tree<DTYPE, kTreeChunkFew, true>(a, stream) : launch_tree<DTYPE, kTreeChunk, true>(a, stream);
+    return few ? launch_tree<DTYPE, kTreeChunkFew, false>(a, stream) : launch_tree<DTYPE, DTYPE == 0 ? kTreeChunk : kTreeChunk16, false>(a, stream);
 }
 
 hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream)

@@ -437,3 +437,11 @@ def test_more_pieces_than_are_merged_at_once(splits):
         assert err == 0
         _check_attn(y, up, got, lse)
         step.close()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_many_rows_scanned_at_odd_places(kind):
+    B, N, V = 9, 60, 69997
+    rng, parents, tokens, x = _walk_inputs(91, B, N, V, 12, kind)
+    for pad, offset in ((3, 0), (6, 5)):
+        _check_walk(x, parents, tokens, None, _walk(x, parents, tokens, None, kind, pad, offset))
