@@ -78,12 +78,17 @@ def _check_rows(name, t, elements, dense) -> None:
 
 
 def _check_logits_rows(name, t, rows, vocab, stride_row) -> None:
-    """The memory behind a tensor of logits, or a view of one, holds that many rows so far apart."""
-    if t.numel() == rows * (stride_row or vocab) and stride_row >= 0:
+    """A tensor of logits, or a view of one, has its rows where the call reads them: row i at i * stride_row from its start."""
+    pitch = stride_row or vocab
+    if t.is_contiguous() and (t.numel() == rows * pitch or t.dim() == 1 and t.numel() >= (rows - 1) * pitch + vocab):
         return
-    behind = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-    if rows > 0 and behind < (rows - 1) * (stride_row or vocab) + vocab or stride_row == 0 and t.numel() != rows * vocab:
-        raise ValueError("%s must hold %d rows of %d logits, %d apart, not %s" % (name, rows, vocab, stride_row or vocab, tuple(t.shape)))
+    fits = t.dim() > 0 and t.shape[-1] >= vocab and (t.shape[-1] == 1 or t.stride(-1) == 1)
+    n = 1   # rows of the dimensions so far
+    for size, stride in zip(t.shape[-2::-1], t.stride()[-2::-1]):
+        fits = fits and (size == 1 or stride == n * pitch)
+        n *= size
+    if not fits or n != rows:
+        raise ValueError("%s must hold %d rows of %d logits, %d apart, not %s with strides %s" % (name, rows, vocab, pitch, tuple(t.shape), t.stride()))
 
 
 class LogitRules:
