@@ -42,6 +42,7 @@ def _logits_type(stride_row, *logits) -> int:
 
 
 _F32, _I32 = torch.float32, torch.int32
+_ROWS_16 = frozenset((torch.bfloat16, torch.int16, torch.uint16))   # bf16, or its bits
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -72,9 +73,17 @@ def _check_filters(batch, temperature, top_k, top_p, min_p) -> None:
 
 
 def _check_rows(name, t, elements, dense) -> None:
-    if t.__class__ is not int and (t.element_size() != 2 or t.numel() != elements or dense and not t.is_contiguous()):
-        raise ValueError("%s must hold %d elements of 16 bits%s, not %s of %s with strides %s"
+    if t.__class__ is not int and (t.dtype not in _ROWS_16 or t.numel() != elements or dense and not t.is_contiguous()):
+        raise ValueError("%s must hold %d elements of bf16%s, not %s of %s with strides %s"
                          % (name, elements, " without gaps" if dense else "", tuple(t.shape), t.dtype, t.stride()))
+
+
+def _check_cache(p, k_pool, v_pool, page_table, seq_lens) -> None:
+    """A call's cache: bf16 pools, pages and lengths of 32 bits (of 64, every other one would be the upper half of its neighbour)."""
+    for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
+        if t is not None and t.__class__ is not int and t.dtype not in _ROWS_16:
+            raise ValueError("%s must be of bf16, not %s" % (name, t.dtype))
+    _check_operands(("page_table", page_table, _I32, p.batch * p.max_pages_per_seq), ("seq_lens", seq_lens, _I32, p.batch))
 
 
 def _check_logits_rows(name, t, rows, vocab, stride_row) -> None:
@@ -402,7 +411,11 @@ class DecodeStep:
         queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
         dense_q, dense = p.q_stride_row == 0 and p.q_stride_head == 0, p.blk_stride_row == 0 and p.blk_stride_head == 0
         try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
-            if parents.dtype is _I32 and parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
+            if parents.dtype is _I32 and page_table.dtype is _I32 and seq_lens.dtype is _I32 and q.dtype in _ROWS_16 and \
+                    q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and \
+                    page_table.numel() >= p.batch * p.max_pages_per_seq and page_table.is_contiguous() and \
+                    seq_lens.numel() >= p.batch and seq_lens.is_contiguous() and \
+                    parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
                     k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and (not dense_q or q.is_contiguous()) and \
                     (not dense or k_blk.is_contiguous() and v_blk.is_contiguous()) and \
                     (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous()):
@@ -421,6 +434,7 @@ class DecodeStep:
         _check_rows("v_blk", v_blk, keys, dense)
         _check_rows("out", out, queries, True)
         _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
+        _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse,
                                    self._tree_attn_ws(nodes), self._stream(stream))
 
@@ -439,6 +453,9 @@ class DecodeStep:
         try:
             if parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
                     accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
+                    page_table.dtype is _I32 and seq_lens.dtype is _I32 and k_blk_ar.dtype in _ROWS_16 and \
+                    k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and page_table.is_contiguous() and \
+                    page_table.numel() >= batch * p.max_pages_per_seq and seq_lens.numel() >= batch and seq_lens.is_contiguous() and \
                     parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == 4 * rows and \
                     accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and parents.is_contiguous() and \
                     node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and accept_len.is_contiguous() and \
@@ -461,6 +478,7 @@ class DecodeStep:
         if k_blk_ar is not None and v_blk_ar is not None:
             _check_rows("k_blk_ar", k_blk_ar, size, dense)
             _check_rows("v_blk_ar", v_blk_ar, size, dense)
+            _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
                                                v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
                                                next_anchor, self._tree_consensus_ws(nodes), self._stream(stream))

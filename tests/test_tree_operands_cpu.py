@@ -94,3 +94,58 @@ def test_dimensions_of_one_have_no_stride():
         _Step().process_logits(_full(B, 8, V)[:, 7], rt.LogitRules(), logits_stride_row=8 * V)
     with pytest.raises(ValueError):
         _Step().process_logits(_full(B, 8, V)[:, 7], rt.LogitRules(), logits_stride_row=V)
+
+
+def _attn_args(**kw):
+    a = dict(parents=_i(B, N), q=_h(B, N, 8, 128), k_blk=_h(B, N, 2, 128), v_blk=_h(B, N, 2, 128), k_pool=_h(50, 2, 16, 128), v_pool=_h(50, 2, 16, 128),
+             page_table=_i(B, 9), seq_lens=_i(B), out=_h(B, N, 8, 128))
+    return dict(a, **kw)
+
+
+def _committed(**kw):
+    return _walk_args(**dict(dict(k_pool=_h(1, 50, 2, 16, 128), v_pool=_h(1, 50, 2, 16, 128), page_table=_i(B, 9), seq_lens=_i(B)), **kw))
+
+
+_ODD_CACHES = [("seq_lens", _i(B).long()), ("seq_lens", _i(B - 1)), ("seq_lens", _i(B, 2)[:, 0]), ("seq_lens", torch.zeros(B)),
+               ("page_table", _i(B, 9).long()), ("page_table", _i(B, 8)), ("page_table", _i(9, B).t()), ("page_table", _i(B, 18)[:, :9])]
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_caches_of_another_type_or_size_are_refused(mixed):
+    """Lengths and pages of 64 bits would be read in halves; `mixed`: with addresses among the other operands."""
+    s = _Step()
+    attn, walk = (dict(k_pool=A), dict(k_pool=A)) if mixed else ({}, {})
+    for call in (lambda: s.tree_attn(**_attn_args(**attn)), lambda: s.tree_consensus_commit(**_committed(**walk))):
+        with pytest.raises(_Accepted):
+            call()
+    for name, bad in _ODD_CACHES:
+        with pytest.raises(ValueError, match=name):
+            s.tree_attn(**_attn_args(**attn, **{name: bad}))
+        with pytest.raises(ValueError, match=name):
+            s.tree_consensus_commit(**_committed(**walk, **{name: bad}))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32, torch.int32, torch.uint8])
+def test_rows_that_are_not_bf16_are_refused(dtype):
+    """As many bytes of another type too."""
+    s, size = _Step(), torch.empty(0, dtype=dtype).element_size()
+    for name in ("q", "k_blk", "v_blk", "out", "k_pool", "v_pool"):
+        good = _attn_args()[name]
+        for bad in (good.to(dtype), torch.zeros(good.numel() * 2 // size, dtype=dtype)):
+            with pytest.raises(ValueError, match=name):
+                s.tree_attn(**_attn_args(**{name: bad}))
+    for name in ("k_blk_ar", "v_blk_ar", "k_pool", "v_pool"):
+        good = _committed()[name]
+        for bad in (good.to(dtype), torch.zeros(good.numel() * 2 // size, dtype=dtype)):
+            with pytest.raises(ValueError, match=name):
+                s.tree_consensus_commit(**_committed(**{name: bad}))
+
+
+def test_bits_of_bf16_are_taken_in_any_mix():
+    s = _Step()
+    for name in ("q", "k_blk", "out", "v_pool"):
+        for dtype in (torch.int16, torch.uint16):
+            with pytest.raises(_Accepted):
+                s.tree_attn(**_attn_args(**{name: _attn_args()[name].view(dtype)}))
+    with pytest.raises(_Accepted):
+        s.tree_consensus_commit(**_committed(k_pool=_committed()["k_pool"].view(torch.int16)))
