@@ -86,6 +86,14 @@ def _check_cache(p, k_pool, v_pool, page_table, seq_lens) -> None:
     _check_operands(("page_table", page_table, _I32, p.batch * p.max_pages_per_seq), ("seq_lens", seq_lens, _I32, p.batch))
 
 
+def _check_device(device, **operands) -> None:
+    """Everything lies on the step's device: a kernel given another address space's would fault.  None and addresses stand for
+    themselves."""
+    for name, t in operands.items():
+        if t is not None and t.__class__ is not int and t.device != device:
+            raise ValueError("%s must be on %s, not on %s" % (name, device, t.device))
+
+
 def _check_logits_rows(name, t, rows, vocab, stride_row) -> None:
     """A tensor of logits, or a view of one, has its rows where the call reads them: row i at i * stride_row from its start."""
     pitch = stride_row or vocab
@@ -411,14 +419,17 @@ class DecodeStep:
         queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
         dense_q, dense = p.q_stride_row == 0 and p.q_stride_head == 0, p.blk_stride_row == 0 and p.blk_stride_head == 0
         try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
-            if parents.dtype is _I32 and page_table.dtype is _I32 and seq_lens.dtype is _I32 and q.dtype in _ROWS_16 and \
+            if self.device.index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
+                    v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
+                    parents.dtype is _I32 and page_table.dtype is _I32 and seq_lens.dtype is _I32 and q.dtype in _ROWS_16 and \
                     q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and \
                     page_table.numel() >= p.batch * p.max_pages_per_seq and page_table.is_contiguous() and \
                     seq_lens.numel() >= p.batch and seq_lens.is_contiguous() and \
                     parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
                     k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and (not dense_q or q.is_contiguous()) and \
                     (not dense or k_blk.is_contiguous() and v_blk.is_contiguous()) and \
-                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous()):
+                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous() and
+                     lse.get_device() == self.device.index):
                 ws = self._tree_attn_ws(nodes)
                 st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
                                               k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(),
@@ -435,8 +446,11 @@ class DecodeStep:
         _check_rows("out", out, queries, True)
         _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
         _check_cache(p, k_pool, v_pool, page_table, seq_lens)
-        return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse,
-                                   self._tree_attn_ws(nodes), self._stream(stream))
+        ws = self._tree_attn_ws(nodes)
+        _check_device(self.device, parents=parents, q=q, k_blk=k_blk, v_blk=v_blk, k_pool=k_pool, v_pool=v_pool, page_table=page_table,
+                      seq_lens=seq_lens, out=out, lse=lse)
+        return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, ws,
+                                   self._stream(stream))
 
     def tree_consensus_commit(self, ar_logits, parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens,
                               accept_len, num_committed, path_nodes, out_tokens, next_anchor, max_path=None, stream=None,
@@ -451,7 +465,11 @@ class DecodeStep:
         size, dense = p.num_layers * rows * p.num_kv_heads * p.head_dim, p.blk_stride_row == 0 and p.blk_stride_head == 0 and p.blk_stride_layer == 0
         longest = nodes if max_path is None else max_path
         try:
-            if parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
+            if self.device.index == ar_logits.get_device() == parents.get_device() == node_tokens.get_device() == path_nodes.get_device() == \
+                    out_tokens.get_device() == accept_len.get_device() == num_committed.get_device() == next_anchor.get_device() == \
+                    k_blk_ar.get_device() == v_blk_ar.get_device() == k_pool.get_device() == v_pool.get_device() == \
+                    page_table.get_device() == seq_lens.get_device() and \
+                    parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
                     accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
                     page_table.dtype is _I32 and seq_lens.dtype is _I32 and k_blk_ar.dtype in _ROWS_16 and \
                     k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and page_table.is_contiguous() and \
@@ -479,9 +497,13 @@ class DecodeStep:
             _check_rows("k_blk_ar", k_blk_ar, size, dense)
             _check_rows("v_blk_ar", v_blk_ar, size, dense)
             _check_cache(p, k_pool, v_pool, page_table, seq_lens)
+        ws = self._tree_consensus_ws(nodes)
+        _check_device(self.device, ar_logits=ar_logits, parents=parents, node_tokens=node_tokens, k_blk_ar=k_blk_ar, v_blk_ar=v_blk_ar, k_pool=k_pool,
+                      v_pool=v_pool, page_table=page_table, seq_lens=seq_lens, accept_len=accept_len, num_committed=num_committed,
+                      path_nodes=path_nodes, out_tokens=out_tokens, next_anchor=next_anchor)
         return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
                                                v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
-                                               next_anchor, self._tree_consensus_ws(nodes), self._stream(stream))
+                                               next_anchor, ws, self._stream(stream))
 
     def process_logits(self, logits, rules, tokens=None, parents=None, out=None, stream=None, logits_stride_row=0, out_stride_row=0):
         """Puts logits [batch, rows, vocab] (or [batch, vocab]) through their requests' LogitRules: in place, or into `out`.  tokens
@@ -504,8 +526,10 @@ class DecodeStep:
             _check_operands(("tokens", tokens, _I32, batch * rows), ("parents", parents, _I32, batch * rows))
         if rules.checked != (batch, rows, p.vocab, logits.device):
             rules.check(batch, rows, p.vocab, logits.device)
-        return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row,
-                                        self._stream(stream))
+        handle = self._stream(stream)
+        if logits.device != self.device or tokens is not None or parents is not None:   # (out and the rules are on the logits' device)
+            _check_device(self.device, logits=logits, tokens=tokens, parents=parents)
+        return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row, handle)
 
     def attn_timing(self, enable: bool) -> None:
         """Attach HIP events to the attention kernels of the following attn() calls (or stop doing so)."""

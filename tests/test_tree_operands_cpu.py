@@ -149,3 +149,47 @@ def test_bits_of_bf16_are_taken_in_any_mix():
                 s.tree_attn(**_attn_args(**{name: _attn_args()[name].view(dtype)}))
     with pytest.raises(_Accepted):
         s.tree_consensus_commit(**_committed(k_pool=_committed()["k_pool"].view(torch.int16)))
+
+
+class _OnGpu(_Step):
+    """Of a device of its own: the workspaces are there, the call into the library is the only thing left."""
+
+    def __init__(self):
+        super().__init__()
+        self.device = torch.device("cuda", 0)
+
+    def _tree_attn_ws(self, nodes):
+        return torch.zeros(256, dtype=torch.uint8, device="meta")
+
+    _tree_consensus_ws = _tree_attn_ws
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("elsewhere", ["cpu", "meta"])
+def test_operands_on_another_device_than_the_step_are_refused(mixed, elsewhere):
+    """All of them in host memory, or one call's parts of them; nothing reaches a stream or the library."""
+    s = _OnGpu()
+    move = lambda a: {k: v.to(elsewhere) if torch.is_tensor(v) else v for k, v in a.items()}  # noqa: E731
+    attn, walk = _attn_args(lse=torch.zeros((B, 8, N))), _committed()
+    if mixed:
+        attn["k_pool"] = walk["k_pool"] = A
+    with pytest.raises(ValueError, match="must be on cuda:0"):
+        s.tree_attn(**move(attn))
+    with pytest.raises(ValueError, match="must be on cuda:0"):
+        s.tree_consensus_commit(**move(walk))
+    with pytest.raises(ValueError, match="must be on cuda:0"):
+        s.tree_consensus_commit(**move(dict(walk, k_blk_ar=None, v_blk_ar=None, k_pool=None, v_pool=None, page_table=None, seq_lens=None)))
+
+
+def test_logits_and_rules_on_another_device_than_the_step_are_refused():
+    class Step(_OnGpu):
+        def _stream(self, stream):
+            return 0
+    s, x = Step(), torch.zeros((B, N, V))
+    for kw in (dict(), dict(tokens=_i(B, N)), dict(out=torch.zeros((B, N, V))), dict(tokens=_i(B, N), parents=_i(B, N))):
+        with pytest.raises(ValueError, match="logits must be on cuda:0"):
+            s.process_logits(x, rt.LogitRules(repetition=torch.ones(B)), **kw)
+    s.device = torch.device("cpu")      # the logits are where the step is, what is fed is not
+    for kw in (dict(tokens=_i(B, N).to("meta")), dict(parents=_i(B, N).to("meta"))):
+        with pytest.raises(ValueError, match="must be on cpu, not on meta"):
+            s.process_logits(x, rt.LogitRules(), **kw)
