@@ -46,6 +46,15 @@ _ROWS_16 = frozenset((torch.bfloat16, torch.int16, torch.uint16))   # bf16, or i
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+def _recording(stream, device) -> bool:
+    """Whether what is called on that stream (a torch Stream or a handle) goes into a graph; None: not asked."""
+    handle = 0 if stream is None else stream if stream.__class__ is int else int(stream.cuda_stream)
+    if handle == 0:   # (the null stream cannot be recorded)
+        return False
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device)):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _check_operands(*operands) -> None:
     """(name, tensor, type, elements): what is of another type (torch makes whole numbers 64 bits wide), too short, or a column of
     something larger would be read as what it is not.  None and addresses stand for themselves."""
@@ -383,31 +392,35 @@ class DecodeStep:
             return stream
         return torch.cuda.current_stream(self.device) if _raw_stream is None else _raw_stream(self.device.index)
 
-    def _sized_workspace(self, name, need):
+    def _sized_workspace(self, name, need, stream):
         """The buffer of a kind of call whose size goes by its arguments; a larger one takes its place (never inside a captured
-        sequence: reserve comes before).  The smaller one stays: graphs and other streams may have it."""
+        sequence: reserve comes before).  The smaller one stays: graphs and other streams may have it.  Each is at least twice
+        as large as the one before, so that all of them together stay below twice the last."""
         ws = getattr(self, name, None)
         if ws is None or ws.numel() < need:
             with torch.cuda.device(self.device):
-                if torch.cuda.is_current_stream_capturing():
+                if _recording(stream, self.device) or torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("reserve() comes before a call is recorded")
-                ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+                size = max(need, 256 if ws is None else 2 * ws.numel())
+                new = torch.empty(size, dtype=torch.uint8, device=self.device)
                 torch.cuda.current_stream().synchronize()   # the call may be on another stream than what used this memory before
-            self._outgrown.append(getattr(self, name, None))
+            if ws is not None:
+                self._outgrown.append(ws)
+            ws = new
             setattr(self, name, ws)
         return ws
 
-    def _tree_attn_ws(self, nodes):
+    def _tree_attn_ws(self, nodes, stream=None):
         key, ws = self._tree_attn_key
         if key != (nodes, self.params.max_seq_len):   # (a query is a call into the library)
-            ws = self._sized_workspace("tree_attn_ws", B.orthrus_tree_attn_workspace_bytes(self.ctx, self.params, nodes))
+            ws = self._sized_workspace("tree_attn_ws", B.orthrus_tree_attn_workspace_bytes(self.ctx, self.params, nodes), stream)
             self._tree_attn_key = (nodes, self.params.max_seq_len), ws
         return ws
 
-    def _tree_consensus_ws(self, nodes):
+    def _tree_consensus_ws(self, nodes, stream=None):
         key, ws = self._tree_consensus_key
         if key != nodes:
-            ws = self._sized_workspace("tree_consensus_ws", B.orthrus_tree_consensus_workspace_bytes(self.params, nodes))
+            ws = self._sized_workspace("tree_consensus_ws", B.orthrus_tree_consensus_workspace_bytes(self.params, nodes), stream)
             self._tree_consensus_key = nodes, ws
         return ws
 
@@ -430,7 +443,7 @@ class DecodeStep:
                     (not dense or k_blk.is_contiguous() and v_blk.is_contiguous()) and \
                     (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous() and
                      lse.get_device() == self.device.index):
-                ws = self._tree_attn_ws(nodes)
+                ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
                 st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
                                               k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(),
                                               None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, B._stream_handle(self._stream(stream)))
@@ -446,7 +459,7 @@ class DecodeStep:
         _check_rows("out", out, queries, True)
         _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
         _check_cache(p, k_pool, v_pool, page_table, seq_lens)
-        ws = self._tree_attn_ws(nodes)
+        ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
         _check_device(self.device, parents=parents, q=q, k_blk=k_blk, v_blk=v_blk, k_pool=k_pool, v_pool=v_pool, page_table=page_table,
                       seq_lens=seq_lens, out=out, lse=lse)
         return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, ws,
@@ -479,7 +492,7 @@ class DecodeStep:
                     node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and accept_len.is_contiguous() and \
                     num_committed.is_contiguous() and next_anchor.is_contiguous() and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * size and \
                     (not dense or k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous()):
-                ws = self._tree_consensus_ws(nodes)
+                ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
                 st = B._lib.orthrus_tree_consensus_commit(
                     self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(), node_tokens.data_ptr(),
                     k_blk_ar.data_ptr(), v_blk_ar.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
@@ -497,7 +510,7 @@ class DecodeStep:
             _check_rows("k_blk_ar", k_blk_ar, size, dense)
             _check_rows("v_blk_ar", v_blk_ar, size, dense)
             _check_cache(p, k_pool, v_pool, page_table, seq_lens)
-        ws = self._tree_consensus_ws(nodes)
+        ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
         _check_device(self.device, ar_logits=ar_logits, parents=parents, node_tokens=node_tokens, k_blk_ar=k_blk_ar, v_blk_ar=v_blk_ar, k_pool=k_pool,
                       v_pool=v_pool, page_table=page_table, seq_lens=seq_lens, accept_len=accept_len, num_committed=num_committed,
                       path_nodes=path_nodes, out_tokens=out_tokens, next_anchor=next_anchor)

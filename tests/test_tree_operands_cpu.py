@@ -193,3 +193,65 @@ def test_logits_and_rules_on_another_device_than_the_step_are_refused():
     for kw in (dict(tokens=_i(B, N).to("meta")), dict(parents=_i(B, N).to("meta"))):
         with pytest.raises(ValueError, match="must be on cpu, not on meta"):
             s.process_logits(x, rt.LogitRules(), **kw)
+
+
+class _Streams:
+    """Torch's streams without a device: which one is current, and which are being recorded."""
+
+    def __init__(self, monkeypatch, recorded):
+        self.current, self.recorded, self.waits = 0, recorded, 0
+        monkeypatch.setattr(torch.cuda, "device", lambda d: self)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: type("S", (), dict(cuda_stream=handle)))
+        monkeypatch.setattr(torch.cuda, "stream", lambda s: type("On", (), dict(__enter__=lambda _: setattr(self, "current", s.cuda_stream),
+                                                                                 __exit__=lambda *_: setattr(self, "current", 0)))())
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: self.current in self.recorded)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: self)
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        return None
+
+    def synchronize(self):
+        self.waits += 1
+
+
+class _Workspaces(rt.DecodeStep):
+    def __init__(self):
+        self.ctx, self._outgrown, self.device = None, [], torch.device("cpu")
+        self.params = orthrus.make_params(batch=2, num_q_heads=4, num_kv_heads=2, head_dim=128, block_k=4, page_size=16, max_pages_per_seq=70000,
+                                          max_seq_len=4000, num_pages=200, vocab=V, num_splits=4)
+        self._tree_attn_key = self._tree_consensus_key = (None, None)
+
+
+def test_no_workspace_is_made_while_the_calls_stream_is_recorded(monkeypatch):
+    """The stream that a call names, while torch's current one is another."""
+    streams, s = _Streams(monkeypatch, {77}), _Workspaces()
+    stream = type("S", (), dict(cuda_stream=77))
+    for kind in (s._tree_attn_ws, s._tree_consensus_ws):
+        for handle in (77, stream):
+            with pytest.raises(RuntimeError, match="reserve"):
+                kind(9, handle)
+        assert not hasattr(s, "tree_attn_ws" if kind == s._tree_attn_ws else "tree_consensus_ws") and streams.waits == 0 and streams.current == 0
+        assert kind(9, 78).numel() > 0 and kind(5, stream).numel() > 0   # on another stream, and no larger one while it is recorded
+        streams.waits = 0
+    streams.recorded = {0}    # torch's own, whatever the call names
+    with pytest.raises(RuntimeError, match="reserve"):
+        s._tree_attn_ws(40, 78)
+
+
+def test_workspaces_that_grow_stay_few(monkeypatch):
+    """Bounds that a loop raises step by step: what all outgrown buffers hold stays below what the last one does, and none is given up."""
+    _Streams(monkeypatch, set())
+    s, seen = _Workspaces(), []
+    s.params.num_splits = 0
+    s.params.num_pages = 100000
+    for bound in range(16, 60000, 16):
+        s.params.max_seq_len = bound
+        need = orthrus.orthrus_tree_attn_workspace_bytes(None, s.params, 33)
+        ws = s._tree_attn_ws(33)
+        assert ws.numel() >= need
+        seen += [] if any(ws is x for x in seen) else [ws]
+    assert len(seen) > 2 and all(any(x is y for y in s._outgrown) for x in seen[:-1])
+    assert sum(x.numel() for x in s._outgrown) < seen[-1].numel()
