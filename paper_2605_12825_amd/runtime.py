@@ -6,6 +6,7 @@ computation happens inside liborthrus.so.
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional
 
 import numpy as np
@@ -43,6 +44,7 @@ def _logits_type(stride_row, *logits) -> int:
 
 _F32, _I32 = torch.float32, torch.int32
 _ROWS_16 = frozenset((torch.bfloat16, torch.int16, torch.uint16))   # bf16, or its bits
+_DENSE = (0, 0, 0)   # strides of layer, row and head
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -81,10 +83,24 @@ def _check_filters(batch, temperature, top_k, top_p, min_p) -> None:
                     ("min_p", min_p, _F32, batch))
 
 
-def _check_rows(name, t, elements, dense) -> None:
-    if t.__class__ is not int and (t.dtype not in _ROWS_16 or t.numel() != elements or dense and not t.is_contiguous()):
-        raise ValueError("%s must hold %d elements of bf16%s, not %s of %s with strides %s"
-                         % (name, elements, " without gaps" if dense else "", tuple(t.shape), t.dtype, t.stride()))
+def _rows_lie(t, shape, strides) -> bool:
+    """Whether a tensor's elements lie where a call looks for rows [layers, rows, heads, d] with these strides of a layer, row and head
+    (0: dense), in whatever dimensions."""
+    layers, rows, heads, d = shape
+    layer, row, head = strides
+    head = head or d
+    row = row or heads * d
+    try:
+        at = t.view(shape).stride()
+    except RuntimeError:   # (its rows are not evenly apart)
+        return False
+    return all(n == 1 or x == y for n, x, y in zip(shape, at, (layer or rows * row, row, head, 1)))
+
+
+def _check_rows(name, t, shape, strides) -> None:
+    if t.__class__ is not int and (t.dtype not in _ROWS_16 or t.numel() != math.prod(shape) or not _rows_lie(t, shape, strides)):
+        raise ValueError("%s must hold [%s] elements of bf16 with strides %s of layer, row and head (0: dense), not %s of %s with strides %s"
+                         % (name, ", ".join(map(str, shape)), strides, tuple(t.shape), t.dtype, t.stride()))
 
 
 def _check_cache(p, k_pool, v_pool, page_table, seq_lens) -> None:
@@ -430,7 +446,7 @@ class DecodeStep:
         p, nodes = self.params, parents.shape[1]
         rows, d = p.batch * nodes, p.head_dim
         queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
-        dense_q, dense = p.q_stride_row == 0 and p.q_stride_head == 0, p.blk_stride_row == 0 and p.blk_stride_head == 0
+        at_q, at_kv = (0, p.q_stride_row, p.q_stride_head), (0, p.blk_stride_row, p.blk_stride_head)
         try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
             if self.device.index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
                     v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
@@ -439,8 +455,10 @@ class DecodeStep:
                     page_table.numel() >= p.batch * p.max_pages_per_seq and page_table.is_contiguous() and \
                     seq_lens.numel() >= p.batch and seq_lens.is_contiguous() and \
                     parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
-                    k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and (not dense_q or q.is_contiguous()) and \
-                    (not dense or k_blk.is_contiguous() and v_blk.is_contiguous()) and \
+                    k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and \
+                    (q.is_contiguous() if at_q == _DENSE else _rows_lie(q, (1, rows, p.num_q_heads, d), at_q)) and \
+                    (k_blk.is_contiguous() and v_blk.is_contiguous() if at_kv == _DENSE else
+                     _rows_lie(k_blk, (1, rows, p.num_kv_heads, d), at_kv) and _rows_lie(v_blk, (1, rows, p.num_kv_heads, d), at_kv)) and \
                     (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous() and
                      lse.get_device() == self.device.index):
                 ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
@@ -453,10 +471,10 @@ class DecodeStep:
         except AttributeError:   # (addresses among the operands)
             pass
         _check_operands(("parents", parents, _I32, rows))
-        _check_rows("q", q, queries, dense_q)
-        _check_rows("k_blk", k_blk, keys, dense)
-        _check_rows("v_blk", v_blk, keys, dense)
-        _check_rows("out", out, queries, True)
+        _check_rows("q", q, (1, rows, p.num_q_heads, d), at_q)
+        _check_rows("k_blk", k_blk, (1, rows, p.num_kv_heads, d), at_kv)
+        _check_rows("v_blk", v_blk, (1, rows, p.num_kv_heads, d), at_kv)
+        _check_rows("out", out, (1, rows, p.num_q_heads, d), _DENSE)
         _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
         _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
@@ -475,7 +493,7 @@ class DecodeStep:
         rows = batch * nodes
         kind = _logits_type(logits_stride_row, ar_logits)
         _check_logits_rows("ar_logits", ar_logits, rows, p.vocab, logits_stride_row)
-        size, dense = p.num_layers * rows * p.num_kv_heads * p.head_dim, p.blk_stride_row == 0 and p.blk_stride_head == 0 and p.blk_stride_layer == 0
+        kv, at_kv = (p.num_layers, rows, p.num_kv_heads, p.head_dim), (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head)
         longest = nodes if max_path is None else max_path
         try:
             if self.device.index == ar_logits.get_device() == parents.get_device() == node_tokens.get_device() == path_nodes.get_device() == \
@@ -490,8 +508,9 @@ class DecodeStep:
                     parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == 4 * rows and \
                     accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and parents.is_contiguous() and \
                     node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and accept_len.is_contiguous() and \
-                    num_committed.is_contiguous() and next_anchor.is_contiguous() and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * size and \
-                    (not dense or k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous()):
+                    num_committed.is_contiguous() and next_anchor.is_contiguous() and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * math.prod(kv) and \
+                    (k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous() if at_kv == _DENSE else
+                     _rows_lie(k_blk_ar, kv, at_kv) and _rows_lie(v_blk_ar, kv, at_kv)):
                 ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
                 st = B._lib.orthrus_tree_consensus_commit(
                     self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(), node_tokens.data_ptr(),
@@ -507,8 +526,8 @@ class DecodeStep:
                         ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, batch),
                         ("num_committed", num_committed, _I32, batch), ("next_anchor", next_anchor, _I32, batch))
         if k_blk_ar is not None and v_blk_ar is not None:
-            _check_rows("k_blk_ar", k_blk_ar, size, dense)
-            _check_rows("v_blk_ar", v_blk_ar, size, dense)
+            _check_rows("k_blk_ar", k_blk_ar, kv, at_kv)
+            _check_rows("v_blk_ar", v_blk_ar, kv, at_kv)
             _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
         _check_device(self.device, ar_logits=ar_logits, parents=parents, node_tokens=node_tokens, k_blk_ar=k_blk_ar, v_blk_ar=v_blk_ar, k_pool=k_pool,

@@ -255,3 +255,46 @@ def test_workspaces_that_grow_stay_few(monkeypatch):
         seen += [] if any(ws is x for x in seen) else [ws]
     assert len(seen) > 2 and all(any(x is y for y in s._outgrown) for x in seen[:-1])
     assert sum(x.numel() for x in s._outgrown) < seen[-1].numel()
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_rows_that_do_not_lie_as_the_steps_strides_say_are_refused(mixed):
+    """Dense rows, or those of a narrower projection, in a step whose rows are the parts of a fused one: the last rows would be read behind
+    the tensors' memory."""
+    row = (8 + 2 + 2) * 128
+    s = _Step(q_stride_row=row, q_stride_head=128, blk_stride_row=row, blk_stride_head=128)
+    other = dict(k_pool=A) if mixed else {}
+    fused, wide = _h(B, N, 12, 128), _h(B, N, 16, 128)
+    parts = lambda f: dict(q=f[:, :, :8], k_blk=f[:, :, 8:10], v_blk=f[:, :, 10:12])  # noqa: E731
+    flat = lambda f: {k: v.flatten(0, 1) for k, v in parts(f).items()}  # noqa: E731
+    for good in (parts(fused), flat(fused)):
+        with pytest.raises(_Accepted):
+            s.tree_attn(**_attn_args(**good, **other))
+    for name in ("q", "k_blk", "v_blk"):
+        good = parts(fused)
+        heads = good[name].shape[2]
+        for bad in (good[name].contiguous(), parts(wide)[name], _h(B, N, 128, heads).transpose(2, 3), _h(B, 2 * N, 12, 128)[:, ::2, :heads],
+                    _h(B, N + 1, 12, 128)[:, :N, :heads], _h(B, N, heads, 1).expand(B, N, heads, 128)):
+            with pytest.raises(ValueError, match=name):
+                s.tree_attn(**_attn_args(**dict(good, **{name: bad}), **other))
+    with pytest.raises(_Accepted):   # a single row has none
+        _Step(batch=1, blk_stride_row=row, blk_stride_head=128).tree_attn(
+            **dict(_attn_args(**other), parents=_i(1, 1), q=_h(1, 1, 8, 128), k_blk=_h(1, 1, 2, 128), v_blk=_h(1, 1, 2, 128), out=_h(1, 1, 8, 128)))
+
+
+@pytest.mark.parametrize("layer", [0, 9000 * 128])
+def test_committed_rows_that_do_not_lie_as_the_steps_strides_say_are_refused(layer):
+    row, L = 12 * 128, 2
+    s = _Step(num_layers=L, blk_stride_row=row, blk_stride_head=128, blk_stride_layer=layer)
+    fused = _h(L, 9000 * 128)[:, :B * N * row].unflatten(1, (B, N, 12, 128)) if layer else _h(L, B, N, 12, 128)
+    pools = dict(k_pool=_h(L, 50, 2, 16, 128), v_pool=_h(L, 50, 2, 16, 128))
+    good = dict(k_blk_ar=fused[:, :, :, 8:10], v_blk_ar=fused[:, :, :, 10:], **pools)
+    with pytest.raises(_Accepted):
+        s.tree_consensus_commit(**_committed(**good))
+    for name in ("k_blk_ar", "v_blk_ar"):
+        for bad in (good[name].contiguous(), _h(L, B, N, 16, 128)[..., 8:10, :], _h(L + 1, B, N, 12, 128)[::2, :, :, :2], _h(L, B + 1, N, 12, 128)[:, :B, :, :2],
+                    _h(L, B, N, 2, 128)):
+            with pytest.raises(ValueError, match=name):
+                s.tree_consensus_commit(**_committed(**dict(good, **{name: bad})))
+            with pytest.raises(ValueError, match=name):
+                s.tree_consensus_commit(**_committed(**dict(good, k_pool=A, **{name: bad})))
