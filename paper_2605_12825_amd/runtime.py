@@ -444,38 +444,41 @@ class DecodeStep:
         """Attention of a tree of drafts per sequence: parents [batch, nodes] (at most 64) names the node that each follows, -1 for
         node 0 and for unused ones; every node sees the cache, the nodes above it and itself.  Block tensors are [batch, nodes, ...]."""
         p, nodes = self.params, parents.shape[1]
-        rows, d = p.batch * nodes, p.head_dim
-        queries, keys = rows * p.num_q_heads * d, rows * p.num_kv_heads * d
-        at_q, at_kv = (0, p.q_stride_row, p.q_stride_head), (0, p.blk_stride_row, p.blk_stride_head)
+        batch, hq, h, d = p.batch, p.num_q_heads, p.num_kv_heads, p.head_dim
+        rows = batch * nodes
         try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
-            if self.device.index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
+            index = self.device.index
+            if index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
                     v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
-                    parents.dtype is _I32 and page_table.dtype is _I32 and seq_lens.dtype is _I32 and q.dtype in _ROWS_16 and \
-                    q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and \
-                    page_table.numel() >= p.batch * p.max_pages_per_seq and page_table.is_contiguous() and \
-                    seq_lens.numel() >= p.batch and seq_lens.is_contiguous() and \
-                    parents.nbytes == 4 * rows and parents.is_contiguous() and q.nbytes == out.nbytes == 2 * queries and \
-                    k_blk.nbytes == v_blk.nbytes == 2 * keys and out.is_contiguous() and \
-                    (q.is_contiguous() if at_q == _DENSE else _rows_lie(q, (1, rows, p.num_q_heads, d), at_q)) and \
-                    (k_blk.is_contiguous() and v_blk.is_contiguous() if at_kv == _DENSE else
-                     _rows_lie(k_blk, (1, rows, p.num_kv_heads, d), at_kv) and _rows_lie(v_blk, (1, rows, p.num_kv_heads, d), at_kv)) and \
-                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * p.num_q_heads and lse.is_contiguous() and
-                     lse.get_device() == self.device.index):
-                ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
+                    _I32 is parents.dtype is page_table.dtype is seq_lens.dtype and \
+                    q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and q.dtype in _ROWS_16 and \
+                    parents.nbytes == 4 * rows and q.nbytes == out.nbytes == 2 * rows * hq * d and k_blk.nbytes == v_blk.nbytes == 2 * rows * h * d and \
+                    page_table.nbytes >= 4 * batch * p.max_pages_per_seq and seq_lens.nbytes >= 4 * batch and \
+                    parents.is_contiguous() and out.is_contiguous() and page_table.is_contiguous() and seq_lens.is_contiguous() and \
+                    (_rows_lie(q, (1, rows, hq, d), (0, p.q_stride_row, p.q_stride_head)) if p.q_stride_row or p.q_stride_head else q.is_contiguous()) and \
+                    (_rows_lie(k_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head)) and
+                     _rows_lie(v_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head)) if p.blk_stride_row or p.blk_stride_head else
+                     k_blk.is_contiguous() and v_blk.is_contiguous()) and \
+                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * hq and lse.is_contiguous() and lse.get_device() == index):
+                key, ws = self._tree_attn_key
+                if key != (nodes, p.max_seq_len):
+                    ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
+                handle = self._stream(stream)
                 st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
                                               k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(),
-                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, B._stream_handle(self._stream(stream)))
+                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
+                                              handle if handle.__class__ is int else B._stream_handle(handle))
                 if st != B.ORTHRUS_OK:
                     raise B.OrthrusError(st, "orthrus_tree_attn")
                 return st
         except AttributeError:   # (addresses among the operands)
             pass
         _check_operands(("parents", parents, _I32, rows))
-        _check_rows("q", q, (1, rows, p.num_q_heads, d), at_q)
-        _check_rows("k_blk", k_blk, (1, rows, p.num_kv_heads, d), at_kv)
-        _check_rows("v_blk", v_blk, (1, rows, p.num_kv_heads, d), at_kv)
-        _check_rows("out", out, (1, rows, p.num_q_heads, d), _DENSE)
-        _check_operands(("lse", lse, _F32, rows * p.num_q_heads))
+        _check_rows("q", q, (1, rows, hq, d), (0, p.q_stride_row, p.q_stride_head))
+        _check_rows("k_blk", k_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head))
+        _check_rows("v_blk", v_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head))
+        _check_rows("out", out, (1, rows, hq, d), _DENSE)
+        _check_operands(("lse", lse, _F32, rows * hq))
         _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
         _check_device(self.device, parents=parents, q=q, k_blk=k_blk, v_blk=v_blk, k_pool=k_pool, v_pool=v_pool, page_table=page_table,
@@ -500,23 +503,26 @@ class DecodeStep:
                     out_tokens.get_device() == accept_len.get_device() == num_committed.get_device() == next_anchor.get_device() == \
                     k_blk_ar.get_device() == v_blk_ar.get_device() == k_pool.get_device() == v_pool.get_device() == \
                     page_table.get_device() == seq_lens.get_device() and \
-                    parents.dtype is _I32 and node_tokens.dtype is _I32 and path_nodes.dtype is _I32 and out_tokens.dtype is _I32 and \
-                    accept_len.dtype is _I32 and num_committed.dtype is _I32 and next_anchor.dtype is _I32 and \
-                    page_table.dtype is _I32 and seq_lens.dtype is _I32 and k_blk_ar.dtype in _ROWS_16 and \
-                    k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and page_table.is_contiguous() and \
-                    page_table.numel() >= batch * p.max_pages_per_seq and seq_lens.numel() >= batch and seq_lens.is_contiguous() and \
+                    _I32 is parents.dtype is node_tokens.dtype is path_nodes.dtype is out_tokens.dtype is accept_len.dtype is num_committed.dtype \
+                    is next_anchor.dtype is page_table.dtype is seq_lens.dtype and \
+                    k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and k_blk_ar.dtype in _ROWS_16 and \
                     parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == 4 * rows and \
-                    accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and parents.is_contiguous() and \
-                    node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and accept_len.is_contiguous() and \
-                    num_committed.is_contiguous() and next_anchor.is_contiguous() and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * math.prod(kv) and \
+                    accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and seq_lens.nbytes >= 4 * batch and \
+                    page_table.nbytes >= 4 * batch * p.max_pages_per_seq and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * math.prod(kv) and \
+                    parents.is_contiguous() and node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and \
+                    accept_len.is_contiguous() and num_committed.is_contiguous() and next_anchor.is_contiguous() and \
+                    page_table.is_contiguous() and seq_lens.is_contiguous() and \
                     (k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous() if at_kv == _DENSE else
                      _rows_lie(k_blk_ar, kv, at_kv) and _rows_lie(v_blk_ar, kv, at_kv)):
-                ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
+                key, ws = self._tree_consensus_key
+                if key != nodes:
+                    ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
+                handle = self._stream(stream)
                 st = B._lib.orthrus_tree_consensus_commit(
                     self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(), node_tokens.data_ptr(),
                     k_blk_ar.data_ptr(), v_blk_ar.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
                     accept_len.data_ptr(), num_committed.data_ptr(), path_nodes.data_ptr(), out_tokens.data_ptr(), next_anchor.data_ptr(),
-                    ws.data_ptr(), ws.nbytes, B._stream_handle(self._stream(stream)))
+                    ws.data_ptr(), ws.nbytes, handle if handle.__class__ is int else B._stream_handle(handle))
                 if st != B.ORTHRUS_OK:
                     raise B.OrthrusError(st, "orthrus_tree_consensus_commit")
                 return st
@@ -559,7 +565,8 @@ class DecodeStep:
         if rules.checked != (batch, rows, p.vocab, logits.device):
             rules.check(batch, rows, p.vocab, logits.device)
         handle = self._stream(stream)
-        if logits.device != self.device or tokens is not None or parents is not None:   # (out and the rules are on the logits' device)
+        index = self.device.index   # (out and the rules are on the logits' device)
+        if logits.get_device() != index or tokens is not None and (tokens.__class__ is int or tokens.get_device() != index) or parents is not None:
             _check_device(self.device, logits=logits, tokens=tokens, parents=parents)
         return B.orthrus_logits_process(self.ctx, p, kind, logits, logits_stride_row, rows, tokens, parents, rules.c, out, out_stride_row, handle)
 
