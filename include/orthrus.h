@@ -434,6 +434,8 @@ orthrus_status orthrus_tree_attn(orthrus_ctx *ctx, const orthrus_params *p, int3
  *   accept_len[b] = m - 1 (drafts kept), num_committed[b] = m; path_nodes[b][0..m-1] = the nodes, -1 behind them;
  *   out_tokens[b][0..m-1] = the tokens (the kept drafts, then the correction), -1 behind them; next_anchor[b] = the last of them;
  *   the path's rows of k_blk_ar / v_blk_ar go to token positions L..L+m-1 of every layer's pool; seq_lens[b] = L + m.
+ * A row of nothing but -inf, which a mask that allows no token leaves, has no next token: the path ends at its node, whatever the
+ * children hold, out_tokens has the first index, 0, there as orthrus_consensus_commit would, and next_anchor[b] is -1.
  *
  *   num_nodes    [host] N, 1 <= N <= 64; max_path [host] >= 1 (more than N counts as N): where the depth of the trees is known, it
  *                bounds the number of launches
@@ -486,7 +488,8 @@ typedef struct {
  * The path is what the row follows of this step's own block: the tokens of nodes A(r) of the tree that `parents` describes (as in
  * orthrus_tree_attn; node r is row r), the anchor's among them; without `parents` those of rows 0..r (a chain: the anchor and the
  * drafts fed before and at row r; a plain decoding step has one row); without `tokens` nothing.
- * A row that its mask leaves nothing of is -inf throughout (orthrus_sample_tokens gives token -1 for it).  Logits that no rule
+ * A row that its mask leaves nothing of is -inf throughout (orthrus_sample_tokens gives token -1 for it, orthrus_tree_consensus_commit
+ * next_anchor -1; orthrus_consensus_commit takes token 0, as of any row of equal logits).  Logits that no rule
  * touches keep their bits; a NaN stays NaN unless its token is not allowed.
  *
  *   num_rows     [host] R, 1 <= R <= 64

@@ -527,14 +527,16 @@ def tree_consensus_commit(ar_logits, parents, node_tokens, max_path: int, k_blk_
     for b in range(B):
         path, tokens = [0], []
         while True:
-            tokens.append(_first_largest(ar_logits[b, path[-1]]))
+            row = ar_logits[b, path[-1]]
+            tokens.append(_first_largest(row))
+            nothing = bool(np.isneginf(np.asarray(row, dtype=np.float64)).all())   # no token is allowed: the path ends
             below = [i for i in range(path[-1] + 1, N) if parents[b, i] == path[-1] and node_tokens[b, i] == tokens[-1]]
-            if not below or len(path) == max_path:
+            if not below or nothing or len(path) == max_path:
                 break
             path.append(below[0])
         m = len(path)
         r["path_nodes"][b, :m], r["out_tokens"][b, :m] = path, tokens
-        r["accept_len"][b], r["num_committed"][b], r["next_anchor"][b] = m - 1, m, tokens[-1]
+        r["accept_len"][b], r["num_committed"][b], r["next_anchor"][b] = m - 1, m, -1 if nothing else tokens[-1]
         if k_blk_ar is None:
             continue
         P, L = k_pool.shape[3], int(seq_lens[b])

@@ -26,7 +26,10 @@ __device__ __forceinline__ u64 argmax_key(float v, int index)
     u = v != v ? 0xffffffffu : (u >> 31) ? ~u : u | 0x80000000u;
     return (u64)u << 32 | (uint32_t)~index;
 }
-__device__ __forceinline__ int key_index(u64 key) { return (int)~(uint32_t)key; }
+// The token of a row's largest key: its index, or kNothing where the row holds nothing but -inf, as a mask that allows no token leaves
+// it.  No child has that token, so the path ends there.
+constexpr int kNothing = -1;
+__device__ __forceinline__ int key_token(u64 key) { return (uint32_t)(key >> 32) == ~0xff800000u ? kNothing : (int)~(uint32_t)key; }
 
 __device__ __forceinline__ u64 larger(u64 x, u64 y) { return x > y ? x : y; }
 __device__ __forceinline__ u64 wave_largest(u64 x)
@@ -125,7 +128,7 @@ struct Node {
     // the first child of `node` with that token, -1: none
     __device__ __forceinline__ int child(int node, int t) const
     {
-        const u64 hit = __ballot(up == node && token == t);
+        const u64 hit = __ballot(up == node && token == t && t != kNothing);
         return hit ? __builtin_ctzll(hit) : -1;
     }
 };
@@ -140,7 +143,7 @@ __global__ void __launch_bounds__(256) tree_level_kernel(const TreeArgs a, int l
     if (level > 0) {  // every wave finds it for itself
         // (the maxima are read whether or not the path came to this level, so that all loads go out together)
         const Node mine(a, b);
-        const int t = key_index(row_max(a.best + ((level - 1) & 1) * half + (int64_t)b * a.chunks, a.chunks));
+        const int t = key_token(row_max(a.best + ((level - 1) & 1) * half + (int64_t)b * a.chunks, a.chunks));
         const int before = __builtin_amdgcn_readfirstlane(a.level_node[(int64_t)b * kMaxNodes + level - 1]);
         node = -1;
         if (before >= 0) {
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
             if (i < a.nodes) {
                 const u64 *row = a.best + ((int64_t)b * a.nodes + i) * a.chunks;
                 for (int c = lane + 64; c < a.chunks; c += 64) key[u] = larger(key[u], row[c]);
-                const int t = key_index(wave_largest(key[u]));
+                const int t = key_token(wave_largest(key[u]));
                 if (lane == 0) s_am[i] = t;
             }
         }
@@ -211,10 +214,9 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
             }
             m = __popcll(__ballot(path >= 0));
             if (m == a.max_path) {  // nobody has looked at the last level's maxima yet
-                const int t = key_index(row_max(a.best + ((m - 1) & 1) * (int64_t)a.batch * a.chunks + (int64_t)b * a.chunks, a.chunks));
+                const int t = key_token(row_max(a.best + ((m - 1) & 1) * (int64_t)a.batch * a.chunks + (int64_t)b * a.chunks, a.chunks));
                 if (lane == m - 1) token = t;
             }
-            if (lane >= m) token = -1;
         } else {
             int node = 0;
             while (node >= 0 && m < a.max_path) {
@@ -241,9 +243,9 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const TreeArgs a)
         if (layer == 0) {
             if (lane < a.nodes) {
                 a.path_nodes[(int64_t)b * a.nodes + lane] = path;
-                a.out_tokens[(int64_t)b * a.nodes + lane] = token;
+                a.out_tokens[(int64_t)b * a.nodes + lane] = lane >= m ? -1 : token == kNothing ? 0 : token;
             }
-            const int anchor = __shfl(token, m - 1);
+            const int anchor = __shfl(token, m - 1);  // kNothing: there is none
             if (lane == 0) {
                 a.accept_len[b] = m - 1;
                 a.num_committed[b] = committed;

@@ -490,7 +490,8 @@ class DecodeStep:
                               accept_len, num_committed, path_nodes, out_tokens, next_anchor, max_path=None, stream=None,
                               logits_stride_row=0):
         """Greedy consensus of a tree of drafts: from node 0 on to the child that holds the node's greedy token, for as long as there
-        is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed."""
+        is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed.
+        A row of nothing but -inf (no token is allowed) ends the path: next_anchor is -1."""
         p, nodes = self.params, parents.shape[1]
         batch = p.batch
         rows = batch * nodes
@@ -625,7 +626,8 @@ class DecodeStack:
         # tree_nodes: the AR view verifies a tree of so many drafts per sequence (node 0 is the anchor) of at most tree_depth levels,
         # greedily: the program writes `parents` and `node_tokens` and the tree's rows into `q_ar`, `k_blk_ar`, `v_blk_ar` and
         # `ar_logits`; the cycle leaves the path in `path_nodes`.  `rules` (LogitRules): `ar_logits` go through them, in place, each
-        # node by its own path.  Their history is the program's to extend between two cycles, by the path's node_tokens.
+        # node by its own path.  Their history is the program's to extend between two cycles, by the path's node_tokens.  Where a
+        # path comes to a node whose mask allows no token, it ends there and `next_anchor` is -1.
         self.tree_nodes, self.rules = int(tree_nodes), rules
         self.tree_depth = int(tree_depth) if tree_depth else self.tree_nodes
         if self.tree_nodes and (self.temperature > 0 or filters):

@@ -81,3 +81,24 @@ def test_hand_worked_rules():
     same, size = oracle.process_logits(x, **dict(rules, repetition=np.array([np.nan]), presence=np.array([np.inf]), frequency=np.array([0.0])))
     np.testing.assert_array_equal(same, x)
     assert not size.any()
+
+
+def test_a_row_of_nothing_ends_the_walk():
+    #        0 -> 1 (tok 3) -> 2 (tok 0) -> 3 (tok 0);   row 1 has nothing left
+    up, tok = np.array([[-1, 0, 1, 2]]), np.array([[9, 3, 0, 0]], np.int32)
+    x = np.zeros((1, 4, 5), np.float32)
+    x[0, 0, 3] = 1.0
+    r = oracle.tree_consensus_commit(x, up, tok, 4)
+    assert r["path_nodes"].tolist() == [[0, 1, 2, 3]] and r["next_anchor"][0] == 0
+    x[0, 1] = -np.inf
+    r = oracle.tree_consensus_commit(x, up, tok, 4)
+    assert r["path_nodes"].tolist() == [[0, 1, -1, -1]] and r["out_tokens"].tolist() == [[3, 0, -1, -1]]
+    assert r["next_anchor"][0] == -1 and r["accept_len"][0] == 1 and r["num_committed"][0] == 2
+    x[0, 1, 4] = np.finfo(np.float32).min       # the lowest number is a token
+    r = oracle.tree_consensus_commit(x, up, tok, 4)
+    assert r["out_tokens"].tolist() == [[3, 4, -1, -1]] and r["next_anchor"][0] == 4
+    x[0, 1, [2, 3]] = np.nan
+    assert oracle.tree_consensus_commit(x, up, tok, 4)["next_anchor"][0] == 2
+    x[0, 0] = -np.inf
+    r = oracle.tree_consensus_commit(x, up, tok, 4)
+    assert r["path_nodes"].tolist() == [[0, -1, -1, -1]] and r["next_anchor"][0] == -1 and r["num_committed"][0] == 1
