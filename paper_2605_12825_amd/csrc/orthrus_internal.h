@@ -340,6 +340,9 @@ hipError_t launch_page_tables(const TablesArgs &a, hipStream_t stream);
 bool kv_store_fits(int rows, int num_kv_heads, int head_dim);
 hipError_t launch_kv_store(const StoreArgs &a, hipStream_t stream);
 size_t tree_best_bytes(int batch, int nodes, int vocab);
+// Whether a tree's consensus goes level by level (1) or scans every row (0), and the logits of a workgroup.
+int tree_walks(int batch, int nodes, int max_path, int vocab, int dtype);
+int tree_chunk(int walk, int batch, int nodes, int vocab, int dtype);
 hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream);
 hipError_t launch_logits_process(const RulesArgs &a, int num_cus, hipStream_t stream);
 int consensus_chunk_elems();

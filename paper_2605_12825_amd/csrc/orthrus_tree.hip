@@ -323,25 +323,36 @@ static hipError_t launch_tree(TreeArgs a, hipStream_t stream)
     return hipGetLastError();
 }
 
+int tree_chunk(int walk, int batch, int nodes, int vocab, int dtype)
+{
+    const int64_t logits = (walk ? batch : (int64_t)batch * nodes) * vocab;
+    if (logits < (int64_t)(walk ? 512 : 4096) * kTreeChunk) return kTreeChunkFew;
+    return walk || dtype == 0 ? kTreeChunk : kTreeChunk16;
+}
+
 template <int DTYPE>
 static hipError_t launch_tree_sized(const TreeArgs &a, hipStream_t stream)
 {
-    const int64_t logits = (a.walk ? a.batch : (int64_t)a.batch * a.nodes) * a.vocab;
-    const bool few = logits < (int64_t)(a.walk ? 512 : 4096) * kTreeChunk;
+    const bool few = tree_chunk(a.walk, a.batch, a.nodes, a.vocab, DTYPE) == kTreeChunkFew;
     if (a.walk) return few ? launch_tree<DTYPE, kTreeChunkFew, true>(a, stream) : launch_tree<DTYPE, kTreeChunk, true>(a, stream);
     return few ? launch_tree<DTYPE, kTreeChunkFew, false>(a, stream) : launch_tree<DTYPE, DTYPE == 0 ? kTreeChunk : kTreeChunk16, false>(a, stream);
+}
+
+// Every row at once runs at 6.2 to 6.6 TB/s, a level costs some 4 us and its rows' share of that (fp32, vocabulary 151936, walked ->
+// every row: 64 sequences of 64 nodes, 8 levels 51 -> 375 us, 16 39 -> 101, 8 37 -> 56, 4 37.9 -> 33.4, 4 of 16 37.5 -> 15, 16 of 16
+// 39 -> 31, 16 of 32 with 5 levels 30 -> 54).
+int tree_walks(int batch, int nodes, int max_path, int vocab, int dtype)
+{
+    const double bytes = (double)vocab * (dtype == 0 ? 4 : 2) * batch;
+    const double all = nodes * bytes / 6.5e6, level = bytes / 6.5e6;  // us
+    return all > (max_path < nodes ? max_path : nodes) * (level + 4.5);
 }
 
 hipError_t launch_tree_consensus(TreeArgs a, hipStream_t stream)
 {
     if (a.batch == 0) return hipSuccess;
     if (a.max_path > a.nodes) a.max_path = a.nodes;
-    // Every row at once runs at 6.2 to 6.6 TB/s, a level costs some 4 us and its rows' share of that (fp32, vocabulary 151936, walked ->
-    // every row: 64 sequences of 64 nodes, 8 levels 51 -> 375 us, 16 39 -> 101, 8 37 -> 56, 4 37.9 -> 33.4, 4 of 16 37.5 -> 15, 16 of 16
-    // 39 -> 31, 16 of 32 with 5 levels 30 -> 54).
-    const double bytes = (double)a.vocab * (a.dtype == 0 ? 4 : 2) * a.batch;
-    const double all = a.nodes * bytes / 6.5e6, level = bytes / 6.5e6;  // us
-    a.walk = all > a.max_path * (level + 4.5);
+    a.walk = tree_walks(a.batch, a.nodes, a.max_path, a.vocab, a.dtype);
     return a.dtype == 0 ? launch_tree_sized<0>(a, stream) : a.dtype == 1 ? launch_tree_sized<1>(a, stream) : launch_tree_sized<2>(a, stream);
 }
 
