@@ -97,6 +97,10 @@ def _rows_lie(t, shape, strides) -> bool:
     return all(n == 1 or x == y for n, x, y in zip(shape, at, (layer or rows * row, row, head, 1)))
 
 
+def _lie(*tensors):
+    return tuple((t.shape, t.stride()) for t in tensors)
+
+
 def _check_rows(name, t, shape, strides) -> None:
     if t.__class__ is not int and (t.dtype not in _ROWS_16 or t.numel() != math.prod(shape) or not _rows_lie(t, shape, strides)):
         raise ValueError("%s must hold [%s] elements of bf16 with strides %s of layer, row and head (0: dense), not %s of %s with strides %s"
@@ -234,6 +238,9 @@ class DecodeStep:
         self.params.max_seq_len = max_seq_len
         self._outgrown = []
         self._tree_attn_key = self._tree_consensus_key = (None, None)   # what their workspaces are made for, and these
+        # the parameters of the last call whose operands were looked at in full, and what a call of the same ones compares: sizes in
+        # bytes, how rows lie, its workspace
+        self._tree_attn_known = self._tree_consensus_known = (None, None)
         self.attn_ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
         self.cons_ws = None
         if vocab > 0:
@@ -444,47 +451,48 @@ class DecodeStep:
         """Attention of a tree of drafts per sequence: parents [batch, nodes] (at most 64) names the node that each follows, -1 for
         node 0 and for unused ones; every node sees the cache, the nodes above it and itself.  Block tensors are [batch, nodes, ...]."""
         p, nodes = self.params, parents.shape[1]
-        batch, hq, h, d = p.batch, p.num_q_heads, p.num_kv_heads, p.head_dim
-        rows = batch * nodes
-        try:   # (in one go, and straight to the library: the smallest calls take as long as the host needs for them)
-            index = self.device.index
-            if index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
-                    v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
-                    _I32 is parents.dtype is page_table.dtype is seq_lens.dtype and \
-                    q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and q.dtype in _ROWS_16 and \
-                    parents.nbytes == 4 * rows and q.nbytes == out.nbytes == 2 * rows * hq * d and k_blk.nbytes == v_blk.nbytes == 2 * rows * h * d and \
-                    page_table.nbytes >= 4 * batch * p.max_pages_per_seq and seq_lens.nbytes >= 4 * batch and \
-                    parents.is_contiguous() and out.is_contiguous() and page_table.is_contiguous() and seq_lens.is_contiguous() and \
-                    (_rows_lie(q, (1, rows, hq, d), (0, p.q_stride_row, p.q_stride_head)) if p.q_stride_row or p.q_stride_head else q.is_contiguous()) and \
-                    (_rows_lie(k_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head)) and
-                     _rows_lie(v_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head)) if p.blk_stride_row or p.blk_stride_head else
-                     k_blk.is_contiguous() and v_blk.is_contiguous()) and \
-                    (lse is None or lse.dtype is _F32 and lse.nbytes == 4 * rows * hq and lse.is_contiguous() and lse.get_device() == index):
-                key, ws = self._tree_attn_key
-                if key != (nodes, p.max_seq_len):
-                    ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
-                handle = self._stream(stream)
-                st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(), v_blk.data_ptr(),
-                                              k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(),
-                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes,
-                                              handle if handle.__class__ is int else B._stream_handle(handle))
-                if st != B.ORTHRUS_OK:
-                    raise B.OrthrusError(st, "orthrus_tree_attn")
-                return st
+        try:   # (the smallest calls take as long as the host needs for them: straight to the library where everything is as it was)
+            key, known = self._tree_attn_known
+            if key == (nodes, bytes(p)):
+                parents_bytes, q_bytes, kv_bytes, table_bytes, lens_bytes, lse_bytes, lie, ws, ws_bytes, _ = known
+                index = self.device.index
+                if index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
+                        v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
+                        _I32 is parents.dtype is page_table.dtype is seq_lens.dtype and \
+                        q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and q.dtype in _ROWS_16 and \
+                        parents.nbytes == parents_bytes and q.nbytes == out.nbytes == q_bytes and k_blk.nbytes == v_blk.nbytes == kv_bytes and \
+                        page_table.nbytes >= table_bytes and seq_lens.nbytes >= lens_bytes and \
+                        parents.is_contiguous() and out.is_contiguous() and page_table.is_contiguous() and seq_lens.is_contiguous() and \
+                        (q.is_contiguous() and k_blk.is_contiguous() and v_blk.is_contiguous() if lie is None else lie == _lie(q, k_blk, v_blk)) and \
+                        (lse is None or lse.dtype is _F32 and lse.nbytes == lse_bytes and lse.is_contiguous() and lse.get_device() == index):
+                    handle = _raw_stream(index) if stream is None and _raw_stream is not None else B._stream_handle(self._stream(stream))
+                    st = B._lib.orthrus_tree_attn(self.ctx, ctypes.byref(p), nodes, parents.data_ptr(), q.data_ptr(), k_blk.data_ptr(),
+                                                  v_blk.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(),
+                                                  seq_lens.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), ws, ws_bytes, handle)
+                    if st != B.ORTHRUS_OK:
+                        raise B.OrthrusError(st, "orthrus_tree_attn")
+                    return st
         except AttributeError:   # (addresses among the operands)
             pass
+        batch, hq, h, d = p.batch, p.num_q_heads, p.num_kv_heads, p.head_dim
+        rows, at_q, at_kv = batch * nodes, (0, p.q_stride_row, p.q_stride_head), (0, p.blk_stride_row, p.blk_stride_head)
         _check_operands(("parents", parents, _I32, rows))
-        _check_rows("q", q, (1, rows, hq, d), (0, p.q_stride_row, p.q_stride_head))
-        _check_rows("k_blk", k_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head))
-        _check_rows("v_blk", v_blk, (1, rows, h, d), (0, p.blk_stride_row, p.blk_stride_head))
+        _check_rows("q", q, (1, rows, hq, d), at_q)
+        _check_rows("k_blk", k_blk, (1, rows, h, d), at_kv)
+        _check_rows("v_blk", v_blk, (1, rows, h, d), at_kv)
         _check_rows("out", out, (1, rows, hq, d), _DENSE)
         _check_operands(("lse", lse, _F32, rows * hq))
         _check_cache(p, k_pool, v_pool, page_table, seq_lens)
         ws = self._tree_attn_ws(nodes) if stream is None else self._tree_attn_ws(nodes, stream)
         _check_device(self.device, parents=parents, q=q, k_blk=k_blk, v_blk=v_blk, k_pool=k_pool, v_pool=v_pool, page_table=page_table,
                       seq_lens=seq_lens, out=out, lse=lse)
-        return B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, ws,
-                                   self._stream(stream))
+        st = B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, ws,
+                                 self._stream(stream))
+        if int not in (q.__class__, k_blk.__class__, v_blk.__class__):
+            lie = None if at_q == at_kv == _DENSE else _lie(q, k_blk, v_blk)
+            self._tree_attn_known = (nodes, bytes(p)), (4 * rows, 2 * rows * hq * d, 2 * rows * h * d, 4 * batch * p.max_pages_per_seq, 4 * batch,
+                                                        4 * rows * hq, lie, ws.data_ptr(), ws.nbytes, ws)
+        return st
 
     def tree_consensus_commit(self, ar_logits, parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens,
                               accept_len, num_committed, path_nodes, out_tokens, next_anchor, max_path=None, stream=None,
@@ -493,42 +501,43 @@ class DecodeStep:
         is one (and at most max_path nodes, where the trees are no deeper a bound on the launches); the path's K/V rows are committed.
         A row of nothing but -inf (no token is allowed) ends the path: next_anchor is -1."""
         p, nodes = self.params, parents.shape[1]
+        longest = nodes if max_path is None else max_path
+        try:
+            key, known = self._tree_consensus_known
+            if key == (nodes, logits_stride_row, bytes(p)):
+                logits, kind, node_bytes, batch_bytes, table_bytes, kv_bytes, lie, ws, ws_bytes, _ = known
+                index = self.device.index
+                if index == ar_logits.get_device() == parents.get_device() == node_tokens.get_device() == path_nodes.get_device() == \
+                        out_tokens.get_device() == accept_len.get_device() == num_committed.get_device() == next_anchor.get_device() == \
+                        k_blk_ar.get_device() == v_blk_ar.get_device() == k_pool.get_device() == v_pool.get_device() == \
+                        page_table.get_device() == seq_lens.get_device() and \
+                        _I32 is parents.dtype is node_tokens.dtype is path_nodes.dtype is out_tokens.dtype is accept_len.dtype is num_committed.dtype \
+                        is next_anchor.dtype is page_table.dtype is seq_lens.dtype and \
+                        k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and k_blk_ar.dtype in _ROWS_16 and \
+                        logits == (ar_logits.dtype, ar_logits.shape, ar_logits.stride()) and \
+                        parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == node_bytes and \
+                        accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == batch_bytes and seq_lens.nbytes >= batch_bytes and \
+                        page_table.nbytes >= table_bytes and k_blk_ar.nbytes == v_blk_ar.nbytes == kv_bytes and \
+                        parents.is_contiguous() and node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and \
+                        accept_len.is_contiguous() and num_committed.is_contiguous() and next_anchor.is_contiguous() and \
+                        page_table.is_contiguous() and seq_lens.is_contiguous() and \
+                        (k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous() if lie is None else lie == _lie(k_blk_ar, v_blk_ar)):
+                    handle = _raw_stream(index) if stream is None and _raw_stream is not None else B._stream_handle(self._stream(stream))
+                    st = B._lib.orthrus_tree_consensus_commit(
+                        self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(),
+                        node_tokens.data_ptr(), k_blk_ar.data_ptr(), v_blk_ar.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(),
+                        seq_lens.data_ptr(), accept_len.data_ptr(), num_committed.data_ptr(), path_nodes.data_ptr(), out_tokens.data_ptr(),
+                        next_anchor.data_ptr(), ws, ws_bytes, handle)
+                    if st != B.ORTHRUS_OK:
+                        raise B.OrthrusError(st, "orthrus_tree_consensus_commit")
+                    return st
+        except AttributeError:   # (addresses among the operands, or no rows to commit)
+            pass
         batch = p.batch
         rows = batch * nodes
         kind = _logits_type(logits_stride_row, ar_logits)
         _check_logits_rows("ar_logits", ar_logits, rows, p.vocab, logits_stride_row)
         kv, at_kv = (p.num_layers, rows, p.num_kv_heads, p.head_dim), (p.blk_stride_layer, p.blk_stride_row, p.blk_stride_head)
-        longest = nodes if max_path is None else max_path
-        try:
-            if self.device.index == ar_logits.get_device() == parents.get_device() == node_tokens.get_device() == path_nodes.get_device() == \
-                    out_tokens.get_device() == accept_len.get_device() == num_committed.get_device() == next_anchor.get_device() == \
-                    k_blk_ar.get_device() == v_blk_ar.get_device() == k_pool.get_device() == v_pool.get_device() == \
-                    page_table.get_device() == seq_lens.get_device() and \
-                    _I32 is parents.dtype is node_tokens.dtype is path_nodes.dtype is out_tokens.dtype is accept_len.dtype is num_committed.dtype \
-                    is next_anchor.dtype is page_table.dtype is seq_lens.dtype and \
-                    k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and k_blk_ar.dtype in _ROWS_16 and \
-                    parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == 4 * rows and \
-                    accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == 4 * batch and seq_lens.nbytes >= 4 * batch and \
-                    page_table.nbytes >= 4 * batch * p.max_pages_per_seq and k_blk_ar.nbytes == v_blk_ar.nbytes == 2 * math.prod(kv) and \
-                    parents.is_contiguous() and node_tokens.is_contiguous() and path_nodes.is_contiguous() and out_tokens.is_contiguous() and \
-                    accept_len.is_contiguous() and num_committed.is_contiguous() and next_anchor.is_contiguous() and \
-                    page_table.is_contiguous() and seq_lens.is_contiguous() and \
-                    (k_blk_ar.is_contiguous() and v_blk_ar.is_contiguous() if at_kv == _DENSE else
-                     _rows_lie(k_blk_ar, kv, at_kv) and _rows_lie(v_blk_ar, kv, at_kv)):
-                key, ws = self._tree_consensus_key
-                if key != nodes:
-                    ws = self._tree_consensus_ws(nodes) if stream is None else self._tree_consensus_ws(nodes, stream)
-                handle = self._stream(stream)
-                st = B._lib.orthrus_tree_consensus_commit(
-                    self.ctx, ctypes.byref(p), kind, ar_logits.data_ptr(), logits_stride_row, nodes, longest, parents.data_ptr(), node_tokens.data_ptr(),
-                    k_blk_ar.data_ptr(), v_blk_ar.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
-                    accept_len.data_ptr(), num_committed.data_ptr(), path_nodes.data_ptr(), out_tokens.data_ptr(), next_anchor.data_ptr(),
-                    ws.data_ptr(), ws.nbytes, handle if handle.__class__ is int else B._stream_handle(handle))
-                if st != B.ORTHRUS_OK:
-                    raise B.OrthrusError(st, "orthrus_tree_consensus_commit")
-                return st
-        except AttributeError:   # (addresses among the operands, or no rows to commit)
-            pass
         _check_operands(("parents", parents, _I32, rows), ("node_tokens", node_tokens, _I32, rows), ("path_nodes", path_nodes, _I32, rows),
                         ("out_tokens", out_tokens, _I32, rows), ("accept_len", accept_len, _I32, batch),
                         ("num_committed", num_committed, _I32, batch), ("next_anchor", next_anchor, _I32, batch))
@@ -540,9 +549,14 @@ class DecodeStep:
         _check_device(self.device, ar_logits=ar_logits, parents=parents, node_tokens=node_tokens, k_blk_ar=k_blk_ar, v_blk_ar=v_blk_ar, k_pool=k_pool,
                       v_pool=v_pool, page_table=page_table, seq_lens=seq_lens, accept_len=accept_len, num_committed=num_committed,
                       path_nodes=path_nodes, out_tokens=out_tokens, next_anchor=next_anchor)
-        return B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
-                                               v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
-                                               next_anchor, ws, self._stream(stream))
+        st = B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
+                                             v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
+                                             next_anchor, ws, self._stream(stream))
+        if torch.is_tensor(k_blk_ar) and torch.is_tensor(v_blk_ar):
+            self._tree_consensus_known = (nodes, logits_stride_row, bytes(p)), (
+                (ar_logits.dtype, ar_logits.shape, ar_logits.stride()), kind, 4 * rows, 4 * batch, 4 * batch * p.max_pages_per_seq, 2 * math.prod(kv),
+                None if at_kv == _DENSE else _lie(k_blk_ar, v_blk_ar), ws.data_ptr(), ws.nbytes, ws)
+        return st
 
     def process_logits(self, logits, rules, tokens=None, parents=None, out=None, stream=None, logits_stride_row=0, out_stride_row=0):
         """Puts logits [batch, rows, vocab] (or [batch, vocab]) through their requests' LogitRules: in place, or into `out`.  tokens

@@ -246,17 +246,17 @@ def test_each_operand_on_another_device_is_refused():
                 k_pool=rows(1, 8, H, 16, d), v_pool=rows(1, 8, H, 16, d), page_table=ints(B, 4), seq_lens=ints(B), accept_len=ints(B), num_committed=ints(B),
                 path_nodes=ints(B, N), out_tokens=ints(B, N), next_anchor=ints(B))
     for call, args in ((step.tree_attn, attn), (step.tree_consensus_commit, walk)):
-        for name in args:
-            with pytest.raises(ValueError, match="%s must be on cuda:0, not on cpu" % name):
-                call(**dict(args, **{name: args[name].cpu()}))
+        for _ in range(2):     # before and after a call of the same sizes
+            for name in args:
+                with pytest.raises(ValueError, match="%s must be on cuda:0, not on cpu" % name):
+                    call(**dict(args, **{name: args[name].cpu()}))
+            call(**args)
     rules = rt.LogitRules(repetition=torch.ones(B, **on))
     x, fed = torch.zeros((B, N, V), **on), ints(B, N)
     for kw in (dict(logits=x.cpu(), rules=rt.LogitRules(repetition=torch.ones(B))), dict(logits=x, rules=rt.LogitRules(repetition=torch.ones(B))),
                dict(logits=x, rules=rules, tokens=fed.cpu()), dict(logits=x, rules=rules, tokens=fed, parents=fed.cpu()), dict(logits=x, rules=rules, out=x.cpu())):
         with pytest.raises(ValueError):
             step.process_logits(**kw)
-    step.tree_attn(**attn)
-    step.tree_consensus_commit(**walk)
     step.process_logits(x, rules, fed, fed)
     torch.cuda.synchronize()
     assert step.device_error() == 0

@@ -298,3 +298,83 @@ def test_committed_rows_that_do_not_lie_as_the_steps_strides_say_are_refused(lay
                 s.tree_consensus_commit(**_committed(**dict(good, **{name: bad})))
             with pytest.raises(ValueError, match=name):
                 s.tree_consensus_commit(**_committed(**dict(good, k_pool=A, **{name: bad})))
+
+
+class _Host:
+    """Stands for the device that the tensors of these tests are on."""
+    index = -1
+
+    def __eq__(self, other):
+        return getattr(other, "type", None) == "cpu"
+
+    def __ne__(self, other):
+        return not self == other
+
+    def __str__(self):
+        return "the host"
+
+
+class _Calling(_Step):
+    """A step whose calls reach a stand-in for the library."""
+
+    def __init__(self, monkeypatch, **kw):
+        super().__init__(**kw)
+        self.device, self.calls = _Host(), []
+        self._tree_attn_known = self._tree_consensus_known = (None, None)
+        for name in ("orthrus_tree_attn", "orthrus_tree_consensus_commit"):
+            monkeypatch.setattr(rt.B._lib, name, lambda *a: self.calls.append(a) or 0)
+
+    def _stream(self, stream):
+        return 0
+
+    def _tree_attn_ws(self, nodes):
+        self.ws = torch.zeros(256, dtype=torch.uint8)
+        return self.ws
+
+    _tree_consensus_ws = _tree_attn_ws
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_a_call_like_the_one_before_is_looked_at_as_closely(monkeypatch, fused):
+    """The second call of the same sizes goes another way through the host: with the same arguments for the library, and the same refusals."""
+    monkeypatch.setattr(rt, "_raw_stream", lambda index: 0)
+    row = 12 * 128 if fused else 0
+    s = _Calling(monkeypatch, q_stride_row=row, q_stride_head=row and 128, blk_stride_row=row, blk_stride_head=row and 128)
+    f, g = _h(B, N, 12, 128), _h(1, B, N, 12, 128)
+    attn = _attn_args(lse=torch.zeros((B, 8, N)), **(dict(q=f[:, :, :8], k_blk=f[:, :, 8:10], v_blk=f[:, :, 10:]) if fused else {}))
+    walk = _committed(**(dict(k_blk_ar=g[..., 8:10, :], v_blk_ar=g[..., 10:, :]) if fused else {}))
+    odd_rows = [("k_blk", _h(B, N, 16, 128)[:, :, :2]), ("q", _h(B, N, 16, 128)[:, :, :8]), ("v_blk", _h(B, N, 4, 128)[:, :, :2])]
+    bad_attn = _ODD_CACHES + odd_rows + [
+        ("parents", _i(B, N).long()), ("parents", _i(N, B).t()), ("parents", _i(B - 1, N)), ("q", attn["q"].half()), ("q", attn["q"].float()),
+        ("k_blk", _h(B, N, 4, 128)), ("v_blk", attn["v_blk"].half()), ("out", _h(B, N, 8, 256)[..., :128]), ("out", _h(B, N, 8, 128).half()),
+        ("lse", torch.zeros((B, 8, N)).double()), ("lse", torch.zeros((B, N, 8)).transpose(1, 2)), ("lse", torch.zeros((B, 4, N))),
+        ("k_pool", attn["k_pool"].half()), ("v_pool", attn["v_pool"].float())]
+    bad_walk = _ODD_CACHES + [(a + "_ar", t[None]) for a, t in odd_rows if a != "q"] + [
+        ("ar_logits", torch.zeros((B, N, V - 1))), ("ar_logits", torch.zeros((B, 8, V))[:, :N]), ("ar_logits", torch.zeros((B, N, V)).double()),
+        ("parents", _i(N, B).t()), ("node_tokens", _i(B, N).long()), ("path_nodes", _i(B, 4)), ("out_tokens", _i(N, B).t()), ("accept_len", _i(B - 1)),
+        ("next_anchor", torch.zeros(B)), ("num_committed", _i(B, 2)[:, 0]), ("k_blk_ar", walk["k_blk_ar"].half()), ("v_pool", walk["v_pool"].half()),
+        ("k_pool", walk["k_pool"].float())]
+    for call, good, bad in ((s.tree_attn, attn, bad_attn), (s.tree_consensus_commit, walk, bad_walk)):
+        assert not s.calls
+        call(**good)
+        ws = s.ws
+        for _ in range(2):
+            call(**good)
+            assert s.ws is ws, "the second call looks at everything anew"
+        first, *others = [[x if not hasattr(x, "_obj") else bytes(x._obj) for x in c] for c in s.calls]
+        assert len(others) == 2 and all(c == first for c in others)
+        for name, t in bad:
+            with pytest.raises(ValueError):
+                call(**dict(good, **{name: t}))
+        assert len(s.calls) == 3
+        call(**dict(good, k_pool=A))          # an address among them
+        assert len(s.calls) == 4
+        s.params.max_seq_len = 90             # parameters that changed: looked at anew
+        call(**good)
+        assert s.ws is not ws
+        s.calls.clear()
+    s.tree_consensus_commit(**dict(walk, k_blk_ar=None, v_blk_ar=None, k_pool=None, v_pool=None, page_table=None, seq_lens=None))
+    s.tree_consensus_commit(**dict(walk, ar_logits=torch.zeros((B, N, V + 3))), logits_stride_row=V + 3)
+    assert len(s.calls) == 2
+    with pytest.raises(ValueError):
+        s.tree_consensus_commit(**walk, logits_stride_row=V + 3)
