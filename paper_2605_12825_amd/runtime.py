@@ -769,8 +769,13 @@ class DecodeStack:
         B.orthrus_graph_begin(self.step.ctx, self.graph_stream)
         try:
             self.cycle(self.graph_stream)
-        finally:
-            self.graph = B.orthrus_graph_end(self.step.ctx, self.graph_stream)
+        except BaseException:   # a call was refused: what has been recorded is part of a cycle
+            try:
+                B.orthrus_graph_destroy(B.orthrus_graph_end(self.step.ctx, self.graph_stream))
+            except B.OrthrusError:
+                pass
+            raise
+        self.graph = B.orthrus_graph_end(self.step.ctx, self.graph_stream)
 
     def replay(self, stream=None) -> None:
         if self.graph is None:

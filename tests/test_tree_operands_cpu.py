@@ -378,3 +378,38 @@ def test_a_call_like_the_one_before_is_looked_at_as_closely(monkeypatch, fused):
     assert len(s.calls) == 2
     with pytest.raises(ValueError):
         s.tree_consensus_commit(**walk, logits_stride_row=V + 3)
+
+
+@pytest.mark.parametrize("ends", [True, False])
+def test_a_cycle_that_is_refused_while_it_is_recorded_leaves_no_graph(monkeypatch, ends):
+    """Part of a cycle would be replayed as a whole one; the same stack can be captured again."""
+    live, n = set(), iter(range(1, 9))
+
+    def end(ctx, stream):
+        if not ends:
+            raise orthrus.OrthrusError(B_EHIP, "orthrus_graph_end")
+        live.add(next(n))
+        return max(live)
+    B_EHIP = rt.B.ORTHRUS_EHIP
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *_: None)
+    monkeypatch.setattr(torch.cuda, "Stream", lambda device=None: object())
+    monkeypatch.setattr(rt.B, "orthrus_graph_begin", lambda ctx, stream: None)
+    monkeypatch.setattr(rt.B, "orthrus_graph_end", end)
+    monkeypatch.setattr(rt.B, "orthrus_graph_destroy", live.discard)
+    stack = rt.DecodeStack.__new__(rt.DecodeStack)
+    stack.graph, stack.step = None, type("Step", (), dict(device="cuda:0", ctx=None, close=lambda self: None))()
+
+    def refused(stream):
+        raise RuntimeError("reserve() comes before a call is recorded")
+    stack.cycle = refused
+    with pytest.raises(RuntimeError, match="reserve"):
+        stack.capture()
+    assert stack.graph is None and not live
+    with pytest.raises(RuntimeError, match="capture"):
+        stack.replay()
+    if ends:
+        stack.cycle = lambda stream: None
+        stack.capture()
+        assert stack.graph in live
+    stack.close()
+    assert not live
