@@ -413,3 +413,14 @@ def test_a_cycle_that_is_refused_while_it_is_recorded_leaves_no_graph(monkeypatc
         assert stack.graph in live
     stack.close()
     assert not live
+
+
+def test_an_attention_workspace_that_is_replaced_stays_for_its_graphs(monkeypatch):
+    s = _Workspaces()
+    monkeypatch.setattr(rt.B, "orthrus_attn_num_splits_on", lambda ctx, p: 4)
+    monkeypatch.setattr(rt.B, "orthrus_attn_workspace_bytes_on", lambda ctx, p: 10 * p.max_seq_len)
+    s.attn_ws = first = torch.empty(2560, dtype=torch.uint8)
+    s.set_max_seq_len(200)
+    assert s.attn_ws is first and not s._outgrown
+    s.set_max_seq_len(4000)
+    assert s.attn_ws.numel() >= 40000 and any(x is first for x in s._outgrown)
