@@ -498,7 +498,7 @@ typedef struct {
  *   tokens       [dev] int32 [B, R] or NULL, values outside [0, V) count for nothing; parents [dev] int32 [B, R] or NULL
  *   rules        [host]
  *   out          [dev] like logits with out_stride_row: logits itself (with the same stride; only what changes is written), or memory
- *                apart from it
+ *                apart from it (rows that share some of it are refused; rows of both in turn in one buffer are not)
  * Arithmetic is fp32, every operation rounded once (frequency * n is subtracted in one), and rounded to the type at the end.
  * Supported: V <= 1048576, B * R * ceil(V / 4096) below 2^24.  Needs no workspace.
  */

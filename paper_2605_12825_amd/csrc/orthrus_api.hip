@@ -251,6 +251,19 @@ TreeLayout tree_layout(const orthrus_params *p, int num_nodes)
     return l;
 }
 
+// Whether a row of `x` and one of `y`, of as many bytes each, share memory; rows lie their stride apart.
+bool rows_overlap(uintptr_t x, uint64_t stride_x, uintptr_t y, uint64_t stride_y, uint64_t rows, uint64_t bytes)
+{
+    if (rows == 0 || x + (rows - 1) * stride_x + bytes <= y || y + (rows - 1) * stride_y + bytes <= x) return false;
+    for (uint64_t i = 0, j = 0; i < rows && j < rows;) {
+        const uintptr_t a = x + i * stride_x, b = y + j * stride_y;
+        if (a + bytes <= b) ++i;
+        else if (b + bytes <= a) ++j;
+        else return true;
+    }
+    return false;
+}
+
 // The context's device as the current one while a call launches: its tensors and stream are there, whatever device the calling
 // thread works on.
 struct OnDevice {
@@ -1078,6 +1091,9 @@ orthrus_status orthrus_logits_process(orthrus_ctx *ctx, const orthrus_params *p,
     a.in_place = logits == out ? 1 : 0;
     if (a.in_place && a.stride_row != a.out_stride_row) return ORTHRUS_EINVAL;
     if (p->batch == 0) return ORTHRUS_OK;
+    const uint64_t size = logits_type == ORTHRUS_F32 ? 4 : 2;
+    if (!a.in_place && rows_overlap((uintptr_t)logits, a.stride_row * size, (uintptr_t)out, a.out_stride_row * size, (uint64_t)p->batch * num_rows, p->vocab * size))
+        return ORTHRUS_EINVAL;
     a.tokens = tokens; a.parents = parents;
     a.history = r.history; a.history_lens = r.history_lens; a.prompt_lens = r.prompt_lens; a.history_stride = r.history_stride;
     a.repetition = r.repetition; a.presence = r.presence; a.frequency = r.frequency;

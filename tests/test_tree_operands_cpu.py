@@ -1,5 +1,7 @@
 """What the tree and rule calls of a DecodeStep make of operands that do not lie as the call would read them: refused on the host, before
 anything touches a device."""
+import ctypes
+
 import pytest
 import torch
 
@@ -424,3 +426,23 @@ def test_an_attention_workspace_that_is_replaced_stays_for_its_graphs(monkeypatc
     assert s.attn_ws is first and not s._outgrown
     s.set_max_seq_len(4000)
     assert s.attn_ws.numel() >= 40000 and any(x is first for x in s._outgrown)
+
+
+@pytest.mark.parametrize("kind,size", [(0, 4), (1, 2)])
+def test_logits_and_out_that_share_memory_are_refused(kind, size):
+    """Rows are read by some workgroups while others write them.  (A call that is not refused ends in ORTHRUS_EHIP here: no device.)"""
+    keep = ctypes.create_string_buffer(1 << 12)
+    p, r = orthrus.make_params(batch=B, num_q_heads=1, num_kv_heads=1, head_dim=64, block_k=1, page_size=16, max_pages_per_seq=1, max_seq_len=0,
+                               num_pages=1, vocab=V), rt.B.orthrus_logit_rules()
+    end, big = (B * N - 1) * V + V, 2 * V + 10
+
+    def call(out_at, stride=0, out_stride=0, base=1 << 30):
+        return orthrus.orthrus_logits_process(ctypes.addressof(keep), p, kind, base, stride, N, None, None, r, base + out_at * size, out_stride, 0, check=False)
+    for at, stride, out_stride in ((1, 0, 0), (-1, 0, 0), (end - 1, 0, 0), (1 - end, 0, 0), (V, 0, 0), (V - 1, big, big), (1 - V, big, big), (big - V + 1, big, big),
+                                   (V + 11, big, big), (3 * big + V - 1, big, big), (V, 2 * V, 3 * V), (5 * V, 2 * V, V), (0, V, V + 1), (-V + 1, 0, big)):
+        assert call(at, stride, out_stride) == rt.B.ORTHRUS_EINVAL, (at, stride, out_stride)
+    if torch.cuda.is_available():
+        return    # what is not refused would be launched
+    for at, stride, out_stride in ((0, 0, 0), (0, V, V), (end, 0, 0), (-end, 0, 0), (V, big, big), (V + 10, big, big), (-V, big, big), (3 * big + V, big, big),
+                                   (V, 2 * V, 4 * V), (V * 2 * B * N, 2 * V, 3 * V), (-3 * V * B * N, 2 * V, 3 * V)):
+        assert call(at, stride, out_stride) == rt.B.ORTHRUS_EHIP, (at, stride, out_stride)
