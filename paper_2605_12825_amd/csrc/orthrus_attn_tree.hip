@@ -7,7 +7,9 @@
 //     steps of lane exchanges (tree_path), next to the first tiles' way through memory.  A tile of the block costs a shift and
 //     16 bit tests; the cache's tiles cost nothing more than a chain's;
 //   - up to 64 nodes, in one or two tiles behind the cache's;
-//   - more than 256 query rows (group x nodes) in two workgroups that each stream the cache.
+//   - more query rows (group x nodes) than eight waves hold, 256, in two workgroups that each stream the cache; in the balanced form, of
+//     at most seven waves, more than 224 in two and more than 448 in three (plan_tree_attn).  64/8 heads, 4 x 32768 tokens: 32 nodes
+//     (256 rows) 158 us a call, 64 nodes (512) 278; one of 4096 22 and 26.
 // Launches with rows and units enough to be bound by the products run the 64-row kernel (orthrus_attn_tree_wide.hip), by the rule
 // of the chains (attn_wide_pays).
 // What bounds it, as it does the chains: 4 x 32768 tokens, 16 nodes (32/8 heads, 64 rows) 86.6 us a call, 6.2 TB/s of the cache; one
@@ -20,7 +22,10 @@
 namespace orthrus {
 
 // Waves per SIMD that the registers must allow.  The balanced form keeps more across its segments than a third of the registers
-// holds next to the tiles (eleven were spilled), so it has half of them, and at most seven row blocks to a workgroup.
+// holds next to the tiles (eleven were spilled), so it has half of them, and at most seven row blocks to a workgroup.  With six and seven
+// that costs no residency; with one to five a CU holds fewer workgroups than of the chains' form (three waves a SIMD), against
+// which it was not timed.  16 trees over 512..8192 tokens at 32/8 heads, balanced / fixed splits: 8 nodes 57 / 71 us, 16 59 / 79,
+// 24 71 / 80, 32 72 / 90, 48 92 / 115, 64 (two workgroups a head) 119 / 133; 64/8 heads, 32 nodes 117 / 133, 64 (three) 230 / 216.
 constexpr int tree_waves(int mode) { return mode == kItemsBalanced ? 2 : 3; }
 constexpr int tree_blocks(bool balanced) { return balanced ? 7 : 8; }
 
