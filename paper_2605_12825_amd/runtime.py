@@ -94,7 +94,7 @@ def _rows_lie(t, shape, strides) -> bool:
         at = t.view(shape).stride()
     except RuntimeError:   # (its rows are not evenly apart)
         return False
-    return all(n == 1 or x == y for n, x, y in zip(shape, at, (layer or rows * row, row, head, 1)))
+    return rows == 0 or all(n == 1 or x == y for n, x, y in zip(shape, at, (layer or rows * row, row, head, 1)))
 
 
 def _lie(*tensors):

@@ -446,3 +446,16 @@ def test_logits_and_out_that_share_memory_are_refused(kind, size):
     for at, stride, out_stride in ((0, 0, 0), (0, V, V), (end, 0, 0), (-end, 0, 0), (V, big, big), (V + 10, big, big), (-V, big, big), (3 * big + V, big, big),
                                    (V, 2 * V, 4 * V), (V * 2 * B * N, 2 * V, 3 * V), (-3 * V * B * N, 2 * V, 3 * V)):
         assert call(at, stride, out_stride) == rt.B.ORTHRUS_EHIP, (at, stride, out_stride)
+
+
+@pytest.mark.parametrize("layers,row", [(1, 0), (2, 0), (2, 12 * 128)])
+def test_a_batch_of_nobody_is_taken(layers, row):
+    s = _Step(batch=0, num_layers=layers, blk_stride_row=row, blk_stride_head=row and 128)
+    walk = dict(ar_logits=torch.zeros((0, N, V)), parents=_i(0, N), node_tokens=_i(0, N), k_blk_ar=_h(layers, 0, N, 2, 128), v_blk_ar=_h(layers, 0, N, 2, 128),
+                k_pool=_h(layers, 50, 2, 16, 128), v_pool=_h(layers, 50, 2, 16, 128), page_table=_i(0, 9), seq_lens=_i(0), accept_len=_i(0),
+                num_committed=_i(0), path_nodes=_i(0, N), out_tokens=_i(0, N), next_anchor=_i(0))
+    for call in (lambda: s.tree_consensus_commit(**walk), lambda: s.process_logits(torch.zeros((0, N, V)), rt.LogitRules()),
+                 lambda: s.tree_attn(**_attn_args(parents=_i(0, N), q=_h(0, N, 8, 128), k_blk=_h(0, N, 2, 128), v_blk=_h(0, N, 2, 128), out=_h(0, N, 8, 128),
+                                                  page_table=_i(0, 9), seq_lens=_i(0)))):
+        with pytest.raises(_Accepted):
+            call()
