@@ -455,12 +455,12 @@ class DecodeStep:
         try:   # (the smallest calls take as long as the host needs for them: straight to the library where everything is as it was)
             key, known = self._tree_attn_known
             if key == (nodes, bytes(p)):
-                parents_bytes, q_bytes, kv_bytes, table_bytes, lens_bytes, lse_bytes, lie, ws, ws_bytes, _ = known
+                types, parents_bytes, q_bytes, kv_bytes, table_bytes, lens_bytes, lse_bytes, lie, ws, ws_bytes, _ = known
                 index = self.device.index
                 if index == parents.get_device() == q.get_device() == k_blk.get_device() == v_blk.get_device() == k_pool.get_device() == \
                         v_pool.get_device() == page_table.get_device() == seq_lens.get_device() == out.get_device() and \
                         _I32 is parents.dtype is page_table.dtype is seq_lens.dtype and \
-                        q.dtype is k_blk.dtype is v_blk.dtype is out.dtype is k_pool.dtype is v_pool.dtype and q.dtype in _ROWS_16 and \
+                        types == (q.dtype, k_blk.dtype, v_blk.dtype, k_pool.dtype, v_pool.dtype, out.dtype) and \
                         parents.nbytes == parents_bytes and q.nbytes == out.nbytes == q_bytes and k_blk.nbytes == v_blk.nbytes == kv_bytes and \
                         page_table.nbytes >= table_bytes and seq_lens.nbytes >= lens_bytes and \
                         parents.is_contiguous() and out.is_contiguous() and page_table.is_contiguous() and seq_lens.is_contiguous() and \
@@ -489,10 +489,11 @@ class DecodeStep:
                       seq_lens=seq_lens, out=out, lse=lse)
         st = B.orthrus_tree_attn(self.ctx, p, nodes, parents, q, k_blk, v_blk, k_pool, v_pool, page_table, seq_lens, out, lse, ws,
                                  self._stream(stream))
-        if int not in (q.__class__, k_blk.__class__, v_blk.__class__):
-            lie = None if at_q == at_kv == _DENSE else _lie(q, k_blk, v_blk)
-            self._tree_attn_known = (nodes, bytes(p)), (4 * rows, 2 * rows * hq * d, 2 * rows * h * d, 4 * batch * p.max_pages_per_seq, 4 * batch,
-                                                        4 * rows * hq, lie, ws.data_ptr(), ws.nbytes, ws)
+        rows_16 = (q, k_blk, v_blk, k_pool, v_pool, out)
+        if not any(t.__class__ is int for t in rows_16):
+            self._tree_attn_known = (nodes, bytes(p)), (
+                tuple(t.dtype for t in rows_16), 4 * rows, 2 * rows * hq * d, 2 * rows * h * d, 4 * batch * p.max_pages_per_seq, 4 * batch, 4 * rows * hq,
+                None if at_q == at_kv == _DENSE else _lie(q, k_blk, v_blk), ws.data_ptr(), ws.nbytes, ws)
         return st
 
     def tree_consensus_commit(self, ar_logits, parents, node_tokens, k_blk_ar, v_blk_ar, k_pool, v_pool, page_table, seq_lens,
@@ -506,7 +507,7 @@ class DecodeStep:
         try:
             key, known = self._tree_consensus_known
             if key == (nodes, logits_stride_row, bytes(p)):
-                logits, kind, node_bytes, batch_bytes, table_bytes, kv_bytes, lie, ws, ws_bytes, _ = known
+                types, logits, kind, node_bytes, batch_bytes, table_bytes, kv_bytes, lie, ws, ws_bytes, _ = known
                 index = self.device.index
                 if index == ar_logits.get_device() == parents.get_device() == node_tokens.get_device() == path_nodes.get_device() == \
                         out_tokens.get_device() == accept_len.get_device() == num_committed.get_device() == next_anchor.get_device() == \
@@ -514,8 +515,7 @@ class DecodeStep:
                         page_table.get_device() == seq_lens.get_device() and \
                         _I32 is parents.dtype is node_tokens.dtype is path_nodes.dtype is out_tokens.dtype is accept_len.dtype is num_committed.dtype \
                         is next_anchor.dtype is page_table.dtype is seq_lens.dtype and \
-                        k_blk_ar.dtype is v_blk_ar.dtype is k_pool.dtype is v_pool.dtype and k_blk_ar.dtype in _ROWS_16 and \
-                        logits == (ar_logits.dtype, ar_logits.shape, ar_logits.stride()) and \
+                        types == (k_blk_ar.dtype, v_blk_ar.dtype, k_pool.dtype, v_pool.dtype) and logits == (ar_logits.dtype, ar_logits.shape, ar_logits.stride()) and \
                         parents.nbytes == node_tokens.nbytes == path_nodes.nbytes == out_tokens.nbytes == node_bytes and \
                         accept_len.nbytes == num_committed.nbytes == next_anchor.nbytes == batch_bytes and seq_lens.nbytes >= batch_bytes and \
                         page_table.nbytes >= table_bytes and k_blk_ar.nbytes == v_blk_ar.nbytes == kv_bytes and \
@@ -553,9 +553,10 @@ class DecodeStep:
         st = B.orthrus_tree_consensus_commit(self.ctx, p, kind, ar_logits, logits_stride_row, nodes, longest, parents, node_tokens, k_blk_ar,
                                              v_blk_ar, k_pool, v_pool, page_table, seq_lens, accept_len, num_committed, path_nodes, out_tokens,
                                              next_anchor, ws, self._stream(stream))
-        if torch.is_tensor(k_blk_ar) and torch.is_tensor(v_blk_ar):
+        rows_16 = (k_blk_ar, v_blk_ar, k_pool, v_pool)
+        if all(torch.is_tensor(t) for t in rows_16):
             self._tree_consensus_known = (nodes, logits_stride_row, bytes(p)), (
-                (ar_logits.dtype, ar_logits.shape, ar_logits.stride()), kind, 4 * rows, 4 * batch, 4 * batch * p.max_pages_per_seq, 2 * math.prod(kv),
+                tuple(t.dtype for t in rows_16), (ar_logits.dtype, ar_logits.shape, ar_logits.stride()), kind, 4 * rows, 4 * batch, 4 * batch * p.max_pages_per_seq, 2 * math.prod(kv),
                 None if at_kv == _DENSE else _lie(k_blk_ar, v_blk_ar), ws.data_ptr(), ws.nbytes, ws)
         return st
 

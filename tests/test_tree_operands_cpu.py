@@ -336,8 +336,9 @@ class _Calling(_Step):
     _tree_consensus_ws = _tree_attn_ws
 
 
+@pytest.mark.parametrize("pools", [torch.bfloat16, torch.int16])
 @pytest.mark.parametrize("fused", [False, True])
-def test_a_call_like_the_one_before_is_looked_at_as_closely(monkeypatch, fused):
+def test_a_call_like_the_one_before_is_looked_at_as_closely(monkeypatch, fused, pools):
     """The second call of the same sizes goes another way through the host: with the same arguments for the library, and the same refusals."""
     monkeypatch.setattr(rt, "_raw_stream", lambda index: 0)
     row = 12 * 128 if fused else 0
@@ -345,6 +346,8 @@ def test_a_call_like_the_one_before_is_looked_at_as_closely(monkeypatch, fused):
     f, g = _h(B, N, 12, 128), _h(1, B, N, 12, 128)
     attn = _attn_args(lse=torch.zeros((B, 8, N)), **(dict(q=f[:, :, :8], k_blk=f[:, :, 8:10], v_blk=f[:, :, 10:]) if fused else {}))
     walk = _committed(**(dict(k_blk_ar=g[..., 8:10, :], v_blk_ar=g[..., 10:, :]) if fused else {}))
+    for a in (attn, walk):     # caches of bits next to rows of bf16 as well
+        a.update(k_pool=a["k_pool"].view(pools), v_pool=a["v_pool"].view(pools))
     odd_rows = [("k_blk", _h(B, N, 16, 128)[:, :, :2]), ("q", _h(B, N, 16, 128)[:, :, :8]), ("v_blk", _h(B, N, 4, 128)[:, :, :2])]
     bad_attn = _ODD_CACHES + odd_rows + [
         ("parents", _i(B, N).long()), ("parents", _i(N, B).t()), ("parents", _i(B - 1, N)), ("q", attn["q"].half()), ("q", attn["q"].float()),
